@@ -46,8 +46,8 @@
  *    may work at the same time.
  *  - CUDA graphs: lv_features, lv_batch_latency, lv_attribute,
  *    lv_attribute_step, lv_tenant_acc_reset, lv_tenant_accumulate,
- *    lv_tenant_totals, lv_whatif
- *    and lv_whatif_admit may be captured into a CUDA graph once an uncaptured call with
+ *    lv_tenant_totals, lv_whatif, lv_whatif_admit, lv_kv_plan, lv_kv_store,
+ *    lv_kv_attend and lv_prompt_attend may be captured into a CUDA graph once an uncaptured call with
  *    the same context, model and sizes has run (it creates the context's
  *    buffers and caches the kernel configuration; a capture never allocates).
  *    The context's ordering events are then recorded and waited for by the
@@ -334,6 +334,114 @@ lv_status lv_whatif_admit(lv_ctx *ctx, const lv_model *model, const lv_batches *
                           const int32_t *c_new, const int32_t *phase_new, const int32_t *tenant_new,
                           int64_t n_pending, const double *L, const double *budget, int32_t n_tenants, double slo,
                           double *T_new, double *share_new, uint8_t *admit, void *stream);
+
+/* ------------------------------------------------ attention work of a step
+ *
+ * The latency that the model explains is that of a serving step, and two of its
+ * terms are attention: sum c is the cache that a step's queries read, sum p^2
+ * the prompts' attention over themselves (Section 2.1).  The four calls below
+ * do that work, so that a step's batches (p and c as in lv_batches) can be run,
+ * timed and fitted on the machine itself: lv_kv_plan places a step's new tokens
+ * in a paged cache, lv_kv_store appends their keys and values to it,
+ * lv_kv_attend reads it for the step's queries, lv_prompt_attend attends over
+ * whole prompts that start on an empty cache.  The paper has no counterpart: it
+ * profiles an engine's own kernels (Section 3).
+ *
+ * Elements of queries, keys, values and outputs are 16-bit floats of one type
+ * per call (dtype LV_BF16 or LV_F16); head_dim is 64 or 128; n_q_heads is a
+ * multiple of n_kv_heads and query head h reads key/value head
+ * h / (n_q_heads / n_kv_heads), for at most LV_MAX_GROUP query heads a
+ * key/value head.  Their arrays are [token][head][element] with the heads of a
+ * token side by side; *_stride is the distance between tokens in elements (a
+ * multiple of 8, at least n_heads * head_dim), so that they may be slices of one
+ * projection's output; base pointers are 16-byte aligned.  Others: LV_EINVAL. */
+#define LV_BF16 0
+#define LV_F16 1
+#define LV_MAX_GROUP 64
+
+/* A paged key/value cache in 8 bits.  Block b holds block_tokens (16, 32, 64 or
+ * 128) tokens of one request; k and v are e4m3 codes
+ * uint8[n_blocks][n_kv_heads][block_tokens][head_dim], 16-byte aligned, and the
+ * value of a code is code * scale, k_scale and v_scale
+ * float[n_blocks][n_kv_heads].  All are caller-owned device memory. */
+typedef struct {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    int64_t n_blocks;
+    int32_t block_tokens, n_kv_heads, head_dim;
+    int32_t reserved;
+} lv_kv_cache;
+
+/* The plan of a step: request i has c[i] tokens in the cache and p[i] new ones
+ * (p = 0 is allowed).  It holds ceil(c/B) blocks (B = block_tokens), listed in
+ * row i of table int32[n_req][table_width], and needs
+ * need_i = ceil((c+p)/B) - ceil(c/B) more.  Blocks are taken from
+ * free_blocks[n_free] in request order: with E_i = need_0 + .. + need_{i-1},
+ * request i gets free_blocks[E_i .. E_i+need_i-1] if E_i + need_i <= n_free,
+ * else -1 in their place (a later request is served only where the earlier
+ * needs leave room, served or not).  Writes:
+ *  table          the new entries of every row; others are untouched;
+ *  token_offsets  int64[n_req+1]: p's running sum from 0 (the new tokens'
+ *                 places in a packed step);
+ *  slots          int64[n_slots], for new token j of request i at
+ *                 token_offsets[i]+j: table[i][(c+j)/B] * B + (c+j) % B, or -1
+ *                 where that entry is negative; entries past the last token
+ *                 are -1, so that a step can be padded to a fixed size;
+ *  counts         int64[2]: tokens, blocks needed (more than n_free: short).
+ * A negative p or c (taken as p = 0, c = 0), a row that table_width cannot hold
+ * (what lies past it is not written, its slots are -1) and more tokens than
+ * n_slots (the rest is not written) record LV_EDATA.  n_req at most 2^24,
+ * block_tokens a power of two up to 2^16, n_slots, table_width and n_free at
+ * least 0; the arrays must not overlap.  int32 arrays 4-byte, int64 arrays
+ * 8-byte aligned.  One launch up to 2,048 requests, two above. */
+lv_status lv_kv_plan(lv_ctx *ctx, const int32_t *p, const int32_t *c, int64_t n_req, int32_t block_tokens,
+                     const int32_t *free_blocks, int64_t n_free, int32_t *table, int64_t table_width,
+                     int64_t *token_offsets, int64_t *slots, int64_t n_slots, int64_t *counts, void *stream);
+
+/* Appends the keys and values of n_tok new tokens: token t of k and v goes to
+ * slot slots[t] = block * block_tokens + offset (lv_kv_plan's); a negative slot
+ * is skipped, one past the cache too, with LV_EDATA.  The new tokens of one
+ * block stand next to each other in the call, in order and without gaps, after
+ * the tokens that the block holds (as lv_kv_plan numbers them).
+ * The scale of a block and head is need, or where the block held tokens before
+ * (its first new offset is not 0) max(its scale, need): need = 2^e for the
+ * least e >= -100 with amax <= 448 * 2^e, amax the largest finite |value| among
+ * the new tokens.  Where the scale grows, the values held before are rounded
+ * again: code' = e4m3(code * (old / new)).  New codes are e4m3(value / scale).
+ * Roundings are to nearest even; what is not finite is held as NaN (e4m3 has no
+ * infinities).  A power of two keeps every normal value's bits when a scale
+ * grows, and makes the roundings the same on every machine. */
+lv_status lv_kv_store(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const int64_t *slots, int64_t n_tok, void *stream);
+
+/* Attention of a step's queries over the cache.  Request i's new tokens are the
+ * queries token_offsets[i] .. token_offsets[i+1]-1 of q, or where token_offsets
+ * is NULL the one query i (n_tok = n_req).  New token j sees the keys at
+ * positions 0 .. c[i]+j whose block is in the table (an entry of -1 hides its
+ * block):
+ *   o[t][h] = sum_k w_k V_k,  w = softmax(scale * q[t][h] . K_k),
+ *   lse[t][h] = log sum_k exp(scale * q[t][h] . K_k)       (lse may be NULL).
+ * A query that sees no key gives 0 and -inf.  o is [n_tok][n_q_heads][head_dim]
+ * without gaps, in q's type; lse float[n_tok][n_q_heads].  Products are summed
+ * and the softmax is held in fp32; a query's 16-bit value is used as it is and a
+ * weight is rounded to 16 bits before it meets V.
+ * A table entry outside [-1, n_blocks) (hidden), a negative c (its queries see
+ * nothing), tokens past the row's table_width (hidden) and offsets that decrease
+ * or leave [0, n_tok] (taken as no queries) record LV_EDATA. */
+lv_status lv_kv_attend(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, int32_t n_q_heads, const void *q,
+                       int64_t q_stride, int64_t n_tok, const int64_t *token_offsets, const int32_t *c, int64_t n_req,
+                       const int32_t *table, int64_t table_width, float scale, void *o, float *lse, void *stream);
+
+/* Causal attention over whole prompts packed one after another: sequence s is
+ * the tokens offsets[s] .. offsets[s+1]-1 of q, k and v (int64[n_seq+1], which
+ * may start past 0 and may hold empty sequences; lv_kv_plan's token_offsets).
+ * Token t sees the tokens of its own sequence up to itself; o and lse as for
+ * lv_kv_attend.  Tokens of no sequence are not written.  Offsets that decrease
+ * or leave [0, n_tok] record LV_EDATA (taken as an empty sequence). */
+lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                           int64_t v_stride, int64_t n_tok, const int64_t *offsets, int64_t n_seq, float scale,
+                           void *o, float *lse, void *stream);
 
 /* Attribution without any allocation (the paper has no counterpart; this is a
  * service to callers that cannot allocate device memory at call time).  A

@@ -24,6 +24,8 @@ LV_OK, LV_EINVAL, LV_EOVERFLOW, LV_ENODATA, LV_ESINGULAR, LV_ECUDA, LV_EDATA, LV
 LV_ARITH_AUTO, LV_ARITH_FP64 = 0, 1
 LV_TIME_TILES, LV_TIME_PAIRS = 1, 2
 LV_STEP_RESET = 1
+LV_BF16, LV_F16 = 0, 1
+LV_MAX_GROUP = 64
 
 EXPORTED = [
     "lv_status_string", "lv_arch_constants", "lv_ctx_create", "lv_ctx_destroy", "lv_ctx_set_arith", "lv_ctx_status",
@@ -32,7 +34,7 @@ EXPORTED = [
     "lv_tenant_acc_create", "lv_tenant_acc_destroy",
     "lv_tenant_acc_reset", "lv_tenant_accumulate", "lv_tenant_totals", "lv_tenant_acc_state_bytes",
     "lv_tenant_acc_export", "lv_tenant_acc_import", "lv_fit", "lv_fit_vtc", "lv_accuracy", "lv_whatif",
-    "lv_whatif_admit", "lv_attribute_noalloc",
+    "lv_whatif_admit", "lv_attribute_noalloc", "lv_kv_plan", "lv_kv_store", "lv_kv_attend", "lv_prompt_attend",
 ]
 
 
@@ -72,6 +74,12 @@ class lv_accuracy_report(ctypes.Structure):
                 ("p99", ctypes.c_double)]
 
 
+class lv_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"LLMVisor CUDA library not built: {LIB_PATH} is missing "
@@ -107,6 +115,10 @@ def _load():
         "lv_whatif": ([P, P, P, P, P, P, I64, P, P, P], I32),
         "lv_whatif_admit": ([P, P, P, P, P, P, P, I64, P, P, I32, ctypes.c_double, P, P, P, P], I32),
         "lv_attribute_noalloc": ([P, P, P, P, P, P], I32),
+        "lv_kv_plan": ([P, P, P, I64, I32, P, I64, P, I64, P, P, I64, P, P], I32),
+        "lv_kv_store": ([P, P, I32, P, I64, P, I64, P, I64, P], I32),
+        "lv_kv_attend": ([P, P, I32, I32, P, I64, I64, P, P, I64, P, I64, ctypes.c_float, P, P, P], I32),
+        "lv_prompt_attend": ([P, I32, I32, I32, I32, P, I64, P, I64, P, I64, I64, P, I64, ctypes.c_float, P, P, P], I32),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -395,3 +407,107 @@ def lv_whatif_admit(ctx: Context, model: lv_model, cand: Batches, p_new, c_new, 
                                 _ptr(phase_new), _ptr(tenant_new), int(p_new.numel()), _ptr(L), _ptr(budget),
                                 int(L.numel()), float(slo), _ptr(T_new), _ptr(share_new), _ptr(admit),
                                 _stream(stream)), "lv_whatif_admit")
+
+
+# ------------------------------------------------------------------ attention work of a step
+
+_dtypes = {}  # torch dtype -> LV_BF16 / LV_F16, and the other types that the calls below check
+
+
+def _types():
+    import torch
+    _dtypes.update({torch.bfloat16: LV_BF16, torch.float16: LV_F16, "i32": torch.int32, "i64": torch.int64,
+                    "f32": torch.float32, "u8": torch.uint8})
+    return _dtypes
+
+
+def _want(ok, where):
+    """The binding knows shapes, types and strides that the C call cannot see: a mismatch is an invalid argument."""
+    if not ok:
+        raise LVError(LV_EINVAL, where)
+
+
+def _rows(x, where):
+    """Token stride in elements of a [token][head][element] tensor whose tokens are without gaps inside."""
+    st = x.stride()
+    _want(x.dim() == 3 and st[2] == 1 and (st[1] == x.shape[2] or x.shape[1] == 1), where)
+    return st[0] if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+class KVCache:
+    """A paged key/value cache in e4m3: uint8 codes k, v [n_blocks][n_kv_heads][block_tokens][head_dim] and float32
+    scales [n_blocks][n_kv_heads], all contiguous CUDA tensors, which it keeps."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        t = _dtypes or _types()
+        n, h, b, d = k.shape
+        _want(k.dtype == v.dtype == t["u8"] and v.shape == k.shape and k.is_contiguous() and v.is_contiguous()
+              and k_scale.dtype == v_scale.dtype == t["f32"] and k_scale.shape == v_scale.shape == (n, h)
+              and k_scale.is_contiguous() and v_scale.is_contiguous(), "KVCache")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.s = lv_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n, b, h, d, 0)
+
+    @classmethod
+    def empty(cls, n_blocks, n_kv_heads, block_tokens, head_dim, device="cuda"):
+        """A cache of zeros: no block holds anything."""
+        import torch
+        shape = (n_blocks, n_kv_heads, block_tokens, head_dim)
+        return cls(*(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in "kv"),
+                   *(torch.zeros(shape[:2], dtype=torch.float32, device=device) for _ in "kv"))
+
+
+def lv_kv_plan(ctx: Context, p, c, block_tokens: int, free_blocks, table, token_offsets, slots, counts, stream=None):
+    """Block tables and slot maps of a step.  int32 p, c [n_req], free_blocks [n_free], table [n_req][width]; int64
+    token_offsets [n_req + 1], slots [n_slots], counts [2]; table's new entries and the last three are written."""
+    t = _dtypes or _types()
+    n = p.numel()
+    _want(p.dtype == c.dtype == free_blocks.dtype == table.dtype == t["i32"] and c.numel() == n
+          and token_offsets.dtype == slots.dtype == counts.dtype == t["i64"] and token_offsets.numel() == n + 1
+          and counts.numel() == 2 and table.dim() == 2 and table.shape[0] == n and table.is_contiguous()
+          and p.is_contiguous() and c.is_contiguous() and free_blocks.is_contiguous() and token_offsets.is_contiguous()
+          and slots.is_contiguous() and counts.is_contiguous(), "lv_kv_plan")
+    _check(_lib.lv_kv_plan(ctx.h, p.data_ptr(), c.data_ptr(), n, int(block_tokens), free_blocks.data_ptr(),
+                           free_blocks.numel(), table.data_ptr(), table.shape[1], token_offsets.data_ptr(),
+                           slots.data_ptr(), slots.numel(), counts.data_ptr(), _stream(stream)), "lv_kv_plan")
+
+
+def lv_kv_store(ctx: Context, cache: KVCache, k, v, slots, stream=None):
+    """Appends k, v [n_tok][n_kv_heads][head_dim] (slices of a wider tensor may be given) to the cache."""
+    t = _dtypes or _types()
+    s, n = cache.s, k.shape[0]
+    _want(k.dtype == v.dtype and k.dtype in t and k.shape == v.shape == (n, s.n_kv_heads, s.head_dim)
+          and slots.dtype == t["i64"] and slots.numel() == n and slots.is_contiguous(), "lv_kv_store")
+    _check(_lib.lv_kv_store(ctx.h, ctypes.byref(s), t[k.dtype], k.data_ptr(), _rows(k, "lv_kv_store"), v.data_ptr(),
+                            _rows(v, "lv_kv_store"), slots.data_ptr(), n, _stream(stream)), "lv_kv_store")
+
+
+def lv_kv_attend(ctx: Context, cache: KVCache, q, c, table, o, lse=None, token_offsets=None, scale=None, stream=None):
+    """Attention of queries q [n_tok][n_q_heads][head_dim] over the cache into o (and lse); scale None: 1/sqrt(head_dim)."""
+    t = _dtypes or _types()
+    s, n, (n_tok, hq, d) = cache.s, c.numel(), q.shape
+    _want(q.dtype in t and d == s.head_dim and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
+          and c.dtype == table.dtype == t["i32"] and c.is_contiguous() and table.dim() == 2 and table.shape[0] == n
+          and table.is_contiguous()
+          and (lse is None or (lse.dtype == t["f32"] and lse.shape == (n_tok, hq) and lse.is_contiguous()))
+          and (token_offsets is None or (token_offsets.dtype == t["i64"] and token_offsets.numel() == n + 1
+                                         and token_offsets.is_contiguous())), "lv_kv_attend")
+    _check(_lib.lv_kv_attend(ctx.h, ctypes.byref(s), t[q.dtype], hq, q.data_ptr(), _rows(q, "lv_kv_attend"), n_tok,
+                             _ptr(token_offsets), c.data_ptr(), n, table.data_ptr(), table.shape[1],
+                             d ** -0.5 if scale is None else scale, o.data_ptr(), _ptr(lse), _stream(stream)),
+           "lv_kv_attend")
+
+
+def lv_prompt_attend(ctx: Context, q, k, v, offsets, o, lse=None, scale=None, stream=None):
+    """Causal attention over packed prompts: q [n_tok][n_q_heads][head_dim], k and v [n_tok][n_kv_heads][head_dim] (slices
+    of a wider tensor may be given), int64 offsets [n_seq + 1]; scale None: 1/sqrt(head_dim)."""
+    t = _dtypes or _types()
+    (n_tok, hq, d), hkv = q.shape, k.shape[1]
+    _want(q.dtype in t and k.dtype == v.dtype == o.dtype == q.dtype and k.shape == v.shape == (n_tok, hkv, d)
+          and o.shape == q.shape and o.is_contiguous() and offsets.dtype == t["i64"] and offsets.numel() >= 1
+          and offsets.is_contiguous()
+          and (lse is None or (lse.dtype == t["f32"] and lse.shape == (n_tok, hq) and lse.is_contiguous())),
+          "lv_prompt_attend")
+    w = "lv_prompt_attend"
+    _check(_lib.lv_prompt_attend(ctx.h, t[q.dtype], hq, hkv, d, q.data_ptr(), _rows(q, w), k.data_ptr(), _rows(k, w),
+                                 v.data_ptr(), _rows(v, w), n_tok, offsets.data_ptr(), offsets.numel() - 1,
+                                 d ** -0.5 if scale is None else scale, o.data_ptr(), _ptr(lse), _stream(stream)), w)

@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 OUT_DIR = os.path.join(HERE, "_build")
 OUT = os.path.join(OUT_DIR, "libllmvisor.so")
-SRC = os.path.join(HERE, "csrc", "lv_api.cu")
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("lv_api.cu", "lv_kv.cu")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -27,7 +27,8 @@ def nvcc() -> str:
 
 
 def _inputs():
-    return [SRC] + glob.glob(os.path.join(HERE, "csrc", "*.cuh")) + [os.path.join(ROOT, "include", "llmvisor.h")]
+    return (SRCS + glob.glob(os.path.join(HERE, "csrc", "*.cuh")) + glob.glob(os.path.join(HERE, "csrc", "*.h"))
+            + [os.path.join(ROOT, "include", "llmvisor.h")])
 
 
 def build(force: bool = False, extra=()) -> str:
@@ -37,9 +38,20 @@ def build(force: bool = False, extra=()) -> str:
         if os.path.getmtime(OUT) >= newest:
             return OUT
     tmp = OUT + f".tmp{os.getpid()}"
-    cmd = [nvcc(), *ARCH, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-shared",
-           "-I", os.path.join(ROOT, "include"), "-o", tmp, SRC, "-lcudart", *extra]
-    subprocess.run(cmd, check=True)
+    objs = [f"{tmp}.{os.path.basename(src)}.o" for src in SRCS]
+    # the translation units side by side
+    jobs = [subprocess.Popen([nvcc(), *ARCH, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-c",
+                              "-I", os.path.join(ROOT, "include"), "-o", obj, src, *extra])
+            for src, obj in zip(SRCS, objs)]
+    codes = [j.wait() for j in jobs]
+    try:
+        if any(codes):
+            raise RuntimeError(f"nvcc failed: {dict(zip(SRCS, codes))}")
+        subprocess.run([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"], check=True)
+    finally:
+        for obj in objs:
+            if os.path.exists(obj):
+                os.remove(obj)
     os.replace(tmp, OUT)
     return OUT
 

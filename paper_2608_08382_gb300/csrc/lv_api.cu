@@ -14,6 +14,7 @@
 #include "llmvisor.h"
 #include "lv_fit.cuh"
 #include "lv_kernels.cuh"
+#include "lv_kv.h"
 #include "lv_metrics.cuh"
 #include "lv_step.cuh"
 #include "lv_tile.cuh"
@@ -61,11 +62,14 @@ struct lv_ctx {
   FitHost *hd_fit = nullptr;
   double *h_acc = nullptr;    // accuracy results: pinned host memory the kernel writes (mapped)
   double *hd_acc = nullptr;   // its device address
+  KvHost kv;                  // what the attention calls keep
   void *d_probe = nullptr;    // barrier self-test: arrivals, generation, error word
   int timing = 0;  // LV_TIME_* mask
   std::vector<cudaEvent_t> tev;  // start/stop pairs
   size_t tev_used = 0;
 };
+
+lv::KvHost *lv::kv_host(lv_ctx *ctx) { return &ctx->kv; }
 
 struct lv_tenant_acc {
   lv_ctx *ctx = nullptr;
@@ -851,6 +855,9 @@ lv_status lv_ctx_create(lv_ctx **out) {
     lv_ctx_destroy(ctx);
     return LV_ECUDA;
   }
+  ctx->kv.device = ctx->device;
+  ctx->kv.sms = ctx->sms;
+  ctx->kv.d_status = ctx->d_status;
   *out = ctx;
   return LV_OK;
 }
@@ -867,6 +874,7 @@ void lv_ctx_destroy(lv_ctx *ctx) {
   if (ctx->h_fit) cudaFreeHost(ctx->h_fit);
   if (ctx->h_acc) cudaFreeHost(ctx->h_acc);
   if (ctx->d_probe) cudaFree(ctx->d_probe);
+  if (ctx->kv.scratch) cudaFree(ctx->kv.scratch);
   if (ctx->ev_built) cudaEventDestroy(ctx->ev_built);
   if (ctx->ev_used) cudaEventDestroy(ctx->ev_used);
   for (cudaEvent_t e : ctx->tev) cudaEventDestroy(e);

@@ -1,0 +1,222 @@
+// Host side of the attention calls: argument checks and launches.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "llmvisor.h"
+#include "lv_attend.cuh"
+#include "lv_kv.h"
+#include "lv_kv_plan.cuh"
+#include "lv_kv_store.cuh"
+
+using namespace lv;
+
+namespace {
+
+#define LV_CUDA(call)                          \
+  do {                                         \
+    if ((call) != cudaSuccess) return LV_ECUDA; \
+  } while (0)
+
+bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int log2_of(int64_t x) { return 63 - __builtin_clzll((unsigned long long)x); }
+
+// The context's scratch, at least `bytes`.
+lv_status scratch_for(KvHost *kv, size_t bytes) {
+  if (bytes <= kv->cap) return LV_OK;
+  LV_CUDA(cudaDeviceSynchronize());
+  if (kv->scratch) cudaFree(kv->scratch);
+  kv->scratch = nullptr;
+  kv->cap = 0;
+  void *p = nullptr;
+  if (cudaMalloc(&p, bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return LV_ENOMEM;
+  }
+  kv->scratch = static_cast<unsigned char *>(p);
+  kv->cap = bytes;
+  return LV_OK;
+}
+
+bool cache_ok(const lv_kv_cache *c) {
+  if (!c || c->n_blocks < 0 || c->n_blocks > (1ll << 31) || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return false;
+  if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->n_blocks == 0) return true;
+  return c->k && c->v && c->k_scale && c->v_scale && aligned(c->k, 16) && aligned(c->v, 16) &&
+         aligned(c->k_scale, 4) && aligned(c->v_scale, 4);
+}
+
+// An array of n_tok tokens of `heads` heads.
+bool rows_ok(const void *p, int64_t stride, int64_t n_tok, int64_t heads, int64_t dim) {
+  return n_tok == 0 || (p && aligned(p, 16) && stride % 8 == 0 && stride >= heads * dim && stride <= (1ll << 40));
+}
+
+bool heads_ok(int32_t dtype, int32_t hq, int32_t hkv) {
+  return (dtype == LV_BF16 || dtype == LV_F16) && hkv >= 1 && hkv <= 1024 && hq >= hkv && hq % hkv == 0 &&
+         hq / hkv <= LV_MAX_GROUP;
+}
+
+constexpr int64_t kMostTokens = 1ll << 31;
+
+template <bool PAGED>
+lv_status run_attend(KvHost *kv, AttendArgs &a, int d, int32_t dtype, cudaStream_t stream) {
+  const unsigned grid = (unsigned)((a.n_tok * a.hq + 3) / 4);
+  if (d == 128 && dtype == LV_F16) k_attend_rows<128, true, PAGED><<<grid, 128, 0, stream>>>(a);
+  if (d == 128 && dtype == LV_BF16) k_attend_rows<128, false, PAGED><<<grid, 128, 0, stream>>>(a);
+  if (d == 64 && dtype == LV_F16) k_attend_rows<64, true, PAGED><<<grid, 128, 0, stream>>>(a);
+  if (d == 64 && dtype == LV_BF16) k_attend_rows<64, false, PAGED><<<grid, 128, 0, stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lv_status lv_kv_plan(lv_ctx *ctx, const int32_t *p, const int32_t *c, int64_t n_req, int32_t block_tokens,
+                     const int32_t *free_blocks, int64_t n_free, int32_t *table, int64_t table_width,
+                     int64_t *token_offsets, int64_t *slots, int64_t n_slots, int64_t *counts, void *stream_) {
+  if (!ctx || n_req < 0 || n_req > (1ll << 24) || n_free < 0 || n_slots < 0 || table_width < 0 ||
+      table_width > (1ll << 31))
+    return LV_EINVAL;
+  if (block_tokens < 1 || block_tokens > (1 << 16) || (block_tokens & (block_tokens - 1))) return LV_EINVAL;
+  if (!token_offsets || !counts || (n_req > 0 && (!p || !c)) || (n_free > 0 && !free_blocks) ||
+      (n_slots > 0 && !slots) || (n_req > 0 && table_width > 0 && !table))
+    return LV_EINVAL;
+  if (!aligned(p, 4) || !aligned(c, 4) || !aligned(free_blocks, 4) || !aligned(table, 4) ||
+      !aligned(token_offsets, 8) || !aligned(slots, 8) || !aligned(counts, 8))
+    return LV_EINVAL;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  KvHost *kv = kv_host(ctx);
+  PlanArgs a{};
+  a.p = p;
+  a.c = c;
+  a.n_req = n_req;
+  a.log_b = log2_of(block_tokens);
+  a.free = free_blocks;
+  a.n_free = n_free;
+  a.table = table;
+  a.width = table_width;
+  a.offsets = token_offsets;
+  a.slots = slots;
+  a.n_slots = n_slots;
+  a.counts = counts;
+  a.status = kv->d_status;
+  const int64_t tiles = std::max<int64_t>(1, (n_req + kPlanTile - 1) / kPlanTile);
+  if (tiles > 1) {
+    const lv_status st = scratch_for(kv, 16 * (size_t)tiles);
+    if (st != LV_OK) return st;
+    a.sums = reinterpret_cast<int64_t *>(kv->scratch);
+    k_plan_sums<<<(unsigned)tiles, kPlanThreads, 0, stream>>>(a);
+    LV_CUDA(cudaGetLastError());
+  }
+  const int64_t per = (std::max(n_slots, n_req) / tiles + kPlanThreads - 1) / kPlanThreads;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(per, 2 * kv->sms / std::min<int64_t>(tiles, kv->sms)));
+  static_assert(sizeof(PlanSmem) <= 48 << 10, "static limit");
+  k_plan<<<dim3((unsigned)slices, (unsigned)tiles), kPlanThreads, sizeof(PlanSmem), stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+lv_status lv_kv_store(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const int64_t *slots, int64_t n_tok, void *stream_) {
+  if (!ctx || !cache_ok(cache) || n_tok < 0 || n_tok > kMostTokens || (dtype != LV_BF16 && dtype != LV_F16))
+    return LV_EINVAL;
+  const int d = cache->head_dim, heads = cache->n_kv_heads;
+  if (!rows_ok(k, k_stride, n_tok, heads, d) || !rows_ok(v, v_stride, n_tok, heads, d)) return LV_EINVAL;
+  if (n_tok == 0) return LV_OK;
+  if (!slots || !aligned(slots, 8)) return LV_EINVAL;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  KvHost *kv = kv_host(ctx);
+  StoreArgs a{};
+  a.x[0] = k, a.x[1] = v;
+  a.stride[0] = k_stride, a.stride[1] = v_stride;
+  a.code[0] = cache->k, a.code[1] = cache->v;
+  a.scale[0] = cache->k_scale, a.scale[1] = cache->v_scale;
+  a.slots = slots;
+  a.n_tok = n_tok;
+  a.n_blocks = cache->n_blocks;
+  a.log_b = log2_of(cache->block_tokens);
+  a.heads = heads;
+  a.status = kv->d_status;
+  const int64_t blocks = (n_tok * 2 * heads + 7) / 8;
+  if (blocks > INT32_MAX) return LV_EINVAL;
+  const unsigned grid = (unsigned)blocks;
+  if (d == 128 && dtype == LV_F16) k_kv_store<128, true><<<grid, 256, 0, stream>>>(a);
+  if (d == 128 && dtype == LV_BF16) k_kv_store<128, false><<<grid, 256, 0, stream>>>(a);
+  if (d == 64 && dtype == LV_F16) k_kv_store<64, true><<<grid, 256, 0, stream>>>(a);
+  if (d == 64 && dtype == LV_BF16) k_kv_store<64, false><<<grid, 256, 0, stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+lv_status lv_kv_attend(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, int32_t n_q_heads, const void *q,
+                       int64_t q_stride, int64_t n_tok, const int64_t *token_offsets, const int32_t *c, int64_t n_req,
+                       const int32_t *table, int64_t table_width, float scale, void *o, float *lse, void *stream_) {
+  if (!ctx || !cache_ok(cache) || !heads_ok(dtype, n_q_heads, cache->n_kv_heads)) return LV_EINVAL;
+  if (n_tok < 0 || n_tok > kMostTokens || n_req < 0 || n_req > (1ll << 24) || table_width < 0 ||
+      table_width > (1ll << 31) || !std::isfinite(scale))
+    return LV_EINVAL;
+  if (!token_offsets && n_tok != n_req) return LV_EINVAL;
+  if (!rows_ok(q, q_stride, n_tok, n_q_heads, cache->head_dim)) return LV_EINVAL;
+  if (n_tok == 0 || n_req == 0) return LV_OK;
+  if (!o || !aligned(o, 16) || !aligned(lse, 4) || !c || !aligned(c, 4) || !aligned(token_offsets, 8) ||
+      (table_width > 0 && !table) || !aligned(table, 4))
+    return LV_EINVAL;
+  AttendArgs a{};
+  a.cache = {cache->k, cache->v, cache->k_scale, cache->v_scale, cache->n_blocks, log2_of(cache->block_tokens),
+             cache->n_kv_heads};
+  a.q = q;
+  a.q_stride = q_stride;
+  a.n_tok = n_tok;
+  a.offsets = token_offsets;
+  a.c = c;
+  a.n_req = n_req;
+  a.table = table;
+  a.width = table_width;
+  a.hq = n_q_heads;
+  a.hkv = cache->n_kv_heads;
+  a.scale = scale * 1.4426950408889634f;
+  a.o = o;
+  a.lse = lse;
+  KvHost *kv = kv_host(ctx);
+  a.status = kv->d_status;
+  return run_attend<true>(kv, a, cache->head_dim, dtype, (cudaStream_t)stream_);
+}
+
+lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                           int64_t v_stride, int64_t n_tok, const int64_t *offsets, int64_t n_seq, float scale,
+                           void *o, float *lse, void *stream_) {
+  if (!ctx || !heads_ok(dtype, n_q_heads, n_kv_heads) || (head_dim != 64 && head_dim != 128)) return LV_EINVAL;
+  if (n_tok < 0 || n_tok > kMostTokens || n_seq < 0 || n_seq > (1ll << 24) || !std::isfinite(scale)) return LV_EINVAL;
+  if (!rows_ok(q, q_stride, n_tok, n_q_heads, head_dim) || !rows_ok(k, k_stride, n_tok, n_kv_heads, head_dim) ||
+      !rows_ok(v, v_stride, n_tok, n_kv_heads, head_dim))
+    return LV_EINVAL;
+  if (n_tok == 0 || n_seq == 0) return LV_OK;
+  if (!o || !aligned(o, 16) || !aligned(lse, 4) || !offsets || !aligned(offsets, 8)) return LV_EINVAL;
+  AttendArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.n_tok = n_tok;
+  a.offsets = offsets;
+  a.n_req = n_seq;
+  a.hq = n_q_heads;
+  a.hkv = n_kv_heads;
+  a.scale = scale * 1.4426950408889634f;
+  a.o = o;
+  a.lse = lse;
+  KvHost *kv = kv_host(ctx);
+  a.status = kv->d_status;
+  return run_attend<false>(kv, a, head_dim, dtype, (cudaStream_t)stream_);
+}
+
+}  // extern "C"

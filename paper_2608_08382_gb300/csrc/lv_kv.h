@@ -1,0 +1,21 @@
+// What a context keeps for the attention calls (lv_kv.cu), whose translation
+// unit does not see the rest of it.
+#pragma once
+
+#include <cstddef>
+
+#include "llmvisor.h"
+
+namespace lv {
+
+struct KvHost {
+  int device = 0;
+  int sms = 0;
+  int *d_status = nullptr;           // the context's status word
+  unsigned char *scratch = nullptr;  // owned
+  size_t cap = 0;
+};
+
+KvHost *kv_host(lv_ctx *ctx);
+
+}  // namespace lv
