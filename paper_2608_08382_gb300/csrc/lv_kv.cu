@@ -7,6 +7,7 @@
 
 #include "llmvisor.h"
 #include "lv_attend.cuh"
+#include "lv_decode.cuh"
 #include "lv_kv.h"
 #include "lv_kv_plan.cuh"
 #include "lv_kv_store.cuh"
@@ -71,6 +72,61 @@ lv_status run_attend(KvHost *kv, AttendArgs &a, int d, int32_t dtype, cudaStream
   if (d == 64 && dtype == LV_BF16) k_attend_rows<64, false, PAGED><<<grid, 128, 0, stream>>>(a);
   LV_CUDA(cudaGetLastError());
   return LV_OK;
+}
+
+// Launches a kernel that may start while the one before it in the stream runs
+// (it calls wait_previous itself).
+template <class... P, class... A>
+lv_status launch_after(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, A... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LV_CUDA(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+  return LV_OK;
+}
+
+template <int D, bool F16, int NT>
+lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
+  constexpr int kPerSm = NT == 1 ? 3 : 2;  // as the kernel's launch bounds have it
+  DecodeArgs d{};
+  d.a = a;
+  d.nt = NT;
+  const int64_t ctas = (int64_t)kv->sms * kPerSm;
+  d.warps = ctas * kDecWarps;
+  // scratch: running sums, the parts
+  const size_t o_part = (8 * ((size_t)a.n_req + 1) + 255) & ~(size_t)255;
+  const size_t slots = 2 * (size_t)d.warps * 8 * NT;
+  const lv_status st = scratch_for(kv, o_part + slots * (D + 2) * sizeof(float));
+  if (st != LV_OK) return st;
+  d.prefix = reinterpret_cast<int64_t *>(kv->scratch);
+  d.part = reinterpret_cast<float *>(kv->scratch + o_part);
+  d.part_ml = d.part + slots * D;
+  d.given = a.n_req > kDecScan;
+  if (d.given) {
+    k_attend_prefix<<<1, kDecScan, 0, stream>>>(d);
+    LV_CUDA(cudaGetLastError());
+  }
+  k_attend_decode<D, F16, NT><<<(unsigned)ctas, kDecWarps * 32, 0, stream>>>(d);
+  LV_CUDA(cudaGetLastError());
+  // a segment of up to kDecMinStrips strips is never shared... unless it lies across two warps' ends
+  const int G = a.hq / a.hkv, tiles = (G + 8 * NT - 1) / (8 * NT);
+  const int64_t segments = a.n_req * a.hkv * tiles;
+  const int per_row = segments < kv->sms ? kJoinWarps : 1;
+  const int64_t y = (int64_t)a.hkv * tiles * (per_row == 1 ? NT : 8 * NT);
+  return launch_after(k_attend_join<D, F16>, dim3((unsigned)a.n_req, (unsigned)std::min<int64_t>(y, 4096)),
+                      kJoinWarps * 32, 0, stream, d, per_row);
+}
+
+template <int D, bool F16>
+lv_status run_decode_rows(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
+  return !a.offsets && a.hq / a.hkv <= 8 ? run_decode<D, F16, 1>(kv, a, stream) : run_decode<D, F16, 2>(kv, a, stream);
 }
 
 }  // namespace
@@ -185,7 +241,10 @@ lv_status lv_kv_attend(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, int
   a.lse = lse;
   KvHost *kv = kv_host(ctx);
   a.status = kv->d_status;
-  return run_attend<true>(kv, a, cache->head_dim, dtype, (cudaStream_t)stream_);
+  cudaStream_t stream = (cudaStream_t)stream_;
+  if (cache->head_dim == 128)
+    return dtype == LV_F16 ? run_decode_rows<128, true>(kv, a, stream) : run_decode_rows<128, false>(kv, a, stream);
+  return dtype == LV_F16 ? run_decode_rows<64, true>(kv, a, stream) : run_decode_rows<64, false>(kv, a, stream);
 }
 
 lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
