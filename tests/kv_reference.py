@@ -67,13 +67,14 @@ def attend_rows(q, K, V, seen, scale, dtype, d):
     """Rows q [R][d] on keys K, V [n][d], seen [R][n]: o, lse and how far a kernel that sums in fp32 and rounds a weight
     and its output to the 16-bit type may be from them.
 
-    With u the type's half unit in the last place (2^-9 for bf16, 2^-12 for f16): the output's own rounding is u |o|; a
+    With u the type's half unit in the last place, relative to the least value that has it (2^-8 for bf16, which has 8
+    significant bits, 2^-11 for f16, which has 11): the output's own rounding is u |o|; a
     weight's is u each, so at most u sum w|v|; the scores' sums of d products (in fp32, each partial sum cut rather than
     rounded: 2^-22) move a weight by at most twice d 2^-22 max scale sum|q||k|; the sums over keys and the softmax's own
     arithmetic by less than 2^-16 (its exponential is good to 2^-22, its running maximum multiplies that by the number of
     times it grows, a few tens at most).  A weight below 2^-24 of the row's largest may be lost where it is rounded to f16."""
     o, lse, to, tl = np.zeros(q.shape), np.full(len(q), -np.inf), np.zeros(q.shape), np.zeros(len(q))
-    u = 2.0**-9 if dtype == "bf16" else 2.0**-12
+    u = 2.0**-8 if dtype == "bf16" else 2.0**-11
     for r in range(len(q)):
         k = np.flatnonzero(seen[r])
         if not len(k):

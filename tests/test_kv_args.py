@@ -49,3 +49,20 @@ def test_reference_attention_against_a_hand_case():
     assert np.allclose(o, [[7.0, 3.0]]) and np.allclose(lse, np.log(4.0)) and to.max() < 0.01
     o, lse, _, _ = ref.attend_rows(q, K, V, np.zeros((1, 2), bool), 1.0, "f16", 2)
     assert np.all(o == 0) and lse[0] == -np.inf
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [1, 2, 3, 10, 200])
+def test_reference_bound_holds_for_its_own_roundings(dtype, n):
+    """Weights rounded once, everything else in 64 bits, the output rounded once: within the bound that is derived for
+    just that, at one key and at many."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float16
+    rnd = lambda x: torch.as_tensor(x).to(t).double().numpy()  # noqa: E731
+    rng = np.random.default_rng(n)
+    for _ in range(200):
+        q, K, V = rnd(rng.normal(size=(1, 8))), rnd(rng.normal(size=(n, 8))), rnd(rng.normal(size=(n, 8)))
+        o, _, tol, _ = ref.attend_rows(q, K, V, np.ones((1, n), bool), 0.7, dtype, 8)
+        s = 0.7 * (K @ q[0])
+        w = np.exp(s - s.max())
+        ref.close(rnd((rnd(w) @ V) / w.sum())[None], o, tol, "rounded")
