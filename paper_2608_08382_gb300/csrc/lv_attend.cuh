@@ -31,102 +31,142 @@ struct AttendArgs {
   int *status;
 };
 
-// One warp per (token, query head), a lane holds D / 32 elements.
-template <int D, bool F16, bool PAGED>
-__global__ void __launch_bounds__(128) k_attend_rows(AttendArgs a) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int64_t t = row / a.hq;
-  const int h = (int)(row % a.hq), g = h / (a.hq / a.hkv);
-  if (t >= a.n_tok) return;
-  // the request of token t
-  int64_t i = t, first = t;
-  if (a.offsets) {
-    int64_t found = -1;
-    bool bad = false;
-    for (int64_t r = lane; r < a.n_req; r += 32) {
-      const int64_t x0 = a.offsets[r], x1 = a.offsets[r + 1];
-      if (x0 < 0 || x1 < x0 || x1 > a.n_tok)
-        bad = true;
-      else if (x0 <= t && t < x1)
-        found = r;
-    }
-    if (bad) flag(a.status, kStatusData);
-    for (int d = 16; d; d >>= 1) found = max(found, (int64_t)__shfl_xor_sync(~0u, found, d));
-    if (found < 0) return;
-    i = found;
-    first = a.offsets[i];
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack_out(float a, float b) {
+  if (F16) return pack_half2(a, b);
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+// Running sums of units(k), k < n <= kScan, by a block of T threads, into
+// S[0 .. n], from base up; returns the last.
+constexpr int kScan = 1024;  // requests whose running sums fit in shared memory
+
+template <int T, class F>
+__device__ __forceinline__ int64_t scan_units(int n, int64_t *S, int64_t base, F units) {
+  constexpr int kPer = (kScan + T - 1) / T;
+  __shared__ int64_t warp_sum[T / 32];
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  int64_t u[kPer], sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = tid * kPer + k;
+    u[k] = i < n ? units(i) : 0;
+    sum += u[k];
   }
-  float q[E], o[E];
+  int64_t x = sum;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const int64_t y = __shfl_up_sync(~0u, x, s);
+    if (lane >= s) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sum[w] = x;
+  __syncthreads();
+  int64_t total = 0, before = 0;
+#pragma unroll
+  for (int k = 0; k < T / 32; ++k) {
+    if (k < w) before += warp_sum[k];
+    total += warp_sum[k];
+  }
+  x += base + before - sum;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = tid * kPer + k;
+    if (i < n) S[i] = x;
+    x += u[k];
+  }
+  if (tid == 0) S[n] = base + total;
+  __syncthreads();
+  return base + total;
+}
+
+// The request whose range of the running sums S[0 .. n] holds u.
+__device__ __forceinline__ int64_t find_unit(const int64_t *S, int64_t n, int64_t u) {
+  int64_t i = 0;
+  while (n - i > 1) {
+    const int64_t m = (i + n) >> 1;
+    if (S[m] <= u) i = m; else n = m;
+  }
+  return i;
+}
+
+// Row (query t, head h) of request i, whose tokens start at `first`, once more by
+// one warp, key by key over the first n keys.  The rows of a tile see different
+// numbers of keys, and a NaN or infinity that only later rows see reaches the
+// others through a weight of zero; only rows that came out as NaN are done so.
+// The largest score first: a weight is at most 1, and an infinite value is not
+// scaled by zero on its way.
+template <int D, bool F16, bool PAGED>
+__device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_t i, int64_t t, int h, int64_t n) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31, g = h / (a.hq / a.hkv);
+  const CacheView &cv = a.cache;
   const uint16_t *qp = (const uint16_t *)a.q + t * a.q_stride + h * D + lane * E;
+  float q[E], o[E];
 #pragma unroll
   for (int k = 0; k < E; k += 2) {
     const float2 f = unpack2<F16>(*(const uint32_t *)(qp + k));
     q[k] = f.x * a.scale, q[k + 1] = f.y * a.scale;
     o[k] = o[k + 1] = 0.f;
   }
-  int64_t n = t - first + 1;
-  if (PAGED) {
-    const int32_t c = a.c[i];
-    n = c < 0 ? 0 : n + c;
-    if (c < 0 || n > (a.width << a.cache.log_b)) {
-      flag(a.status, kStatusData);
-      n = min(n, a.width << a.cache.log_b);
-    }
-  }
   float m = -INFINITY, l = 0.f;
-  for (int64_t j = 0; j < n; ++j) {
-    float kf[E], vf[E];
-    if (PAGED) {
-      const CacheView &cv = a.cache;
-      const int32_t b = a.table[i * a.width + (j >> cv.log_b)];
-      if (b < 0 || b >= cv.n_blocks) {
-        if (b != -1) flag(a.status, kStatusData);
+  bool nan = false;
+  for (int pass = 0; pass < 2; ++pass)
+    for (int64_t j = 0; j < n; ++j) {
+      float x = 0.f, v[E];
+      if (PAGED) {
+        const int32_t b = a.table[i * a.width + (j >> cv.log_b)];
+        if (b < 0 || b >= cv.n_blocks) continue;
+        const int64_t bh = (int64_t)b * cv.heads + g;
+        const int64_t at = ((bh << cv.log_b) + (j & ((1 << cv.log_b) - 1))) * D + lane * E;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          __nv_fp8_e4m3 e;
+          e.__x = cv.k[at + k];
+          x += q[k] * (float)e;
+          e.__x = cv.v[at + k];
+          v[k] = (float)e * cv.v_scale[bh];
+        }
+        x *= cv.k_scale[bh];
+      } else {
+        const uint16_t *kp = (const uint16_t *)a.k + (first + j) * a.k_stride + g * D + lane * E;
+        const uint16_t *vp = (const uint16_t *)a.v + (first + j) * a.v_stride + g * D + lane * E;
+#pragma unroll
+        for (int k = 0; k < E; k += 2) {
+          const float2 f = unpack2<F16>(*(const uint32_t *)(kp + k)), y = unpack2<F16>(*(const uint32_t *)(vp + k));
+          x += q[k] * f.x + q[k + 1] * f.y;
+          v[k] = y.x, v[k + 1] = y.y;
+        }
+      }
+      for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+      if (pass == 0) {
+        nan |= isnan(x);
+        m = fmaxf(m, x);
         continue;
       }
-      const int64_t bh = (int64_t)b * cv.heads + g;
-      const int64_t at = ((bh << cv.log_b) + (j & ((1 << cv.log_b) - 1))) * D + lane * E;
+      const float w = nan ? NAN : m == -INFINITY ? 0.f : exp2f(x - m);
+      l += w;
 #pragma unroll
-      for (int k = 0; k < E; ++k) {
-        __nv_fp8_e4m3 x;
-        x.__x = cv.k[at + k];
-        kf[k] = (float)x * cv.k_scale[bh];
-        x.__x = cv.v[at + k];
-        vf[k] = (float)x * cv.v_scale[bh];
-      }
-    } else {
-      const uint16_t *kp = (const uint16_t *)a.k + (first + j) * a.k_stride + g * D + lane * E;
-      const uint16_t *vp = (const uint16_t *)a.v + (first + j) * a.v_stride + g * D + lane * E;
-#pragma unroll
-      for (int k = 0; k < E; k += 2) {
-        float2 f = unpack2<F16>(*(const uint32_t *)(kp + k));
-        kf[k] = f.x, kf[k + 1] = f.y;
-        f = unpack2<F16>(*(const uint32_t *)(vp + k));
-        vf[k] = f.x, vf[k + 1] = f.y;
-      }
+      for (int k = 0; k < E; ++k) o[k] += w * v[k];
     }
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < E; ++k) s += q[k] * kf[k];
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-    const float mn = fmaxf(m, s), base = mn == -INFINITY ? 0.f : mn;
-    const float up = exp2f(m - base), w = exp2f(s - base);
-    l = l * up + w;
-#pragma unroll
-    for (int k = 0; k < E; ++k) o[k] = o[k] * up + w * vf[k];
-    m = mn;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;  // a NaN stays
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t *op = (uint16_t *)a.o + (t * a.hq + h) * D + lane * E;
 #pragma unroll
-  for (int k = 0; k < E; ++k) {
-    if (F16)
-      ((__half *)op)[k] = __float2half_rn(o[k] * inv);
-    else
-      ((__nv_bfloat16 *)op)[k] = __float2bfloat16_rn(o[k] * inv);
-  }
-  if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  for (int k = 0; k < E; k += 2) *(uint32_t *)(op + k) = pack_out<F16>(o[k] * inv, o[k + 1] * inv);
 }
 
 }  // namespace lv

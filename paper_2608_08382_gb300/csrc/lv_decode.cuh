@@ -34,7 +34,6 @@
 namespace lv {
 
 constexpr int kDecWarps = 4;       // warps of a CTA; they share only the scan
-constexpr int kDecScan = 1024;     // requests whose running sums fit in shared memory
 constexpr int kDecMinStrips = 8;   // strips a warp takes at least
 constexpr int kJoinWarps = 8;
 constexpr float kWeightExp = 12.f;
@@ -101,54 +100,13 @@ __device__ __forceinline__ int64_t request_units(const DecodeArgs &d, int64_t i,
   return s.p == 0 ? 0 : span_strips(d.a, s) * span_tiles(d.a, s, 8 * d.nt) * d.a.hkv;
 }
 
-// Running sums of request_units over up to kDecScan requests from `i0`, by a
-// block of T threads, into S[0 .. n]; returns the total.
-template <int T>
-__device__ __forceinline__ int64_t scan_units(const DecodeArgs &d, int64_t i0, int n, int64_t *S, int64_t base,
-                                              bool *bad) {
-  constexpr int kPer = kDecScan / T;
-  __shared__ int64_t warp_sum[T / 32];
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-  int64_t u[kPer], sum = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = tid * kPer + k;
-    u[k] = i < n ? request_units(d, i0 + i, bad) : 0;
-    sum += u[k];
-  }
-  int64_t x = sum;
-#pragma unroll
-  for (int s = 1; s < 32; s <<= 1) {
-    const int64_t y = __shfl_up_sync(~0u, x, s);
-    if (lane >= s) x += y;
-  }
-  if (lane == 31) warp_sum[w] = x;
-  __syncthreads();
-  int64_t total = 0, before = 0;
-#pragma unroll
-  for (int k = 0; k < T / 32; ++k) {
-    if (k < w) before += warp_sum[k];
-    total += warp_sum[k];
-  }
-  x += base + before - sum;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int i = tid * kPer + k;
-    if (i < n) S[i] = x;
-    x += u[k];
-  }
-  if (tid == 0) S[n] = base + total;
-  __syncthreads();
-  return base + total;
-}
-
-// The running sums of more than kDecScan requests, by one CTA.
-__global__ void __launch_bounds__(kDecScan) k_attend_prefix(DecodeArgs d) {
+// The running sums of more than kScan requests, by one CTA.
+__global__ void __launch_bounds__(kScan) k_attend_prefix(DecodeArgs d) {
   bool bad = false;
   int64_t base = 0;
-  for (int64_t i0 = 0; i0 < d.a.n_req; i0 += kDecScan) {
-    const int n = (int)min((int64_t)kDecScan, d.a.n_req - i0);
-    base = scan_units<kDecScan>(d, i0, n, d.prefix + i0, base, &bad);
+  for (int64_t i0 = 0; i0 < d.a.n_req; i0 += kScan) {
+    const int n = (int)min((int64_t)kScan, d.a.n_req - i0);
+    base = scan_units<kScan>(n, d.prefix + i0, base, [&](int k) { return request_units(d, i0 + k, &bad); });
   }
   if (bad) flag(d.a.status, kStatusData);
 }
@@ -187,26 +145,6 @@ __device__ __forceinline__ uint32_t hi_half2(uint32_t w) {
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-  return r;
-}
-
-template <bool F16>
-__device__ __forceinline__ uint32_t pack_out(float a, float b) {
-  if (F16) return pack_half2(a, b);
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
 }
 
@@ -259,62 +197,10 @@ struct Strip {
   }
 };
 
-// A row once more by one warp, key by key: the rows of a tile see different
-// numbers of keys, and a NaN or infinity that only later rows see reaches the
-// others through a weight of zero.  Only rows that came out as NaN are done so.
-template <int D, bool F16>
-__device__ __noinline__ void redo_row(const AttendArgs &a, const Span &s, int64_t i, int64_t t, int h, int64_t n) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31, g = h / (a.hq / a.hkv);
-  const CacheView &cv = a.cache;
-  const uint16_t *qp = (const uint16_t *)a.q + t * a.q_stride + h * D + lane * E;
-  float q[E], o[E];
-#pragma unroll
-  for (int k = 0; k < E; k += 2) {
-    const float2 f = unpack2<F16>(*(const uint32_t *)(qp + k));
-    q[k] = f.x * a.scale, q[k + 1] = f.y * a.scale;
-    o[k] = o[k + 1] = 0.f;
-  }
-  float m = -INFINITY, l = 0.f;
-  bool nan = false;
-  for (int pass = 0; pass < 2; ++pass)
-    for (int64_t j = 0; j < n; ++j) {
-      const int32_t b = a.table[i * a.width + (j >> cv.log_b)];
-      if (b < 0 || b >= cv.n_blocks) continue;
-      const int64_t bh = (int64_t)b * cv.heads + g;
-      const int64_t at = ((bh << cv.log_b) + (j & ((1 << cv.log_b) - 1))) * D + lane * E;
-      float x = 0.f;
-      __nv_fp8_e4m3 e;
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        e.__x = cv.k[at + k];
-        x += q[k] * (float)e;
-      }
-      x *= cv.k_scale[bh];
-      for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
-      if (pass == 0) {
-        nan |= isnan(x);
-        m = fmaxf(m, x);
-        continue;
-      }
-      const float w = nan ? x - x + NAN : exp2f(x - m);
-      l += w;
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        e.__x = cv.v[at + k];
-        o[k] += w * ((float)e * cv.v_scale[bh]);
-      }
-    }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t *op = (uint16_t *)a.o + (t * a.hq + h) * D + lane * E;
-#pragma unroll
-  for (int k = 0; k < E; k += 2) *(uint32_t *)(op + k) = pack_out<F16>(o[k] * inv, o[k + 1] * inv);
-}
-
 template <int D, bool F16, int NT>
 __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_decode(DecodeArgs d) {
   constexpr int kRows = 8 * NT, kM = D / 16;  // row tile; tiles of 16 elements of the output
-  __shared__ int64_t shared_sums[kDecScan + 1];
+  __shared__ int64_t shared_sums[kScan + 1];
   const AttendArgs &a = d.a;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   wait_previous();
@@ -324,7 +210,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
   if (d.given) {
     units = sums[a.n_req];
   } else {
-    units = scan_units<kDecWarps * 32>(d, 0, (int)a.n_req, shared_sums, 0, &bad);
+    units = scan_units<kDecWarps * 32>((int)a.n_req, shared_sums, 0, [&](int k) { return request_units(d, k, &bad); });
     sums = shared_sums;
     if (blockIdx.x == 0)
       for (int i = threadIdx.x; i <= a.n_req; i += kDecWarps * 32) d.prefix[i] = shared_sums[i];
@@ -336,11 +222,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
   const int64_t begin = me < W ? warp_start(me, W, units) : 0, end = me < W ? warp_start(me + 1, W, units) : 0;
   for (int64_t u = begin; u < end;) {
     // the segment that unit u is in
-    int64_t i = 0;
-    for (int64_t hi = a.n_req; hi - i > 1;) {
-      const int64_t m = (i + hi) >> 1;
-      if (sums[m] <= u) i = m; else hi = m;
-    }
+    const int64_t i = find_unit(sums, a.n_req, u);
     bool ignore = false;
     const Span sp = request_span(a, i, &ignore);
     const int64_t strips = span_strips(a, sp);
@@ -549,6 +431,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
         }
       }
     if (whole && sp.p > 1) {
+      __syncwarp();
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
         for (int row = 0; row < 8; ++row) {
@@ -561,7 +444,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
             }
           const int rr = row0 + 8 * nt + row, j = rr / G;
           if (__any_sync(~0u, nan) && j < sp.p)
-            redo_row<D, F16>(a, sp, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j));
+            redo_row<D, F16, true>(a, sp.first, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j));
         }
     }
     u += s1 - s0;
@@ -661,7 +544,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
       }
       if (a.lse && lane == 0)
         a.lse[at] = l == 0.f ? -INFINITY : (top - kWeightExp + log2f(l)) * 0.6931471805599453f;
-      if (sp.p > 1 && __any_sync(~0u, nan)) redo_row<D, F16>(a, sp, i, sp.first + j, hh, row_limit(a, sp, j));
+      if (sp.p > 1 && __any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, sp.first + j, hh, row_limit(a, sp, j));
     }
     if (per_row > 1) __syncthreads();
   }

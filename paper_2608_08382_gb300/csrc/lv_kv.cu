@@ -1,4 +1,5 @@
 // Host side of the attention calls: argument checks and launches.
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -11,6 +12,7 @@
 #include "lv_kv.h"
 #include "lv_kv_plan.cuh"
 #include "lv_kv_store.cuh"
+#include "lv_prompt.cuh"
 
 using namespace lv;
 
@@ -63,17 +65,6 @@ bool heads_ok(int32_t dtype, int32_t hq, int32_t hkv) {
 
 constexpr int64_t kMostTokens = 1ll << 31;
 
-template <bool PAGED>
-lv_status run_attend(KvHost *kv, AttendArgs &a, int d, int32_t dtype, cudaStream_t stream) {
-  const unsigned grid = (unsigned)((a.n_tok * a.hq + 3) / 4);
-  if (d == 128 && dtype == LV_F16) k_attend_rows<128, true, PAGED><<<grid, 128, 0, stream>>>(a);
-  if (d == 128 && dtype == LV_BF16) k_attend_rows<128, false, PAGED><<<grid, 128, 0, stream>>>(a);
-  if (d == 64 && dtype == LV_F16) k_attend_rows<64, true, PAGED><<<grid, 128, 0, stream>>>(a);
-  if (d == 64 && dtype == LV_BF16) k_attend_rows<64, false, PAGED><<<grid, 128, 0, stream>>>(a);
-  LV_CUDA(cudaGetLastError());
-  return LV_OK;
-}
-
 // Launches a kernel that may start while the one before it in the stream runs
 // (it calls wait_previous itself).
 template <class... P, class... A>
@@ -108,9 +99,9 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   d.prefix = reinterpret_cast<int64_t *>(kv->scratch);
   d.part = reinterpret_cast<float *>(kv->scratch + o_part);
   d.part_ml = d.part + slots * D;
-  d.given = a.n_req > kDecScan;
+  d.given = a.n_req > kScan;
   if (d.given) {
-    k_attend_prefix<<<1, kDecScan, 0, stream>>>(d);
+    k_attend_prefix<<<1, kScan, 0, stream>>>(d);
     LV_CUDA(cudaGetLastError());
   }
   k_attend_decode<D, F16, NT><<<(unsigned)ctas, kDecWarps * 32, 0, stream>>>(d);
@@ -127,6 +118,81 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
 template <int D, bool F16>
 lv_status run_decode_rows(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   return !a.offsets && a.hq / a.hkv <= 8 ? run_decode<D, F16, 1>(kv, a, stream) : run_decode<D, F16, 2>(kv, a, stream);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps, through the runtime (no link against the
+// driver's library); null where it is missing.
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    const cudaError_t rc = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found);
+    return rc == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+  }();
+  return f;
+}
+
+// The map of a [token][head][element] array whose boxes are `tokens` tokens of
+// `heads` heads and 64 elements.
+lv_status map_rows(CUtensorMap *map, const void *at, int32_t dtype, int64_t n_tok, int64_t n_heads, int64_t dim,
+                   int64_t stride, int tokens, int heads) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return LV_ECUDA;
+  const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)n_heads, (cuuint64_t)n_tok};
+  const cuuint64_t step[2] = {(cuuint64_t)dim * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens}, one[3] = {1, 1, 1};
+  const CUresult rc =
+      encode(map, dtype == LV_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+             const_cast<void *>(at), size, step, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? LV_OK : LV_ECUDA;
+}
+
+template <int D, bool F16>
+lv_status run_prompt(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
+  PromptArgs p{};
+  p.a = a;
+  const int G = a.hq / a.hkv;
+  p.tile = 128 / G;
+  const int32_t dtype = F16 ? LV_F16 : LV_BF16;
+  CUtensorMap mq, mk, mv;
+  lv_status st = map_rows(&mq, a.q, dtype, a.n_tok, a.hq, D, a.q_stride, p.tile, G);
+  if (st == LV_OK) st = map_rows(&mk, a.k, dtype, a.n_tok, a.hkv, D, a.k_stride, kPrBlock, 1);
+  if (st == LV_OK) st = map_rows(&mv, a.v, dtype, a.n_tok, a.hkv, D, a.v_stride, kPrBlock, 1);
+  if (st != LV_OK) return st;
+  if (!kv->counter) {
+    void *c = nullptr;
+    if (cudaMalloc(&c, 2 * sizeof(unsigned long long)) != cudaSuccess) {
+      cudaGetLastError();
+      return LV_ENOMEM;
+    }
+    if (cudaMemset(c, 0, 2 * sizeof(unsigned long long)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+      cudaFree(c);
+      return LV_ECUDA;
+    }
+    kv->counter = static_cast<unsigned long long *>(c);
+  }
+  p.counter = kv->counter;
+  p.given = a.n_req > kScan;
+  if (p.given) {
+    st = scratch_for(kv, 8 * ((size_t)a.n_req + 1));
+    if (st != LV_OK) return st;
+    p.prefix = reinterpret_cast<int64_t *>(kv->scratch);
+    k_prompt_prefix<<<1, kScan, 0, stream>>>(p);
+    LV_CUDA(cudaGetLastError());
+  }
+  constexpr size_t smem = sizeof(PromptSmem<D>) + 1024;
+  LV_CUDA(cudaFuncSetAttribute(k_prompt<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  // a CTA an SM; no more than there can be items
+  const int64_t items = (a.n_tok / (2 * p.tile) + std::min(a.n_req, a.n_tok)) * a.hkv;
+  const unsigned grid = (unsigned)std::min<int64_t>(items, kv->sms);
+  k_prompt<D, F16><<<grid, kPrThreads, smem, stream>>>(p, mq, mk, mv);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
 }
 
 }  // namespace
@@ -275,7 +341,11 @@ lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_
   a.lse = lse;
   KvHost *kv = kv_host(ctx);
   a.status = kv->d_status;
-  return run_attend<false>(kv, a, head_dim, dtype, (cudaStream_t)stream_);
+  if (a.scale == 0.f) a.scale = 1e-37f;  // a masked score is -infinity: its product with the scale must be too
+  cudaStream_t stream = (cudaStream_t)stream_;
+  if (head_dim == 128)
+    return dtype == LV_F16 ? run_prompt<128, true>(kv, a, stream) : run_prompt<128, false>(kv, a, stream);
+  return dtype == LV_F16 ? run_prompt<64, true>(kv, a, stream) : run_prompt<64, false>(kv, a, stream);
 }
 
 }  // extern "C"

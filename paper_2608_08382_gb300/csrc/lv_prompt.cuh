@@ -1,0 +1,412 @@
+// Causal attention over packed prompts (lv_prompt_attend) on the tensor cores.
+//
+// S = Q K^T and O += P V cost 4 D FLOPs a (query, key, head), and that bounds all
+// but the shortest calls; the softmax between them costs an exponential a score.
+// A work item is two tiles of up to 128 rows of one key/value head.  A row is a
+// (token, query head) pair and a tile holds whole tokens, 128 / G of them with
+// all G query heads that share the keys, so the keys are fetched once for the
+// group and few of a tile's scores are masked (a tile spans 128 / G tokens).
+//
+// One CTA a SM, ten warps:
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row a thread;
+//   warp 8          issues every tcgen05.mma (one lane);
+//   warp 9          takes the items and issues every TMA load (one lane).
+// Tensor memory holds both tiles' scores and outputs, 128 + D columns each.  The
+// weights go back over the scores' columns as 16-bit values and are the second
+// product's A operand from there.  The issue order PV_0(j) QK_0(j+1) PV_1(j)
+// QK_1(j+1) has the tensor core at one tile while the other's softmax runs; it is
+// in order, so a tile's scores are overwritten only after its weights were used,
+// and when a tile's scores are ready the product before them is done as well and its
+// outputs may be rescaled.
+//
+// The running maximum that a row's weights refer to moves only when the true
+// one is more than 2^8 above it (weights are at most 2^8, sums are fp32): after
+// the first blocks of keys hardly any output is read back to be rescaled.
+// Weights are rounded to the inputs' 16-bit type, as V is.
+//
+// Items are handed out by a counter, longest first within a sequence, and the
+// loads run ahead of the products across items.
+#pragma once
+
+#include "lv_attend.cuh"
+#include "lv_tc.cuh"
+
+namespace lv {
+
+constexpr int kPrThreads = 320;
+constexpr int kPrBlock = 128;   // keys of a block
+constexpr int kPrStages = 4;    // blocks of keys or values in shared memory
+constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that weights absorb
+
+struct PromptArgs {
+  AttendArgs a;
+  int tile;             // tokens of a tile: 128 / G
+  int64_t *prefix;      // [n_req + 1] items before each sequence, given for more than kScan
+  bool given;
+  unsigned long long *counter; // items handed out beyond the first of each CTA; CTAs done (zero between launches)
+};
+
+struct PromptItem {
+  int64_t first;  // the sequence's first token
+  int64_t seq;
+  int t0, len;    // first token of the item in the sequence, the sequence's length
+  int head;       // key/value head, or -1: no more items
+  int n[2];       // key blocks of each tile
+  int tail[2];    // keys of the last one that its rows see, in steps of 16
+};
+
+template <int D>
+struct PromptSmem {
+  static constexpr int kRowBytes = 128;                    // a row of 64 elements
+  static constexpr int kTile = 128 * D * 2;                // bytes of a tile of Q or a block of K or V
+  unsigned char q[2][kTile];
+  unsigned char kv[kPrStages][kTile];
+  uint64_t q_full[2], q_empty[2], kv_full[kPrStages], kv_empty[kPrStages], s_full[2], p_full[2], o_full[2];
+  uint64_t item_full[2], item_empty[2];
+  PromptItem item[2];
+  int64_t sums[kScan + 1];
+  uint32_t tmem;
+  int stop;
+};
+
+// Items of sequence i.
+__device__ __forceinline__ int64_t prompt_items(const PromptArgs &p, int64_t i, bool *bad) {
+  const int64_t x0 = p.a.offsets[i], x1 = p.a.offsets[i + 1];
+  if (x0 < 0 || x1 < x0 || x1 > p.a.n_tok) {
+    *bad = true;
+    return 0;
+  }
+  return (x1 - x0 + 2 * p.tile - 1) / (2 * p.tile) * p.a.hkv;
+}
+
+__global__ void __launch_bounds__(kScan) k_prompt_prefix(PromptArgs p) {
+  bool bad = false;
+  int64_t base = 0;
+  for (int64_t i0 = 0; i0 < p.a.n_req; i0 += kScan) {
+    const int n = (int)min((int64_t)kScan, p.a.n_req - i0);
+    base = scan_units<kScan>(n, p.prefix + i0, base, [&](int k) { return prompt_items(p, i0 + k, &bad); });
+  }
+  if (bad) flag(p.a.status, kStatusData);
+}
+
+// bar_wait by a whole warp, the same answer for all lanes.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *stop) {
+  return __all_sync(~0u, bar_wait(bar, parity, stop));
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kPrThreads, 1)
+    k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap map_q,
+             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  extern __shared__ unsigned char raw_prompt[];
+  using Smem = PromptSmem<D>;
+  Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw_prompt) + 1023) & ~(uintptr_t)1023);
+  const AttendArgs &a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.hq / a.hkv;
+  constexpr int kChunk = 128 * 128;  // bytes of 64 elements of a tile's rows
+  if (warp == 8) tmem_alloc(&sm.tmem, 512);
+  if (threadIdx.x == 0) {
+    sm.stop = 0;
+    for (int k = 0; k < 2; ++k) {
+      bar_init(&sm.q_full[k], 1);
+      bar_init(&sm.q_empty[k], 1);
+      bar_init(&sm.s_full[k], 1);
+      bar_init(&sm.p_full[k], 128);
+      bar_init(&sm.o_full[k], 1);
+      bar_init(&sm.item_full[k], 1);
+      bar_init(&sm.item_empty[k], 9);
+    }
+    for (int k = 0; k < kPrStages; ++k) {
+      bar_init(&sm.kv_full[k], 1);
+      bar_init(&sm.kv_empty[k], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  bool bad = false;
+  const int64_t *sums = p.prefix;
+  int64_t items;
+  if (p.given) {
+    items = sums[a.n_req];
+  } else {
+    items = scan_units<kPrThreads>((int)a.n_req, sm.sums, 0, [&](int k) { return prompt_items(p, k, &bad); });
+    sums = sm.sums;
+  }
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = sm.tmem;
+  volatile int *stop = &sm.stop;
+  // columns: scores of tile 0, of tile 1, outputs of tile 0, of tile 1
+  constexpr uint32_t kCols = 128;
+
+  if (warp == 9) {
+    if (lane == 0) {
+      int64_t u = blockIdx.x;
+      int qk[2] = {0, 0};
+      uint32_t kv = 0;
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
+        if (n >= 2) ok = bar_wait(&sm.item_empty[n & 1], ((n >> 1) - 1) & 1, stop);
+        PromptItem &it = sm.item[n & 1];
+        if (!ok) break;
+        if (u >= items) {
+          it.head = -1;
+          bar_arrive(&sm.item_full[n & 1]);
+          break;
+        }
+        const int64_t i = find_unit(sums, a.n_req, u), local = u - sums[i];
+        const int64_t x0 = a.offsets[i], len = a.offsets[i + 1] - x0, pairs = (len + 2 * p.tile - 1) / (2 * p.tile);
+        const int head = (int)(local % a.hkv);
+        const int64_t t0 = (pairs - 1 - local / a.hkv) * 2 * p.tile;
+        it.first = x0;
+        it.seq = i;
+        it.t0 = (int)t0;
+        it.len = (int)len;
+        it.head = head;
+        int blocks[2];
+        for (int k = 0; k < 2; ++k) {
+          const int64_t from = t0 + k * p.tile;
+          const int64_t keys = min(len, from + p.tile);
+          blocks[k] = from >= len ? 0 : (int)((keys + kPrBlock - 1) / kPrBlock);
+          it.n[k] = blocks[k];
+          it.tail[k] = (int)(keys - (int64_t)(blocks[k] - 1) * kPrBlock + 15) >> 4;
+        }
+        bar_arrive(&sm.item_full[n & 1]);
+        u = (int64_t)gridDim.x + (int64_t)atomicAdd(&p.counter[0], 1ull);
+        const int most = max(blocks[0], blocks[1]);
+        for (int j = 0; j < most && ok; ++j) {
+          for (int k = 0; k < 2 && ok; ++k) {
+            // the block's keys, then its values
+            if (j == 0 && blocks[k] > 0) {
+              // the tiles' queries: tile 0's before the first keys, tile 1's after them
+              if (qk[k] > 0) ok = bar_wait(&sm.q_empty[k], (qk[k] - 1) & 1, stop);
+              if (!ok) break;
+              ++qk[k];
+              bar_expect(&sm.q_full[k], (uint32_t)(p.tile * G * D * 2));
+              for (int c = 0; c < D / 64; ++c)
+                tma_load3(sm.q[k] + c * kChunk, &map_q, c * 64, head * G, (int)(x0 + t0 + k * p.tile), &sm.q_full[k]);
+            }
+            const uint32_t st = kv % kPrStages;
+            if (kv >= kPrStages) ok = bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
+            if (!ok) break;
+            ++kv;
+            bar_expect(&sm.kv_full[st], Smem::kTile);
+            for (int c = 0; c < D / 64; ++c)
+              tma_load3(sm.kv[st] + c * kChunk, k == 0 ? &map_k : &map_v, c * 64, head, (int)(x0 + (int64_t)j * kPrBlock),
+                        &sm.kv_full[st]);
+          }
+        }
+      }
+      // no load is in flight when the block ends: what was asked for is waited for
+      for (uint32_t st = 0; st < kPrStages; ++st)
+        if (kv > st) {
+          const uint32_t uses = (kv - st + kPrStages - 1) / kPrStages;
+          bar_wait(&sm.kv_full[st], (uses - 1) & 1, stop);
+        }
+    }
+  } else if (warp == 8) {
+    if (lane == 0) {
+      const bool neg = a.scale < 0.f;
+      const uint32_t id_qk = tc_idesc(128, 0, F16, neg, false), id_pv = tc_idesc(128, D, F16, false, true);
+      uint32_t kv = 0;
+      int used[2] = {0, 0}, ps[2] = {0, 0};
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
+        ok = bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+        if (!ok || sm.item[n & 1].head < 0) break;
+        const int blocks[2] = {sm.item[n & 1].n[0], sm.item[n & 1].n[1]};
+        const int tail[2] = {sm.item[n & 1].tail[0], sm.item[n & 1].tail[1]};
+        bar_arrive(&sm.item_empty[n & 1]);
+        const int most = max(blocks[0], blocks[1]);
+        // scores of tile k, block j; a last block's only as far as the tile sees it
+        auto qk = [&](int k, int j, uint32_t st) {
+          const uint32_t id = id_qk + (j + 1 == blocks[k] ? (uint32_t)(tail[k] * 2) << 17 : (kPrBlock / 8u) << 17);
+          const uint32_t qa = smem_addr(sm.q[k]), ka = smem_addr(sm.kv[st]);
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint32_t off = (c / 4) * kChunk + (c % 4) * 32;
+            tc_mma(tmem + k * kCols, tc_desc(qa + off, 16, 1024), tc_desc(ka + off, 16, 1024), id, c > 0);
+          }
+          tc_commit(&sm.s_full[k]);
+        };
+        auto ring = [&](uint32_t at) { return bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
+        // first scores of both tiles
+        ok = ring(kv);
+        for (int k = 0; k < 2 && ok; ++k) {
+          if (!blocks[k]) continue;
+          ok = bar_wait(&sm.q_full[k], used[k] & 1, stop);
+          if (!ok) break;
+          ++used[k];
+          tc_after_sync();
+          qk(k, 0, kv % kPrStages);
+          if (blocks[k] == 1) tc_commit(&sm.q_empty[k]);
+        }
+        if (!ok) break;
+        tc_commit(&sm.kv_empty[kv % kPrStages]);
+        for (int j = 0; j < most && ok; ++j) {
+          const uint32_t vst = (kv + 1) % kPrStages, kst = (kv + 2) % kPrStages;
+          ok = ring(kv + 1);
+          bool next = false;  // the next keys are there
+          for (int k = 0; k < 2 && ok; ++k) {
+            if (j >= blocks[k]) continue;
+            ok = bar_wait(&sm.p_full[k], ps[k] & 1, stop);
+            if (!ok) break;
+            ++ps[k];
+            tc_after_sync();
+            const uint32_t va = smem_addr(sm.kv[vst]);
+            const int steps = j + 1 == blocks[k] ? tail[k] : kPrBlock / 16;
+            for (int c = 0; c < steps; ++c)
+              tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, tc_desc(va + c * 2048, kChunk, 1024), id_pv, j > 0 || c > 0);
+            if (j + 1 == blocks[k]) {
+              tc_commit(&sm.o_full[k]);
+              continue;
+            }
+            if (!next) ok = ring(kv + 2);
+            if (!ok) break;
+            next = true;
+            qk(k, j + 1, kst);
+            if (j + 2 == blocks[k]) tc_commit(&sm.q_empty[k]);
+          }
+          if (!ok) break;
+          tc_commit(&sm.kv_empty[vst]);
+          if (next) tc_commit(&sm.kv_empty[kst]);
+          kv += 2;
+        }
+      }
+    }
+  } else {
+    const int k = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
+    const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
+    const float sl = fabsf(a.scale);
+    int ss = 0, os = 0;
+    for (int n = 0;; ++n) {
+      if (!warp_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop)) break;
+      const PromptItem it = sm.item[n & 1];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
+      if (it.head < 0) break;
+      const int blocks = it.n[k];
+      if (blocks == 0) continue;
+      const int tok = it.t0 + k * p.tile + row / G;  // the row's token in the sequence
+      const bool valid = row < p.tile * G && tok < it.len;
+      const int lim = valid ? tok + 1 : 0;           // keys that it sees
+      const int all = it.t0 + k * p.tile + 1;        // keys that every row of the tile sees
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      for (int j = 0; j < blocks; ++j) {
+        ok = warp_wait(&sm.s_full[k], ss & 1, stop);
+        if (!ok) break;
+        ++ss;
+        tc_after_sync();
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_load32(s + 32 * c, ts + 32 * c);
+        tmem_wait_load();
+        if ((j + 1) * kPrBlock > all) {
+          const int rel = lim - j * kPrBlock;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= rel) s[c] = 0xff800000u;
+        }
+        float top = m;
+#pragma unroll
+        for (int c = 0; c < 128; c += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+        if (j == 0) {
+          m = top;
+        } else if (__any_sync(~0u, (top - m) * sl > kPrLazy)) {
+          const float up = m == -INFINITY ? 1.f : exp2_fast((m - top) * sl);
+          m = top;
+          l *= up;
+#pragma unroll
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_load32(o, to + c);
+            tmem_wait_load();
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * up);
+            tmem_store32(to + c, o);
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m * sl;
+        float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+        for (int c = 0; c < 128; c += 64) {
+          uint32_t w[32];
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            const float p0 = exp2_fast(__fmaf_rn(__uint_as_float(s[c + 2 * x]), sl, -base));
+            const float p1 = exp2_fast(__fmaf_rn(__uint_as_float(s[c + 2 * x + 1]), sl, -base));
+            l0 += p0;
+            l1 += p1;
+            w[x] = pack_out<F16>(p0, p1);
+          }
+          tmem_store32(ts + c / 2, w);
+        }
+        l += l0 + l1;
+        tmem_wait_store();
+        tc_before_sync();
+        bar_arrive(&sm.p_full[k]);
+      }
+      if (!ok) break;
+      if (!warp_wait(&sm.o_full[k], os & 1, stop)) break;
+      ++os;
+      tc_after_sync();
+      const int64_t t = it.first + tok, h = (int64_t)it.head * G + row % G;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bool nan = false;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        tmem_load32(o, to + c);
+        tmem_wait_load();
+        if (valid) {
+          uint4 *op = reinterpret_cast<uint4 *>((uint16_t *)a.o + (t * a.hq + h) * D + c);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t w[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float v0 = __uint_as_float(o[8 * x + 2 * y]) * inv, v1 = __uint_as_float(o[8 * x + 2 * y + 1]) * inv;
+              nan |= isnan(v0) || isnan(v1);
+              w[y] = pack_out<F16>(v0, v1);
+            }
+            op[x] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (valid && a.lse) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m * sl + log2f(l)) * 0.6931471805599453f;
+      // the outputs are read: the next item's first product may write them (p_full says so, after this)
+      unsigned again = __ballot_sync(~0u, nan);
+      __syncwarp();
+      while (again) {
+        const int r = __ffs(again) - 1;
+        again &= again - 1;
+        const int rt = __shfl_sync(~0u, tok, r);
+        const int rh = __shfl_sync(~0u, (int)h, r);
+        redo_row<D, F16, false>(a, it.first, it.seq, it.first + rt, rh, rt + 1);
+      }
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (sm.stop && threadIdx.x == 0) {
+    flag(a.status, kStatusTimeout);
+    for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // what was issued may still be at work on shared memory
+  }
+  if (bad) flag(a.status, kStatusData);
+  if (threadIdx.x == 0) {
+    // the last CTA out sets the counters back
+    if (atomicAdd(&p.counter[1], 1ull) == gridDim.x - 1) {
+      p.counter[0] = 0;
+      p.counter[1] = 0;
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  if (warp == 8) tmem_free(tmem, 512);
+}
+
+}  // namespace lv
