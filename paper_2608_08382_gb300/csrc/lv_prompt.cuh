@@ -7,10 +7,13 @@
 // all G query heads that share the keys, so the keys are fetched once for the
 // group and few of a tile's scores are masked (a tile spans 128 / G tokens).
 //
-// One CTA a SM, ten warps:
+// One CTA a SM, three warpgroups:
 //   warps 0-3, 4-7  softmax of tile 0 and of tile 1, a row a thread;
 //   warp 8          issues every tcgen05.mma (one lane);
-//   warp 9          takes the items and issues every TMA load (one lane).
+//   warp 9          takes the items and issues every TMA load (one lane); warps 10
+//                   and 11 only fill the warpgroup.
+// A row's 128 scores stay in its thread's registers: the softmax warpgroups take
+// 216 a thread, the third 72, together the 384 x 168 that the block starts with.
 // Tensor memory holds both tiles' scores and outputs, 128 + D columns each.  The
 // weights go back over the scores' columns as 16-bit values and are the second
 // product's A operand from there.  The issue order PV_0(j) QK_0(j+1) PV_1(j)
@@ -33,7 +36,7 @@
 
 namespace lv {
 
-constexpr int kPrThreads = 320;
+constexpr int kPrThreads = 384;
 constexpr int kPrBlock = 128;   // keys of a block
 constexpr int kPrStages = 4;    // blocks of keys or values in shared memory
 constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that weights absorb
@@ -140,8 +143,9 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   // columns: scores of tile 0, of tile 1, outputs of tile 0, of tile 1
   constexpr uint32_t kCols = 128;
 
-  if (warp == 9) {
-    if (lane == 0) {
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 9 && lane == 0) {
       int64_t u = blockIdx.x;
       int qk[2] = {0, 0};
       uint32_t kv = 0;
@@ -204,9 +208,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const uint32_t uses = (kv - st + kPrStages - 1) / kPrStages;
           bar_wait(&sm.kv_full[st], (uses - 1) & 1, stop);
         }
-    }
-  } else if (warp == 8) {
-    if (lane == 0) {
+    } else if (warp == 8 && lane == 0) {
       const bool neg = a.scale < 0.f;
       const uint32_t id_qk = tc_idesc(128, 0, F16, neg, false), id_pv = tc_idesc(128, D, F16, false, true);
       uint32_t kv = 0;
@@ -276,6 +278,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int k = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
     const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
@@ -310,9 +313,13 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           for (int c = 0; c < 128; ++c)
             if (c >= rel) s[c] = 0xff800000u;
         }
-        float top = m;
+        float tops[4] = {m, m, m, m};
 #pragma unroll
-        for (int c = 0; c < 128; c += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+        for (int c = 0; c < 128; c += 8)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            tops[x] = fmaxf(tops[x], fmaxf(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])));
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         if (j == 0) {
           m = top;
         } else if (__any_sync(~0u, (top - m) * sl > kPrLazy)) {
@@ -330,20 +337,24 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           }
         }
         const float base = m == -INFINITY ? 0.f : m * sl;
-        float l0 = 0.f, l1 = 0.f;
+        const uint64_t sl2 = pair(sl, sl), base2 = pair(-base, -base);
+        uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 128; c += 64) {
-          uint32_t w[32];
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t w[16];
 #pragma unroll
-          for (int x = 0; x < 32; ++x) {
-            const float p0 = exp2_fast(__fmaf_rn(__uint_as_float(s[c + 2 * x]), sl, -base));
-            const float p1 = exp2_fast(__fmaf_rn(__uint_as_float(s[c + 2 * x + 1]), sl, -base));
-            l0 += p0;
-            l1 += p1;
+          for (int x = 0; x < 16; ++x) {
+            float p0, p1;
+            unpair(fma2(pair(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), sl2, base2), &p0, &p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            sum[x & 1] = add2(sum[x & 1], pair(p0, p1));
             w[x] = pack_out<F16>(p0, p1);
           }
-          tmem_store32(ts + c / 2, w);
+          tmem_store16(ts + c / 2, w);
         }
+        float l0, l1;
+        unpair(add2(sum[0], sum[1]), &l0, &l1);
         l += l0 + l1;
         tmem_wait_store();
         tc_before_sync();
