@@ -50,8 +50,7 @@ struct PromptArgs {
 };
 
 struct PromptItem {
-  int64_t first;  // the sequence's first token
-  int64_t seq;
+  int first;      // the sequence's first token
   int t0, len;    // first token of the item in the sequence, the sequence's length
   int head;       // key/value head, or -1: no more items
   int n[2];       // key blocks of each tile
@@ -92,11 +91,6 @@ __global__ void __launch_bounds__(kScan) k_prompt_prefix(PromptArgs p) {
   if (bad) flag(p.a.status, kStatusData);
 }
 
-// bar_wait by a whole warp, the same answer for all lanes.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *stop) {
-  return __all_sync(~0u, bar_wait(bar, parity, stop));
-}
-
 template <int D, bool F16>
 __global__ void __launch_bounds__(kPrThreads, 1)
     k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap map_q,
@@ -105,16 +99,17 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   using Smem = PromptSmem<D>;
   Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw_prompt) + 1023) & ~(uintptr_t)1023);
   const AttendArgs &a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.hq / a.hkv;
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = a.hq / a.hkv;
   constexpr int kChunk = 128 * 128;  // bytes of 64 elements of a tile's rows
   if (warp == 8) tmem_alloc(&sm.tmem, 512);
   if (threadIdx.x == 0) {
     sm.stop = 0;
+    sm.item[0].head = sm.item[1].head = -1;
     for (int k = 0; k < 2; ++k) {
       bar_init(&sm.q_full[k], 1);
       bar_init(&sm.q_empty[k], 1);
       bar_init(&sm.s_full[k], 1);
-      bar_init(&sm.p_full[k], 128);
+      bar_init(&sm.p_full[k], 4);
       bar_init(&sm.o_full[k], 1);
       bar_init(&sm.item_full[k], 1);
       bar_init(&sm.item_empty[k], 9);
@@ -138,7 +133,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  const uint32_t tmem = sm.tmem;
+  const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
   volatile int *stop = &sm.stop;
   // columns: scores of tile 0, of tile 1, outputs of tile 0, of tile 1
   constexpr uint32_t kCols = 128;
@@ -147,14 +142,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 9 && lane == 0) {
       int64_t u = blockIdx.x;
-      int qk[2] = {0, 0};
+      int q_used[2] = {0, 0};
       uint32_t kv = 0;
-      bool ok = true;
-      for (int n = 0; ok; ++n) {
-        if (n >= 2) ok = bar_wait(&sm.item_empty[n & 1], ((n >> 1) - 1) & 1, stop);
+      for (int n = 0;; ++n) {
+        if (n >= 2) bar_wait(&sm.item_empty[n & 1], ((n >> 1) - 1) & 1, stop);
         PromptItem &it = sm.item[n & 1];
-        if (!ok) break;
-        if (u >= items) {
+        if (u >= items || *stop) {
           it.head = -1;
           bar_arrive(&sm.item_full[n & 1]);
           break;
@@ -163,12 +156,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         const int64_t x0 = a.offsets[i], len = a.offsets[i + 1] - x0, pairs = (len + 2 * p.tile - 1) / (2 * p.tile);
         const int head = (int)(local % a.hkv);
         const int64_t t0 = (pairs - 1 - local / a.hkv) * 2 * p.tile;
-        it.first = x0;
-        it.seq = i;
+        it.first = (int)x0;
         it.t0 = (int)t0;
         it.len = (int)len;
         it.head = head;
         int blocks[2];
+#pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int64_t from = t0 + k * p.tile;
           const int64_t keys = min(len, from + p.tile);
@@ -179,21 +172,21 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         bar_arrive(&sm.item_full[n & 1]);
         u = (int64_t)gridDim.x + (int64_t)atomicAdd(&p.counter[0], 1ull);
         const int most = max(blocks[0], blocks[1]);
-        for (int j = 0; j < most && ok; ++j) {
-          for (int k = 0; k < 2 && ok; ++k) {
+        for (int j = 0; j < most; ++j) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
             // the block's keys, then its values
             if (j == 0 && blocks[k] > 0) {
               // the tiles' queries: tile 0's before the first keys, tile 1's after them
-              if (qk[k] > 0) ok = bar_wait(&sm.q_empty[k], (qk[k] - 1) & 1, stop);
-              if (!ok) break;
-              ++qk[k];
+              if (q_used[k] > 0) bar_wait(&sm.q_empty[k], (q_used[k] - 1) & 1, stop);
+              ++q_used[k];
               bar_expect(&sm.q_full[k], (uint32_t)(p.tile * G * D * 2));
               for (int c = 0; c < D / 64; ++c)
                 tma_load3(sm.q[k] + c * kChunk, &map_q, c * 64, head * G, (int)(x0 + t0 + k * p.tile), &sm.q_full[k]);
             }
             const uint32_t st = kv % kPrStages;
-            if (kv >= kPrStages) ok = bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
-            if (!ok) break;
+            if (kv >= kPrStages) bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
+            if (*stop) break;
             ++kv;
             bar_expect(&sm.kv_full[st], Smem::kTile);
             for (int c = 0; c < D / 64; ++c)
@@ -204,75 +197,105 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       }
       // no load is in flight when the block ends: what was asked for is waited for
       for (uint32_t st = 0; st < kPrStages; ++st)
-        if (kv > st) {
-          const uint32_t uses = (kv - st + kPrStages - 1) / kPrStages;
-          bar_wait(&sm.kv_full[st], (uses - 1) & 1, stop);
-        }
-    } else if (warp == 8 && lane == 0) {
-      const bool neg = a.scale < 0.f;
-      const uint32_t id_qk = tc_idesc(128, 0, F16, neg, false), id_pv = tc_idesc(128, D, F16, false, true);
-      uint32_t kv = 0;
-      int used[2] = {0, 0}, ps[2] = {0, 0};
-      bool ok = true;
-      for (int n = 0; ok; ++n) {
-        ok = bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
-        if (!ok || sm.item[n & 1].head < 0) break;
-        const int blocks[2] = {sm.item[n & 1].n[0], sm.item[n & 1].n[1]};
-        const int tail[2] = {sm.item[n & 1].tail[0], sm.item[n & 1].tail[1]};
-        bar_arrive(&sm.item_empty[n & 1]);
-        const int most = max(blocks[0], blocks[1]);
-        // scores of tile k, block j; a last block's only as far as the tile sees it
-        auto qk = [&](int k, int j, uint32_t st) {
-          const uint32_t id = id_qk + (j + 1 == blocks[k] ? (uint32_t)(tail[k] * 2) << 17 : (kPrBlock / 8u) << 17);
-          const uint32_t qa = smem_addr(sm.q[k]), ka = smem_addr(sm.kv[st]);
+        if (kv > st) bar_wait(&sm.kv_full[st], ((kv - st + kPrStages - 1) / kPrStages - 1) & 1, stop);
+    } else if (warp == 8) {
+      // One instruction takes 64 clocks and few wait in line, so what this warp does
+      // between two of them soon stops the tensor core.  The loop over whole blocks of
+      // two tiles has one look at a barrier in each gap, constant descriptors and no
+      // decision; what comes before and after it goes through `step`.  (With the
+      // decisions in the loop and waits that answer: 3,900 clocks for a block of both
+      // tiles with the softmax taken out, 2,048 of them the products'.)
+      const uint32_t id_qk = tc_idesc(128, kPrBlock, F16, a.scale < 0.f, false), id_pv = tc_idesc(128, D, F16, false, true);
+      constexpr uint32_t kStep = Smem::kTile >> 4;  // a tile or block on, in a descriptor
+      const uint32_t q_desc = tc_desc(smem_addr(sm.q), 16), k_desc = tc_desc(smem_addr(sm.kv), 16),
+                     v_desc = tc_desc(smem_addr(sm.kv), kChunk);
+      uint32_t kv = 0, q_phase = 0, p_phase = 0;  // p_phase, q_phase: bit k of tile k
+      auto ring = [&](uint32_t at) { bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
+      // scores of tile k on the block at `at`, n steps of 16 keys
+      auto qk = [&](int k, uint32_t at, uint32_t id) {
+        const uint32_t qd = q_desc + k * kStep, kd = k_desc + at % kPrStages * kStep;
 #pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint32_t off = (c / 4) * kChunk + (c % 4) * 32;
-            tc_mma(tmem + k * kCols, tc_desc(qa + off, 16, 1024), tc_desc(ka + off, 16, 1024), id, c > 0);
-          }
-          tc_commit(&sm.s_full[k]);
-        };
-        auto ring = [&](uint32_t at) { return bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
-        // first scores of both tiles
-        ok = ring(kv);
-        for (int k = 0; k < 2 && ok; ++k) {
-          if (!blocks[k]) continue;
-          ok = bar_wait(&sm.q_full[k], used[k] & 1, stop);
-          if (!ok) break;
-          ++used[k];
-          tc_after_sync();
-          qk(k, 0, kv % kPrStages);
-          if (blocks[k] == 1) tc_commit(&sm.q_empty[k]);
+        for (int c = 0; c < D / 16; ++c) {
+          const int off = ((c / 4) * kChunk + (c % 4) * 32) >> 4;
+          tc_mma(tmem + k * kCols, qd + off, kd + off, id, c > 0);
         }
-        if (!ok) break;
-        tc_commit(&sm.kv_empty[kv % kPrStages]);
-        for (int j = 0; j < most && ok; ++j) {
-          const uint32_t vst = (kv + 1) % kPrStages, kst = (kv + 2) % kPrStages;
-          ok = ring(kv + 1);
-          bool next = false;  // the next keys are there
-          for (int k = 0; k < 2 && ok; ++k) {
-            if (j >= blocks[k]) continue;
-            ok = bar_wait(&sm.p_full[k], ps[k] & 1, stop);
-            if (!ok) break;
-            ++ps[k];
-            tc_after_sync();
-            const uint32_t va = smem_addr(sm.kv[vst]);
-            const int steps = j + 1 == blocks[k] ? tail[k] : kPrBlock / 16;
-            for (int c = 0; c < steps; ++c)
-              tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, tc_desc(va + c * 2048, kChunk, 1024), id_pv, j > 0 || c > 0);
-            if (j + 1 == blocks[k]) {
-              tc_commit(&sm.o_full[k]);
-              continue;
-            }
-            if (!next) ok = ring(kv + 2);
-            if (!ok) break;
-            next = true;
-            qk(k, j + 1, kst);
-            if (j + 2 == blocks[k]) tc_commit(&sm.q_empty[k]);
+        tc_commit(&sm.s_full[k]);
+      };
+      for (int n = 0;; ++n) {
+        bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+        const PromptItem &it = sm.item[n & 1];
+        const int head = __shfl_sync(~0u, it.head, 0), n0 = __shfl_sync(~0u, it.n[0], 0), n1 = __shfl_sync(~0u, it.n[1], 0);
+        const int tail0 = __shfl_sync(~0u, it.tail[0], 0), tail1 = __shfl_sync(~0u, it.tail[1], 0);
+        if (__any_sync(~0u, head < 0 || *stop)) break;
+        if (elect_one()) bar_arrive(&sm.item_empty[n & 1]);
+        const int most = max(n0, n1);
+        // the scores of a last block only as far as the tile sees it
+        auto qk_any = [&](int k, int j, uint32_t at) {
+          const bool last = j + 1 == (k ? n1 : n0);
+          const uint32_t id = last ? tc_idesc(128, 0, F16, a.scale < 0.f, false) | (uint32_t)((k ? tail1 : tail0) * 2) << 17 : id_qk;
+          if (elect_one()) {
+            qk(k, at, id);
+            if (last) tc_commit(&sm.q_empty[k]);
           }
-          if (!ok) break;
-          tc_commit(&sm.kv_empty[vst]);
-          if (next) tc_commit(&sm.kv_empty[kst]);
+        };
+        // first scores of both tiles
+        ring(kv);
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+          if (!(k ? n1 : n0)) continue;
+          bar_wait(&sm.q_full[k], q_phase >> k & 1, stop);
+          q_phase ^= 1u << k;
+          qk_any(k, 0, kv);
+        }
+        if (elect_one()) tc_commit(&sm.kv_empty[kv % kPrStages]);
+        ring(kv + 1);
+        int j = 0;
+        for (; j + 2 < min(n0, n1); ++j) {
+          const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
+            tc_after_sync();
+            if (elect_one()) {
+#pragma unroll
+              for (int c = 0; c < kPrBlock / 16; ++c)
+                tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
+              if (k == 1) tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
+            }
+            ring(kv + 2 + k);  // these keys; the next values, for the next turn
+            if (elect_one()) {
+              qk(k, kv + 2, id_qk);
+              if (k == 1) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+            }
+          }
+          p_phase ^= 3;
+          kv += 2;
+        }
+#pragma unroll 1
+        for (; j < most; ++j) {
+          const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
+          ring(kv + 1);
+          if (j + 1 < most) ring(kv + 2);
+#pragma unroll 1
+          for (int k = 0; k < 2; ++k) {
+            const int blocks = k ? n1 : n0;
+            if (j >= blocks) continue;
+            bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
+            p_phase ^= 1u << k;
+            tc_after_sync();
+            const int steps = j + 1 == blocks ? (k ? tail1 : tail0) : kPrBlock / 16;
+            if (elect_one()) {
+#pragma unroll 1
+              for (int c = 0; c < steps; ++c)
+                tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
+              if (j + 1 == blocks) tc_commit(&sm.o_full[k]);
+            }
+            if (j + 1 < blocks) qk_any(k, j + 1, kv + 2);
+          }
+          if (elect_one()) {
+            tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
+            if (j + 1 < most) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+          }
           kv += 2;
         }
       }
@@ -285,22 +308,21 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     const float sl = fabsf(a.scale);
     int ss = 0, os = 0;
     for (int n = 0;; ++n) {
-      if (!warp_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop)) break;
+      bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
       const PromptItem it = sm.item[n & 1];
       __syncwarp();
       if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
-      if (it.head < 0) break;
-      const int blocks = it.n[k];
+      if (__any_sync(~0u, it.head < 0 || *stop)) break;
+      const int blocks = k ? it.n[1] : it.n[0];
       if (blocks == 0) continue;
       const int tok = it.t0 + k * p.tile + row / G;  // the row's token in the sequence
       const bool valid = row < p.tile * G && tok < it.len;
       const int lim = valid ? tok + 1 : 0;           // keys that it sees
       const int all = it.t0 + k * p.tile + 1;        // keys that every row of the tile sees
       float m = -INFINITY, l = 0.f;
-      bool ok = true;
       for (int j = 0; j < blocks; ++j) {
-        ok = warp_wait(&sm.s_full[k], ss & 1, stop);
-        if (!ok) break;
+        bar_wait(&sm.s_full[k], ss & 1, stop);
+        __syncwarp();
         ++ss;
         tc_after_sync();
         uint32_t s[128];
@@ -326,14 +348,14 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           const float up = m == -INFINITY ? 1.f : exp2_fast((m - top) * sl);
           m = top;
           l *= up;
-#pragma unroll
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            tmem_load32(o, to + c);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_load16(o, to + c);
             tmem_wait_load();
 #pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * up);
-            tmem_store32(to + c, o);
+            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * up);
+            tmem_store16(to + c, o);
           }
         }
         const float base = m == -INFINITY ? 0.f : m * sl;
@@ -358,13 +380,14 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         l += l0 + l1;
         tmem_wait_store();
         tc_before_sync();
-        bar_arrive(&sm.p_full[k]);
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.p_full[k]);
       }
-      if (!ok) break;
-      if (!warp_wait(&sm.o_full[k], os & 1, stop)) break;
+      bar_wait(&sm.o_full[k], os & 1, stop);
+      __syncwarp();
       ++os;
       tc_after_sync();
-      const int64_t t = it.first + tok, h = (int64_t)it.head * G + row % G;
+      const int64_t t = (int64_t)it.first + tok, h = (int64_t)it.head * G + row % G;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       bool nan = false;
 #pragma unroll
@@ -396,7 +419,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         again &= again - 1;
         const int rt = __shfl_sync(~0u, tok, r);
         const int rh = __shfl_sync(~0u, (int)h, r);
-        redo_row<D, F16, false>(a, it.first, it.seq, it.first + rt, rh, rt + 1);
+        redo_row<D, F16, false>(a, it.first, 0, (int64_t)it.first + rt, rh, rt + 1);
       }
     }
   }

@@ -31,17 +31,19 @@ __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Waits for the phase of that parity, at most a few seconds.  One wait of a block
-// that runs out sets *stop, and with it every other one of the block ends.
-constexpr int kWaitTries = 1 << 21;
-__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *stop) {
-  if (bar_try(bar, parity)) return true;
-  for (int k = 0; k < kWaitTries; ++k) {
-    if (bar_try(bar, parity)) return true;
-    if ((k & 63) == 63 && *stop) return false;
+// Waits for the phase of that parity, at most a few seconds.  A wait that runs out
+// sets *stop, and every later one of the block ends at once: the block runs on
+// over whatever is there, takes no further work and says at its end that it is
+// void.  So the way through the code never depends on a wait, whose answer would
+// cost the issuing warp more than the look itself.
+constexpr int kWaitTries = (1 << 21) - 1;
+__device__ __forceinline__ void bar_wait(uint64_t *bar, uint32_t parity, volatile int *stop) {
+  if (bar_try(bar, parity)) return;
+#pragma unroll 1
+  for (int k = 0; !bar_try(bar, parity); ++k) {
+    if (k == kWaitTries) *stop = 1;
+    if ((k & 63) == 63 && *stop) return;
   }
-  *stop = 1;
-  return false;
 }
 
 // A box of a tensor [z][y][x] into shared memory; what lies outside the tensor is
@@ -66,25 +68,43 @@ __device__ __forceinline__ void tmem_free(uint32_t at, int columns) {  // one wh
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// True in one lane of a converged warp, the same one each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0;
+}
+
 // The barrier's phase gets one arrival when all that this thread has issued is done.
 __device__ __forceinline__ void tc_commit(uint64_t *bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
-// D (128 rows, tensor memory) (+)= A B^T of one step of 16 along the sum.
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// Shared-memory descriptor of an operand in rows of 128 bytes, swizzled as TMA
+// writes them (16-byte pieces of a row exchanged by the row's place in eight).
+// Groups of eight rows stand 1,024 bytes apart; lead: bytes between neighbouring
+// columns of 64 elements where the rows run along the sum (else unused).
+// Its upper half (group = 1024) is the same for all; the lower one is what moves.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t tc_desc(uint32_t addr, uint32_t lead) {
+  return ((addr >> 4) & 0x3fff) | ((lead >> 4) & 0x3fff) << 16;
+}
+
+// D (128 rows, tensor memory) (+)= A B^T of one step of 16 along the sum; a and b:
+// the lower halves of their descriptors.
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n.reg .pred p;\n.reg .b64 da, db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 da, {%1, %5};\nmov.b64 db, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
       : "memory");
 }
 // The same with A in tensor memory.
-__device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n.reg .pred p;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 db, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
       : "memory");
 }
 
@@ -92,15 +112,6 @@ __device__ __forceinline__ void tc_mma_ta(uint32_t d, uint32_t a, uint64_t b, ui
 __host__ __device__ constexpr uint32_t tc_idesc(int m, int n, bool f16, bool negate_a, bool b_major_n) {
   return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | (negate_a ? 1u << 13 : 0u) | (b_major_n ? 1u << 16 : 0u) |
          ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-
-// Shared-memory descriptor of an operand in rows of 128 bytes, swizzled as TMA
-// writes them (16-byte pieces of a row exchanged by the row's place in eight).
-// group: bytes between groups of eight rows; lead: bytes between neighbouring
-// columns of 64 elements where the rows run along the sum (else unused).
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead, uint32_t group) {
-  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)((lead >> 4) & 0x3fff) << 16) |
-         ((uint64_t)((group >> 4) & 0x3fff) << 32) | (1ull << 46) | (2ull << 61);
 }
 
 #define LV_R32(r, o)                                                                                                  \
@@ -133,6 +144,13 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *r) {
           LV_I32(r, 0),
       "r"(at)
       : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t *r, uint32_t at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at));
 }
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t *r) {
   asm volatile(
