@@ -1,0 +1,578 @@
+// Attention of many query rows over the 8-bit cache (lv_kv_attend): chunks of a
+// prompt on the context before them, and single tokens of wide head groups.
+//
+// As in lv_prompt.cuh two tiles of up to 128 rows (whole tokens with their G query
+// heads) alternate on the tensor core and in softmax.  The products are fp16:
+// four warps turn a block of 128 keys' codes into fp16 (exact) in the layout that
+// TMA would leave, the softmax warps bring their own query rows to fp16 (bf16
+// ones scaled by a power of two to a largest element of 2^14).  A strip of 16 keys
+// lies in one block of the cache; its key scale goes into the factor of its
+// scores, its value scale vs, as vs / ref, to its weights.  ref follows the
+// largest vs once that is past 2^3 ref, as the weights' maximum follows the true
+// one past 2^8: a weight is at most 2^(8 + 4 + 3) then.
+//
+// The blocks of keys of all items stand in one line and every CTA takes an even
+// share of it, so a few long contexts keep every SM busy; an item that several
+// CTAs share leaves a part for each, and k_chunk_join adds them in the line's order.
+#pragma once
+
+#include "lv_decode.cuh"
+#include "lv_prompt.cuh"
+
+namespace lv {
+
+constexpr int kChThreads = 512;
+constexpr int kChScales = 8;       // blocks whose scales are kept: more than the copies run ahead
+constexpr float kChExp = 4.f;      // weights are 2^4 at the maximum they refer to
+constexpr float kChRef = 8.f;      // largest vs / ref
+
+struct ChunkArgs {
+  AttendArgs a;
+  int tile;            // tokens of a tile
+  int least_rows;      // requests of fewer rows are k_attend_decode's
+  int64_t *prefix;     // [n_req + 1] units before each request
+  bool given;
+  float *part;         // [CTAs][2][256][D], then m and l [CTAs][2][256][2]
+  float *part_ml;
+};
+
+template <int D>
+struct ChunkSmem {
+  static constexpr int kTile = 128 * D * 2;
+  unsigned char q[2][kTile];
+  unsigned char kv[kPrStages][kTile];
+  uint64_t q_full[2], q_empty[2], kv_full[kPrStages], kv_empty[kPrStages], s_full[2], p_full[2], o_full[2];
+  uint64_t item_full[2], item_empty[2], scale_full[kChScales];
+  PromptItem item[2];
+  int64_t sums[kScan + 1];
+  float ks[kChScales][8], vs[kChScales][8];  // of a block's strips; ks < 0: hidden
+  int64_t req[2], from[2];  // of each item: its request, its first block
+  int whole[2], slot[2];    // no other CTA has a share of it; where its part goes
+  uint32_t tmem;
+  int stop;
+};
+
+// Pairs of tiles of a request, and blocks of keys of each, counted alike.
+__device__ __forceinline__ int64_t chunk_pairs(const ChunkArgs &c, const Span &s) {
+  const int G = c.a.hq / c.a.hkv;
+  return (int64_t)s.p * G < c.least_rows ? 0 : (s.p + 2 * c.tile - 1) / (2 * c.tile);
+}
+__device__ __forceinline__ int64_t chunk_blocks(const ChunkArgs &c, const Span &s) {
+  return max((int64_t)1, (row_limit(c.a, s, s.p - 1) + kPrBlock - 1) / kPrBlock);
+}
+__device__ __forceinline__ int64_t chunk_units(const ChunkArgs &c, int64_t i, bool *bad) {
+  const Span s = request_span(c.a, i, bad);
+  return s.p == 0 ? 0 : chunk_pairs(c, s) * c.a.hkv * chunk_blocks(c, s);
+}
+
+__global__ void __launch_bounds__(kScan) k_chunk_prefix(ChunkArgs c) {
+  bool bad = false;
+  int64_t base = 0;
+  for (int64_t i0 = 0; i0 < c.a.n_req; i0 += kScan) {
+    const int n = (int)min((int64_t)kScan, c.a.n_req - i0);
+    base = scan_units<kScan>(n, c.prefix + i0, base, [&](int k) { return chunk_units(c, i0 + k, &bad); });
+  }
+  if (bad) flag(c.a.status, kStatusData);
+}
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__ ChunkArgs c) {
+  extern __shared__ unsigned char raw_prompt[];
+  using Smem = ChunkSmem<D>;
+  Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw_prompt) + 1023) & ~(uintptr_t)1023);
+  const AttendArgs &a = c.a;
+  const CacheView &cv = a.cache;
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = a.hq / a.hkv;
+  constexpr int kChunk = 128 * 128;  // bytes of 64 elements of a tile's rows
+  wait_previous();
+  if (warp == 12) tmem_alloc(&sm.tmem, 512);
+  if (threadIdx.x == 0) {
+    sm.stop = 0;
+    sm.item[0].head = sm.item[1].head = -1;
+    for (int k = 0; k < 2; ++k) {
+      bar_init(&sm.q_full[k], 4);
+      bar_init(&sm.q_empty[k], 1);
+      bar_init(&sm.s_full[k], 1);
+      bar_init(&sm.p_full[k], 4);
+      bar_init(&sm.o_full[k], 1);
+      bar_init(&sm.item_full[k], 1);
+      bar_init(&sm.item_empty[k], 13);
+    }
+    for (int k = 0; k < kPrStages; ++k) {
+      bar_init(&sm.kv_full[k], 4);
+      bar_init(&sm.kv_empty[k], 1);
+    }
+    for (int k = 0; k < kChScales; ++k) bar_init(&sm.scale_full[k], 4);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  bool bad = false;
+  const int64_t *sums = c.prefix;
+  int64_t units;
+  if (c.given) {
+    units = sums[a.n_req];
+  } else {
+    units = scan_units<kChThreads>((int)a.n_req, sm.sums, 0, [&](int k) { return chunk_units(c, k, &bad); });
+    sums = sm.sums;
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i <= a.n_req; i += kChThreads) c.prefix[i] = sm.sums[i];
+  }
+  let_next();
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
+  volatile int *stop = &sm.stop;
+  constexpr uint32_t kCols = 128;
+
+  if (warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 12) {
+      issue_products<D, true>(sm, tmem, a.scale < 0.f, stop);
+    } else if (warp == 13 && lane == 0) {
+      // the CTA's share of the line, an item or a part of one at a time
+      const int64_t end = warp_start(blockIdx.x + 1, gridDim.x, units), begin = warp_start(blockIdx.x, gridDim.x, units);
+      int64_t u = begin;
+      for (int n = 0;; ++n) {
+        if (n >= 2) bar_wait(&sm.item_empty[n & 1], ((n >> 1) - 1) & 1, stop);
+        PromptItem &it = sm.item[n & 1];
+        if (u >= end || *stop) {
+          it.head = -1;
+          bar_arrive(&sm.item_full[n & 1]);
+          break;
+        }
+        bool ignore = false;
+        const int64_t i = find_unit(sums, a.n_req, u);
+        const Span sp = request_span(a, i, &ignore);
+        const int64_t blocks = chunk_blocks(c, sp), local = u - sums[i], seg = local / blocks;
+        const int64_t b0 = local % blocks, b1 = min(blocks, b0 + end - u);
+        const int t0 = (int)(seg / a.hkv) * 2 * c.tile;
+        it.first = (int)sp.first;
+        it.t0 = t0;
+        it.len = sp.p;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int from = t0 + k * c.tile, last = min(sp.p, from + c.tile) - 1;
+          int64_t n_all = 0, keys = 0;
+          if (from < sp.p) {
+            keys = row_limit(a, sp, last);
+            n_all = max((int64_t)1, (keys + kPrBlock - 1) / kPrBlock);
+          }
+          const int64_t top = min(n_all, b1);
+          it.n[k] = (int)max((int64_t)0, top - b0);
+          it.tail[k] = top == n_all ? (int)max((int64_t)1, (keys - (n_all - 1) * kPrBlock + 15) >> 4) : kPrBlock / 16;
+        }
+        sm.req[n & 1] = i;
+        sm.from[n & 1] = b0;
+        sm.whole[n & 1] = b0 == 0 && b1 == blocks;
+        sm.slot[n & 1] = (int)blockIdx.x * 2 + (u == begin ? 0 : 1);
+        it.head = (int)(seg % a.hkv);
+        bar_arrive(&sm.item_full[n & 1]);
+        u += b1 - b0;
+      }
+    }
+  } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    // Codes to fp16, two strips of each block a warp: eight lanes a key, so that a
+    // key's D bytes are read together; of the two pieces of 16 bytes that a lane's
+    // codes become the upper half of the lanes stores the second one first, and no
+    // two lanes of a quarter warp meet in a bank.
+    constexpr int kLanes = D / 16, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads of two strips
+    const int w = warp - 8, sub = lane % kLanes, key_of = lane / kLanes;
+    uint32_t kv = 0, block = 0;
+    for (int n = 0;; ++n) {
+      bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+      const int head = sm.item[n & 1].head, most = max(sm.item[n & 1].n[0], sm.item[n & 1].n[1]);
+      const int64_t i = sm.req[n & 1], from = sm.from[n & 1];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
+      if (__any_sync(~0u, head < 0 || *stop)) break;
+      bool ignore = false;
+      const Span sp = request_span(a, i, &ignore);
+      const int64_t keys = row_limit(a, sp, sp.p - 1);
+      // blocks and scales of 32 strips (16 blocks) at a time, a strip a lane, the next 32 ahead
+      int32_t id[2];
+      float ks[2], vs[2];
+      auto look_up = [&](int set, int m) {
+        const int64_t strip = (from + (m + lane) / 2) * 8 + 2 * w + (lane & 1);
+        id[set] = -1;
+        ks[set] = vs[set] = 0.f;
+        if ((m + lane) / 2 < most && strip * 16 < keys) {
+          int32_t b = a.table[i * a.width + ((strip * 16) >> cv.log_b)];
+          if (b < -1 || b >= cv.n_blocks) {
+            bad = true;
+            b = -1;
+          }
+          id[set] = b;
+          if (b >= 0) {
+            ks[set] = cv.k_scale[(int64_t)b * cv.heads + head];
+            vs[set] = cv.v_scale[(int64_t)b * cv.heads + head];
+          }
+        }
+      };
+      uint4 code[2][kSteps];
+      // the two strips of block j: keys or values
+      auto fetch = [&](int to, int j, bool values) {
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x) {
+          const int key = x * kKeys + key_of;  // of the warp's 32
+          const int32_t b = __shfl_sync(~0u, id[0], (2 * j + (key >> 4)) & 31);
+          const int64_t pos = (from + j) * kPrBlock + 32 * w + key;
+          code[to][x] = make_uint4(0, 0, 0, 0);
+          if (b >= 0 && pos < keys)
+            code[to][x] = load16((values ? cv.v : cv.k) +
+                                 ((((int64_t)b * cv.heads + head) << cv.log_b) + (pos & ((1 << cv.log_b) - 1))) * D + sub * 16);
+        }
+      };
+      auto put = [&](int from_set, uint32_t flip) {
+        const uint32_t st = kv % kPrStages;
+        if (kv >= kPrStages) bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x) {
+          const int key = x * kKeys + key_of, row = 32 * w + key;
+          const uint4 q = code[from_set][x];
+          const uint32_t f = flip >> (16 * (key >> 4)) & 1 ? 0x80808080u : 0u;
+          const uint32_t y[4] = {q.x ^ f, q.y ^ f, q.z ^ f, q.w ^ f};
+          uint4 h[2];
+          h[0] = make_uint4(lo_half2(y[0]), hi_half2(y[0]), lo_half2(y[1]), hi_half2(y[1]));
+          h[1] = make_uint4(lo_half2(y[2]), hi_half2(y[2]), lo_half2(y[3]), hi_half2(y[3]));
+          unsigned char *to = sm.kv[st] + (sub / 4) * kChunk + row * 128;
+          const int first = sub >= 4 ? 1 : 0, piece = (sub % 4) * 2;
+          const uint4 ha = first ? h[1] : h[0], hb = first ? h[0] : h[1];
+          *reinterpret_cast<uint4 *>(to + (((piece + first) ^ (row & 7)) << 4)) = ha;
+          *reinterpret_cast<uint4 *>(to + (((piece + 1 - first) ^ (row & 7)) << 4)) = hb;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.kv_full[st]);
+        ++kv;
+      };
+      if (most > 0) {
+        look_up(0, 0);
+        look_up(1, 32);
+        fetch(0, 0, false);
+      }
+      for (int j = 0; j < most; ++j) {
+        // a negative key scale goes into the codes' signs
+        const bool hidden = id[0] < 0, minus = ks[0] < 0.f;
+        const uint32_t flips = __ballot_sync(~0u, minus) >> ((2 * j) & 31);
+        if ((lane >> 1) == (j & 15)) {
+          sm.ks[block % kChScales][2 * w + (lane & 1)] = hidden ? -1.f : fabsf(ks[0]);
+          sm.vs[block % kChScales][2 * w + (lane & 1)] = vs[0];
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.scale_full[block % kChScales]);
+        ++block;
+        fetch(1, j, true);
+        put(0, (flips & 1) | (flips >> 1 & 1) << 16);
+        if ((j & 15) == 15) {
+          id[0] = id[1], ks[0] = ks[1], vs[0] = vs[1];
+          look_up(1, 2 * (j + 1) + 32);
+        }
+        if (j + 1 < most) fetch(0, j + 1, false);
+        put(1, 0);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    const int k = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
+    const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
+    uint32_t ss = 0, qs = 0, os = 0, block = 0;
+    for (int n = 0;; ++n) {
+      bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+      const PromptItem it = sm.item[n & 1];
+      const int64_t i = sm.req[n & 1], from = sm.from[n & 1];
+      const bool whole = sm.whole[n & 1];
+      const int slot = sm.slot[n & 1];
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
+      if (__any_sync(~0u, it.head < 0 || *stop)) break;
+      const int blocks = k ? it.n[1] : it.n[0], most = max(it.n[0], it.n[1]);
+      const uint32_t block0 = block;
+      block += most;
+      const int tok = it.t0 + k * c.tile + row / G, h = it.head * G + row % G;
+      const bool valid = row < c.tile * G && tok < it.len;
+      float m = -INFINITY, l = 0.f, ref = 0.f, inv_ref = 0.f;
+      int64_t lim = 0;  // keys that the row sees
+      if (blocks > 0) {
+        bool ignore = false;
+        const Span sp = request_span(a, i, &ignore);
+        lim = valid ? row_limit(a, sp, tok) : 0;
+        const int64_t all = row_limit(a, sp, it.t0 + k * c.tile);  // what every row of the tile sees
+        // the row's query
+        float sl = fabsf(a.scale);
+        if (qs > 0) bar_wait(&sm.q_empty[k], (qs - 1) & 1, stop);
+        __syncwarp();
+        {
+          const uint16_t *qp = (const uint16_t *)a.q + ((int64_t)it.first + tok) * a.q_stride + (int64_t)h * D;
+          uint4 x[D / 8];
+#pragma unroll
+          for (int y = 0; y < D / 8; ++y) x[y] = valid ? reinterpret_cast<const uint4 *>(qp)[y] : make_uint4(0, 0, 0, 0);
+          float up = 1.f;
+          if (!F16) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int y = 0; y < D / 8; ++y) {
+              const uint32_t v[4] = {x[y].x, x[y].y, x[y].z, x[y].w};
+#pragma unroll
+              for (int z = 0; z < 4; ++z) top = max(top, max(v[z] & 0x7fff0000u, (v[z] & 0x7fffu) << 16));
+            }
+            const int e = top ? min(max((int)(top >> 23) - 127, -100), 127) : 14;  // 2^e <= largest < 2^(e+1)
+            up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+            sl *= __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+          }
+#pragma unroll
+          for (int y = 0; y < D / 8; ++y) {
+            if (!F16) {
+              uint32_t v[4] = {x[y].x, x[y].y, x[y].z, x[y].w};
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const float2 f = unpack2<false>(v[z]);
+                v[z] = pack_half2(f.x * up, f.y * up);
+              }
+              x[y] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+            *reinterpret_cast<uint4 *>(sm.q[k] + (y / 8) * kChunk + row * 128 + (((y % 8) ^ (row & 7)) << 4)) = x[y];
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sm.q_full[k]);
+          ++qs;
+        }
+        for (int j = 0; j < blocks; ++j) {
+          const uint32_t b = block0 + j;
+          bar_wait(&sm.s_full[k], ss & 1, stop);
+          ++ss;
+          // the scores are there, so the scales are: this look never waits (before the
+          // scores it could take an older phase of the barrier for this one)
+          bar_wait(&sm.scale_full[b % kChScales], (b / kChScales) & 1, stop);
+          float f[8], vr[8];  // a strip's factor of scores and of weights
+          bool hidden = false;
+          float top_vs = 0.f;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            f[x] = sm.ks[b % kChScales][x];
+            vr[x] = sm.vs[b % kChScales][x];
+            hidden |= f[x] < 0.f;
+            top_vs = fmaxf(top_vs, fabsf(vr[x]));
+          }
+          __syncwarp();
+          tc_after_sync();
+          uint32_t s[128];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) tmem_load32(s + 32 * x, ts + 32 * x);
+          tmem_wait_load();
+          if (hidden) {
+#pragma unroll
+            for (int x = 0; x < 128; ++x)
+              if (f[x / 16] < 0.f) s[x] = 0xff800000u;
+          }
+          if ((from + j + 1) * kPrBlock > all) {
+            const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
+#pragma unroll
+            for (int x = 0; x < 128; ++x)
+              if (x >= rel) s[x] = 0xff800000u;
+          }
+          float top = m;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            f[x] = f[x] < 0.f ? sl : f[x] * sl;
+            float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < 16; y += 4) {
+              t0 = fmaxf(t0, fmaxf(__uint_as_float(s[16 * x + y]), __uint_as_float(s[16 * x + y + 1])));
+              t1 = fmaxf(t1, fmaxf(__uint_as_float(s[16 * x + y + 2]), __uint_as_float(s[16 * x + y + 3])));
+            }
+            // a factor of zero must leave what is masked at -infinity
+            f[x] = f[x] == 0.f ? 1e-37f : f[x];
+            top = fmaxf(top, fmaxf(t0, t1) * f[x]);
+          }
+          const bool grow_ref = !(top_vs <= kChRef * ref);
+          if (j == 0) {
+            m = top;
+            ref = top_vs;
+            inv_ref = ref > 0.f ? 1.f / ref : 0.f;
+          } else if (__any_sync(~0u, top - m > kPrLazy || grow_ref)) {
+            const float up = m == -INFINITY ? 1.f : exp2_fast(m - top);
+            m = top;
+            l *= up;
+            const float nref = fmaxf(ref, top_vs), shrink = ref > 0.f ? up * (ref / nref) : up;
+            ref = nref;
+            inv_ref = ref > 0.f ? 1.f / ref : 0.f;
+#pragma unroll 1
+            for (int x = 0; x < D; x += 16) {
+              uint32_t o[16];
+              tmem_load16(o, to + x);
+              tmem_wait_load();
+#pragma unroll
+              for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * shrink);
+              tmem_store16(to + x, o);
+            }
+          }
+          const float base = m == -INFINITY ? -kChExp : m - kChExp;
+          const uint64_t base2 = pair(-base, -base);
+          uint64_t sum[2] = {0, 0};
+#pragma unroll
+          for (int x = 0; x < 128; x += 32) {
+            uint32_t w[16];
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+              const int strip = (x + 2 * y) / 16;
+              float p0, p1;
+              unpair(fma2(pair(__uint_as_float(s[x + 2 * y]), __uint_as_float(s[x + 2 * y + 1])), pair(f[strip], f[strip]), base2),
+                     &p0, &p1);
+              const uint64_t pp = pair(exp2_fast(p0), exp2_fast(p1));
+              sum[y & 1] = add2(sum[y & 1], pp);
+              const float r = vr[strip] * inv_ref;
+              unpair(mul2(pp, pair(r, r)), &p0, &p1);
+              w[y] = pack_half2(p0, p1);
+            }
+            tmem_store16(ts + x / 2, w);
+          }
+          float l0, l1;
+          unpair(add2(sum[0], sum[1]), &l0, &l1);
+          l += l0 + l1;
+          tmem_wait_store();
+          tc_before_sync();
+          __syncwarp();
+          if (lane == 0) bar_arrive(&sm.p_full[k]);
+        }
+        bar_wait(&sm.o_full[k], os & 1, stop);
+        ++os;
+        __syncwarp();
+        tc_after_sync();
+      }
+      const int64_t t = (int64_t)it.first + tok;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int64_t at = (int64_t)slot * 256 + k * 128 + row;
+      bool nan = false;
+      if (blocks > 0) {
+#pragma unroll 1
+        for (int x = 0; x < D; x += 16) {
+          uint32_t o[16];
+          tmem_load16(o, to + x);
+          tmem_wait_load();
+          if (!valid) continue;
+          if (whole) {
+            uint4 *op = reinterpret_cast<uint4 *>((uint16_t *)a.o + (t * a.hq + h) * D + x);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              uint32_t w[4];
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const float v0 = __uint_as_float(o[8 * y + 2 * z]) * inv * ref, v1 = __uint_as_float(o[8 * y + 2 * z + 1]) * inv * ref;
+                nan |= isnan(v0) || isnan(v1);
+                w[z] = pack_out<F16>(v0, v1);
+              }
+              op[y] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          } else {
+            float4 *pp = reinterpret_cast<float4 *>(c.part + at * D + x);
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              pp[y] = make_float4(__uint_as_float(o[4 * y]) * ref, __uint_as_float(o[4 * y + 1]) * ref,
+                                  __uint_as_float(o[4 * y + 2]) * ref, __uint_as_float(o[4 * y + 3]) * ref);
+          }
+        }
+      }
+      if (valid && whole && a.lse)
+        a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m - kChExp + log2f(l)) * 0.6931471805599453f;
+      if (!whole) *reinterpret_cast<float2 *>(c.part_ml + 2 * at) = make_float2(m, l);
+      unsigned again = __ballot_sync(~0u, nan);
+      __syncwarp();
+      while (again) {
+        const int r = __ffs(again) - 1;
+        again &= again - 1;
+        const int rt = __shfl_sync(~0u, tok, r), rh = __shfl_sync(~0u, h, r);
+        const int64_t rl = __shfl_sync(~0u, lim, r);
+        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl);
+      }
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (sm.stop && threadIdx.x == 0) flag(a.status, kStatusTimeout);
+  if (sm.stop)
+    for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // products that were issued may still read shared memory
+  if (bad) flag(a.status, kStatusData);
+  __syncthreads();
+  if (warp == 12) tmem_free(tmem, 512);
+}
+
+// The items that several CTAs shared: a warp a row adds its parts in the line's
+// order.  A part whose keys the row does not see has l = 0 and no sums.
+template <int D, bool F16>
+__global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
+  constexpr int E = D / 32, kBatch = 4;
+  const AttendArgs &a = c.a;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, G = a.hq / a.hkv;
+  wait_previous();
+  const int64_t units = c.prefix[a.n_req], i = blockIdx.x;
+  if (c.prefix[i + 1] == c.prefix[i]) return;
+  bool ignore = false;
+  const Span sp = request_span(a, i, &ignore);
+  const int64_t blocks = chunk_blocks(c, sp), items = chunk_pairs(c, sp) * a.hkv;
+  for (int64_t y = blockIdx.y; y < items * 32; y += gridDim.y) {
+    const int64_t seg = y / 32, u0 = c.prefix[i] + seg * blocks;
+    const int64_t w0 = warp_of(u0, ctas, units), w1 = warp_of(u0 + blocks - 1, ctas, units);
+    if (w0 == w1) continue;
+    const int r = (int)(y % 32) * 8 + w, row = r & 127, k = r >> 7;
+    const int tok = (int)(seg / a.hkv) * 2 * c.tile + k * c.tile + row / G, h = (int)(seg % a.hkv) * G + row % G;
+    if (row >= c.tile * G || tok >= sp.p) continue;
+    float top = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int64_t x0 = w0; x0 <= w1; x0 += kBatch) {
+      float pm[kBatch], pl[kBatch], po[kBatch][E], nm = top;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int64_t x = x0 + b;
+        pm[b] = -INFINITY, pl[b] = 0.f;
+        if (x <= w1) {
+          const int64_t at = (x * 2 + (x == w0 && warp_start(x, ctas, units) < u0 ? 1 : 0)) * 256 + r;
+          const float2 ml = *reinterpret_cast<const float2 *>(c.part_ml + 2 * at);
+          pm[b] = ml.x, pl[b] = ml.y;
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const float2 v = *reinterpret_cast<const float2 *>(c.part + at * D + lane * E + e);
+            po[b][e] = v.x, po[b][e + 1] = v.y;
+          }
+        }
+        nm = fmaxf(nm, pm[b]);
+      }
+      const float base = nm == -INFINITY ? 0.f : nm, up = top == -INFINITY ? 1.f : exp2_fast(top - base);
+      l *= up;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= up;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (pl[b] == 0.f) continue;
+        const float f = pm[b] == -INFINITY ? 1.f : exp2_fast(pm[b] - base);
+        l += pl[b] * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += po[b][e] * f;
+      }
+      top = nm;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t t = sp.first + tok;
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      *reinterpret_cast<uint32_t *>((uint16_t *)a.o + (t * a.hq + h) * D + lane * E + e) = pack_out<F16>(o[e] * inv, o[e + 1] * inv);
+      nan |= isnan(o[e]) || isnan(o[e + 1]);
+    }
+    if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (top - kChExp + log2f(l)) * 0.6931471805599453f;
+    if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok));
+  }
+}
+
+}  // namespace lv

@@ -35,12 +35,14 @@ namespace lv {
 
 constexpr int kDecWarps = 4;       // warps of a CTA; they share only the scan
 constexpr int kDecMinStrips = 8;   // strips a warp takes at least
+constexpr int kDecRows = 16;       // rows of a request that go here: two row tiles of 8
 constexpr int kJoinWarps = 8;
 constexpr float kWeightExp = 12.f;
 
 struct DecodeArgs {
   AttendArgs a;
   int nt;               // row tiles of 8 nt rows
+  int most_rows;        // requests of more rows are k_chunk's
   int64_t warps;        // warps launched
   int64_t *prefix;      // [n_req + 1] strips before each request
   bool given;           // prefix is there already, not formed here
@@ -97,7 +99,7 @@ __device__ __forceinline__ int span_tiles(const AttendArgs &a, const Span &s, in
 
 __device__ __forceinline__ int64_t request_units(const DecodeArgs &d, int64_t i, bool *bad) {
   const Span s = request_span(d.a, i, bad);
-  return s.p == 0 ? 0 : span_strips(d.a, s) * span_tiles(d.a, s, 8 * d.nt) * d.a.hkv;
+  return s.p == 0 || (int64_t)s.p * (d.a.hq / d.a.hkv) > d.most_rows ? 0 : span_strips(d.a, s) * span_tiles(d.a, s, 8 * d.nt) * d.a.hkv;
 }
 
 // The running sums of more than kScan requests, by one CTA.
@@ -468,7 +470,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
   const int64_t i = blockIdx.x;
   bool ignore = false;
   const Span sp = request_span(a, i, &ignore);
-  if (sp.p == 0) return;
+  if (d.prefix[i + 1] == d.prefix[i]) return;
   const int64_t strips = span_strips(a, sp);
   const int tiles = span_tiles(a, sp, rows), groups = per_row == 1 ? rows / kJoinWarps : rows;
   for (int64_t y = blockIdx.y; y < (int64_t)tiles * a.hkv * groups; y += gridDim.y) {

@@ -8,6 +8,7 @@
 
 #include "llmvisor.h"
 #include "lv_attend.cuh"
+#include "lv_chunk.cuh"
 #include "lv_decode.cuh"
 #include "lv_kv.h"
 #include "lv_kv_plan.cuh"
@@ -89,6 +90,7 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   DecodeArgs d{};
   d.a = a;
   d.nt = NT;
+  d.most_rows = kDecRows;
   const int64_t ctas = (int64_t)kv->sms * kPerSm;
   d.warps = ctas * kDecWarps;
   // scratch: running sums, the parts
@@ -116,8 +118,46 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
 }
 
 template <int D, bool F16>
-lv_status run_decode_rows(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
-  return !a.offsets && a.hq / a.hkv <= 8 ? run_decode<D, F16, 1>(kv, a, stream) : run_decode<D, F16, 2>(kv, a, stream);
+lv_status run_chunk(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
+  ChunkArgs c{};
+  c.a = a;
+  if (c.a.scale == 0.f) c.a.scale = 1e-37f;  // a masked score is -infinity: its product with the scale must be too
+  const int G = a.hq / a.hkv, ctas = kv->sms;
+  c.tile = 128 / G;
+  c.least_rows = kDecRows + 1;
+  const size_t o_part = (8 * ((size_t)a.n_req + 1) + 255) & ~(size_t)255;
+  const size_t slots = 2 * (size_t)ctas * 256;
+  lv_status st = scratch_for(kv, o_part + slots * (D + 2) * sizeof(float));
+  if (st != LV_OK) return st;
+  c.prefix = reinterpret_cast<int64_t *>(kv->scratch);
+  c.part = reinterpret_cast<float *>(kv->scratch + o_part);
+  c.part_ml = c.part + slots * D;
+  c.given = a.n_req > kScan;
+  if (c.given) {
+    k_chunk_prefix<<<1, kScan, 0, stream>>>(c);
+    LV_CUDA(cudaGetLastError());
+  }
+  constexpr size_t smem = sizeof(ChunkSmem<D>) + 1024;
+  LV_CUDA(cudaFuncSetAttribute(k_chunk<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  k_chunk<D, F16><<<(unsigned)ctas, kChThreads, smem, stream>>>(c);
+  LV_CUDA(cudaGetLastError());
+  const int64_t y = (a.n_tok / (2 * c.tile) + 1) * a.hkv * 32;  // rows of eight of the longest request there can be
+  return launch_after(k_chunk_join<D, F16>, dim3((unsigned)a.n_req, (unsigned)std::min<int64_t>(y, 2048)), 256, 0, stream,
+                      c, ctas);
+}
+
+// Requests of up to kDecRows rows (new tokens times query heads of a key/value
+// head) by k_attend_decode, others by k_chunk.  Where every request has one token
+// all are of one kind; else the device's offsets say, and both go over the
+// requests, each taking its own.
+template <int D, bool F16>
+lv_status run_cached(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
+  const int64_t G = a.hq / a.hkv, most = (a.offsets ? a.n_tok : 1) * G;  // rows of a request, at most
+  if (G <= kDecRows) {
+    const lv_status st = !a.offsets && G <= 8 ? run_decode<D, F16, 1>(kv, a, stream) : run_decode<D, F16, 2>(kv, a, stream);
+    if (st != LV_OK) return st;
+  }
+  return most > kDecRows ? run_chunk<D, F16>(kv, a, stream) : LV_OK;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -309,8 +349,8 @@ lv_status lv_kv_attend(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, int
   a.status = kv->d_status;
   cudaStream_t stream = (cudaStream_t)stream_;
   if (cache->head_dim == 128)
-    return dtype == LV_F16 ? run_decode_rows<128, true>(kv, a, stream) : run_decode_rows<128, false>(kv, a, stream);
-  return dtype == LV_F16 ? run_decode_rows<64, true>(kv, a, stream) : run_decode_rows<64, false>(kv, a, stream);
+    return dtype == LV_F16 ? run_cached<128, true>(kv, a, stream) : run_cached<128, false>(kv, a, stream);
+  return dtype == LV_F16 ? run_cached<64, true>(kv, a, stream) : run_cached<64, false>(kv, a, stream);
 }
 
 lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -91,6 +91,114 @@ __global__ void __launch_bounds__(kScan) k_prompt_prefix(PromptArgs p) {
   if (bad) flag(p.a.status, kStatusData);
 }
 
+// The warp that issues every product, for kernels of two tiles of rows.
+// One instruction takes 64 clocks and few wait in line, so what this warp does
+// between two of them soon stops the tensor core.  The loop over whole blocks of
+// two tiles has one look at a barrier in each gap, constant descriptors and no
+// decision; what comes before and after it goes through `step`.  (With the
+// decisions in the loop and waits that answer: 3,900 clocks for a block of both
+// tiles with the softmax taken out, 2,048 of them the products'.)
+template <int D, bool F16, class Smem>
+__device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool negate, volatile int *stop) {
+  constexpr uint32_t kCols = 128;      // columns of a tile's scores
+  constexpr int kChunk = 128 * 128;    // bytes of 64 elements of a tile's rows
+  const uint32_t id_qk = tc_idesc(128, kPrBlock, F16, negate, false), id_pv = tc_idesc(128, D, F16, false, true);
+  constexpr uint32_t kStep = (128 * D * 2) >> 4;  // a tile or block on, in a descriptor
+  const uint32_t q_desc = tc_desc(smem_addr(sm.q), 16), k_desc = tc_desc(smem_addr(sm.kv), 16),
+                 v_desc = tc_desc(smem_addr(sm.kv), kChunk);
+  uint32_t kv = 0, q_phase = 0, p_phase = 0;  // p_phase, q_phase: bit k of tile k
+  auto ring = [&](uint32_t at) { bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
+  // scores of tile k on the block at `at`, n steps of 16 keys
+  auto qk = [&](int k, uint32_t at, uint32_t id) {
+    const uint32_t qd = q_desc + k * kStep, kd = k_desc + at % kPrStages * kStep;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      const int off = ((c / 4) * kChunk + (c % 4) * 32) >> 4;
+      tc_mma(tmem + k * kCols, qd + off, kd + off, id, c > 0);
+    }
+    tc_commit(&sm.s_full[k]);
+  };
+  for (int n = 0;; ++n) {
+    bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+    const PromptItem &it = sm.item[n & 1];
+    const int head = __shfl_sync(~0u, it.head, 0), n0 = __shfl_sync(~0u, it.n[0], 0), n1 = __shfl_sync(~0u, it.n[1], 0);
+    const int tail0 = __shfl_sync(~0u, it.tail[0], 0), tail1 = __shfl_sync(~0u, it.tail[1], 0);
+    if (__any_sync(~0u, head < 0 || *stop)) break;
+    if (elect_one()) bar_arrive(&sm.item_empty[n & 1]);
+    const int most = max(n0, n1);
+    if (most == 0) continue;
+    // the scores of a last block only as far as the tile sees it
+    auto qk_any = [&](int k, int j, uint32_t at) {
+      const bool last = j + 1 == (k ? n1 : n0);
+      const uint32_t id = last ? tc_idesc(128, 0, F16, negate, false) | (uint32_t)((k ? tail1 : tail0) * 2) << 17 : id_qk;
+      if (elect_one()) {
+        qk(k, at, id);
+        if (last) tc_commit(&sm.q_empty[k]);
+      }
+    };
+    // first scores of both tiles
+    ring(kv);
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      if (!(k ? n1 : n0)) continue;
+      bar_wait(&sm.q_full[k], q_phase >> k & 1, stop);
+      q_phase ^= 1u << k;
+      qk_any(k, 0, kv);
+    }
+    if (elect_one()) tc_commit(&sm.kv_empty[kv % kPrStages]);
+    ring(kv + 1);
+    int j = 0;
+    for (; j + 2 < min(n0, n1); ++j) {
+      const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
+        tc_after_sync();
+        if (elect_one()) {
+#pragma unroll
+          for (int c = 0; c < kPrBlock / 16; ++c)
+            tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
+          if (k == 1) tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
+        }
+        ring(kv + 2 + k);  // these keys; the next values, for the next turn
+        if (elect_one()) {
+          qk(k, kv + 2, id_qk);
+          if (k == 1) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+        }
+      }
+      p_phase ^= 3;
+      kv += 2;
+    }
+#pragma unroll 1
+    for (; j < most; ++j) {
+      const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
+      ring(kv + 1);
+      if (j + 1 < most) ring(kv + 2);
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k) {
+        const int blocks = k ? n1 : n0;
+        if (j >= blocks) continue;
+        bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
+        p_phase ^= 1u << k;
+        tc_after_sync();
+        const int steps = j + 1 == blocks ? (k ? tail1 : tail0) : kPrBlock / 16;
+        if (elect_one()) {
+#pragma unroll 1
+          for (int c = 0; c < steps; ++c)
+            tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
+          if (j + 1 == blocks) tc_commit(&sm.o_full[k]);
+        }
+        if (j + 1 < blocks) qk_any(k, j + 1, kv + 2);
+      }
+      if (elect_one()) {
+        tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
+        if (j + 1 < most) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+      }
+      kv += 2;
+    }
+  }
+}
+
 template <int D, bool F16>
 __global__ void __launch_bounds__(kPrThreads, 1)
     k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap map_q,
@@ -199,106 +307,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       for (uint32_t st = 0; st < kPrStages; ++st)
         if (kv > st) bar_wait(&sm.kv_full[st], ((kv - st + kPrStages - 1) / kPrStages - 1) & 1, stop);
     } else if (warp == 8) {
-      // One instruction takes 64 clocks and few wait in line, so what this warp does
-      // between two of them soon stops the tensor core.  The loop over whole blocks of
-      // two tiles has one look at a barrier in each gap, constant descriptors and no
-      // decision; what comes before and after it goes through `step`.  (With the
-      // decisions in the loop and waits that answer: 3,900 clocks for a block of both
-      // tiles with the softmax taken out, 2,048 of them the products'.)
-      const uint32_t id_qk = tc_idesc(128, kPrBlock, F16, a.scale < 0.f, false), id_pv = tc_idesc(128, D, F16, false, true);
-      constexpr uint32_t kStep = Smem::kTile >> 4;  // a tile or block on, in a descriptor
-      const uint32_t q_desc = tc_desc(smem_addr(sm.q), 16), k_desc = tc_desc(smem_addr(sm.kv), 16),
-                     v_desc = tc_desc(smem_addr(sm.kv), kChunk);
-      uint32_t kv = 0, q_phase = 0, p_phase = 0;  // p_phase, q_phase: bit k of tile k
-      auto ring = [&](uint32_t at) { bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
-      // scores of tile k on the block at `at`, n steps of 16 keys
-      auto qk = [&](int k, uint32_t at, uint32_t id) {
-        const uint32_t qd = q_desc + k * kStep, kd = k_desc + at % kPrStages * kStep;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          const int off = ((c / 4) * kChunk + (c % 4) * 32) >> 4;
-          tc_mma(tmem + k * kCols, qd + off, kd + off, id, c > 0);
-        }
-        tc_commit(&sm.s_full[k]);
-      };
-      for (int n = 0;; ++n) {
-        bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
-        const PromptItem &it = sm.item[n & 1];
-        const int head = __shfl_sync(~0u, it.head, 0), n0 = __shfl_sync(~0u, it.n[0], 0), n1 = __shfl_sync(~0u, it.n[1], 0);
-        const int tail0 = __shfl_sync(~0u, it.tail[0], 0), tail1 = __shfl_sync(~0u, it.tail[1], 0);
-        if (__any_sync(~0u, head < 0 || *stop)) break;
-        if (elect_one()) bar_arrive(&sm.item_empty[n & 1]);
-        const int most = max(n0, n1);
-        // the scores of a last block only as far as the tile sees it
-        auto qk_any = [&](int k, int j, uint32_t at) {
-          const bool last = j + 1 == (k ? n1 : n0);
-          const uint32_t id = last ? tc_idesc(128, 0, F16, a.scale < 0.f, false) | (uint32_t)((k ? tail1 : tail0) * 2) << 17 : id_qk;
-          if (elect_one()) {
-            qk(k, at, id);
-            if (last) tc_commit(&sm.q_empty[k]);
-          }
-        };
-        // first scores of both tiles
-        ring(kv);
-#pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-          if (!(k ? n1 : n0)) continue;
-          bar_wait(&sm.q_full[k], q_phase >> k & 1, stop);
-          q_phase ^= 1u << k;
-          qk_any(k, 0, kv);
-        }
-        if (elect_one()) tc_commit(&sm.kv_empty[kv % kPrStages]);
-        ring(kv + 1);
-        int j = 0;
-        for (; j + 2 < min(n0, n1); ++j) {
-          const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
-            tc_after_sync();
-            if (elect_one()) {
-#pragma unroll
-              for (int c = 0; c < kPrBlock / 16; ++c)
-                tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
-              if (k == 1) tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
-            }
-            ring(kv + 2 + k);  // these keys; the next values, for the next turn
-            if (elect_one()) {
-              qk(k, kv + 2, id_qk);
-              if (k == 1) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
-            }
-          }
-          p_phase ^= 3;
-          kv += 2;
-        }
-#pragma unroll 1
-        for (; j < most; ++j) {
-          const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
-          ring(kv + 1);
-          if (j + 1 < most) ring(kv + 2);
-#pragma unroll 1
-          for (int k = 0; k < 2; ++k) {
-            const int blocks = k ? n1 : n0;
-            if (j >= blocks) continue;
-            bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
-            p_phase ^= 1u << k;
-            tc_after_sync();
-            const int steps = j + 1 == blocks ? (k ? tail1 : tail0) : kPrBlock / 16;
-            if (elect_one()) {
-#pragma unroll 1
-              for (int c = 0; c < steps; ++c)
-                tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
-              if (j + 1 == blocks) tc_commit(&sm.o_full[k]);
-            }
-            if (j + 1 < blocks) qk_any(k, j + 1, kv + 2);
-          }
-          if (elect_one()) {
-            tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
-            if (j + 1 < most) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
-          }
-          kv += 2;
-        }
-      }
+      issue_products<D, F16>(sm, tmem, a.scale < 0.f, stop);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
