@@ -39,13 +39,17 @@ struct ChunkArgs {
 template <int D>
 struct ChunkSmem {
   static constexpr int kTile = 128 * D * 2;
+  static constexpr int kStages = 3;   // blocks of keys or values in fp16
+  static constexpr int kCodes = 4;    // blocks of them as codes, on their way
   unsigned char q[2][kTile];
-  unsigned char kv[kPrStages][kTile];
-  uint64_t q_full[2], q_empty[2], kv_full[kPrStages], kv_empty[kPrStages], s_full[2], p_full[2], o_full[2];
+  unsigned char kv[kStages][kTile];
+  unsigned char code[kCodes][128 * D];  // at the start: the requests' running sums
+  uint64_t code_full[kCodes], code_empty[kCodes];
+  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2], scale_full[kChScales];
   PromptItem item[2];
-  int64_t sums[kScan + 1];
   float ks[kChScales][8], vs[kChScales][8];  // of a block's strips; ks < 0: hidden
+  uint32_t state[kCodes][8];  // of a block's strips: keys that are there, bit 8: their sign is changed
   int64_t req[2], from[2];  // of each item: its request, its first block
   int whole[2], slot[2];    // no other CTA has a share of it; where its part goes
   uint32_t tmem;
@@ -102,13 +106,17 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       bar_init(&sm.p_full[k], 4);
       bar_init(&sm.o_full[k], 1);
       bar_init(&sm.item_full[k], 1);
-      bar_init(&sm.item_empty[k], 13);
+      bar_init(&sm.item_empty[k], 14);
     }
-    for (int k = 0; k < kPrStages; ++k) {
+    for (int k = 0; k < Smem::kStages; ++k) {
       bar_init(&sm.kv_full[k], 4);
       bar_init(&sm.kv_empty[k], 1);
     }
-    for (int k = 0; k < kChScales; ++k) bar_init(&sm.scale_full[k], 4);
+    for (int k = 0; k < Smem::kCodes; ++k) {
+      bar_init(&sm.code_full[k], 8);
+      bar_init(&sm.code_empty[k], 4);
+    }
+    for (int k = 0; k < kChScales; ++k) bar_init(&sm.scale_full[k], 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   bool bad = false;
@@ -117,12 +125,18 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   if (c.given) {
     units = sums[a.n_req];
   } else {
-    units = scan_units<kChThreads>((int)a.n_req, sm.sums, 0, [&](int k) { return chunk_units(c, k, &bad); });
-    sums = sm.sums;
+    int64_t *const S = reinterpret_cast<int64_t *>(sm.code);  // before any copy arrives there
+    static_assert(sizeof(sm.code) >= 8 * (kScan + 1), "room for the sums");
+    units = scan_units<kChThreads>((int)a.n_req, S, 0, [&](int k) { return chunk_units(c, k, &bad); });
+    sums = S;
     if (blockIdx.x == 0)
-      for (int i = threadIdx.x; i <= a.n_req; i += kChThreads) c.prefix[i] = sm.sums[i];
+      for (int i = threadIdx.x; i <= a.n_req; i += kChThreads) c.prefix[i] = S[i];
   }
+  // the CTA's share of the line and the request it begins in
+  const int64_t end = warp_start(blockIdx.x + 1, gridDim.x, units), begin = warp_start(blockIdx.x, gridDim.x, units);
+  const int64_t first_req = find_unit(sums, a.n_req, begin), first_sum = sums[first_req];
   let_next();
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the copies will write where the sums were
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
@@ -131,13 +145,12 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   constexpr uint32_t kCols = 128;
 
   if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 12) {
       issue_products<D, true>(sm, tmem, a.scale < 0.f, stop);
     } else if (warp == 13 && lane == 0) {
-      // the CTA's share of the line, an item or a part of one at a time
-      const int64_t end = warp_start(blockIdx.x + 1, gridDim.x, units), begin = warp_start(blockIdx.x, gridDim.x, units);
-      int64_t u = begin;
+      // the share, an item or a part of one at a time
+      int64_t u = begin, i = first_req, before = first_sum;  // units before request i
       for (int n = 0;; ++n) {
         if (n >= 2) bar_wait(&sm.item_empty[n & 1], ((n >> 1) - 1) & 1, stop);
         PromptItem &it = sm.item[n & 1];
@@ -147,9 +160,9 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           break;
         }
         bool ignore = false;
-        const int64_t i = find_unit(sums, a.n_req, u);
+        for (int64_t more; u >= before + (more = chunk_units(c, i, &ignore)); ++i) before += more;
         const Span sp = request_span(a, i, &ignore);
-        const int64_t blocks = chunk_blocks(c, sp), local = u - sums[i], seg = local / blocks;
+        const int64_t blocks = chunk_blocks(c, sp), local = u - before, seg = local / blocks;
         const int64_t b0 = local % blocks, b1 = min(blocks, b0 + end - u);
         const int t0 = (int)(seg / a.hkv) * 2 * c.tile;
         it.first = (int)sp.first;
@@ -175,112 +188,125 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         bar_arrive(&sm.item_full[n & 1]);
         u += b1 - b0;
       }
+    } else if (warp == 14) {
+      // The codes' copies, a strip a lane: 16 keys of one block and head are 16 D bytes
+      // in a row.  Eight lanes a block; ids and scales of 32 strips (four blocks) at a
+      // time, the next 32 ahead.
+      RingAt code{0, 1};  // the first turn's slots are free
+      uint32_t block = 0;
+      for (int n = 0;; ++n) {
+        bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
+        const int head = sm.item[n & 1].head, most = max(sm.item[n & 1].n[0], sm.item[n & 1].n[1]);
+        const int64_t i = sm.req[n & 1], from = sm.from[n & 1];
+        __syncwarp();
+        if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
+        if (__any_sync(~0u, head < 0 || *stop)) break;
+        bool ignore = false;
+        const Span sp = request_span(a, i, &ignore);
+        const int64_t keys = row_limit(a, sp, sp.p - 1);
+        int32_t id[2];
+        float ks[2], vs[2];
+        auto look_up = [&](int set, int group) {
+          const int64_t strip = (from + 4 * group) * 8 + lane;
+          id[set] = -1;
+          ks[set] = vs[set] = 0.f;
+          if (4 * group + (lane >> 3) < most && strip * 16 < keys) {
+            int32_t b = a.table[i * a.width + ((strip * 16) >> cv.log_b)];
+            if (b < -1 || b >= cv.n_blocks) {
+              bad = true;
+              b = -1;
+            }
+            id[set] = b;
+            if (b >= 0) {
+              ks[set] = cv.k_scale[(int64_t)b * cv.heads + head];
+              vs[set] = cv.v_scale[(int64_t)b * cv.heads + head];
+            }
+          }
+        };
+        if (most > 0) look_up(0, 0);
+        for (int j = 0; j < most; ++j) {
+          if ((j & 3) == 0) {
+            if (j > 0) id[0] = id[1], ks[0] = ks[1], vs[0] = vs[1];
+            look_up(1, j / 4 + 1);
+          }
+          const bool mine = (lane >> 3) == (j & 3);
+          const int strip = lane & 7;
+          const int64_t pos = (from + j) * kPrBlock + strip * 16;
+          const int there = id[0] < 0 ? 0 : (int)max((int64_t)0, min((int64_t)16, keys - pos));
+          if (mine) {
+            const uint32_t at = (block + j) % kChScales;
+            sm.ks[at][strip] = id[0] < 0 ? -1.f : fabsf(ks[0]);
+            sm.vs[at][strip] = vs[0];
+            bar_arrive(&sm.scale_full[at]);
+          }
+          const int64_t off = ((((int64_t)max(id[0], 0) * cv.heads + head) << cv.log_b) + (pos & ((1 << cv.log_b) - 1))) * D;
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            bar_wait(&sm.code_empty[code.st], code.phase, stop);
+            if (mine) {
+              sm.state[code.st][strip] = (uint32_t)there | (v == 0 && ks[0] < 0.f ? 256u : 0u);
+              if (there > 0 && !*stop) {
+                bar_expect(&sm.code_full[code.st], there * D);
+                copy_bytes(sm.code[code.st] + strip * 16 * D, (v ? cv.v : cv.k) + off, there * D, &sm.code_full[code.st]);
+              } else {
+                bar_arrive(&sm.code_full[code.st]);
+              }
+            }
+            __syncwarp();
+            code = code.next(Smem::kCodes);
+          }
+        }
+        block += most;
+      }
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    // Codes to fp16, two strips of each block a warp: eight lanes a key, so that a
-    // key's D bytes are read together; of the two pieces of 16 bytes that a lane's
-    // codes become the upper half of the lanes stores the second one first, and no
-    // two lanes of a quarter warp meet in a bank.
-    constexpr int kLanes = D / 16, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads of two strips
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    // Codes to fp16, 32 keys of each block a warp: eight lanes a key (D = 128), and of the
+    // two pieces of 16 bytes that a lane's codes become the upper half of the lanes
+    // stores the second one first, so that no two lanes of a quarter warp meet in a bank.
+    constexpr int kLanes = D / 16, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads
     const int w = warp - 8, sub = lane % kLanes, key_of = lane / kLanes;
-    uint32_t kv = 0, block = 0;
+    const int second = sub >= 4 ? 1 : 0, piece = (sub % 4) * 2;
+    RingAt code{0, 0}, to{0, 1};  // the first turn's stages are free
     for (int n = 0;; ++n) {
       bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
       const int head = sm.item[n & 1].head, most = max(sm.item[n & 1].n[0], sm.item[n & 1].n[1]);
-      const int64_t i = sm.req[n & 1], from = sm.from[n & 1];
       __syncwarp();
       if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
       if (__any_sync(~0u, head < 0 || *stop)) break;
-      bool ignore = false;
-      const Span sp = request_span(a, i, &ignore);
-      const int64_t keys = row_limit(a, sp, sp.p - 1);
-      // blocks and scales of 32 strips (16 blocks) at a time, a strip a lane, the next 32 ahead
-      int32_t id[2];
-      float ks[2], vs[2];
-      auto look_up = [&](int set, int m) {
-        const int64_t strip = (from + (m + lane) / 2) * 8 + 2 * w + (lane & 1);
-        id[set] = -1;
-        ks[set] = vs[set] = 0.f;
-        if ((m + lane) / 2 < most && strip * 16 < keys) {
-          int32_t b = a.table[i * a.width + ((strip * 16) >> cv.log_b)];
-          if (b < -1 || b >= cv.n_blocks) {
-            bad = true;
-            b = -1;
-          }
-          id[set] = b;
-          if (b >= 0) {
-            ks[set] = cv.k_scale[(int64_t)b * cv.heads + head];
-            vs[set] = cv.v_scale[(int64_t)b * cv.heads + head];
-          }
-        }
-      };
-      uint4 code[2][kSteps];
-      // the two strips of block j: keys or values
-      auto fetch = [&](int to, int j, bool values) {
-#pragma unroll
-        for (int x = 0; x < kSteps; ++x) {
-          const int key = x * kKeys + key_of;  // of the warp's 32
-          const int32_t b = __shfl_sync(~0u, id[0], (2 * j + (key >> 4)) & 31);
-          const int64_t pos = (from + j) * kPrBlock + 32 * w + key;
-          code[to][x] = make_uint4(0, 0, 0, 0);
-          if (b >= 0 && pos < keys)
-            code[to][x] = load16((values ? cv.v : cv.k) +
-                                 ((((int64_t)b * cv.heads + head) << cv.log_b) + (pos & ((1 << cv.log_b) - 1))) * D + sub * 16);
-        }
-      };
-      auto put = [&](int from_set, uint32_t flip) {
-        const uint32_t st = kv % kPrStages;
-        if (kv >= kPrStages) bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
+      for (int j = 0; j < 2 * most; ++j) {
+        bar_wait(&sm.code_full[code.st], code.phase, stop);
+        bar_wait(&sm.kv_empty[to.st], to.phase, stop);
         __syncwarp();
-#pragma unroll
+        const uint32_t state[2] = {sm.state[code.st][2 * w], sm.state[code.st][2 * w + 1]};
+        const unsigned char *from = sm.code[code.st] + 32 * w * D;
+        unsigned char *const at = sm.kv[to.st] + (sub / 4) * kChunk + 32 * w * 128;
+#pragma unroll 4
         for (int x = 0; x < kSteps; ++x) {
-          const int key = x * kKeys + key_of, row = 32 * w + key;
-          const uint4 q = code[from_set][x];
-          const uint32_t f = flip >> (16 * (key >> 4)) & 1 ? 0x80808080u : 0u;
-          const uint32_t y[4] = {q.x ^ f, q.y ^ f, q.z ^ f, q.w ^ f};
-          uint4 h[2];
-          h[0] = make_uint4(lo_half2(y[0]), hi_half2(y[0]), lo_half2(y[1]), hi_half2(y[1]));
-          h[1] = make_uint4(lo_half2(y[2]), hi_half2(y[2]), lo_half2(y[3]), hi_half2(y[3]));
-          unsigned char *to = sm.kv[st] + (sub / 4) * kChunk + row * 128;
-          const int first = sub >= 4 ? 1 : 0, piece = (sub % 4) * 2;
-          const uint4 ha = first ? h[1] : h[0], hb = first ? h[0] : h[1];
-          *reinterpret_cast<uint4 *>(to + (((piece + first) ^ (row & 7)) << 4)) = ha;
-          *reinterpret_cast<uint4 *>(to + (((piece + 1 - first) ^ (row & 7)) << 4)) = hb;
+          const int key = x * kKeys + key_of;
+          const uint32_t st = x * kKeys >= 16 ? state[1] : state[0];
+          uint4 q = *reinterpret_cast<const uint4 *>(from + key * D + sub * 16);
+          if ((uint32_t)(key & 15) >= (st & 31)) q = make_uint4(0, 0, 0, 0);
+          const uint32_t flip = st & 256 ? 0x80808080u : 0u;
+          q.x ^= flip, q.y ^= flip, q.z ^= flip, q.w ^= flip;
+          const uint4 h0 = make_uint4(lo_half2(q.x), hi_half2(q.x), lo_half2(q.y), hi_half2(q.y));
+          const uint4 h1 = make_uint4(lo_half2(q.z), hi_half2(q.z), lo_half2(q.w), hi_half2(q.w));
+          unsigned char *const row = at + key * 128;
+          *reinterpret_cast<uint4 *>(row + (((piece + second) ^ (key & 7)) << 4)) = second ? h1 : h0;
+          *reinterpret_cast<uint4 *>(row + (((piece + 1 - second) ^ (key & 7)) << 4)) = second ? h0 : h1;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) bar_arrive(&sm.kv_full[st]);
-        ++kv;
-      };
-      if (most > 0) {
-        look_up(0, 0);
-        look_up(1, 32);
-        fetch(0, 0, false);
-      }
-      for (int j = 0; j < most; ++j) {
-        // a negative key scale goes into the codes' signs
-        const bool hidden = id[0] < 0, minus = ks[0] < 0.f;
-        const uint32_t flips = __ballot_sync(~0u, minus) >> ((2 * j) & 31);
-        if ((lane >> 1) == (j & 15)) {
-          sm.ks[block % kChScales][2 * w + (lane & 1)] = hidden ? -1.f : fabsf(ks[0]);
-          sm.vs[block % kChScales][2 * w + (lane & 1)] = vs[0];
+        if (lane == 0) {
+          bar_arrive(&sm.kv_full[to.st]);
+          bar_arrive(&sm.code_empty[code.st]);
         }
-        __syncwarp();
-        if (lane == 0) bar_arrive(&sm.scale_full[block % kChScales]);
-        ++block;
-        fetch(1, j, true);
-        put(0, (flips & 1) | (flips >> 1 & 1) << 16);
-        if ((j & 15) == 15) {
-          id[0] = id[1], ks[0] = ks[1], vs[0] = vs[1];
-          look_up(1, 2 * (j + 1) + 32);
-        }
-        if (j + 1 < most) fetch(0, j + 1, false);
-        put(1, 0);
+        code = code.next(Smem::kCodes);
+        to = to.next(Smem::kStages);
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const int k = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
     const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
@@ -353,46 +379,48 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           // the scores are there, so the scales are: this look never waits (before the
           // scores it could take an older phase of the barrier for this one)
           bar_wait(&sm.scale_full[b % kChScales], (b / kChScales) & 1, stop);
-          float f[8], vr[8];  // a strip's factor of scores and of weights
+          const float *ksb = sm.ks[b % kChScales], *vsb = sm.vs[b % kChScales];
           bool hidden = false;
           float top_vs = 0.f;
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            f[x] = sm.ks[b % kChScales][x];
-            vr[x] = sm.vs[b % kChScales][x];
-            hidden |= f[x] < 0.f;
-            top_vs = fmaxf(top_vs, fabsf(vr[x]));
+            hidden |= ksb[x] < 0.f;
+            top_vs = fmaxf(top_vs, fabsf(vsb[x]));
           }
           __syncwarp();
           tc_after_sync();
-          uint32_t s[128];
+          const bool masked = hidden || (from + j + 1) * kPrBlock > all;
+          const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
+          // a strip's factor of scores; one of zero must leave what is masked at -infinity
+          auto factor = [&](int strip) {
+            const float f = fabsf(ksb[strip]) * sl;
+            return f == 0.f ? 1e-37f : f;
+          };
+          // 32 scores from column x, those that the row does not see at -infinity
+          auto mask = [&](uint32_t *s, int x) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) tmem_load32(s + 32 * x, ts + 32 * x);
-          tmem_wait_load();
-          if (hidden) {
-#pragma unroll
-            for (int x = 0; x < 128; ++x)
-              if (f[x / 16] < 0.f) s[x] = 0xff800000u;
-          }
-          if ((from + j + 1) * kPrBlock > all) {
-            const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
-#pragma unroll
-            for (int x = 0; x < 128; ++x)
-              if (x >= rel) s[x] = 0xff800000u;
-          }
+            for (int y = 0; y < 32; ++y)
+              if (x + y >= rel || ksb[(x + y) / 16] < 0.f) s[y] = 0xff800000u;
+          };
+          // The scores are read from tensor memory twice, for the maximum and for the
+          // weights: a thread that keeps its 128 has no registers left for the rest.
           float top = m;
+          uint32_t s[32];
+#pragma unroll 1
+          for (int x = 0; x < 4; ++x) {
+            tmem_load32(s, ts + 32 * x);
+            tmem_wait_load();
+            if (masked) mask(s, 32 * x);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            f[x] = f[x] < 0.f ? sl : f[x] * sl;
-            float t0 = -INFINITY, t1 = -INFINITY;
+            for (int y = 0; y < 2; ++y) {
+              float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-            for (int y = 0; y < 16; y += 4) {
-              t0 = fmaxf(t0, fmaxf(__uint_as_float(s[16 * x + y]), __uint_as_float(s[16 * x + y + 1])));
-              t1 = fmaxf(t1, fmaxf(__uint_as_float(s[16 * x + y + 2]), __uint_as_float(s[16 * x + y + 3])));
+              for (int z = 0; z < 16; z += 4) {
+                t0 = fmaxf(t0, fmaxf(__uint_as_float(s[16 * y + z]), __uint_as_float(s[16 * y + z + 1])));
+                t1 = fmaxf(t1, fmaxf(__uint_as_float(s[16 * y + z + 2]), __uint_as_float(s[16 * y + z + 3])));
+              }
+              top = fmaxf(top, fmaxf(t0, t1) * factor(2 * x + y));
             }
-            // a factor of zero must leave what is masked at -infinity
-            f[x] = f[x] == 0.f ? 1e-37f : f[x];
-            top = fmaxf(top, fmaxf(t0, t1) * f[x]);
           }
           const bool grow_ref = !(top_vs <= kChRef * ref);
           if (j == 0) {
@@ -419,22 +447,24 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           const float base = m == -INFINITY ? -kChExp : m - kChExp;
           const uint64_t base2 = pair(-base, -base);
           uint64_t sum[2] = {0, 0};
-#pragma unroll
-          for (int x = 0; x < 128; x += 32) {
+#pragma unroll 1
+          for (int x = 0; x < 4; ++x) {
+            tmem_load32(s, ts + 32 * x);
+            tmem_wait_load();
+            if (masked) mask(s, 32 * x);
             uint32_t w[16];
 #pragma unroll
             for (int y = 0; y < 16; ++y) {
-              const int strip = (x + 2 * y) / 16;
+              const int strip = 2 * x + y / 8;
+              const float f = factor(strip), r = vsb[strip] * inv_ref;
               float p0, p1;
-              unpair(fma2(pair(__uint_as_float(s[x + 2 * y]), __uint_as_float(s[x + 2 * y + 1])), pair(f[strip], f[strip]), base2),
-                     &p0, &p1);
+              unpair(fma2(pair(__uint_as_float(s[2 * y]), __uint_as_float(s[2 * y + 1])), pair(f, f), base2), &p0, &p1);
               const uint64_t pp = pair(exp2_fast(p0), exp2_fast(p1));
               sum[y & 1] = add2(sum[y & 1], pp);
-              const float r = vr[strip] * inv_ref;
               unpair(mul2(pp, pair(r, r)), &p0, &p1);
               w[y] = pack_half2(p0, p1);
             }
-            tmem_store16(ts + x / 2, w);
+            tmem_store16(ts + 16 * x, w);  // over columns that were read
           }
           float l0, l1;
           unpair(add2(sum[0], sum[1]), &l0, &l1);

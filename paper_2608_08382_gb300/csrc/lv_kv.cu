@@ -138,6 +138,7 @@ lv_status run_chunk(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
     LV_CUDA(cudaGetLastError());
   }
   constexpr size_t smem = sizeof(ChunkSmem<D>) + 1024;
+  static_assert(smem <= 227 << 10, "an SM's shared memory");
   LV_CUDA(cudaFuncSetAttribute(k_chunk<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   k_chunk<D, F16><<<(unsigned)ctas, kChThreads, smem, stream>>>(c);
   LV_CUDA(cudaGetLastError());
@@ -226,6 +227,7 @@ lv_status run_prompt(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
     LV_CUDA(cudaGetLastError());
   }
   constexpr size_t smem = sizeof(PromptSmem<D>) + 1024;
+  static_assert(smem <= 227 << 10, "an SM's shared memory");
   LV_CUDA(cudaFuncSetAttribute(k_prompt<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   // a CTA an SM; no more than there can be items
   const int64_t items = (a.n_tok / (2 * p.tile) + std::min(a.n_req, a.n_tok)) * a.hkv;

@@ -38,7 +38,6 @@ namespace lv {
 
 constexpr int kPrThreads = 384;
 constexpr int kPrBlock = 128;   // keys of a block
-constexpr int kPrStages = 4;    // blocks of keys or values in shared memory
 constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that weights absorb
 
 struct PromptArgs {
@@ -61,9 +60,10 @@ template <int D>
 struct PromptSmem {
   static constexpr int kRowBytes = 128;                    // a row of 64 elements
   static constexpr int kTile = 128 * D * 2;                // bytes of a tile of Q or a block of K or V
+  static constexpr int kStages = 4;                        // blocks of keys or values
   unsigned char q[2][kTile];
-  unsigned char kv[kPrStages][kTile];
-  uint64_t q_full[2], q_empty[2], kv_full[kPrStages], kv_empty[kPrStages], s_full[2], p_full[2], o_full[2];
+  unsigned char kv[kStages][kTile];
+  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2];
   PromptItem item[2];
   int64_t sums[kScan + 1];
@@ -91,6 +91,14 @@ __global__ void __launch_bounds__(kScan) k_prompt_prefix(PromptArgs p) {
   if (bad) flag(p.a.status, kStatusData);
 }
 
+// A place in a ring of stages.
+struct RingAt {
+  uint32_t st, phase;
+  __device__ __forceinline__ RingAt next(uint32_t stages) const {
+    return st + 1 == stages ? RingAt{0, phase ^ 1} : RingAt{st + 1, phase};
+  }
+};
+
 // The warp that issues every product, for kernels of two tiles of rows.
 // One instruction takes 64 clocks and few wait in line, so what this warp does
 // between two of them soon stops the tensor core.  The loop over whole blocks of
@@ -106,11 +114,15 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
   constexpr uint32_t kStep = (128 * D * 2) >> 4;  // a tile or block on, in a descriptor
   const uint32_t q_desc = tc_desc(smem_addr(sm.q), 16), k_desc = tc_desc(smem_addr(sm.kv), 16),
                  v_desc = tc_desc(smem_addr(sm.kv), kChunk);
-  uint32_t kv = 0, q_phase = 0, p_phase = 0;  // p_phase, q_phase: bit k of tile k
-  auto ring = [&](uint32_t at) { bar_wait(&sm.kv_full[at % kPrStages], (at / kPrStages) & 1, stop); };
+  constexpr uint32_t kStages = Smem::kStages;
+  uint32_t q_phase = 0, p_phase = 0;  // bit k of tile k
+  // the stages of block j's values and block j + 1's keys and values, and their phases
+  RingAt v0{0, 0}, k1{0, 0}, v1{0, 0}, k0{0, 0};  // k0: of an item's first keys
+  auto ring = [&](const RingAt &at) { bar_wait(&sm.kv_full[at.st], at.phase, stop); };
+  auto release = [&](const RingAt &at) { tc_commit(&sm.kv_empty[at.st]); };
   // scores of tile k on the block at `at`, n steps of 16 keys
-  auto qk = [&](int k, uint32_t at, uint32_t id) {
-    const uint32_t qd = q_desc + k * kStep, kd = k_desc + at % kPrStages * kStep;
+  auto qk = [&](int k, const RingAt &at, uint32_t id) {
+    const uint32_t qd = q_desc + k * kStep, kd = k_desc + at.st * kStep;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       const int off = ((c / 4) * kChunk + (c % 4) * 32) >> 4;
@@ -128,7 +140,7 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
     const int most = max(n0, n1);
     if (most == 0) continue;
     // the scores of a last block only as far as the tile sees it
-    auto qk_any = [&](int k, int j, uint32_t at) {
+    auto qk_any = [&](int k, int j, const RingAt &at) {
       const bool last = j + 1 == (k ? n1 : n0);
       const uint32_t id = last ? tc_idesc(128, 0, F16, negate, false) | (uint32_t)((k ? tail1 : tail0) * 2) << 17 : id_qk;
       if (elect_one()) {
@@ -137,19 +149,22 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
       }
     };
     // first scores of both tiles
-    ring(kv);
+    v0 = k0.next(kStages);
+    k1 = v0.next(kStages);
+    v1 = k1.next(kStages);
+    ring(k0);
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
       if (!(k ? n1 : n0)) continue;
       bar_wait(&sm.q_full[k], q_phase >> k & 1, stop);
       q_phase ^= 1u << k;
-      qk_any(k, 0, kv);
+      qk_any(k, 0, k0);
     }
-    if (elect_one()) tc_commit(&sm.kv_empty[kv % kPrStages]);
-    ring(kv + 1);
+    if (elect_one()) release(k0);
+    ring(v0);
     int j = 0;
     for (; j + 2 < min(n0, n1); ++j) {
-      const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
+      const uint32_t vd = v_desc + v0.st * kStep;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
@@ -158,22 +173,24 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
 #pragma unroll
           for (int c = 0; c < kPrBlock / 16; ++c)
             tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
-          if (k == 1) tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
+          if (k == 1) release(v0);
         }
-        ring(kv + 2 + k);  // these keys; the next values, for the next turn
+        ring(k == 0 ? k1 : v1);  // these keys; the next values, for the next turn
         if (elect_one()) {
-          qk(k, kv + 2, id_qk);
-          if (k == 1) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+          qk(k, k1, id_qk);
+          if (k == 1) release(k1);
         }
       }
       p_phase ^= 3;
-      kv += 2;
+      v0 = v1;
+      k1 = v0.next(kStages);
+      v1 = k1.next(kStages);
     }
 #pragma unroll 1
     for (; j < most; ++j) {
-      const uint32_t vd = v_desc + (kv + 1) % kPrStages * kStep;
-      ring(kv + 1);
-      if (j + 1 < most) ring(kv + 2);
+      const uint32_t vd = v_desc + v0.st * kStep;
+      ring(v0);
+      if (j + 1 < most) ring(k1);
 #pragma unroll 1
       for (int k = 0; k < 2; ++k) {
         const int blocks = k ? n1 : n0;
@@ -188,13 +205,16 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
             tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
           if (j + 1 == blocks) tc_commit(&sm.o_full[k]);
         }
-        if (j + 1 < blocks) qk_any(k, j + 1, kv + 2);
+        if (j + 1 < blocks) qk_any(k, j + 1, k1);
       }
       if (elect_one()) {
-        tc_commit(&sm.kv_empty[(kv + 1) % kPrStages]);
-        if (j + 1 < most) tc_commit(&sm.kv_empty[(kv + 2) % kPrStages]);
+        release(v0);
+        if (j + 1 < most) release(k1);
       }
-      kv += 2;
+      k0 = k1;  // the next item's, after the last block
+      v0 = v1;
+      k1 = v0.next(kStages);
+      v1 = k1.next(kStages);
     }
   }
 }
@@ -222,7 +242,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       bar_init(&sm.item_full[k], 1);
       bar_init(&sm.item_empty[k], 9);
     }
-    for (int k = 0; k < kPrStages; ++k) {
+    for (int k = 0; k < Smem::kStages; ++k) {
       bar_init(&sm.kv_full[k], 1);
       bar_init(&sm.kv_empty[k], 1);
     }
@@ -292,8 +312,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
               for (int c = 0; c < D / 64; ++c)
                 tma_load3(sm.q[k] + c * kChunk, &map_q, c * 64, head * G, (int)(x0 + t0 + k * p.tile), &sm.q_full[k]);
             }
-            const uint32_t st = kv % kPrStages;
-            if (kv >= kPrStages) bar_wait(&sm.kv_empty[st], (kv / kPrStages - 1) & 1, stop);
+            const uint32_t st = kv % Smem::kStages;
+            if (kv >= Smem::kStages) bar_wait(&sm.kv_empty[st], (kv / Smem::kStages - 1) & 1, stop);
             if (*stop) break;
             ++kv;
             bar_expect(&sm.kv_full[st], Smem::kTile);
@@ -304,8 +324,8 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         }
       }
       // no load is in flight when the block ends: what was asked for is waited for
-      for (uint32_t st = 0; st < kPrStages; ++st)
-        if (kv > st) bar_wait(&sm.kv_full[st], ((kv - st + kPrStages - 1) / kPrStages - 1) & 1, stop);
+      for (uint32_t st = 0; st < Smem::kStages; ++st)
+        if (kv > st) bar_wait(&sm.kv_full[st], ((kv - st + Smem::kStages - 1) / Smem::kStages - 1) & 1, stop);
     } else if (warp == 8) {
       issue_products<D, F16>(sm, tmem, a.scale < 0.f, stop);
     }

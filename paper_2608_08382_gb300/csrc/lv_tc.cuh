@@ -56,6 +56,13 @@ __device__ __forceinline__ void tma_load3(void *to, const CUtensorMap *map, int 
       : "memory");
 }
 
+// n bytes in a row into shared memory: both addresses and n multiples of 16.
+__device__ __forceinline__ void copy_bytes(void *to, const void *from, uint32_t n, uint64_t *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(to)),
+               "l"(from), "r"(n), "r"(smem_addr(bar))
+               : "memory");
+}
+
 __device__ __forceinline__ void tmem_alloc(uint32_t *to, int columns) {  // one whole warp
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
                : "memory");
