@@ -21,7 +21,7 @@
 
 namespace lv {
 
-constexpr int kChThreads = 512;
+constexpr int kChThreads = 640;
 constexpr int kChScales = 8;       // blocks whose scales are kept: more than the copies run ahead
 constexpr float kChExp = 4.f;      // weights are 2^4 at the maximum they refer to
 constexpr float kChRef = 8.f;      // largest vs / ref
@@ -48,7 +48,7 @@ struct ChunkSmem {
   uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2], scale_full[kChScales];
   PromptItem item[2];
-  float ks[kChScales][8], vs[kChScales][8];  // of a block's strips; ks < 0: hidden
+  alignas(16) float ks[kChScales][8], vs[kChScales][8];  // of a block's strips; ks < 0: hidden
   uint32_t state[kCodes][8];  // of a block's strips: keys that are there, bit 8: their sign is changed
   int64_t req[2], from[2];  // of each item: its request, its first block
   int whole[2], slot[2];    // no other CTA has a share of it; where its part goes
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = a.hq / a.hkv;
   constexpr int kChunk = 128 * 128;  // bytes of 64 elements of a tile's rows
   wait_previous();
-  if (warp == 12) tmem_alloc(&sm.tmem, 512);
+  if (warp == 16) tmem_alloc(&sm.tmem, 512);
   if (threadIdx.x == 0) {
     sm.stop = 0;
     sm.item[0].head = sm.item[1].head = -1;
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       bar_init(&sm.p_full[k], 4);
       bar_init(&sm.o_full[k], 1);
       bar_init(&sm.item_full[k], 1);
-      bar_init(&sm.item_empty[k], 14);
+      bar_init(&sm.item_empty[k], 18);
     }
     for (int k = 0; k < Smem::kStages; ++k) {
       bar_init(&sm.kv_full[k], 4);
@@ -144,11 +144,11 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   volatile int *stop = &sm.stop;
   constexpr uint32_t kCols = 128;
 
-  if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == 12) {
+  if (warp >= 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 16) {
       issue_products<D, true>(sm, tmem, a.scale < 0.f, stop);
-    } else if (warp == 13 && lane == 0) {
+    } else if (warp == 17 && lane == 0) {
       // the share, an item or a part of one at a time
       int64_t u = begin, i = first_req, before = first_sum;  // units before request i
       for (int n = 0;; ++n) {
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         bar_arrive(&sm.item_full[n & 1]);
         u += b1 - b0;
       }
-    } else if (warp == 14) {
+    } else if (warp == 18) {
       // The codes' copies, a strip a lane: 16 keys of one block and head are 16 D bytes
       // in a row.  Eight lanes a block; ids and scales of 32 strips (four blocks) at a
       // time, the next 32 ahead.
@@ -260,21 +260,23 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       }
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     // Codes to fp16, 32 keys of each block a warp: eight lanes a key (D = 128), and of the
     // two pieces of 16 bytes that a lane's codes become the upper half of the lanes
     // stores the second one first, so that no two lanes of a quarter warp meet in a bank.
     constexpr int kLanes = D / 16, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads
-    const int w = warp - 8, sub = lane % kLanes, key_of = lane / kLanes;
+    const int w = warp & 3, sub = lane % kLanes, key_of = lane / kLanes;
     const int second = sub >= 4 ? 1 : 0, piece = (sub % 4) * 2;
+    // warps 8 to 11 the keys, 12 to 15 the values, which take turns in both rings
     RingAt code{0, 0}, to{0, 1};  // the first turn's stages are free
+    if (warp >= 12) code = code.next(Smem::kCodes), to = to.next(Smem::kStages);
     for (int n = 0;; ++n) {
       bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
       const int head = sm.item[n & 1].head, most = max(sm.item[n & 1].n[0], sm.item[n & 1].n[1]);
       __syncwarp();
       if (lane == 0) bar_arrive(&sm.item_empty[n & 1]);
       if (__any_sync(~0u, head < 0 || *stop)) break;
-      for (int j = 0; j < 2 * most; ++j) {
+      for (int j = 0; j < most; ++j) {
         bar_wait(&sm.code_full[code.st], code.phase, stop);
         bar_wait(&sm.kv_empty[to.st], to.phase, stop);
         __syncwarp();
@@ -301,12 +303,12 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           bar_arrive(&sm.kv_full[to.st]);
           bar_arrive(&sm.code_empty[code.st]);
         }
-        code = code.next(Smem::kCodes);
-        to = to.next(Smem::kStages);
+        code = code.next(Smem::kCodes).next(Smem::kCodes);
+        to = to.next(Smem::kStages).next(Smem::kStages);
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int k = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
     const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
@@ -372,54 +374,73 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           if (lane == 0) bar_arrive(&sm.q_full[k]);
           ++qs;
         }
-        for (int j = 0; j < blocks; ++j) {
-          const uint32_t b = block0 + j;
-          bar_wait(&sm.s_full[k], ss & 1, stop);
-          ++ss;
-          // the scores are there, so the scales are: this look never waits (before the
-          // scores it could take an older phase of the barrier for this one)
+        float f[8], r[8];  // a strip's factor of scores, its value scale
+        bool hidden = false;
+        float top_vs = 0.f;
+        auto scales = [&](uint32_t b) {
           bar_wait(&sm.scale_full[b % kChScales], (b / kChScales) & 1, stop);
-          const float *ksb = sm.ks[b % kChScales], *vsb = sm.vs[b % kChScales];
-          bool hidden = false;
-          float top_vs = 0.f;
+          const float4 *kp = reinterpret_cast<const float4 *>(sm.ks[b % kChScales]);
+          const float4 *vp = reinterpret_cast<const float4 *>(sm.vs[b % kChScales]);
+          const float4 k0 = kp[0], k1 = kp[1], v0 = vp[0], v1 = vp[1];
+          const float kk[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
+          const float vv[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+          hidden = false;
+          top_vs = 0.f;
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            hidden |= ksb[x] < 0.f;
-            top_vs = fmaxf(top_vs, fabsf(vsb[x]));
+            hidden |= kk[x] < 0.f;
+            f[x] = fabsf(kk[x]) * sl;
+            if (f[x] == 0.f) f[x] = 1e-37f;  // what is masked must stay at -infinity
+            r[x] = vv[x];
+            top_vs = fmaxf(top_vs, fabsf(vv[x]));
           }
+        };
+        for (int j = 0; j < blocks; ++j) {
+          // A block's scales are there before its scores.  Of the first block they are
+          // looked at after the scores: earlier an older phase of their barrier could be
+          // taken for this one.
+          if (j > 0) scales(block0 + j);
+          bar_wait(&sm.s_full[k], ss & 1, stop);
+          ++ss;
+          if (j == 0) scales(block0);
           __syncwarp();
           tc_after_sync();
-          const bool masked = hidden || (from + j + 1) * kPrBlock > all;
-          const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
-          // a strip's factor of scores; one of zero must leave what is masked at -infinity
-          auto factor = [&](int strip) {
-            const float f = fabsf(ksb[strip]) * sl;
-            return f == 0.f ? 1e-37f : f;
-          };
-          // 32 scores from column x, those that the row does not see at -infinity
-          auto mask = [&](uint32_t *s, int x) {
+          // what the row does not see goes to -infinity where it stands
+          if (hidden || (from + j + 1) * kPrBlock > all) {
+            const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
+            const float *ksb = sm.ks[(block0 + j) % kChScales];
+#pragma unroll 1
+            for (int x = 0; x < 128; x += 16) {
+              uint32_t v[16];
+              tmem_load16(v, ts + x);
+              tmem_wait_load();
+              const bool no = ksb[x / 16] < 0.f;
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (x + y >= rel || ksb[(x + y) / 16] < 0.f) s[y] = 0xff800000u;
-          };
+              for (int y = 0; y < 16; ++y)
+                if (no || x + y >= rel) v[y] = 0xff800000u;
+              tmem_store16(ts + x, v);
+            }
+            tmem_wait_store();
+          }
           // The scores are read from tensor memory twice, for the maximum and for the
           // weights: a thread that keeps its 128 has no registers left for the rest.
           float top = m;
-          uint32_t s[32];
-#pragma unroll 1
+          uint32_t s[2][32];
+          tmem_load32(s[0], ts);
+#pragma unroll
           for (int x = 0; x < 4; ++x) {
-            tmem_load32(s, ts + 32 * x);
             tmem_wait_load();
-            if (masked) mask(s, 32 * x);
+            tmem_load32(s[(x + 1) & 1], ts + 32 * ((x + 1) & 3));  // after the last the first again
+            const uint32_t *v = s[x & 1];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
               for (int z = 0; z < 16; z += 4) {
-                t0 = fmaxf(t0, fmaxf(__uint_as_float(s[16 * y + z]), __uint_as_float(s[16 * y + z + 1])));
-                t1 = fmaxf(t1, fmaxf(__uint_as_float(s[16 * y + z + 2]), __uint_as_float(s[16 * y + z + 3])));
+                t0 = fmaxf(t0, fmaxf(__uint_as_float(v[16 * y + z]), __uint_as_float(v[16 * y + z + 1])));
+                t1 = fmaxf(t1, fmaxf(__uint_as_float(v[16 * y + z + 2]), __uint_as_float(v[16 * y + z + 3])));
               }
-              top = fmaxf(top, fmaxf(t0, t1) * factor(2 * x + y));
+              top = fmaxf(top, fmaxf(t0, t1) * f[2 * x + y]);
             }
           }
           const bool grow_ref = !(top_vs <= kChRef * ref);
@@ -447,21 +468,20 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           const float base = m == -INFINITY ? -kChExp : m - kChExp;
           const uint64_t base2 = pair(-base, -base);
           uint64_t sum[2] = {0, 0};
-#pragma unroll 1
+#pragma unroll
           for (int x = 0; x < 4; ++x) {
-            tmem_load32(s, ts + 32 * x);
             tmem_wait_load();
-            if (masked) mask(s, 32 * x);
+            if (x < 3) tmem_load32(s[(x + 1) & 1], ts + 32 * (x + 1));
+            const uint32_t *v = s[x & 1];
             uint32_t w[16];
 #pragma unroll
             for (int y = 0; y < 16; ++y) {
-              const int strip = 2 * x + y / 8;
-              const float f = factor(strip), r = vsb[strip] * inv_ref;
+              const float fs = f[2 * x + y / 8], rs = r[2 * x + y / 8] * inv_ref;
               float p0, p1;
-              unpair(fma2(pair(__uint_as_float(s[2 * y]), __uint_as_float(s[2 * y + 1])), pair(f, f), base2), &p0, &p1);
+              unpair(fma2(pair(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1])), pair(fs, fs), base2), &p0, &p1);
               const uint64_t pp = pair(exp2_fast(p0), exp2_fast(p1));
               sum[y & 1] = add2(sum[y & 1], pp);
-              unpair(mul2(pp, pair(r, r)), &p0, &p1);
+              unpair(mul2(pp, pair(rs, rs)), &p0, &p1);
               w[y] = pack_half2(p0, p1);
             }
             tmem_store16(ts + 16 * x, w);  // over columns that were read
@@ -534,7 +554,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // products that were issued may still read shared memory
   if (bad) flag(a.status, kStatusData);
   __syncthreads();
-  if (warp == 12) tmem_free(tmem, 512);
+  if (warp == 16) tmem_free(tmem, 512);
 }
 
 // The items that several CTAs shared: a warp a row adds its parts in the line's
