@@ -48,7 +48,9 @@ struct ChunkSmem {
   uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2], scale_full[kChScales];
   PromptItem item[2];
-  alignas(16) float ks[kChScales][8], vs[kChScales][8];  // of a block's strips; ks < 0: hidden
+  alignas(16) float ks[kChScales][8], vs[kChScales][8];  // of a block's strips
+  float top_vs[kChScales];          // the largest |vs| of a block
+  uint32_t hidden[kChScales];       // its strips whose block is hidden, a bit each
   uint32_t state[kCodes][8];  // of a block's strips: keys that are there, bit 8: their sign is changed
   int64_t req[2], from[2];  // of each item: its request, its first block
   int whole[2], slot[2];    // no other CTA has a share of it; where its part goes
@@ -233,10 +235,15 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           const int strip = lane & 7;
           const int64_t pos = (from + j) * kPrBlock + strip * 16;
           const int there = id[0] < 0 ? 0 : (int)max((int64_t)0, min((int64_t)16, keys - pos));
+          float top = fabsf(vs[0]);
+#pragma unroll
+          for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+          const uint32_t gone = __ballot_sync(~0u, id[0] < 0) >> (lane & 24) & 255;
           if (mine) {
             const uint32_t at = (block + j) % kChScales;
-            sm.ks[at][strip] = id[0] < 0 ? -1.f : fabsf(ks[0]);
+            sm.ks[at][strip] = fabsf(ks[0]);
             sm.vs[at][strip] = vs[0];
+            if (strip == 0) sm.top_vs[at] = top, sm.hidden[at] = gone;
             bar_arrive(&sm.scale_full[at]);
           }
           const int64_t off = ((((int64_t)max(id[0], 0) * cv.heads + head) << cv.log_b) + (pos & ((1 << cv.log_b) - 1))) * D;
@@ -261,12 +268,11 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
     }
   } else if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    // Codes to fp16, 32 keys of each block a warp: eight lanes a key (D = 128), and of the
-    // two pieces of 16 bytes that a lane's codes become the upper half of the lanes
-    // stores the second one first, so that no two lanes of a quarter warp meet in a bank.
-    constexpr int kLanes = D / 16, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads
+    // Codes to fp16, 32 keys of each block a warp: a lane takes 8 codes of a key, which
+    // become one piece of 16 bytes; a quarter warp stores eight pieces of one row of
+    // 128 bytes, wherever the swizzle puts them, and no two of them meet in a bank.
+    constexpr int kLanes = D / 8, kKeys = 32 / kLanes, kSteps = 32 / kKeys;  // lanes a key, keys a load, loads
     const int w = warp & 3, sub = lane % kLanes, key_of = lane / kLanes;
-    const int second = sub >= 4 ? 1 : 0, piece = (sub % 4) * 2;
     // warps 8 to 11 the keys, 12 to 15 the values, which take turns in both rings
     RingAt code{0, 0}, to{0, 1};  // the first turn's stages are free
     if (warp >= 12) code = code.next(Smem::kCodes), to = to.next(Smem::kStages);
@@ -280,22 +286,26 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         bar_wait(&sm.code_full[code.st], code.phase, stop);
         bar_wait(&sm.kv_empty[to.st], to.phase, stop);
         __syncwarp();
-        const uint32_t state[2] = {sm.state[code.st][2 * w], sm.state[code.st][2 * w + 1]};
-        const unsigned char *from = sm.code[code.st] + 32 * w * D;
-        unsigned char *const at = sm.kv[to.st] + (sub / 4) * kChunk + 32 * w * 128;
-#pragma unroll 4
-        for (int x = 0; x < kSteps; ++x) {
-          const int key = x * kKeys + key_of;
-          const uint32_t st = x * kKeys >= 16 ? state[1] : state[0];
-          uint4 q = *reinterpret_cast<const uint4 *>(from + key * D + sub * 16);
-          if ((uint32_t)(key & 15) >= (st & 31)) q = make_uint4(0, 0, 0, 0);
-          const uint32_t flip = st & 256 ? 0x80808080u : 0u;
-          q.x ^= flip, q.y ^= flip, q.z ^= flip, q.w ^= flip;
-          const uint4 h0 = make_uint4(lo_half2(q.x), hi_half2(q.x), lo_half2(q.y), hi_half2(q.y));
-          const uint4 h1 = make_uint4(lo_half2(q.z), hi_half2(q.z), lo_half2(q.w), hi_half2(q.w));
-          unsigned char *const row = at + key * 128;
-          *reinterpret_cast<uint4 *>(row + (((piece + second) ^ (key & 7)) << 4)) = second ? h1 : h0;
-          *reinterpret_cast<uint4 *>(row + (((piece + 1 - second) ^ (key & 7)) << 4)) = second ? h0 : h1;
+        const uint32_t state0 = sm.state[code.st][2 * w], state1 = sm.state[code.st][2 * w + 1];
+        const unsigned char *from = sm.code[code.st] + 32 * w * D + key_of * D + sub * 8;
+        unsigned char *const at = sm.kv[to.st] + (sub / 8) * kChunk + (32 * w + key_of) * 128;
+        if (state0 == 16 && state1 == 16) {
+#pragma unroll
+          for (int x = 0; x < kSteps; ++x) {
+            const uint2 q = *reinterpret_cast<const uint2 *>(from + x * kKeys * D);
+            *reinterpret_cast<uint4 *>(at + x * kKeys * 128 + ((sub % 8 ^ (x * kKeys + key_of) % 8) << 4)) =
+                make_uint4(lo_half2(q.x), hi_half2(q.x), lo_half2(q.y), hi_half2(q.y));
+          }
+        } else {  // keys that are not there, or signs to change
+#pragma unroll 1
+          for (int x = 0; x < kSteps; ++x) {
+            const int key = x * kKeys + key_of;
+            const uint32_t st = key >= 16 ? state1 : state0, flip = st & 256 ? 0x80808080u : 0u;
+            uint2 q = *reinterpret_cast<const uint2 *>(from + x * kKeys * D);
+            q = (uint32_t)(key & 15) < (st & 31) ? make_uint2(q.x ^ flip, q.y ^ flip) : make_uint2(0, 0);
+            *reinterpret_cast<uint4 *>(at + x * kKeys * 128 + ((sub % 8 ^ key % 8) << 4)) =
+                make_uint4(lo_half2(q.x), hi_half2(q.x), lo_half2(q.y), hi_half2(q.y));
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -340,15 +350,14 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         __syncwarp();
         {
           const uint16_t *qp = (const uint16_t *)a.q + ((int64_t)it.first + tok) * a.q_stride + (int64_t)h * D;
-          uint4 x[D / 8];
-#pragma unroll
-          for (int y = 0; y < D / 8; ++y) x[y] = valid ? reinterpret_cast<const uint4 *>(qp)[y] : make_uint4(0, 0, 0, 0);
+          const uint4 *qv = reinterpret_cast<const uint4 *>(qp);
           float up = 1.f;
           if (!F16) {
             uint32_t top = 0;
-#pragma unroll
+#pragma unroll 4
             for (int y = 0; y < D / 8; ++y) {
-              const uint32_t v[4] = {x[y].x, x[y].y, x[y].z, x[y].w};
+              const uint4 x = valid ? qv[y] : make_uint4(0, 0, 0, 0);
+              const uint32_t v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int z = 0; z < 4; ++z) top = max(top, max(v[z] & 0x7fff0000u, (v[z] & 0x7fffu) << 16));
             }
@@ -356,44 +365,42 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
             up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
             sl *= __uint_as_float((uint32_t)(127 - 14 + e) << 23);
           }
-#pragma unroll
+#pragma unroll 4
           for (int y = 0; y < D / 8; ++y) {
+            uint4 x = valid ? qv[y] : make_uint4(0, 0, 0, 0);
             if (!F16) {
-              uint32_t v[4] = {x[y].x, x[y].y, x[y].z, x[y].w};
+              uint32_t v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int z = 0; z < 4; ++z) {
                 const float2 f = unpack2<false>(v[z]);
                 v[z] = pack_half2(f.x * up, f.y * up);
               }
-              x[y] = make_uint4(v[0], v[1], v[2], v[3]);
+              x = make_uint4(v[0], v[1], v[2], v[3]);
             }
-            *reinterpret_cast<uint4 *>(sm.q[k] + (y / 8) * kChunk + row * 128 + (((y % 8) ^ (row & 7)) << 4)) = x[y];
+            *reinterpret_cast<uint4 *>(sm.q[k] + (y / 8) * kChunk + row * 128 + (((y % 8) ^ (row & 7)) << 4)) = x;
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) bar_arrive(&sm.q_full[k]);
           ++qs;
         }
+        // in keys from the item's first on: what the row sees, what every row of the tile sees
+        const int sees = (int)max((int64_t)0, min((int64_t)INT32_MAX, lim - from * kPrBlock));
+        const int all_see = (int)max((int64_t)0, min((int64_t)INT32_MAX, all - from * kPrBlock));
         float f[8], r[8];  // a strip's factor of scores, its value scale
-        bool hidden = false;
         float top_vs = 0.f;
+        uint32_t hidden = 0;
         auto scales = [&](uint32_t b) {
           bar_wait(&sm.scale_full[b % kChScales], (b / kChScales) & 1, stop);
           const float4 *kp = reinterpret_cast<const float4 *>(sm.ks[b % kChScales]);
           const float4 *vp = reinterpret_cast<const float4 *>(sm.vs[b % kChScales]);
           const float4 k0 = kp[0], k1 = kp[1], v0 = vp[0], v1 = vp[1];
-          const float kk[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
-          const float vv[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-          hidden = false;
-          top_vs = 0.f;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            hidden |= kk[x] < 0.f;
-            f[x] = fabsf(kk[x]) * sl;
-            if (f[x] == 0.f) f[x] = 1e-37f;  // what is masked must stay at -infinity
-            r[x] = vv[x];
-            top_vs = fmaxf(top_vs, fabsf(vv[x]));
-          }
+          top_vs = sm.top_vs[b % kChScales];
+          hidden = sm.hidden[b % kChScales];
+          f[0] = k0.x * sl, f[1] = k0.y * sl, f[2] = k0.z * sl, f[3] = k0.w * sl;
+          f[4] = k1.x * sl, f[5] = k1.y * sl, f[6] = k1.z * sl, f[7] = k1.w * sl;
+          r[0] = v0.x, r[1] = v0.y, r[2] = v0.z, r[3] = v0.w;
+          r[4] = v1.x, r[5] = v1.y, r[6] = v1.z, r[7] = v1.w;
         };
         for (int j = 0; j < blocks; ++j) {
           // A block's scales are there before its scores.  Of the first block they are
@@ -406,21 +413,23 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           __syncwarp();
           tc_after_sync();
           // what the row does not see goes to -infinity where it stands
-          if (hidden || (from + j + 1) * kPrBlock > all) {
-            const int rel = (int)max((int64_t)0, min((int64_t)128, lim - (from + j) * kPrBlock));
-            const float *ksb = sm.ks[(block0 + j) % kChScales];
+          if (hidden || (j + 1) * kPrBlock > all_see) {
+            const int rel = sees - j * kPrBlock;
 #pragma unroll 1
             for (int x = 0; x < 128; x += 16) {
               uint32_t v[16];
               tmem_load16(v, ts + x);
               tmem_wait_load();
-              const bool no = ksb[x / 16] < 0.f;
+              const bool no = hidden >> (x / 16) & 1;
 #pragma unroll
               for (int y = 0; y < 16; ++y)
                 if (no || x + y >= rel) v[y] = 0xff800000u;
               tmem_store16(ts + x, v);
             }
             tmem_wait_store();
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (f[x] == 0.f) f[x] = 1e-37f;  // it must stay there
           }
           // The scores are read from tensor memory twice, for the maximum and for the
           // weights: a thread that keeps its 128 has no registers left for the rest.
