@@ -51,20 +51,27 @@ __device__ __forceinline__ uint32_t pack_out(float a, float b) {
   return r;
 }
 
+// a / b for 0 <= a, 0 < b: a 64-bit division is a long chain of instructions, and
+// hardly ever needed.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Running sums of units(k), k < n <= kScan, by a block of T threads, into
-// S[0 .. n], from base up; returns the last.
+// S[0 .. n], from base up; returns the last.  A thread takes neighbours, no more
+// than there must be, and asks for all of them before it adds up any.
 constexpr int kScan = 1024;  // requests whose running sums fit in shared memory
 
 template <int T, class F>
 __device__ __forceinline__ int64_t scan_units(int n, int64_t *S, int64_t base, F units) {
   constexpr int kPer = (kScan + T - 1) / T;
   __shared__ int64_t warp_sum[T / 32];
-  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, per = (n + T - 1) / T;
   int64_t u[kPer], sum = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const int i = tid * kPer + k;
-    u[k] = i < n ? units(i) : 0;
+    const int i = tid * per + k;
+    u[k] = k < per && i < n ? units(i) : 0;
     sum += u[k];
   }
   int64_t x = sum;
@@ -85,8 +92,8 @@ __device__ __forceinline__ int64_t scan_units(int n, int64_t *S, int64_t base, F
   x += base + before - sum;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const int i = tid * kPer + k;
-    if (i < n) S[i] = x;
+    const int i = tid * per + k;
+    if (k < per && i < n) S[i] = x;
     x += u[k];
   }
   if (tid == 0) S[n] = base + total;

@@ -12,7 +12,7 @@
 // memory into the registers of one warp in the order in which the products want
 // it: the sums over D and over keys may take their terms in any order, so lane
 // (g, t) = (lane / 4, lane % 4) takes D/4 neighbouring codes of keys g and g + 8
-// for K, and D/8 of keys 2t, 2t+1, 2t+8, 2t+9 for V, and no shared memory is
+// for K (16 and, 64 on, 16 more), and D/8 of keys 2t, 2t+1, 2t+8, 2t+9 for V, and no shared memory is
 // passed.  e4m3 to fp16 is exact.  P^T is S^T's registers transposed (movmatrix).
 //
 // Weights are 2^(x - m + 12) with m the row's running maximum of x = log2(e)
@@ -33,7 +33,10 @@
 
 namespace lv {
 
+// CTAs of an SM, with one and two row tiles of 8.
+constexpr int kDecCtas1 = 4, kDecCtas2 = 2;
 constexpr int kDecWarps = 4;       // warps of a CTA; they share only the scan
+constexpr int kDecSegment = 4;
 constexpr int kDecMinStrips = 8;   // strips a warp takes at least
 constexpr int kDecRows = 16;       // rows of a request that go here: two row tiles of 8
 constexpr int kJoinWarps = 8;
@@ -93,13 +96,17 @@ __device__ __forceinline__ int64_t span_strips(const AttendArgs &a, const Span &
   return max((int64_t)1, (row_limit(a, s, s.p - 1) + 15) >> 4);  // one of none, so that its rows are written
 }
 
+// What a segment counts for in the line: its strips, and what its beginning and its
+// end cost in strips' time, so that a warp of many short ones is given fewer.
+__device__ __forceinline__ int64_t segment_units(int64_t strips) { return strips + kDecSegment; }
+
 __device__ __forceinline__ int span_tiles(const AttendArgs &a, const Span &s, int rows) {
-  return (int)(((int64_t)s.p * (a.hq / a.hkv) + rows - 1) / rows);
+  return (int)quotient((int64_t)s.p * (a.hq / a.hkv) + rows - 1, rows);
 }
 
 __device__ __forceinline__ int64_t request_units(const DecodeArgs &d, int64_t i, bool *bad) {
   const Span s = request_span(d.a, i, bad);
-  return s.p == 0 || (int64_t)s.p * (d.a.hq / d.a.hkv) > d.most_rows ? 0 : span_strips(d.a, s) * span_tiles(d.a, s, 8 * d.nt) * d.a.hkv;
+  return s.p == 0 || (int64_t)s.p * (d.a.hq / d.a.hkv) > d.most_rows ? 0 : segment_units(span_strips(d.a, s)) * span_tiles(d.a, s, 8 * d.nt) * d.a.hkv;
 }
 
 // The running sums of more than kScan requests, by one CTA.
@@ -115,15 +122,15 @@ __global__ void __launch_bounds__(kScan) k_attend_prefix(DecodeArgs d) {
 
 // Warps that take strips, and the first strip of warp w.
 __device__ __forceinline__ int64_t busy_warps(int64_t warps, int64_t units) {
-  return max((int64_t)1, min(warps, units / kDecMinStrips));
+  return max((int64_t)1, min(warps, quotient(units, kDecMinStrips)));
 }
 __device__ __forceinline__ int64_t warp_start(int64_t w, int64_t W, int64_t units) {
-  const int64_t q = units / W, r = units % W;  // the first r warps take one more
+  const int64_t q = quotient(units, W), r = units - q * W;  // the first r warps take one more
   return w * q + min(w, r);
 }
 __device__ __forceinline__ int64_t warp_of(int64_t u, int64_t W, int64_t units) {
-  const int64_t q = units / W, r = units % W, cut = r * (q + 1);
-  return u < cut ? u / (q + 1) : r + (u - cut) / q;
+  const int64_t q = quotient(units, W), r = units - q * W, cut = r * (q + 1);
+  return u < cut ? quotient(u, q + 1) : r + quotient(u - cut, q);
 }
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -170,29 +177,29 @@ struct Strip {
   uint32_t k[2][D / 16];
   uint32_t v[4][D / 32];
 
-  __device__ __forceinline__ void load(const uint8_t *kp, const uint8_t *vp, int lane, int keys) {
+  __device__ __forceinline__ void load_keys(const uint8_t *p, int lane, int keys) {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const bool in = g + 8 * r < keys;
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int j = 0; j < D / 16; j += 4) {
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (in) x = load16(kp + (g + 8 * r) * D + t * (D / 4) + 4 * j);
+        if (g + 8 * r < keys) x = load16(p + (g + 8 * r) * D + 16 * j + t * 16);  // 64 bytes in a row
         k[r][j] = x.x, k[r][j + 1] = x.y, k[r][j + 2] = x.z, k[r][j + 3] = x.w;
       }
-    }
+  }
+  __device__ __forceinline__ void load_values(const uint8_t *p, int lane, int keys) {
+    const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int key = 2 * t + (r & 1) + 8 * (r >> 1);
-      const bool in = key < keys;
       if (D == 128) {
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (in) x = load16(vp + key * D + g * (D / 8));
+        if (key < keys) x = load16(p + key * D + g * (D / 8));
         v[r][0] = x.x, v[r][1] = x.y, v[r][D / 32 - 2] = x.z, v[r][D / 32 - 1] = x.w;
       } else {
         uint2 x = make_uint2(0, 0);
-        if (in) x = load8(vp + key * D + g * (D / 8));
+        if (key < keys) x = load8(p + key * D + g * (D / 8));
         v[r][0] = x.x, v[r][1] = x.y;
       }
     }
@@ -200,7 +207,7 @@ struct Strip {
 };
 
 template <int D, bool F16, int NT>
-__global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_decode(DecodeArgs d) {
+__global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas2) k_attend_decode(DecodeArgs d) {
   constexpr int kRows = 8 * NT, kM = D / 16;  // row tile; tiles of 16 elements of the output
   __shared__ int64_t shared_sums[kScan + 1];
   const AttendArgs &a = d.a;
@@ -227,25 +234,57 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
     const int64_t i = find_unit(sums, a.n_req, u);
     bool ignore = false;
     const Span sp = request_span(a, i, &ignore);
-    const int64_t strips = span_strips(a, sp);
+    const int64_t strips = span_strips(a, sp), all_units = segment_units(strips);
     const int tiles = span_tiles(a, sp, kRows);
-    const int64_t seg = (u - sums[i]) / strips, s0 = (u - sums[i]) % strips, s1 = min(strips, s0 + end - u);
-    const int h = (int)(seg / tiles), row0 = (int)(seg % tiles) * kRows;
+    const int64_t seg = quotient(u - sums[i], all_units), s0 = u - sums[i] - seg * all_units, s1 = min(strips, s0 + end - u);
+    if (s0 >= strips) {
+      u += all_units - s0;
+      continue;
+    }
+    const int h = (int)seg / tiles, row0 = ((int)seg - h * tiles) * kRows;
     // query rows: lane (g, t) holds D/4 elements of rows g + 8 nt
     uint32_t qf[NT][D / 8];
     float f[NT][2];       // x = f ks S, rows 2t and 2t + 1
-    int64_t lim[NT][2];   // keys these rows see
-    int64_t least = INT64_MAX;
+    int lim[NT][2];       // keys these rows see, from the first strip on
+    int least = INT32_MAX;
+    const int64_t key0 = s0 << 4;
+    auto from_key0 = [&](int64_t keys) { return (int)max((int64_t)0, min((int64_t)INT32_MAX, keys - key0)); };
+    const int most = from_key0(row_limit(a, sp, sp.p - 1)), count = (int)(s1 - s0);
+    // 32 strips at a time, a strip a lane: the blocks of these, of the next 32 and of
+    // those after, the scales of these and of the next, so that no load is waited
+    // for where it is issued
+    int32_t id0, id1, id2;
+    float ks, vs, next_ks, next_vs;
+    const int32_t *const table_row = a.table + i * a.width;
+    auto look_up = [&](int s) {
+      const int mine = s + lane;
+      return mine < count && (mine << 4) < most ? table_row[(key0 + (mine << 4)) >> a.cache.log_b] : -1;
+    };
+    auto checked = [&](int32_t id) {
+      if (id >= -1 && id < a.cache.n_blocks) return id;
+      bad = true;
+      return -1;
+    };
+    auto scales_of = [&](int32_t id, float *k, float *v) {
+      *k = *v = 0.f;
+      if (id >= 0) {
+        *k = a.cache.k_scale[(int64_t)id * a.cache.heads + h];
+        *v = a.cache.v_scale[(int64_t)id * a.cache.heads + h];
+      }
+    };
+    id0 = look_up(0);
+    id1 = look_up(32);
+    id2 = look_up(64);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int row = row0 + 8 * nt + g, j = row / G, hh = row % G;
       const bool in = j < sp.p;
-      const uint16_t *qp = (const uint16_t *)a.q + (sp.first + j) * a.q_stride + ((int64_t)h * G + hh) * D + t * (D / 4);
+      const uint16_t *qp = (const uint16_t *)a.q + (sp.first + j) * a.q_stride + ((int64_t)h * G + hh) * D + t * 16;
       float mine = a.scale;
 #pragma unroll
-      for (int k = 0; k < D / 8; k += 4) {
+      for (int k = 0; k < D / 8; k += 4) {  // 16 elements, and those 64 elements on
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (in) x = *reinterpret_cast<const uint4 *>(qp + 2 * k);
+        if (in) x = *reinterpret_cast<const uint4 *>(qp + k / 8 * 64 + k % 8 * 2);
         qf[nt][k] = x.x, qf[nt][k + 1] = x.y, qf[nt][k + 2] = x.z, qf[nt][k + 3] = x.w;
       }
       if (!F16) {
@@ -269,13 +308,12 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
       for (int r = 0; r < 2; ++r) {
         f[nt][r] = __shfl_sync(~0u, mine, (2 * t + r) * 4);
         const int jr = (row0 + 8 * nt + 2 * t + r) / G;
-        lim[nt][r] = jr < sp.p ? row_limit(a, sp, jr) : 0;
+        lim[nt][r] = jr < sp.p ? from_key0(row_limit(a, sp, jr)) : 0;
         if (jr < sp.p) least = min(least, lim[nt][r]);
       }
     }
-    least = min(least, (int64_t)__shfl_xor_sync(~0u, least, 1));
-    least = min(least, (int64_t)__shfl_xor_sync(~0u, least, 2));
-    const int64_t most = row_limit(a, sp, sp.p - 1);
+    least = min(least, __shfl_xor_sync(~0u, least, 1));
+    least = min(least, __shfl_xor_sync(~0u, least, 2));
 
     float o[NT][kM][4], m[NT][2], l[NT][2], ref = 0.f, inv_ref = 0.f;
 #pragma unroll
@@ -285,34 +323,36 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
       m[nt][0] = m[nt][1] = -INFINITY;
       l[nt][0] = l[nt][1] = 0.f;
     }
-    // 32 strips' blocks and scales at a time, a strip a lane
-    int32_t id = -1;
-    float ks = 0.f, vs = 0.f;
-    auto look_up = [&](int64_t s) {
-      id = -1;
-      const int64_t mine = s + lane;
-      if (mine < s1 && (mine << 4) < most) {
-        id = a.table[i * a.width + ((mine << 4) >> a.cache.log_b)];
-        if (id < -1 || id >= a.cache.n_blocks) {
-          bad = true;
-          id = -1;
-        }
-        if (id >= 0) {
-          ks = a.cache.k_scale[(int64_t)id * a.cache.heads + h];
-          vs = a.cache.v_scale[(int64_t)id * a.cache.heads + h];
-        }
+    // One strip's registers: the next keys are loaded once these have met the
+    // queries, the next values once these have met the weights, each a whole strip's
+    // time ahead.  (Two strips' registers and 12 warps an SM: 4.5 TB/s.)
+    Strip<D> x;
+    auto place = [&](int s) {  // of strip s, whose id the lanes hold; negative: hidden
+      const int32_t b = __shfl_sync(~0u, id0, s & 31);
+      return b < 0 ? (int64_t)-1
+                   : ((((int64_t)b * a.cache.heads + h) << a.cache.log_b) +
+                      ((key0 + (s << 4)) & ((1 << a.cache.log_b) - 1))) * D;
+    };
+    id0 = checked(id0);
+    scales_of(id0, &ks, &vs);
+    int64_t at = place(0);
+    if (at >= 0) {
+      x.load_keys(a.cache.k + at, lane, min(16, most));
+      x.load_values(a.cache.v + at, lane, min(16, most));
+    }
+    id1 = checked(id1);
+    scales_of(id1, &next_ks, &next_vs);
+    for (int s = 0; s < count; ++s) {
+      const float kss = __shfl_sync(~0u, ks, s & 31), vss = __shfl_sync(~0u, vs, s & 31);
+      const bool here = at >= 0;
+      if (((s + 1) & 31) == 0) {
+        id0 = id1, ks = next_ks, vs = next_vs;
+        id1 = checked(id2);
+        scales_of(id1, &next_ks, &next_vs);
+        id2 = look_up(s + 65);
       }
-    };
-    Strip<D> strip[2];
-    auto fetch = [&](Strip<D> &to, int64_t s, int at) {
-      const int32_t b = __shfl_sync(~0u, id, at);
-      if (b < 0) return;
-      const int64_t off = ((((int64_t)b * a.cache.heads + h) << a.cache.log_b) + ((s << 4) & ((1 << a.cache.log_b) - 1))) * D;
-      to.load(a.cache.k + off, a.cache.v + off, lane, (int)min((int64_t)16, most - (s << 4)));
-    };
-    auto use = [&](const Strip<D> &x, int64_t s, int at) {
-      if (__shfl_sync(~0u, id, at) < 0) return;
-      const float kss = __shfl_sync(~0u, ks, at), vss = __shfl_sync(~0u, vs, at);
+      at = s + 1 < count ? place(s + 1) : -1;
+      const int keys = min(16, most - ((s + 1) << 4));
       float c[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
@@ -321,6 +361,11 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
         const uint32_t ka[4] = {lo_half2(x.k[0][k]), lo_half2(x.k[1][k]), hi_half2(x.k[0][k]), hi_half2(x.k[1][k])};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mma16816(c[nt], ka, qf[nt][2 * k], qf[nt][2 * k + 1]);
+      }
+      if (at >= 0) x.load_keys(a.cache.k + at, lane, keys);
+      if (!here) {
+        if (at >= 0) x.load_values(a.cache.v + at, lane, keys);
+        continue;
       }
       bool grow = !(fabsf(vss) <= ref);
 #pragma unroll
@@ -385,17 +430,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
           mma16816(o[nt][2 * q4 + 1], vb, pb[nt][0], pb[nt][1]);
         }
       }
-    };
-    for (int64_t s = s0; s < s1; s += 32) {
-      look_up(s);
-      const int n = (int)min((int64_t)32, s1 - s);
-      fetch(strip[0], s, 0);
-      for (int k = 0; k < n; k += 2) {
-        if (k + 1 < n) fetch(strip[1], s + k + 1, k + 1);
-        use(strip[0], s + k, k);
-        if (k + 2 < n) fetch(strip[0], s + k + 2, k + 2);
-        if (k + 1 < n) use(strip[1], s + k + 1, k + 1);
-      }
+      if (at >= 0) x.load_values(a.cache.v + at, lane, keys);
     }
     // l over the keys' lanes; lane (g, t) has elements D/8 g .. of rows 2t, 2t + 1
     const bool whole = s0 == 0 && s1 == strips;
@@ -449,7 +484,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? 3 : 2) k_attend_deco
             redo_row<D, F16, true>(a, sp.first, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j));
         }
     }
-    u += s1 - s0;
+    u += s1 == strips ? all_units - s0 : s1 - s0;
   }
   if (bad) flag(a.status, kStatusData);
 }
@@ -474,11 +509,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
   const int64_t strips = span_strips(a, sp);
   const int tiles = span_tiles(a, sp, rows), groups = per_row == 1 ? rows / kJoinWarps : rows;
   for (int64_t y = blockIdx.y; y < (int64_t)tiles * a.hkv * groups; y += gridDim.y) {
-    const int64_t seg = y / groups;
-    const int64_t u0 = d.prefix[i] + seg * strips, w0 = warp_of(u0, W, units), w1 = warp_of(u0 + strips - 1, W, units);
+    const int64_t seg = (int)y / groups;
+    const int64_t u0 = d.prefix[i] + seg * segment_units(strips), w0 = warp_of(u0, W, units), w1 = warp_of(u0 + strips - 1, W, units);
     if (w0 == w1) continue;
-    const int h = (int)(seg / tiles), r = (int)(y % groups) * (per_row == 1 ? kJoinWarps : 1) + (per_row == 1 ? w : 0);
-    const int row = (int)(seg % tiles) * rows + r, j = row / G, hh = h * G + row % G;
+    const int h = (int)seg / tiles, r = ((int)y % groups) * (per_row == 1 ? kJoinWarps : 1) + (per_row == 1 ? w : 0);
+    const int row = ((int)seg % tiles) * rows + r, j = row / G, hh = h * G + row % G;
     float top = -INFINITY, l = 0.f, o[E];
 #pragma unroll
     for (int k = 0; k < E; ++k) o[k] = 0.f;

@@ -45,6 +45,23 @@ lv_status scratch_for(KvHost *kv, size_t bytes) {
   return LV_OK;
 }
 
+// The context's two counters for work that kernels hand out.
+lv_status counters_for(KvHost *kv) {
+  if (!kv->counter) {
+    void *c = nullptr;
+    if (cudaMalloc(&c, 2 * sizeof(unsigned long long)) != cudaSuccess) {
+      cudaGetLastError();
+      return LV_ENOMEM;
+    }
+    if (cudaMemset(c, 0, 2 * sizeof(unsigned long long)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+      cudaFree(c);
+      return LV_ECUDA;
+    }
+    kv->counter = static_cast<unsigned long long *>(c);
+  }
+  return LV_OK;
+}
+
 bool cache_ok(const lv_kv_cache *c) {
   if (!c || c->n_blocks < 0 || c->n_blocks > (1ll << 31) || c->n_kv_heads < 1 || c->n_kv_heads > 1024) return false;
   if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128) return false;
@@ -86,13 +103,14 @@ lv_status launch_after(void (*kernel)(P...), dim3 grid, unsigned block, size_t s
 
 template <int D, bool F16, int NT>
 lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
-  constexpr int kPerSm = NT == 1 ? 3 : 2;  // as the kernel's launch bounds have it
   DecodeArgs d{};
   d.a = a;
   d.nt = NT;
   d.most_rows = kDecRows;
-  const int64_t ctas = (int64_t)kv->sms * kPerSm;
+  const int64_t ctas = (int64_t)kv->sms * (NT == 1 ? kDecCtas1 : kDecCtas2);
   d.warps = ctas * kDecWarps;
+  const int G = a.hq / a.hkv, tiles = (G + 8 * NT - 1) / (8 * NT);
+  const int64_t segments = a.n_req * a.hkv * tiles;
   // scratch: running sums, the parts
   const size_t o_part = (8 * ((size_t)a.n_req + 1) + 255) & ~(size_t)255;
   const size_t slots = 2 * (size_t)d.warps * 8 * NT;
@@ -108,9 +126,6 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   }
   k_attend_decode<D, F16, NT><<<(unsigned)ctas, kDecWarps * 32, 0, stream>>>(d);
   LV_CUDA(cudaGetLastError());
-  // a segment of up to kDecMinStrips strips is never shared... unless it lies across two warps' ends
-  const int G = a.hq / a.hkv, tiles = (G + 8 * NT - 1) / (8 * NT);
-  const int64_t segments = a.n_req * a.hkv * tiles;
   const int per_row = segments < kv->sms ? kJoinWarps : 1;
   const int64_t y = (int64_t)a.hkv * tiles * (per_row == 1 ? NT : 8 * NT);
   return launch_after(k_attend_join<D, F16>, dim3((unsigned)a.n_req, (unsigned)std::min<int64_t>(y, 4096)),
@@ -205,18 +220,8 @@ lv_status run_prompt(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   if (st == LV_OK) st = map_rows(&mk, a.k, dtype, a.n_tok, a.hkv, D, a.k_stride, kPrBlock, 1);
   if (st == LV_OK) st = map_rows(&mv, a.v, dtype, a.n_tok, a.hkv, D, a.v_stride, kPrBlock, 1);
   if (st != LV_OK) return st;
-  if (!kv->counter) {
-    void *c = nullptr;
-    if (cudaMalloc(&c, 2 * sizeof(unsigned long long)) != cudaSuccess) {
-      cudaGetLastError();
-      return LV_ENOMEM;
-    }
-    if (cudaMemset(c, 0, 2 * sizeof(unsigned long long)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
-      cudaFree(c);
-      return LV_ECUDA;
-    }
-    kv->counter = static_cast<unsigned long long *>(c);
-  }
+  st = counters_for(kv);
+  if (st != LV_OK) return st;
   p.counter = kv->counter;
   p.given = a.n_req > kScan;
   if (p.given) {

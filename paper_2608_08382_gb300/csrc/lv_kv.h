@@ -14,7 +14,7 @@ struct KvHost {
   int *d_status = nullptr;           // the context's status word
   unsigned char *scratch = nullptr;  // owned
   size_t cap = 0;
-  unsigned long long *counter = nullptr;       // owned: work handed out by lv_prompt_attend's kernel, zero between calls
+  unsigned long long *counter = nullptr;  // owned: two counters of work that kernels hand out, zero between calls
 };
 
 KvHost *kv_host(lv_ctx *ctx);
