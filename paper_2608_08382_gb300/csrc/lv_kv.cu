@@ -283,10 +283,13 @@ lv_status lv_kv_plan(lv_ctx *ctx, const int32_t *p, const int32_t *c, int64_t n_
     k_plan_sums<<<(unsigned)tiles, kPlanThreads, 0, stream>>>(a);
     LV_CUDA(cudaGetLastError());
   }
-  const int64_t per = (std::max(n_slots, n_req) / tiles + kPlanThreads - 1) / kPlanThreads;
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(per, 2 * kv->sms / std::min<int64_t>(tiles, kv->sms)));
+  // CTAs of a tile: one for each 2,048 slots, up to three an SM in all
+  const int64_t per = (std::max(n_slots, n_req) / tiles + 2047) / 2048;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(per, 3 * kv->sms / std::min<int64_t>(tiles, kv->sms)));
   static_assert(sizeof(PlanSmem) <= 48 << 10, "static limit");
-  k_plan<<<dim3((unsigned)slices, (unsigned)tiles), kPlanThreads, sizeof(PlanSmem), stream>>>(a);
+  const dim3 grid((unsigned)slices, (unsigned)tiles);
+  if (tiles > 1) return launch_after(k_plan, grid, kPlanThreads, sizeof(PlanSmem), stream, a);
+  k_plan<<<grid, kPlanThreads, sizeof(PlanSmem), stream>>>(a);
   LV_CUDA(cudaGetLastError());
   return LV_OK;
 }
@@ -312,13 +315,13 @@ lv_status lv_kv_store(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, cons
   a.log_b = log2_of(cache->block_tokens);
   a.heads = heads;
   a.status = kv->d_status;
-  const int64_t blocks = (n_tok * 2 * heads + 7) / 8;
-  if (blocks > INT32_MAX) return LV_EINVAL;
-  const unsigned grid = (unsigned)blocks;
-  if (d == 128 && dtype == LV_F16) k_kv_store<128, true><<<grid, 256, 0, stream>>>(a);
-  if (d == 128 && dtype == LV_BF16) k_kv_store<128, false><<<grid, 256, 0, stream>>>(a);
-  if (d == 64 && dtype == LV_F16) k_kv_store<64, true><<<grid, 256, 0, stream>>>(a);
-  if (d == 64 && dtype == LV_BF16) k_kv_store<64, false><<<grid, 256, 0, stream>>>(a);
+  int window = 1;  // four CTAs an SM, where there are tokens for them
+  while (window < kStoreWindow && n_tok / (2 * window) >= 4 * kv->sms) window *= 2;
+  const unsigned grid = (unsigned)((n_tok + window - 1) / window);
+  if (d == 128 && dtype == LV_F16) k_kv_store<128, true><<<grid, kStoreWarps * 32, 0, stream>>>(a, window);
+  if (d == 128 && dtype == LV_BF16) k_kv_store<128, false><<<grid, kStoreWarps * 32, 0, stream>>>(a, window);
+  if (d == 64 && dtype == LV_F16) k_kv_store<64, true><<<grid, kStoreWarps * 32, 0, stream>>>(a, window);
+  if (d == 64 && dtype == LV_BF16) k_kv_store<64, false><<<grid, kStoreWarps * 32, 0, stream>>>(a, window);
   LV_CUDA(cudaGetLastError());
   return LV_OK;
 }

@@ -19,6 +19,7 @@ namespace lv {
 constexpr int kPlanThreads = 512;
 constexpr int kPlanPer = 4;                             // requests of one thread
 constexpr int kPlanTile = kPlanThreads * kPlanPer;      // requests of a tile
+constexpr int kPlanSpan = 128;                          // entries or slots of a warp's turn
 
 struct PlanArgs {
   const int32_t *p, *c;
@@ -87,9 +88,9 @@ struct PlanSmem {
   int64_t before[2];
 };
 
-// The request of the tile whose range [S[i], S[i+1]) holds x.
-__device__ __forceinline__ int plan_find(const int64_t *S, int64_t x) {
-  int lo = 0, hi = kPlanTile;  // S[lo] <= x < S[hi]
+// The last request of lo .. hi - 1 whose range [S[i], S[i+1]) begins at or before
+// x; S[lo] <= x.
+__device__ __forceinline__ int plan_find(const int64_t *S, int64_t x, int lo, int hi) {
   while (hi - lo > 1) {
     const int m = (lo + hi) >> 1;
     if (S[m] <= x) lo = m; else hi = m;
@@ -163,30 +164,52 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs a) {
     a.counts[1] = s.E[kPlanTile];
     bad |= s.X[kPlanTile] > a.n_slots;
   }
+  // Where there is little, a quarter of the warps takes the entries and the others
+  // the slots, so that one does not wait for the other.
+  const bool little = s.X[kPlanTile] - s.X[0] <= 12 * kPlanSpan && s.E[kPlanTile] - s.E[0] <= 4 * kPlanSpan && gridDim.x == 1;
+  const int top = (int)n;  // requests to search among
+  // A warp takes 128 entries or slots at a time: two searches find the requests of
+  // the first and the last of them, and the lanes search between those (a long
+  // prompt's tokens not at all).
+  const int64_t wfirst = ((int64_t)blockIdx.x * (kPlanThreads / 32) + w) * kPlanSpan, wstep = step * (kPlanSpan / 32);
+  const int64_t efirst = !little ? wfirst : w % 4 == 0 ? w / 4 * kPlanSpan : 4 * kPlanSpan;
+  const int64_t xfirst = !little ? wfirst : w % 4 != 0 ? (w / 4 * 3 + w % 4 - 1) * kPlanSpan : 12 * kPlanSpan;
   // new table entries
   const int64_t e1 = s.E[kPlanTile];
-  for (int64_t k = s.E[0] + first; k < e1; k += step) {
-    const int i = plan_find(s.E, k);
-    const int64_t col = ceil_blocks(s.c[i], a.log_b) + (k - s.E[i]);
-    if (col < a.width)
-      a.table[(base + i) * a.width + col] = s.E[i + 1] <= a.n_free ? a.free[k] : -1;
-    else
-      bad = true;
+  for (int64_t k0 = s.E[0] + efirst; k0 < e1; k0 += wstep) {
+    const int lo = plan_find(s.E, k0, 0, top), hi = plan_find(s.E, min(k0 + kPlanSpan, e1) - 1, lo, kPlanTile) + 1;
+#pragma unroll
+    for (int y = 0; y < kPlanSpan; y += 32) {
+      const int64_t k = k0 + y + lane;
+      if (k >= e1) break;
+      const int i = plan_find(s.E, k, lo, hi);
+      const int64_t col = ceil_blocks(s.c[i], a.log_b) + (k - s.E[i]);
+      if (col < a.width)
+        a.table[(base + i) * a.width + col] = s.E[i + 1] <= a.n_free ? a.free[k] : -1;
+      else
+        bad = true;
+    }
   }
   // slots
   const int64_t x1 = min(s.X[kPlanTile], a.n_slots);
-  for (int64_t t = s.X[0] + first; t < x1; t += step) {
-    const int i = plan_find(s.X, t);
-    const int64_t pos = (int64_t)s.c[i] + (t - s.X[i]), col = pos >> a.log_b;
-    const int64_t fresh = col - ceil_blocks(s.c[i], a.log_b);  // which of the new blocks
-    int64_t b = -1;
-    if (col >= a.width)
-      bad = true;
-    else if (fresh < 0)
-      b = a.table[(base + i) * a.width + col];
-    else if (s.E[i + 1] <= a.n_free)
-      b = a.free[s.E[i] + fresh];
-    a.slots[t] = b < 0 ? -1 : (b << a.log_b) + (pos & ((1 << a.log_b) - 1));
+  for (int64_t t1 = s.X[0] + xfirst; t1 < x1; t1 += wstep) {
+    const int lo = plan_find(s.X, t1, 0, top), hi = plan_find(s.X, min(t1 + kPlanSpan, x1) - 1, lo, kPlanTile) + 1;
+#pragma unroll
+    for (int y = 0; y < kPlanSpan; y += 32) {
+      const int64_t t = t1 + y + lane;
+      if (t >= x1) break;
+      const int i = plan_find(s.X, t, lo, hi);
+      const int64_t pos = (int64_t)s.c[i] + (t - s.X[i]), col = pos >> a.log_b;
+      const int64_t fresh = col - ceil_blocks(s.c[i], a.log_b);  // which of the new blocks
+      int64_t b = -1;
+      if (col >= a.width)
+        bad = true;
+      else if (fresh < 0)
+        b = a.table[(base + i) * a.width + col];
+      else if (s.E[i + 1] <= a.n_free)
+        b = a.free[s.E[i] + fresh];
+      a.slots[t] = b < 0 ? -1 : (b << a.log_b) + (pos & ((1 << a.log_b) - 1));
+    }
   }
   if (last)
     for (int64_t t = s.X[kPlanTile] + first; t < a.n_slots; t += step) a.slots[t] = -1;

@@ -5,7 +5,13 @@
 // token begins one where its slot is a block's first or does not follow the slot
 // before it.  One warp does a run's keys or values of one head: the largest
 // magnitude, the scale 2^e, the codes; where the scale of a block with tokens in
-// it grows it also rounds those again.
+// it grows it also rounds those again.  16 bytes a load, a run of up to 16 tokens
+// of 128 stays in registers between the two steps: memory is read and written
+// once, and that bounds all but small calls.
+//
+// A CTA looks through a window of tokens for the runs that begin there and deals
+// them out, run by run and head by head, to its warps.  The window is small where
+// there are few tokens (a step of single tokens: every one is a run).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -54,74 +60,161 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
 
 __device__ __forceinline__ float no_inf(float x) { return isinf(x) ? __int_as_float(0x7fffffff) : x; }
 
+constexpr int kStoreWarps = 8;
+constexpr int kStoreWindow = 16;  // tokens of a window, at most
+constexpr int kStoreRun = 128;    // tokens of a run, at most: a block's
+
+// The larger ones of two pairs of 16 bits.
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Four codes as fp32.
+__device__ __forceinline__ void decode4(uint32_t q, float *v) {
+  uint32_t lo, hi;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)q));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(q >> 16)));
+  const float2 a = __half22float2(*reinterpret_cast<__half2 *>(&lo)), b = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+
 template <int D, bool F16>
-__global__ void __launch_bounds__(256) k_kv_store(StoreArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int per = 2 * a.heads;
-  const int64_t t0 = unit / per;
-  if (t0 >= a.n_tok) return;
-  const int h = (int)(unit % per) >> 1, kv = (int)unit & 1;
-  const int64_t B = 1ll << a.log_b, slot = a.slots[t0];
-  if (slot < 0) return;
-  const int64_t blk = slot >> a.log_b, off = slot & (B - 1);
-  if (blk >= a.n_blocks) {
-    flag(a.status, kStatusData);
-    return;
-  }
-  if (off != 0 && t0 > 0 && a.slots[t0 - 1] == slot - 1) return;  // inside a run
-  // the run's length
-  int n = 1;
-  while (off + n < B && t0 + n < a.n_tok && a.slots[t0 + n] == slot + n) ++n;
-  constexpr int kPart = D / 32;  // elements of a lane
-  const uint16_t *x = reinterpret_cast<const uint16_t *>(a.x[kv]) + (int64_t)h * D + lane * kPart;
-  auto load = [&](int64_t t, float *v) {
-#pragma unroll
-    for (int k = 0; k < kPart; k += 2) {
-      const float2 f = unpack2<F16>(*reinterpret_cast<const uint32_t *>(x + t * a.stride[kv] + k));
-      v[k] = f.x;
-      v[k + 1] = f.y;
+__global__ void __launch_bounds__(kStoreWarps * 32) k_kv_store(StoreArgs a, int window) {
+  constexpr int kLanes = D / 8, kRows = 32 / kLanes;   // lanes of a token, tokens of a load
+  constexpr int kHeld = 16 / kRows;                    // loads of 16 tokens
+  __shared__ int64_t slot[kStoreWindow + kStoreRun];
+  __shared__ int run_at[kStoreWindow], run_n[kStoreWindow], runs;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t t0 = (int64_t)blockIdx.x * window, B = 1ll << a.log_b, cap = a.n_blocks << a.log_b;
+  // slots of the window and as far as a run of it may go; what is not in the cache is -1
+  bool bad = false;
+  const int look = (int)min(a.n_tok - t0, (int64_t)window + (B - 1));
+  for (int i = threadIdx.x; i < look; i += kStoreWarps * 32) {
+    int64_t s = a.slots[t0 + i];
+    if (s >= cap) {
+      bad |= i < window;
+      s = -1;
     }
-  };
-  float amax = 0.f;
-  for (int j = 0; j < n; ++j) {
-    float v[kPart];
-    load(t0 + j, v);
-#pragma unroll
-    for (int k = 0; k < kPart; ++k)
-      if (fabsf(v[k]) <= 3.4028235e38f) amax = fmaxf(amax, fabsf(v[k]));
+    slot[i] = s;
   }
-  for (int d = 16; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-  float *sp = a.scale[kv] + blk * a.heads + h;
-  uint8_t *code = a.code[kv] + ((blk * a.heads + h) << a.log_b) * D;
-  float s = pow2_scale(amax);
-  if (off > 0) {
-    const float old = *sp;
-    if (old >= s) {
-      s = old;
-    } else {
-      const float r = old / s;
-      for (int64_t i = lane; i < off * D; i += 32) {
-        __nv_fp8_e4m3 q;
-        q.__x = code[i];
-        code[i] = (uint8_t)encode4((float)q * r, 0.f, 0.f, 0.f);
+  __syncthreads();
+  if (warp == 0) {
+    // the runs that begin in the window
+    bool begins = false;
+    if (lane < window && lane < look && slot[lane] >= 0) {
+      const int64_t s = slot[lane], before = lane > 0 ? slot[lane - 1] : t0 > 0 ? a.slots[t0 - 1] : -1;
+      begins = (s & (B - 1)) == 0 || before != s - 1;
+    }
+    const unsigned all = __ballot_sync(~0u, begins);
+    if (begins) {
+      const int k = __popc(all & ((1u << lane) - 1));
+      int n = 1;
+      while (lane + n < look && slot[lane + n] == slot[lane] + n && (slot[lane + n] & (B - 1)) != 0) ++n;
+      run_at[k] = lane;
+      run_n[k] = n;
+    }
+    if (lane == 0) runs = __popc(all);
+  }
+  __syncthreads();
+  const int per = 2 * a.heads, items = runs * per;
+  const int sub = lane % kLanes, of = lane / kLanes;
+  for (int item = warp; item < items; item += kStoreWarps) {
+    const int run = item / per, h = (item % per) >> 1, kv = item & 1, n = run_n[run];
+    const int64_t s0 = slot[run_at[run]], blk = s0 >> a.log_b, off = s0 & (B - 1);
+    const int64_t stride = kv ? a.stride[1] : a.stride[0];
+    float *sp = (kv ? a.scale[1] : a.scale[0]) + blk * a.heads + h;
+    const float old = off > 0 ? *sp : 0.f;
+    const uint16_t *x =
+        reinterpret_cast<const uint16_t *>(kv ? a.x[1] : a.x[0]) + (t0 + run_at[run]) * stride + (int64_t)h * D + sub * 8;
+    uint4 v[kHeld];
+    auto load = [&](int from) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int j = from + k * kRows + of;
+        v[k] = j < n ? *reinterpret_cast<const uint4 *>(x + j * stride) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    // the largest magnitude by its bits, two elements at a time; where it is not
+    // finite, once more over those that are
+    uint32_t top = 0;
+    for (int from = 0; from < n; from += 16) {
+      load(from);
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        if (from + k * kRows >= n) break;
+        top = max2(max2(top, v[k].x & 0x7fff7fff), max2(v[k].y & 0x7fff7fff, max2(v[k].z & 0x7fff7fff, v[k].w & 0x7fff7fff)));
+      }
+    }
+    top = __reduce_max_sync(~0u, max(top & 0xffff, top >> 16));
+    const uint32_t infinite = F16 ? 0x7c00 : 0x7f80;
+    const bool all_finite = top < infinite;
+    if (!all_finite) {
+      top = 0;
+#pragma unroll 1
+      for (int j = of; j < n; j += kRows) {
+        const uint4 y = *reinterpret_cast<const uint4 *>(x + j * stride);
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          const uint32_t lo = w[z] & 0x7fff, hi = w[z] >> 16 & 0x7fff;
+          top = max(top, max(lo < infinite ? lo : 0, hi < infinite ? hi : 0));
+        }
+      }
+      top = __reduce_max_sync(~0u, top);
+    }
+    const float amax = unpack2<F16>(top).x;
+    uint8_t *const code = (kv ? a.code[1] : a.code[0]) + ((blk * a.heads + h) << a.log_b) * D;
+    float s = pow2_scale(amax);
+    if (off > 0) {
+      if (old >= s) {
+        s = old;
+      } else {
+        const float r = old / s;
+        for (int64_t i = lane * 16; i < off * D; i += 512) {
+          uint4 q = *reinterpret_cast<const uint4 *>(code + i);
+          uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            float f[4];
+            decode4(w[y], f);
+            w[y] = encode4(f[0] * r, f[1] * r, f[2] * r, f[3] * r);
+          }
+          *reinterpret_cast<uint4 *>(code + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+    if (lane == 0) *sp = s;
+    // by a power of two a product is the quotient; a scale of another kind is the caller's own
+    const bool pow2 = (__float_as_uint(s) & 0x7fffff) == 0;
+    const float inv = 1.f / s;
+    for (int from = 0; from < n; from += 16) {
+      if (n > 16) load(from);
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        if (from + k * kRows >= n) break;
+        const int j = from + k * kRows + of;
+        if (j >= n) continue;
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        float f[8];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float2 p = unpack2<F16>(w[y]);
+          f[2 * y] = p.x, f[2 * y + 1] = p.y;
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y) f[y] = pow2 ? f[y] * inv : f[y] / s;
+        if (!all_finite) {
+#pragma unroll
+          for (int y = 0; y < 8; ++y) f[y] = no_inf(f[y]);
+        }
+        *reinterpret_cast<uint2 *>(code + (off + j) * D + sub * 8) =
+            make_uint2(encode4(f[0], f[1], f[2], f[3]), encode4(f[4], f[5], f[6], f[7]));
       }
     }
   }
-  __syncwarp();
-  if (lane == 0) *sp = s;
-  for (int j = 0; j < n; ++j) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    load(t0 + j, v);
-#pragma unroll
-    for (int k = 0; k < kPart; ++k) v[k] = no_inf(v[k] / s);
-    const uint32_t q = encode4(v[0], v[1], v[2], v[3]);
-    uint8_t *to = code + (off + j) * D + lane * kPart;
-    if (kPart == 4)
-      *reinterpret_cast<uint32_t *>(to) = q;
-    else
-      *reinterpret_cast<uint16_t *>(to) = (uint16_t)q;
-  }
+  if (bad) flag(a.status, kStatusData);
 }
 
 }  // namespace lv
