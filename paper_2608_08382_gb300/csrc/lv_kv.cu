@@ -283,9 +283,9 @@ lv_status lv_kv_plan(lv_ctx *ctx, const int32_t *p, const int32_t *c, int64_t n_
     k_plan_sums<<<(unsigned)tiles, kPlanThreads, 0, stream>>>(a);
     LV_CUDA(cudaGetLastError());
   }
-  // CTAs of a tile: one for each 2,048 slots, up to three an SM in all
+  // CTAs of a tile: one for each 2,048 slots, up to two an SM in all, which is what fits
   const int64_t per = (std::max(n_slots, n_req) / tiles + 2047) / 2048;
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(per, 3 * kv->sms / std::min<int64_t>(tiles, kv->sms)));
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(per, 2 * kv->sms / std::min<int64_t>(tiles, kv->sms)));
   static_assert(sizeof(PlanSmem) <= 48 << 10, "static limit");
   const dim3 grid((unsigned)slices, (unsigned)tiles);
   if (tiles > 1) return launch_after(k_plan, grid, kPlanThreads, sizeof(PlanSmem), stream, a);

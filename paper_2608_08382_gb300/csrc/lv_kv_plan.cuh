@@ -12,6 +12,8 @@
 // slots and one long prompt has as many as thousands of decodes.
 #pragma once
 
+#include <climits>
+
 #include "lv_base.cuh"
 
 namespace lv {
@@ -98,7 +100,32 @@ __device__ __forceinline__ int plan_find(const int64_t *S, int64_t x, int lo, in
   return lo;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs a) {
+// The requests of items x .. x + 127 (below x1), four a lane: item x + 32 y + lane's
+// goes to i[y].  *lo is that of an item at or before x and moves to the last one's.
+// The warp looks ahead from *lo for the last item's request in steps that double,
+// and the lanes search between, all four in step (a long prompt's tokens not at all).
+__device__ __forceinline__ void plan_requests(const int64_t *S, int n, int64_t x, int64_t x1, int lane, int *lo, int *i) {
+  const int64_t last = min(x + kPlanSpan, x1) - 1;
+  int from = *lo, to = from + 1;  // S[from] <= last; S[to] > last at the end, or to = n
+  for (int step = 1; to < n && S[to] <= last; step *= 2) {
+    from = to;
+    to = min(n, to + step);
+  }
+  const int end = plan_find(S, last, from, to) + 1;
+  int len = end - *lo;
+#pragma unroll
+  for (int y = 0; y < kPlanSpan / 32; ++y) i[y] = *lo;
+  while (len > 1) {
+    const int half = len >> 1;
+#pragma unroll
+    for (int y = 0; y < kPlanSpan / 32; ++y)
+      if (S[i[y] + half] <= x + 32 * y + lane) i[y] += half;
+    len -= half;
+  }
+  *lo = end - 1;
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 2) k_plan(PlanArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
   PlanSmem &s = *reinterpret_cast<PlanSmem *>(raw);
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
@@ -168,47 +195,94 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs a) {
   // the slots, so that one does not wait for the other.
   const bool little = s.X[kPlanTile] - s.X[0] <= 12 * kPlanSpan && s.E[kPlanTile] - s.E[0] <= 4 * kPlanSpan && gridDim.x == 1;
   const int top = (int)n;  // requests to search among
-  // A warp takes 128 entries or slots at a time: two searches find the requests of
-  // the first and the last of them, and the lanes search between those (a long
-  // prompt's tokens not at all).
-  const int64_t wfirst = ((int64_t)blockIdx.x * (kPlanThreads / 32) + w) * kPlanSpan, wstep = step * (kPlanSpan / 32);
-  const int64_t efirst = !little ? wfirst : w % 4 == 0 ? w / 4 * kPlanSpan : 4 * kPlanSpan;
-  const int64_t xfirst = !little ? wfirst : w % 4 != 0 ? (w / 4 * 3 + w % 4 - 1) * kPlanSpan : 12 * kPlanSpan;
+  // Each warp its own stretch of the tile's entries and of its slots, 128 at a time.
+  const int64_t warps = little ? 1 : (int64_t)gridDim.x * (kPlanThreads / 32), me = (int64_t)blockIdx.x * (kPlanThreads / 32) + w;
+  auto stretch = [&](int64_t all, int64_t share, int64_t of) { return (all + of * kPlanSpan - 1) / (of * kPlanSpan) * kPlanSpan * share; };
   // new table entries
-  const int64_t e1 = s.E[kPlanTile];
-  for (int64_t k0 = s.E[0] + efirst; k0 < e1; k0 += wstep) {
-    const int lo = plan_find(s.E, k0, 0, top), hi = plan_find(s.E, min(k0 + kPlanSpan, e1) - 1, lo, kPlanTile) + 1;
+  {
+    const int64_t e0 = s.E[0], e1 = s.E[kPlanTile], of = little ? 4 : warps, mine = little ? (w % 4 == 0 ? w / 4 : of) : me;
+    const int64_t k1 = min(e1, e0 + stretch(e1 - e0, mine + 1, of));
+    int64_t k0 = e0 + stretch(e1 - e0, mine, of);
+    int lo = k0 < k1 ? plan_find(s.E, k0, 0, top) : 0;
+    for (; k0 < k1; k0 += kPlanSpan) {
+      int i[kPlanSpan / 32];
+      plan_requests(s.E, top, k0, k1, lane, &lo, i);
+      int32_t id[kPlanSpan / 32];
 #pragma unroll
-    for (int y = 0; y < kPlanSpan; y += 32) {
-      const int64_t k = k0 + y + lane;
-      if (k >= e1) break;
-      const int i = plan_find(s.E, k, lo, hi);
-      const int64_t col = ceil_blocks(s.c[i], a.log_b) + (k - s.E[i]);
-      if (col < a.width)
-        a.table[(base + i) * a.width + col] = s.E[i + 1] <= a.n_free ? a.free[k] : -1;
-      else
-        bad = true;
+      for (int y = 0; y < kPlanSpan / 32; ++y) {
+        const int64_t k = k0 + 32 * y + lane;
+        id[y] = k < k1 && s.E[i[y] + 1] <= a.n_free ? a.free[k] : -1;
+      }
+#pragma unroll
+      for (int y = 0; y < kPlanSpan / 32; ++y) {
+        const int64_t k = k0 + 32 * y + lane, col = ceil_blocks(s.c[i[y]], a.log_b) + (k - s.E[i[y]]);
+        if (k >= k1) continue;
+        if (col < a.width)
+          a.table[(base + i[y]) * a.width + col] = id[y];
+        else
+          bad = true;
+      }
     }
   }
   // slots
-  const int64_t x1 = min(s.X[kPlanTile], a.n_slots);
-  for (int64_t t1 = s.X[0] + xfirst; t1 < x1; t1 += wstep) {
-    const int lo = plan_find(s.X, t1, 0, top), hi = plan_find(s.X, min(t1 + kPlanSpan, x1) - 1, lo, kPlanTile) + 1;
+  {
+    const int64_t x0 = s.X[0], x1 = min(s.X[kPlanTile], a.n_slots), of = little ? 12 : warps;
+    const int64_t mine = little ? (w % 4 != 0 ? w / 4 * 3 + w % 4 - 1 : of) : me;
+    const int64_t t1 = min(x1, x0 + stretch(x1 - x0, mine + 1, of));
+    int64_t t0 = x0 + stretch(x1 - x0, mine, of);
+    int lo = t0 < t1 ? plan_find(s.X, t0, 0, top) : 0;
+    for (; t0 < t1; t0 += kPlanSpan) {
+      const int64_t next = s.X[lo + 1];
+      if (next >= min(t0 + kPlanSpan, t1) && t0 + kPlanSpan <= t1) {
+        // all 128 are one request's: what is theirs alone in 32 bits (a thread's part of
+        // the general way is five times as long, and prompts have most tokens)
+        const int64_t pos0 = (int64_t)s.c[lo] + (t0 - s.X[lo]), col0 = pos0 >> a.log_b;
+        const int64_t held = ceil_blocks(s.c[lo], a.log_b), room = a.width - col0;
+        const int32_t *const row = a.table + (base + lo) * a.width + col0;
+        const int32_t *const fresh = s.E[lo + 1] <= a.n_free ? a.free + s.E[lo] + (col0 - held) : nullptr;
+        const int mask = (1 << a.log_b) - 1, x0 = ((int)pos0 & mask) + lane;
+        const int old = (int)max((int64_t)-1, min((int64_t)INT32_MAX, held - col0));  // columns that were held before
+        int64_t b[kPlanSpan / 32];
 #pragma unroll
-    for (int y = 0; y < kPlanSpan; y += 32) {
-      const int64_t t = t1 + y + lane;
-      if (t >= x1) break;
-      const int i = plan_find(s.X, t, lo, hi);
-      const int64_t pos = (int64_t)s.c[i] + (t - s.X[i]), col = pos >> a.log_b;
-      const int64_t fresh = col - ceil_blocks(s.c[i], a.log_b);  // which of the new blocks
-      int64_t b = -1;
-      if (col >= a.width)
-        bad = true;
-      else if (fresh < 0)
-        b = a.table[(base + i) * a.width + col];
-      else if (s.E[i + 1] <= a.n_free)
-        b = a.free[s.E[i] + fresh];
-      a.slots[t] = b < 0 ? -1 : (b << a.log_b) + (pos & ((1 << a.log_b) - 1));
+        for (int y = 0; y < kPlanSpan / 32; ++y) {
+          const int col = (x0 + 32 * y) >> a.log_b;
+          b[y] = -1;
+          if (col >= room)
+            bad = true;
+          else if (col < old)
+            b[y] = row[col];
+          else if (fresh)
+            b[y] = fresh[col];
+        }
+#pragma unroll
+        for (int y = 0; y < kPlanSpan / 32; ++y)
+          a.slots[t0 + 32 * y + lane] = b[y] < 0 ? -1 : (b[y] << a.log_b) + ((x0 + 32 * y) & mask);
+        continue;
+      }
+      int i[kPlanSpan / 32];
+      plan_requests(s.X, top, t0, t1, lane, &lo, i);
+      // the blocks' numbers are all asked for before the first is waited for
+      int64_t b[kPlanSpan / 32];
+      int off[kPlanSpan / 32];
+#pragma unroll
+      for (int y = 0; y < kPlanSpan / 32; ++y) {
+        const int64_t t = t0 + 32 * y + lane, pos = (int64_t)s.c[i[y]] + (t - s.X[i[y]]), col = pos >> a.log_b;
+        const int64_t fresh = col - ceil_blocks(s.c[i[y]], a.log_b);  // which of the new blocks
+        const int32_t *from = nullptr;
+        off[y] = (int)pos & ((1 << a.log_b) - 1);
+        if (t < t1) {
+          if (col >= a.width)
+            bad = true;
+          else if (fresh < 0)
+            from = a.table + (base + i[y]) * a.width + col;
+          else if (s.E[i[y] + 1] <= a.n_free)
+            from = a.free + s.E[i[y]] + fresh;
+        }
+        b[y] = from ? *from : -1;
+      }
+#pragma unroll
+      for (int y = 0; y < kPlanSpan / 32; ++y)
+        if (t0 + 32 * y + lane < t1) a.slots[t0 + 32 * y + lane] = b[y] < 0 ? -1 : (b[y] << a.log_b) + off[y];
     }
   }
   if (last)
