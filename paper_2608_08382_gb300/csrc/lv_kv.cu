@@ -83,6 +83,15 @@ bool heads_ok(int32_t dtype, int32_t hq, int32_t hkv) {
 
 constexpr int64_t kMostTokens = 1ll << 31;
 
+// A kernel's shared-memory limit, once for a context; `kind` numbers the kernels.
+template <class K>
+lv_status limit_smem(KvHost *kv, K kernel, int kind, size_t bytes) {
+  if (kv->configured >> kind & 1) return LV_OK;
+  LV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  kv->configured |= 1u << kind;
+  return LV_OK;
+}
+
 // Launches a kernel that may start while the one before it in the stream runs
 // (it calls wait_previous itself).
 template <class... P, class... A>
@@ -154,7 +163,8 @@ lv_status run_chunk(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   }
   constexpr size_t smem = sizeof(ChunkSmem<D>) + 1024;
   static_assert(smem <= 227 << 10, "an SM's shared memory");
-  LV_CUDA(cudaFuncSetAttribute(k_chunk<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  st = limit_smem(kv, k_chunk<D, F16>, (D == 128 ? 0 : 2) + (F16 ? 1 : 0), smem);
+  if (st != LV_OK) return st;
   k_chunk<D, F16><<<(unsigned)ctas, kChThreads, smem, stream>>>(c);
   LV_CUDA(cudaGetLastError());
   const int64_t y = (a.n_tok / (2 * c.tile) + 1) * a.hkv * 32;  // rows of eight of the longest request there can be
@@ -233,7 +243,8 @@ lv_status run_prompt(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   }
   constexpr size_t smem = sizeof(PromptSmem<D>) + 1024;
   static_assert(smem <= 227 << 10, "an SM's shared memory");
-  LV_CUDA(cudaFuncSetAttribute(k_prompt<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  st = limit_smem(kv, k_prompt<D, F16>, 4 + (D == 128 ? 0 : 2) + (F16 ? 1 : 0), smem);
+  if (st != LV_OK) return st;
   // a CTA an SM; no more than there can be items
   const int64_t items = (a.n_tok / (2 * p.tile) + std::min(a.n_req, a.n_tok)) * a.hkv;
   const unsigned grid = (unsigned)std::min<int64_t>(items, kv->sms);

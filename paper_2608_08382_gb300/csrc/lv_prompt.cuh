@@ -27,9 +27,12 @@
 // the first blocks of keys hardly any output is read back to be rescaled.
 // Weights are rounded to the inputs' 16-bit type, as V is.
 //
-// Items are handed out by a counter, longest first within a sequence, and the
-// loads run ahead of the products across items.
+// Items are handed out by a counter, longest first within a sequence and the
+// longest sequence first (twelve prompts of up to 4,096 tokens: 84 us in the order
+// that they came), and the loads run ahead of the products across items.
 #pragma once
+
+#include <climits>
 
 #include "lv_attend.cuh"
 #include "lv_tc.cuh"
@@ -38,6 +41,7 @@ namespace lv {
 
 constexpr int kPrThreads = 384;
 constexpr int kPrBlock = 128;   // keys of a block
+constexpr int kSort = 512;      // sequences that are taken longest first
 constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that weights absorb
 
 struct PromptArgs {
@@ -67,6 +71,7 @@ struct PromptSmem {
   uint64_t item_full[2], item_empty[2];
   PromptItem item[2];
   int64_t sums[kScan + 1];
+  int order[kSort], length[kSort];  // sequences, longest first; a sequence's items
   uint32_t tmem;
   int stop;
 };
@@ -230,6 +235,11 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, G = a.hq / a.hkv;
   constexpr int kChunk = 128 * 128;  // bytes of 64 elements of a tile's rows
   if (warp == 8) tmem_alloc(&sm.tmem, 512);
+  if (threadIdx.x == 9 * 32) {
+    map_ahead(&map_q);
+    map_ahead(&map_k);
+    map_ahead(&map_v);
+  }
   if (threadIdx.x == 0) {
     sm.stop = 0;
     sm.item[0].head = sm.item[1].head = -1;
@@ -255,7 +265,23 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   if (p.given) {
     items = sums[a.n_req];
   } else {
-    items = scan_units<kPrThreads>((int)a.n_req, sm.sums, 0, [&](int k) { return prompt_items(p, k, &bad); });
+    const int n = (int)a.n_req;
+    if (n <= kSort) {
+      // longest first: a long item begun late would be the call's end.  Each sequence
+      // counts those before it
+      for (int i = threadIdx.x; i < n; i += kPrThreads) sm.length[i] = (int)min((int64_t)INT32_MAX, prompt_items(p, i, &bad));
+      __syncthreads();
+      for (int i = threadIdx.x; i < n; i += kPrThreads) {
+        const int mine = sm.length[i];
+        int at = 0;
+        for (int j = 0; j < n; ++j) at += sm.length[j] > mine || (sm.length[j] == mine && j < i) ? 1 : 0;
+        sm.order[at] = i;
+      }
+      __syncthreads();
+      items = scan_units<kPrThreads>(n, sm.sums, 0, [&](int k) { return (int64_t)sm.length[sm.order[k]]; });
+    } else {
+      items = scan_units<kPrThreads>(n, sm.sums, 0, [&](int k) { return prompt_items(p, k, &bad); });
+    }
     sums = sm.sums;
   }
   tc_before_sync();
@@ -280,7 +306,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           bar_arrive(&sm.item_full[n & 1]);
           break;
         }
-        const int64_t i = find_unit(sums, a.n_req, u), local = u - sums[i];
+        const int64_t at = find_unit(sums, a.n_req, u), local = u - sums[at], i = a.n_req <= kSort ? sm.order[at] : at;
         const int64_t x0 = a.offsets[i], len = a.offsets[i + 1] - x0, pairs = (len + 2 * p.tile - 1) / (2 * p.tile);
         const int head = (int)(local % a.hkv);
         const int64_t t0 = (pairs - 1 - local / a.hkv) * 2 * p.tile;

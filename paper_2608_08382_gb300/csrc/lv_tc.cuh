@@ -56,6 +56,8 @@ __device__ __forceinline__ void tma_load3(void *to, const CUtensorMap *map, int 
       : "memory");
 }
 
+__device__ __forceinline__ void map_ahead(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 // n bytes in a row into shared memory: both addresses and n multiples of 16.
 __device__ __forceinline__ void copy_bytes(void *to, const void *from, uint32_t n, uint64_t *bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(to)),
