@@ -51,6 +51,20 @@ __device__ __forceinline__ uint32_t pack_out(float a, float b) {
   return r;
 }
 
+// 64 bytes in a row: whole sectors at a time where the address allows it.
+__device__ __forceinline__ void store64(void *p, const uint32_t *w, bool wide) {
+  if (wide) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"((uint32_t *)p + k), "r"(w[k]),
+                   "r"(w[k + 1]), "r"(w[k + 2]), "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4 *>((uint32_t *)p + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+  }
+}
+
 // a / b for 0 <= a, 0 < b: a 64-bit division is a long chain of instructions, and
 // hardly ever needed.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {

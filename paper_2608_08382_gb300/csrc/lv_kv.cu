@@ -224,6 +224,7 @@ lv_status run_prompt(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   p.a = a;
   const int G = a.hq / a.hkv;
   p.tile = 128 / G;
+  p.wide = aligned(a.o, 32);
   const int32_t dtype = F16 ? LV_F16 : LV_BF16;
   CUtensorMap mq, mk, mv;
   lv_status st = map_rows(&mq, a.q, dtype, a.n_tok, a.hq, D, a.q_stride, p.tile, G);

@@ -47,6 +47,7 @@ constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that
 struct PromptArgs {
   AttendArgs a;
   int tile;             // tokens of a tile: 128 / G
+  bool wide;            // o is 32-byte aligned
   int64_t *prefix;      // [n_req + 1] items before each sequence, given for more than kScan
   bool given;
   unsigned long long *counter; // items handed out beyond the first of each CTA; CTAs done (zero between launches)
@@ -445,24 +446,21 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       const int64_t t = (int64_t)it.first + tok, h = (int64_t)it.head * G + row % G;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       bool nan = false;
+      uint16_t *const op = (uint16_t *)a.o + (t * a.hq + h) * D;
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
         tmem_load32(o, to + c);
         tmem_wait_load();
         if (valid) {
-          uint4 *op = reinterpret_cast<uint4 *>((uint16_t *)a.o + (t * a.hq + h) * D + c);
+          uint32_t w[16];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            uint32_t w[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const float v0 = __uint_as_float(o[8 * x + 2 * y]) * inv, v1 = __uint_as_float(o[8 * x + 2 * y + 1]) * inv;
-              nan |= isnan(v0) || isnan(v1);
-              w[y] = pack_out<F16>(v0, v1);
-            }
-            op[x] = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int y = 0; y < 16; ++y) {
+            const float v0 = __uint_as_float(o[2 * y]) * inv, v1 = __uint_as_float(o[2 * y + 1]) * inv;
+            nan |= isnan(v0) || isnan(v1);
+            w[y] = pack_out<F16>(v0, v1);
           }
+          store64(op + c, w, p.wide);
         }
       }
       if (valid && a.lse) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m * sl + log2f(l)) * 0.6931471805599453f;
