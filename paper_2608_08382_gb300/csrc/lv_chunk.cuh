@@ -45,7 +45,7 @@ struct ChunkSmem {
   unsigned char kv[kStages][kTile];
   unsigned char code[kCodes][128 * D];  // at the start: the requests' running sums
   uint64_t code_full[kCodes], code_empty[kCodes];
-  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_half[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2], scale_full[kChScales];
   PromptItem item[2];
   alignas(16) float ks[kChScales][8], vs[kChScales][8];  // of a block's strips
@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       bar_init(&sm.q_full[k], 4);
       bar_init(&sm.q_empty[k], 1);
       bar_init(&sm.s_full[k], 1);
+      bar_init(&sm.p_half[k], 4);
       bar_init(&sm.p_full[k], 4);
       bar_init(&sm.o_full[k], 1);
       bar_init(&sm.item_full[k], 1);
@@ -494,6 +495,12 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
               w[y] = pack_half2(p0, p1);
             }
             tmem_store16(ts + 16 * x, w);  // over columns that were read
+            if (x == 1) {
+              tmem_wait_store();
+              tc_before_sync();
+              __syncwarp();
+              if (lane == 0) bar_arrive(&sm.p_half[k]);
+            }
           }
           float l0, l1;
           unpair(add2(sum[0], sum[1]), &l0, &l1);

@@ -68,7 +68,7 @@ struct PromptSmem {
   static constexpr int kStages = 4;                        // blocks of keys or values
   unsigned char q[2][kTile];
   unsigned char kv[kStages][kTile];
-  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_half[2], p_full[2], o_full[2];
   uint64_t item_full[2], item_empty[2];
   PromptItem item[2];
   int64_t sums[kScan + 1];
@@ -173,13 +173,17 @@ __device__ __forceinline__ void issue_products(Smem &sm, uint32_t tmem, bool neg
       const uint32_t vd = v_desc + v0.st * kStep;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        bar_wait(&sm.p_full[k], p_phase >> k & 1, stop);
-        tc_after_sync();
-        if (elect_one()) {
+        // half of the weights at a time: the first half's products run while the second is formed
 #pragma unroll
-          for (int c = 0; c < kPrBlock / 16; ++c)
-            tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
-          if (k == 1) release(v0);
+        for (int half = 0; half < 2; ++half) {
+          bar_wait(half ? &sm.p_full[k] : &sm.p_half[k], p_phase >> k & 1, stop);
+          tc_after_sync();
+          if (elect_one()) {
+#pragma unroll
+            for (int c = 4 * half; c < 4 * half + 4; ++c)
+              tc_mma_ta(tmem + 256 + k * D, tmem + k * kCols + c * 8, vd + c * (2048 >> 4), id_pv, j > 0 || c > 0);
+            if (half && k == 1) release(v0);
+          }
         }
         ring(k == 0 ? k1 : v1);  // these keys; the next values, for the next turn
         if (elect_one()) {
@@ -248,6 +252,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       bar_init(&sm.q_full[k], 1);
       bar_init(&sm.q_empty[k], 1);
       bar_init(&sm.s_full[k], 1);
+      bar_init(&sm.p_half[k], 4);
       bar_init(&sm.p_full[k], 4);
       bar_init(&sm.o_full[k], 1);
       bar_init(&sm.item_full[k], 1);
@@ -430,6 +435,12 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             w[x] = pack_out<F16>(p0, p1);
           }
           tmem_store16(ts + c / 2, w);
+          if (c == 32) {
+            tmem_wait_store();
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sm.p_half[k]);
+          }
         }
         float l0, l1;
         unpair(add2(sum[0], sum[1]), &l0, &l1);
