@@ -39,7 +39,7 @@ constexpr int kDecWarps = 4;       // warps of a CTA; they share only the scan
 constexpr int kDecSegment = 4;
 constexpr int kDecMinStrips = 8;   // strips a warp takes at least
 constexpr int kDecRows = 16;       // rows of a request that go here: two row tiles of 8
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 8;      // rows of a CTA that joins, a warp each
 constexpr float kWeightExp = 12.f;
 
 struct DecodeArgs {
@@ -490,13 +490,14 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
 }
 
 // The segments that several warps shared: their parts are added in the line's
-// order, eight at a time, by one warp a row (per_row = 1; a CTA takes eight rows
-// of a segment), or by eight warps a row, each an eighth of the parts, where
-// there are few segments and so many parts in each (per_row = 8).
-template <int D, bool F16>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, int per_row) {
+// order, eight at a time, by one warp a row (PER_ROW = 1; a CTA takes eight rows
+// of a segment), or by PER_ROW warps a row, each its share of the parts, where
+// there are few segments and so many parts in each.
+template <int D, bool F16, int PER_ROW>
+__global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_attend_join(DecodeArgs d) {
+  constexpr int per_row = PER_ROW;
   constexpr int E = D / 32, kBatch = 8;
-  __shared__ float sm[kJoinWarps][2], so[kJoinWarps][D];
+  __shared__ float sm[PER_ROW][2], so[PER_ROW][D];
   const AttendArgs &a = d.a;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, G = a.hq / a.hkv, rows = 8 * d.nt;
   wait_previous();
@@ -507,11 +508,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
   const Span sp = request_span(a, i, &ignore);
   if (d.prefix[i + 1] == d.prefix[i]) return;
   const int64_t strips = span_strips(a, sp);
-  const int tiles = span_tiles(a, sp, rows), groups = per_row == 1 ? rows / kJoinWarps : rows;
+  const int tiles = span_tiles(a, sp, rows), groups = per_row == 1 ? rows / kJoinWarps : min(rows, d.a.offsets ? rows : G);
   for (int64_t y = blockIdx.y; y < (int64_t)tiles * a.hkv * groups; y += gridDim.y) {
     const int64_t seg = (int)y / groups;
     const int64_t u0 = d.prefix[i] + seg * segment_units(strips), w0 = warp_of(u0, W, units), w1 = warp_of(u0 + strips - 1, W, units);
     if (w0 == w1) continue;
+    const int64_t slot0 = w0 * 2 + (warp_start(w0, W, units) < u0 ? 1 : 0);
     const int h = (int)seg / tiles, r = ((int)y % groups) * (per_row == 1 ? kJoinWarps : 1) + (per_row == 1 ? w : 0);
     const int row = ((int)seg % tiles) * rows + r, j = row / G, hh = h * G + row % G;
     float top = -INFINITY, l = 0.f, o[E];
@@ -527,7 +529,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
 #pragma unroll
           for (int k = 0; k < E; ++k) po[b][k] = 0.f;
           if (x <= w1) {
-            const int64_t slot = (x * 2 + (x == w0 && warp_start(x, W, units) < u0 ? 1 : 0)) * rows + r;
+            const int64_t slot = (x == w0 ? slot0 : x * 2) * rows + r;
             const float2 ml = *reinterpret_cast<const float2 *>(d.part_ml + 2 * slot);
             pm[b] = ml.x, pl[b] = ml.y;
 #pragma unroll
@@ -556,10 +558,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(DecodeArgs d, i
     if (per_row > 1) {
 #pragma unroll
       for (int k = 0; k < E; ++k) so[w][lane * E + k] = o[k];
-      if (lane == 0) sm[w][0] = top, sm[w][1] = l;
+      if (lane == 0) sm[w % PER_ROW][0] = top, sm[w % PER_ROW][1] = l;
       __syncthreads();
       if (w == 0) {
-        for (int x = 1; x < kJoinWarps; ++x) {
+        for (int x = 1; x < PER_ROW; ++x) {
           const float nm = fmaxf(top, sm[x][0]), base = nm == -INFINITY ? 0.f : nm;
           const float f0 = top == -INFINITY ? 1.f : exp2_fast(top - base);
           const float f1 = sm[x][0] == -INFINITY ? 1.f : exp2_fast(sm[x][0] - base);

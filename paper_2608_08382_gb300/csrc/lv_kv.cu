@@ -135,10 +135,17 @@ lv_status run_decode(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   }
   k_attend_decode<D, F16, NT><<<(unsigned)ctas, kDecWarps * 32, 0, stream>>>(d);
   LV_CUDA(cudaGetLastError());
-  const int per_row = segments < kv->sms ? kJoinWarps : 1;
-  const int64_t y = (int64_t)a.hkv * tiles * (per_row == 1 ? NT : 8 * NT);
-  return launch_after(k_attend_join<D, F16>, dim3((unsigned)a.n_req, (unsigned)std::min<int64_t>(y, 4096)),
-                      kJoinWarps * 32, 0, stream, d, per_row);
+  // Warps of a row that is joined, by the parts there are in a segment (us a call, 16
+  // decodes of 128 segments, about 19 parts each, and 3 long ones of 6, about 400):
+  // one 43.4, four 41.7 and 56.1, eight 43.8 and 52.0, sixteen 51.6 and 51.3
+  const int64_t y = (int64_t)a.hkv * tiles * 8 * NT, y1 = (int64_t)a.hkv * tiles * NT;
+  const unsigned n = (unsigned)a.n_req;
+  if (segments * 64 < d.warps)
+    return launch_after(k_attend_join<D, F16, 16>, dim3(n, (unsigned)std::min<int64_t>(y, 4096)), 16 * 32, 0, stream, d);
+  if (segments * 8 < d.warps)
+    return launch_after(k_attend_join<D, F16, 4>, dim3(n, (unsigned)std::min<int64_t>(y, 4096)), 4 * 32, 0, stream, d);
+  return launch_after(k_attend_join<D, F16, 1>, dim3(n, (unsigned)std::min<int64_t>(y1, 4096)), kJoinWarps * 32, 0,
+                      stream, d);
 }
 
 template <int D, bool F16>

@@ -61,7 +61,7 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
 __device__ __forceinline__ float no_inf(float x) { return isinf(x) ? __int_as_float(0x7fffffff) : x; }
 
 constexpr int kStoreWarps = 8;
-constexpr int kStoreWindow = 16;  // tokens of a window, at most
+constexpr int kStoreWindow = 32;  // tokens of a window, at most
 constexpr int kStoreRun = 128;    // tokens of a run, at most: a block's
 
 // The larger ones of two pairs of 16 bits.
@@ -81,7 +81,7 @@ __device__ __forceinline__ void decode4(uint32_t q, float *v) {
 }
 
 template <int D, bool F16>
-__global__ void __launch_bounds__(kStoreWarps * 32) k_kv_store(StoreArgs a, int window) {
+__global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, int window) {
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;   // lanes of a token, tokens of a load
   constexpr int kHeld = 16 / kRows;                    // loads of 16 tokens
   __shared__ int64_t slot[kStoreWindow + kStoreRun];
