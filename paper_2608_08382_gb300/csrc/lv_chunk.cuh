@@ -586,58 +586,62 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
   bool ignore = false;
   const Span sp = request_span(a, i, &ignore);
   const int64_t blocks = chunk_blocks(c, sp), items = chunk_pairs(c, sp) * a.hkv;
-  for (int64_t y = blockIdx.y; y < items * 32; y += gridDim.y) {
-    const int64_t seg = y / 32, u0 = c.prefix[i] + seg * blocks;
+  // a CTA takes a quarter of an item's rows, its warps eight each
+  for (int64_t y = blockIdx.y; y < items * 4; y += gridDim.y) {
+    const int64_t seg = y >> 2, u0 = c.prefix[i] + seg * blocks;
     const int64_t w0 = warp_of(u0, ctas, units), w1 = warp_of(u0 + blocks - 1, ctas, units);
     if (w0 == w1) continue;
-    const int r = (int)(y % 32) * 8 + w, row = r & 127, k = r >> 7;
-    const int tok = (int)(seg / a.hkv) * 2 * c.tile + k * c.tile + row / G, h = (int)(seg % a.hkv) * G + row % G;
-    if (row >= c.tile * G || tok >= sp.p) continue;
-    float top = -INFINITY, l = 0.f, o[E];
+    const int64_t slot0 = w0 * 2 + (warp_start(w0, ctas, units) < u0 ? 1 : 0);
+    for (int r = (int)(y & 3) * 64 + w; r < ((int)(y & 3) + 1) * 64; r += 8) {
+      const int row = r & 127, k = r >> 7;
+      const int tok = (int)seg / a.hkv * 2 * c.tile + k * c.tile + row / G, h = (int)seg % a.hkv * G + row % G;
+      if (row >= c.tile * G || tok >= sp.p) continue;
+      float top = -INFINITY, l = 0.f, o[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int64_t x0 = w0; x0 <= w1; x0 += kBatch) {
-      float pm[kBatch], pl[kBatch], po[kBatch][E], nm = top;
+      for (int e = 0; e < E; ++e) o[e] = 0.f;
+      for (int64_t x0 = w0; x0 <= w1; x0 += kBatch) {
+        float pm[kBatch], pl[kBatch], po[kBatch][E], nm = top;
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int64_t x = x0 + b;
-        pm[b] = -INFINITY, pl[b] = 0.f;
-        if (x <= w1) {
-          const int64_t at = (x * 2 + (x == w0 && warp_start(x, ctas, units) < u0 ? 1 : 0)) * 256 + r;
-          const float2 ml = *reinterpret_cast<const float2 *>(c.part_ml + 2 * at);
-          pm[b] = ml.x, pl[b] = ml.y;
+        for (int b = 0; b < kBatch; ++b) {
+          const int64_t x = x0 + b;
+          pm[b] = -INFINITY, pl[b] = 0.f;
+          if (x <= w1) {
+            const int64_t at = (x == w0 ? slot0 : x * 2) * 256 + r;
+            const float2 ml = *reinterpret_cast<const float2 *>(c.part_ml + 2 * at);
+            pm[b] = ml.x, pl[b] = ml.y;
 #pragma unroll
-          for (int e = 0; e < E; e += 2) {
-            const float2 v = *reinterpret_cast<const float2 *>(c.part + at * D + lane * E + e);
-            po[b][e] = v.x, po[b][e + 1] = v.y;
+            for (int e = 0; e < E; e += 2) {
+              const float2 v = *reinterpret_cast<const float2 *>(c.part + at * D + lane * E + e);
+              po[b][e] = v.x, po[b][e + 1] = v.y;
+            }
           }
+          nm = fmaxf(nm, pm[b]);
         }
-        nm = fmaxf(nm, pm[b]);
+        const float base = nm == -INFINITY ? 0.f : nm, up = top == -INFINITY ? 1.f : exp2_fast(top - base);
+        l *= up;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= up;
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          if (pl[b] == 0.f) continue;
+          const float f = pm[b] == -INFINITY ? 1.f : exp2_fast(pm[b] - base);
+          l += pl[b] * f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] += po[b][e] * f;
+        }
+        top = nm;
       }
-      const float base = nm == -INFINITY ? 0.f : nm, up = top == -INFINITY ? 1.f : exp2_fast(top - base);
-      l *= up;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int64_t t = sp.first + tok;
+      bool nan = false;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= up;
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        if (pl[b] == 0.f) continue;
-        const float f = pm[b] == -INFINITY ? 1.f : exp2_fast(pm[b] - base);
-        l += pl[b] * f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += po[b][e] * f;
+      for (int e = 0; e < E; e += 2) {
+        *reinterpret_cast<uint32_t *>((uint16_t *)a.o + (t * a.hq + h) * D + lane * E + e) = pack_out<F16>(o[e] * inv, o[e + 1] * inv);
+        nan |= isnan(o[e]) || isnan(o[e + 1]);
       }
-      top = nm;
+      if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (top - kChExp + log2f(l)) * 0.6931471805599453f;
+      if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok));
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t t = sp.first + tok;
-    bool nan = false;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      *reinterpret_cast<uint32_t *>((uint16_t *)a.o + (t * a.hq + h) * D + lane * E + e) = pack_out<F16>(o[e] * inv, o[e + 1] * inv);
-      nan |= isnan(o[e]) || isnan(o[e + 1]);
-    }
-    if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (top - kChExp + log2f(l)) * 0.6931471805599453f;
-    if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok));
   }
 }
 

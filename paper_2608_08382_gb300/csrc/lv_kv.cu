@@ -174,7 +174,7 @@ lv_status run_chunk(KvHost *kv, const AttendArgs &a, cudaStream_t stream) {
   if (st != LV_OK) return st;
   k_chunk<D, F16><<<(unsigned)ctas, kChThreads, smem, stream>>>(c);
   LV_CUDA(cudaGetLastError());
-  const int64_t y = (a.n_tok / (2 * c.tile) + 1) * a.hkv * 32;  // rows of eight of the longest request there can be
+  const int64_t y = (a.n_tok / (2 * c.tile) + 1) * a.hkv * 4;  // quarters of the items of the longest request there can be
   return launch_after(k_chunk_join<D, F16>, dim3((unsigned)a.n_req, (unsigned)std::min<int64_t>(y, 2048)), 256, 0, stream,
                       c, ctas);
 }
