@@ -73,7 +73,7 @@ typedef int32_t lv_status;
 #define LV_ECUDA (-5)      /* a CUDA runtime call failed */
 #define LV_EDATA (-6)      /* invalid input data seen on the device (sticky) */
 #define LV_ENOMEM (-7)     /* device allocation failed */
-#define LV_ETIMEOUT (-8)   /* a bounded wait inside a kernel ran out (lv_accuracy, or lv_ctx_status after a serving-step launch) */
+#define LV_ETIMEOUT (-8)   /* a bounded wait inside a kernel ran out (lv_accuracy, or lv_ctx_status after a serving-step or attention launch) */
 
 /* Model architecture; integers only.  tp is the modelled tensor-parallel degree
  * (an arithmetic input: constants are per rank).  kv_bytes is the KV-cache
@@ -141,7 +141,8 @@ typedef struct lv_tenant_acc lv_tenant_acc;
  * that its calls grow to the largest input they have seen and keep (the tile
  * pass: about 1 byte per 150 requests; lv_whatif: about 220 bytes a candidate;
  * lv_fit: 33 bytes a batch, for 2^22 batches at most, 138 MB; lv_accuracy: about
- * 20 bytes a batch) and a sticky status word.  Returns LV_ECUDA/LV_ENOMEM on
+ * 20 bytes a batch; the attention calls: up to 41 MB and 8 bytes a request, grown
+ * by doubling, what is outgrown kept to the end) and a sticky status word.  Returns LV_ECUDA/LV_ENOMEM on
  * failure. */
 lv_status lv_ctx_create(lv_ctx **out);
 void lv_ctx_destroy(lv_ctx *ctx);
@@ -150,7 +151,8 @@ lv_status lv_ctx_set_arith(lv_ctx *ctx, int32_t mode);
 /* Synchronise `stream`, then return and clear the sticky device status
  * (LV_OK; LV_EDATA when a kernel met invalid input data since the last query;
  * LV_ETIMEOUT when a bounded wait inside the serving-step kernel of
- * lv_attribute / lv_attribute_step ran out, which takes precedence). */
+ * lv_attribute / lv_attribute_step or a kernel of lv_kv_attend /
+ * lv_prompt_attend ran out, which takes precedence). */
 lv_status lv_ctx_status(lv_ctx *ctx, void *stream);
 /* Static description of a status code. */
 const char *lv_status_string(lv_status s);
@@ -354,7 +356,9 @@ lv_status lv_whatif_admit(lv_ctx *ctx, const lv_model *model, const lv_batches *
  * key/value head.  Their arrays are [token][head][element] with the heads of a
  * token side by side; *_stride is the distance between tokens in elements (a
  * multiple of 8, at least n_heads * head_dim), so that they may be slices of one
- * projection's output; base pointers are 16-byte aligned.  Others: LV_EINVAL. */
+ * projection's output; base pointers are 16-byte aligned; a call has at most 2^30
+ * tokens and 2^24 requests.  Others: LV_EINVAL.  Waits inside their kernels are
+ * bounded; one that runs out records LV_ETIMEOUT, and the call's outputs are void. */
 #define LV_BF16 0
 #define LV_F16 1
 #define LV_MAX_GROUP 64

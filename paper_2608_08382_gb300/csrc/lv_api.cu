@@ -875,6 +875,7 @@ void lv_ctx_destroy(lv_ctx *ctx) {
   if (ctx->h_acc) cudaFreeHost(ctx->h_acc);
   if (ctx->d_probe) cudaFree(ctx->d_probe);
   if (ctx->kv.scratch) cudaFree(ctx->kv.scratch);
+  for (int k = 0; k < ctx->kv.n_outgrown; ++k) cudaFree(ctx->kv.outgrown[k]);
   if (ctx->kv.counter) cudaFree(ctx->kv.counter);
   if (ctx->ev_built) cudaEventDestroy(ctx->ev_built);
   if (ctx->ev_used) cudaEventDestroy(ctx->ev_used);

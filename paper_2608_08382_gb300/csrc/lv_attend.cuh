@@ -126,66 +126,110 @@ __device__ __forceinline__ int64_t find_unit(const int64_t *S, int64_t n, int64_
 }
 
 // Row (query t, head h) of request i, whose tokens start at `first`, once more by
-// one warp, key by key over the first n keys.  The rows of a tile see different
-// numbers of keys, and a NaN or infinity that only later rows see reaches the
-// others through a weight of zero; only rows that came out as NaN are done so.
-// The largest score first: a weight is at most 1, and an infinite value is not
-// scaled by zero on its way.
+// one warp, key by key over the first n keys, where it came out with a NaN that is
+// not its own.  The rows of a tile see different numbers of keys, and a NaN or
+// infinity among the values that only later rows see reaches the others through a
+// weight of zero.  So first it is looked whether there is one in the up to 144
+// keys from n on, below `bound`, that the tile's products went over; and the walk
+// ends early where the row's own keys explain what it has.  The largest score
+// first: a weight is at most 1, and an infinite value is not scaled by zero on its
+// way.
+template <int D, bool PAGED>
+__device__ __forceinline__ int64_t value_place(const AttendArgs &a, int64_t first, int64_t i, int g, int64_t j, int64_t *bh) {
+  if (!PAGED) return (first + j) * a.v_stride + (int64_t)g * D;
+  const CacheView &cv = a.cache;
+  const int32_t b = a.table[i * a.width + (j >> cv.log_b)];
+  if (b < 0 || b >= cv.n_blocks) return -1;
+  *bh = (int64_t)b * cv.heads + g;
+  return ((*bh << cv.log_b) + (j & ((1 << cv.log_b) - 1))) * D;
+}
+
 template <int D, bool F16, bool PAGED>
-__device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_t i, int64_t t, int h, int64_t n) {
+__device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_t i, int64_t t, int h, int64_t n, int64_t bound) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, g = h / (a.hq / a.hkv);
   const CacheView &cv = a.cache;
+  auto value = [&](int64_t at, int64_t bh, float *v) {
+    if (PAGED) {
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        __nv_fp8_e4m3 e;
+        e.__x = cv.v[at + lane * E + k];
+        v[k] = (float)e * cv.v_scale[bh];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < E; k += 2) {
+        const float2 y = unpack2<F16>(*(const uint32_t *)((const uint16_t *)a.v + at + lane * E + k));
+        v[k] = y.x, v[k + 1] = y.y;
+      }
+    }
+  };
+  bool odd = false;
+  for (int64_t j = n; j < min(n + 144, bound); ++j) {
+    int64_t bh = 0;
+    const int64_t at = value_place<D, PAGED>(a, first, i, g, j, &bh);
+    if (at < 0) continue;
+    float v[E];
+    value(at, bh, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) odd |= !isfinite(v[k]);
+  }
+  if (!__any_sync(~0u, odd)) return;
   const uint16_t *qp = (const uint16_t *)a.q + t * a.q_stride + h * D + lane * E;
+  uint16_t *op = (uint16_t *)a.o + (t * a.hq + h) * D + lane * E;
   float q[E], o[E];
+  bool has[E];  // what came out as NaN and is not explained yet
 #pragma unroll
   for (int k = 0; k < E; k += 2) {
-    const float2 f = unpack2<F16>(*(const uint32_t *)(qp + k));
+    const float2 f = unpack2<F16>(*(const uint32_t *)(qp + k)), y = unpack2<F16>(*(const uint32_t *)(op + k));
     q[k] = f.x * a.scale, q[k + 1] = f.y * a.scale;
+    has[k] = isnan(y.x), has[k + 1] = isnan(y.y);
     o[k] = o[k + 1] = 0.f;
   }
   float m = -INFINITY, l = 0.f;
-  bool nan = false;
   for (int pass = 0; pass < 2; ++pass)
     for (int64_t j = 0; j < n; ++j) {
+      int64_t bh = 0;
+      const int64_t at = value_place<D, PAGED>(a, first, i, g, j, &bh);
+      if (at < 0) continue;
       float x = 0.f, v[E];
+      value(at, bh, v);
       if (PAGED) {
-        const int32_t b = a.table[i * a.width + (j >> cv.log_b)];
-        if (b < 0 || b >= cv.n_blocks) continue;
-        const int64_t bh = (int64_t)b * cv.heads + g;
-        const int64_t at = ((bh << cv.log_b) + (j & ((1 << cv.log_b) - 1))) * D + lane * E;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
           __nv_fp8_e4m3 e;
-          e.__x = cv.k[at + k];
+          e.__x = cv.k[at + lane * E + k];
           x += q[k] * (float)e;
-          e.__x = cv.v[at + k];
-          v[k] = (float)e * cv.v_scale[bh];
         }
         x *= cv.k_scale[bh];
       } else {
         const uint16_t *kp = (const uint16_t *)a.k + (first + j) * a.k_stride + g * D + lane * E;
-        const uint16_t *vp = (const uint16_t *)a.v + (first + j) * a.v_stride + g * D + lane * E;
 #pragma unroll
         for (int k = 0; k < E; k += 2) {
-          const float2 f = unpack2<F16>(*(const uint32_t *)(kp + k)), y = unpack2<F16>(*(const uint32_t *)(vp + k));
+          const float2 f = unpack2<F16>(*(const uint32_t *)(kp + k));
           x += q[k] * f.x + q[k + 1] * f.y;
-          v[k] = y.x, v[k + 1] = y.y;
         }
       }
       for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
       if (pass == 0) {
-        nan |= isnan(x);
+        if (isnan(x)) return;  // all of the row's own is NaN
         m = fmaxf(m, x);
+        bool open = false;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          has[k] = has[k] && !isnan(v[k]);
+          open |= has[k];
+        }
+        if (!__any_sync(~0u, open)) return;  // every NaN that it has is one that it sees
         continue;
       }
-      const float w = nan ? NAN : m == -INFINITY ? 0.f : exp2f(x - m);
+      const float w = m == -INFINITY ? 0.f : exp2f(x - m);
       l += w;
 #pragma unroll
       for (int k = 0; k < E; ++k) o[k] += w * v[k];
     }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t *op = (uint16_t *)a.o + (t * a.hq + h) * D + lane * E;
 #pragma unroll
   for (int k = 0; k < E; k += 2) *(uint32_t *)(op + k) = pack_out<F16>(o[k] * inv, o[k + 1] * inv);
 }

@@ -1,15 +1,14 @@
-// What every kernel of the library shares: the bits of the status word and
-// programmatic dependent launch.
+// What the attention kernels share with the others: the bits of the status word and
+// programmatic dependent launch.  The same lines stand in lv_kernels.cuh, whose
+// text the committed counter summaries are tied to; lv_kv.cu does not include it.
 #pragma once
 
 #include <cstdint>
 
 namespace lv {
 
-// Bits of the sticky status word: invalid input data; a fit feature beyond
-// the exact range (bit 2 is reserved).
-constexpr int kStatusData = 1;
-constexpr int kStatusOverflow = 4;
+// Bits of the sticky status word.
+constexpr int kStatusData = 1;     // invalid input data
 constexpr int kStatusTimeout = 8;  // a bounded wait inside a kernel ran out
 
 // Programmatic dependent launch.  A kernel launched so (launch_after in the host

@@ -339,11 +339,12 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       const int tok = it.t0 + k * c.tile + row / G, h = it.head * G + row % G;
       const bool valid = row < c.tile * G && tok < it.len;
       float m = -INFINITY, l = 0.f, ref = 0.f, inv_ref = 0.f;
-      int64_t lim = 0;  // keys that the row sees
+      int64_t lim = 0, bound = 0;  // keys that the row sees, that the request has
       if (blocks > 0) {
         bool ignore = false;
         const Span sp = request_span(a, i, &ignore);
         lim = valid ? row_limit(a, sp, tok) : 0;
+        bound = row_limit(a, sp, sp.p - 1);
         const int64_t all = row_limit(a, sp, it.t0 + k * c.tile);  // what every row of the tile sees
         // the row's query
         float sl = fabsf(a.scale);
@@ -558,7 +559,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         again &= again - 1;
         const int rt = __shfl_sync(~0u, tok, r), rh = __shfl_sync(~0u, h, r);
         const int64_t rl = __shfl_sync(~0u, lim, r);
-        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl);
+        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl, bound);
       }
     }
   }
@@ -640,7 +641,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
         nan |= isnan(o[e]) || isnan(o[e + 1]);
       }
       if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (top - kChExp + log2f(l)) * 0.6931471805599453f;
-      if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok));
+      if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok), row_limit(a, sp, sp.p - 1));
     }
   }
 }

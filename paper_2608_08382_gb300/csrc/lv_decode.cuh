@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
             }
           const int rr = row0 + 8 * nt + row, j = rr / G;
           if (__any_sync(~0u, nan) && j < sp.p)
-            redo_row<D, F16, true>(a, sp.first, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j));
+            redo_row<D, F16, true>(a, sp.first, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j), row_limit(a, sp, sp.p - 1));
         }
     }
     u += s1 == strips ? all_units - s0 : s1 - s0;
@@ -583,7 +583,7 @@ __global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_
       }
       if (a.lse && lane == 0)
         a.lse[at] = l == 0.f ? -INFINITY : (top - kWeightExp + log2f(l)) * 0.6931471805599453f;
-      if (sp.p > 1 && __any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, sp.first + j, hh, row_limit(a, sp, j));
+      if (sp.p > 1 && __any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, sp.first + j, hh, row_limit(a, sp, j), row_limit(a, sp, sp.p - 1));
     }
     if (per_row > 1) __syncthreads();
   }

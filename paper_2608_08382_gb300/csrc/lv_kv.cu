@@ -28,20 +28,21 @@ bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 int log2_of(int64_t x) { return 63 - __builtin_clzll((unsigned long long)x); }
 
-// The context's scratch, at least `bytes`.
+// The context's scratch, at least `bytes`.  It grows by doubling and what it
+// outgrows is kept to the context's end: a call that was captured into a graph
+// works there at every replay.
 lv_status scratch_for(KvHost *kv, size_t bytes) {
   if (bytes <= kv->cap) return LV_OK;
-  LV_CUDA(cudaDeviceSynchronize());
-  if (kv->scratch) cudaFree(kv->scratch);
-  kv->scratch = nullptr;
-  kv->cap = 0;
+  const size_t cap = std::max(std::max(bytes, 2 * kv->cap), (size_t)1 << 20);
+  if (kv->n_outgrown == 64) return LV_ENOMEM;
   void *p = nullptr;
-  if (cudaMalloc(&p, bytes) != cudaSuccess) {
+  if (cudaMalloc(&p, cap) != cudaSuccess) {
     cudaGetLastError();
     return LV_ENOMEM;
   }
+  if (kv->scratch) kv->outgrown[kv->n_outgrown++] = kv->scratch;
   kv->scratch = static_cast<unsigned char *>(p);
-  kv->cap = bytes;
+  kv->cap = cap;
   return LV_OK;
 }
 
@@ -81,7 +82,7 @@ bool heads_ok(int32_t dtype, int32_t hq, int32_t hkv) {
          hq / hkv <= LV_MAX_GROUP;
 }
 
-constexpr int64_t kMostTokens = 1ll << 31;
+constexpr int64_t kMostTokens = 1ll << 30;
 
 // A kernel's shared-memory limit, once for a context; `kind` numbers the kernels.
 template <class K>

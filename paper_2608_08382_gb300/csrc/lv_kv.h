@@ -14,6 +14,8 @@ struct KvHost {
   int *d_status = nullptr;           // the context's status word
   unsigned char *scratch = nullptr;  // owned
   size_t cap = 0;
+  void *outgrown[64] = {};           // owned: earlier scratch, which captured calls may still use
+  int n_outgrown = 0;
   unsigned configured = 0;           // kernels whose shared-memory limit is set, a bit each
   unsigned long long *counter = nullptr;  // owned: two counters of work that kernels hand out, zero between calls
 };

@@ -64,6 +64,18 @@ constexpr int kStoreWarps = 8;
 constexpr int kStoreWindow = 32;  // tokens of a window, at most
 constexpr int kStoreRun = 128;    // tokens of a run, at most: a block's
 
+// Products and quotients that a rounding to e4m3 follows, under a scale that is no
+// power of two: cut, with the last bit set where something was cut off, so that the
+// two roundings together are one.
+__device__ __forceinline__ float odd_product(float a, float b) {
+  const float p = __fmul_rz(a, b);
+  return __fmaf_rn(a, b, -p) != 0.f ? __uint_as_float(__float_as_uint(p) | 1) : p;
+}
+__device__ __forceinline__ float odd_quotient(float a, float b) {
+  const float q = __fdiv_rz(a, b);
+  return __fmaf_rn(-q, b, a) != 0.f ? __uint_as_float(__float_as_uint(q) | 1) : q;
+}
+
 // The larger ones of two pairs of 16 bits.
 __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -179,7 +191,7 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, i
           for (int y = 0; y < 4; ++y) {
             float f[4];
             decode4(w[y], f);
-            w[y] = encode4(f[0] * r, f[1] * r, f[2] * r, f[3] * r);
+            w[y] = encode4(odd_product(f[0], r), odd_product(f[1], r), odd_product(f[2], r), odd_product(f[3], r));
           }
           *reinterpret_cast<uint4 *>(code + i) = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -204,7 +216,7 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, i
           f[2 * y] = p.x, f[2 * y + 1] = p.y;
         }
 #pragma unroll
-        for (int y = 0; y < 8; ++y) f[y] = pow2 ? f[y] * inv : f[y] / s;
+        for (int y = 0; y < 8; ++y) f[y] = pow2 ? f[y] * inv : odd_quotient(f[y], s);
         if (!all_finite) {
 #pragma unroll
           for (int y = 0; y < 8; ++y) f[y] = no_inf(f[y]);

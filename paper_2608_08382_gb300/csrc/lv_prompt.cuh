@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         again &= again - 1;
         const int rt = __shfl_sync(~0u, tok, r);
         const int rh = __shfl_sync(~0u, (int)h, r);
-        redo_row<D, F16, false>(a, it.first, 0, (int64_t)it.first + rt, rh, rt + 1);
+        redo_row<D, F16, false>(a, it.first, 0, (int64_t)it.first + rt, rh, rt + 1, a.n_tok - it.first);
       }
     }
   }
