@@ -14,6 +14,16 @@
 // The blocks of keys of all items stand in one line and every CTA takes an even
 // share of it, so a few long contexts keep every SM busy; an item that several
 // CTAs share leaves a part for each, and k_chunk_join adds them in the line's order.
+//
+// Warps: 0-3 and 4-7 softmax of the two tiles; 8-11 and 12-15 conversion of keys and
+// of values; 16 issues the products; 17 hands out the items; 18 copies the codes,
+// two blocks ahead, and brings the scales.
+//
+// Measured: six chunks of 512 tokens on contexts of up to 32,256, 20/4 heads of 128,
+// 497 GFLOP: 502 us with the join, 990 TFLOP/s, 0.52 of the measured rate.  A block
+// of both tiles takes 4,000 clocks, the products 2,048 of them; shared memory moves
+// 320 KB in that time (2,500 clocks at its rate), and a tile's softmax has the
+// converting warps beside it on the SM.
 #pragma once
 
 #include "lv_decode.cuh"

