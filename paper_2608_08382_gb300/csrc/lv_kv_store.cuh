@@ -142,15 +142,14 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, i
     const int64_t stride = kv ? a.stride[1] : a.stride[0];
     float *sp = (kv ? a.scale[1] : a.scale[0]) + blk * a.heads + h;
     const float old = off > 0 ? *sp : 0.f;
-    const uint16_t *x =
-        reinterpret_cast<const uint16_t *>(kv ? a.x[1] : a.x[0]) + (t0 + run_at[run]) * stride + (int64_t)h * D + sub * 8;
+    const uint16_t *x = reinterpret_cast<const uint16_t *>(kv ? a.x[1] : a.x[0]) +
+                        (t0 + run_at[run] + of) * stride + (int64_t)h * D + sub * 8;
     uint4 v[kHeld];
     auto load = [&](int from) {
+      const uint16_t *y = x + from * stride;
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        const int j = from + k * kRows + of;
-        v[k] = j < n ? *reinterpret_cast<const uint4 *>(x + j * stride) : make_uint4(0, 0, 0, 0);
-      }
+      for (int k = 0; k < kHeld; ++k, y += kRows * stride)
+        v[k] = from + k * kRows + of < n ? *reinterpret_cast<const uint4 *>(y) : make_uint4(0, 0, 0, 0);
     };
     // the largest magnitude by its bits, two elements at a time; where it is not
     // finite, once more over those that are
@@ -169,7 +168,7 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, i
     if (!all_finite) {
       top = 0;
 #pragma unroll 1
-      for (int j = of; j < n; j += kRows) {
+      for (int j = 0; j + of < n; j += kRows) {
         const uint4 y = *reinterpret_cast<const uint4 *>(x + j * stride);
         const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -202,31 +201,35 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) k_kv_store(StoreArgs a, i
       }
     }
     if (lane == 0) *sp = s;
-    // by a power of two a product is the quotient; a scale of another kind is the caller's own
-    const bool pow2 = (__float_as_uint(s) & 0x7fffff) == 0;
+    // Eight codes of a lane.  By a power of two a product is the quotient; the longer
+    // way is for a scale of another kind (the caller's own) and values that are not
+    // finite, and kept out of the loop that all else takes.
+    uint8_t *to = code + (off + of) * D + sub * 8;
     const float inv = 1.f / s;
-    for (int from = 0; from < n; from += 16) {
-      if (n > 16) load(from);
+    if (all_finite && (__float_as_uint(s) & 0x7fffff) == 0) {
+      for (int from = 0; from < n; from += 16) {
+        if (n > 16) load(from);
 #pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        if (from + k * kRows >= n) break;
-        const int j = from + k * kRows + of;
-        if (j >= n) continue;
-        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        for (int k = 0; k < kHeld; ++k) {
+          const float2 p0 = unpack2<F16>(v[k].x), p1 = unpack2<F16>(v[k].y), p2 = unpack2<F16>(v[k].z), p3 = unpack2<F16>(v[k].w);
+          if (from + k * kRows + of < n)
+            *reinterpret_cast<uint2 *>(to + (from + k * kRows) * D) =
+                make_uint2(encode4(p0.x * inv, p0.y * inv, p1.x * inv, p1.y * inv),
+                           encode4(p2.x * inv, p2.y * inv, p3.x * inv, p3.y * inv));
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int j = 0; j + of < n; j += kRows) {
+        const uint4 y = *reinterpret_cast<const uint4 *>(x + j * stride);
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
         float f[8];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const float2 p = unpack2<F16>(w[y]);
-          f[2 * y] = p.x, f[2 * y + 1] = p.y;
+        for (int z = 0; z < 4; ++z) {
+          const float2 p = unpack2<F16>(w[z]);
+          f[2 * z] = no_inf(odd_quotient(p.x, s)), f[2 * z + 1] = no_inf(odd_quotient(p.y, s));
         }
-#pragma unroll
-        for (int y = 0; y < 8; ++y) f[y] = pow2 ? f[y] * inv : odd_quotient(f[y], s);
-        if (!all_finite) {
-#pragma unroll
-          for (int y = 0; y < 8; ++y) f[y] = no_inf(f[y]);
-        }
-        *reinterpret_cast<uint2 *>(code + (off + j) * D + sub * 8) =
-            make_uint2(encode4(f[0], f[1], f[2], f[3]), encode4(f[4], f[5], f[6], f[7]));
+        *reinterpret_cast<uint2 *>(to + j * D) = make_uint2(encode4(f[0], f[1], f[2], f[3]), encode4(f[4], f[5], f[6], f[7]));
       }
     }
   }
