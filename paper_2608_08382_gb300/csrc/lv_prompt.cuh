@@ -375,7 +375,6 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     const int k = warp >> 2, row = threadIdx.x & 127;
     const uint32_t lane0 = (uint32_t)(warp & 3) * 32 << 16;
     const uint32_t ts = tmem + lane0 + k * kCols, to = tmem + lane0 + 256 + k * D;
-    const float sl = fabsf(a.scale);
     int ss = 0, os = 0;
     for (int n = 0;; ++n) {
       bar_wait(&sm.item_full[n & 1], (n >> 1) & 1, stop);
@@ -389,6 +388,9 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       const bool valid = row < p.tile * G && tok < it.len;
       const int lim = valid ? tok + 1 : 0;           // keys that it sees
       const int all = it.t0 + k * p.tile + 1;        // keys that every row of the tile sees
+      // A row without a query holds what shared memory held or another sequence's query: its
+      // scores count as zero, so that it has no say in when the warp's maxima move
+      const float sl = valid ? fabsf(a.scale) : 0.f;
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < blocks; ++j) {
         bar_wait(&sm.s_full[k], ss & 1, stop);
