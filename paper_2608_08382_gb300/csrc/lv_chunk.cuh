@@ -8,8 +8,9 @@
 // ones scaled by a power of two to a largest element of 2^14).  A strip of 16 keys
 // lies in one block of the cache; its key scale goes into the factor of its
 // scores, its value scale vs, as vs / ref, to its weights.  ref follows the
-// largest vs once that is past 2^3 ref, as the weights' maximum follows the true
-// one past 2^8: a weight is at most 2^(8 + 4 + 3) then.
+// largest vs of the strips that the row sees, once that is past 2^3 ref, as the
+// weights' maximum follows the true one past 2^8: a weight is at most 2^(8 + 4 + 3)
+// then.
 //
 // The blocks of keys of all items stand in one line and every CTA takes an even
 // share of it, so a few long contexts keep every SM busy; an item that several
@@ -439,9 +440,15 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
               tmem_store16(ts + x, v);
             }
             tmem_wait_store();
+            // A value scale is the row's from the first key of its strip on that the row sees: one
+            // of later keys would raise ref and take the weights' bits.
+            top_vs = 0.f;
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
+            for (int x = 0; x < 8; ++x) {
               if (f[x] == 0.f) f[x] = 1e-37f;  // it must stay there
+              if ((hidden >> x & 1) || 16 * x >= rel) r[x] = 0.f;
+              top_vs = fmaxf(top_vs, fabsf(r[x]));
+            }
           }
           // The scores are read from tensor memory twice, for the maximum and for the
           // weights: a thread that keeps its 128 has no registers left for the rest.

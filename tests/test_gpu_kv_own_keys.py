@@ -1,10 +1,12 @@
 """The attention calls where values that a query does not see, or scales far apart, could reach its output: every row is
 its own keys' alone, whatever stands beside them."""
 
+import numpy as np
 import pytest
 
+import kv_reference as ref
 import test_gpu_attribute as base
-from test_gpu_kv import _t
+from test_gpu_kv import _cached, _check_rows, _gather, _np, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +53,43 @@ def test_prompt_rows_of_the_next_sequence(lv, ctx, len0):
         q[len0:] = q[:300] * size
         o, lse = _prompts(lv, ctx, q, k, v, [0, len0, T])
         assert torch.equal(o[:len0], want[0][:len0]) and torch.equal(lse[:len0], want[1][:len0])
+
+
+def _chunk_case(lv, ctx, rng, lens, new, B, hq, hkv, d, change, dtype="bfloat16"):
+    """Requests over a cache whose codes and scales `change` has had; their outputs and what these are formed from."""
+    import torch
+    lens, new = np.asarray(lens, np.int64), np.asarray(new, np.int64)
+    codes, scales, table = _cached(rng, lens, B, hkv, d)
+    change(codes, scales, table)
+    X = np.concatenate([[0], np.cumsum(new)])
+    q = torch.as_tensor(rng.normal(size=(X[-1], hq, d))).to(getattr(torch, dtype)).cuda()
+    o, lse = torch.full_like(q, 9.0), torch.full((int(X[-1]), hq), 9.0, device="cuda")
+    cache = lv.KVCache(*(_t(a, "uint8") for a in codes), *(_t(a, "float32") for a in scales))
+    lv.lv_kv_attend(ctx, cache, q, _t(lens - new, "int32"), _t(table, "int32"), o, lse=lse, token_offsets=_t(X, "int64"))
+    assert ctx.status() == lv.LV_OK
+    return X, _np(q), _np(o), _np(lse), codes, scales, table
+
+
+def _check_own_keys(case, i, n, new, B, hq, hkv, d, rows, unit=1.0):
+    """Rows of request i (n keys, the last `new` of them its queries') against the keys that they see and no other."""
+    X, q, o, lse, codes, scales, table = case
+    K, V = _gather(codes, scales, table, i, n, B)
+    for j in rows:
+        at, m = X[i] + j, n - new + j + 1
+        _check_rows(o[at:at + 1] * unit, lse[at:at + 1], q[at:at + 1], (K[:m], V[:m] * unit), np.ones((1, m), bool), d ** -0.5,
+                    "bf16", hq, hkv, f"row {j}")
+
+
+@pytest.mark.parametrize("up", [2.0**28, 2.0**30, 2.0**90])
+@pytest.mark.parametrize("n, new, hq, hkv", [(64, 64, 4, 1), (300, 64, 4, 1), (150, 150, 2, 2), (280, 64, 20, 1)])
+def test_chunk_value_scales_of_later_tokens(lv, ctx, up, n, new, hq, hkv):
+    """The last block's values are far larger than the others: rows before it keep their own values' weights."""
+    B, d = 16, 128
+    rng = np.random.default_rng(n)
+    last = (n - 1) // B
+
+    def change(codes, scales, table):
+        scales[1, table[0, last]] *= up
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, hkv, d, change)
+    _check_own_keys(case, 0, n, new, B, hq, hkv, d, range(new - (n - last * B)))
