@@ -445,8 +445,9 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
             top_vs = 0.f;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-              if (f[x] == 0.f) f[x] = 1e-37f;  // it must stay there
-              if ((hidden >> x & 1) || 16 * x >= rel) r[x] = 0.f;
+              const bool no = (hidden >> x & 1) || 16 * x >= rel;  // nothing of the strip is seen
+              if (no) r[x] = 0.f;
+              if (no || f[x] == 0.f) f[x] = 1e-37f;  // it must stay there, under a NaN scale too
               top_vs = fmaxf(top_vs, fabsf(r[x]));
             }
           }

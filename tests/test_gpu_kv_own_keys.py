@@ -93,3 +93,21 @@ def test_chunk_value_scales_of_later_tokens(lv, ctx, up, n, new, hq, hkv):
 
     case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, hkv, d, change)
     _check_own_keys(case, 0, n, new, B, hq, hkv, d, range(new - (n - last * B)))
+
+
+@pytest.mark.parametrize("n, new, hq, hkv, d", [(64, 64, 4, 1, 128), (300, 64, 4, 1, 64), (150, 150, 2, 2, 128), (35, 5, 2, 1, 64)])
+@pytest.mark.parametrize("which", [0, 1])
+def test_nan_scales_of_later_tokens(lv, ctx, which, n, new, hq, hkv, d):
+    """A NaN scale of the last block's keys or values is no matter of the rows before it."""
+    B = 16
+    rng = np.random.default_rng(n + which)
+    last = (n - 1) // B
+    before = max(0, new - (n - last * B))
+
+    def change(codes, scales, table):
+        scales[which, table[0, last]] = np.nan
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, hkv, d, change)
+    _check_own_keys(case, 0, n, new, B, hq, hkv, d, range(before))
+    o, lse = case[2], case[3]
+    assert np.isnan(o[before:]).all() and np.isnan(lse[before:]).all() == (which == 0)
