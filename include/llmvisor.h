@@ -428,7 +428,10 @@ lv_status lv_kv_store(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, cons
  * A query that sees no key gives 0 and -inf.  o is [n_tok][n_q_heads][head_dim]
  * without gaps, in q's type; lse float[n_tok][n_q_heads].  Products are summed
  * and the softmax is held in fp32; a query's 16-bit value is used as it is and a
- * weight is rounded to 16 bits before it meets V.
+ * weight, times its key's value scale, is rounded to fp16 before it meets V.  Where
+ * the value scales (those above 2^-100) lie so far apart that the rounding could
+ * take more than 2^-15 of the largest weight, rows are formed in fp32, key by key:
+ * exact, but slow, about 0.8 us for a row and key.
  * A table entry outside [-1, n_blocks) (hidden), a negative c (its queries see
  * nothing), tokens past the row's table_width (hidden) and offsets that decrease
  * or leave [0, n_tok] (taken as no queries) record LV_EDATA. */

@@ -31,6 +31,13 @@ struct AttendArgs {
   int *status;
 };
 
+// Over the cache a weight w meets its value as w vs / ref in fp16, vs the value scale
+// of the key's block and ref the largest so far: a scale far below ref takes bits
+// from its weights, though ref may be of keys whose values are zeros.  Beyond 2^-15
+// of the largest weight a row is done again alone (redo_row).  A scale of at most
+// kLeastScale, the least that an append sets and so a block of zeros, brings nothing.
+constexpr float kLeastScale = 0x1p-100f;
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -126,14 +133,15 @@ __device__ __forceinline__ int64_t find_unit(const int64_t *S, int64_t n, int64_
 }
 
 // Row (query t, head h) of request i, whose tokens start at `first`, once more by
-// one warp, key by key over the first n keys, where it came out with a NaN that is
-// not its own.  The rows of a tile see different numbers of keys, and a NaN or
-// infinity among the values that only later rows see reaches the others through a
-// weight of zero.  So first it is looked whether there is one in the up to 144
-// keys from n on, below `bound`, that the tile's products went over; and the walk
-// ends early where the row's own keys explain what it has.  The largest score
-// first: a weight is at most 1, and an infinite value is not scaled by zero on its
-// way.
+// one warp, key by key over the first n keys, in fp32 alone.  With `all` false,
+// where the row came out with a NaN that is not its own.  The rows of a tile see
+// different numbers of keys, and a NaN or infinity among the values that only later
+// rows see reaches the others through a weight of zero.  So first it is looked
+// whether there is one in the up to 144 keys from n on, below `bound`, that the
+// tile's products went over; and the walk ends early where the row's own keys
+// explain what it has.  With `all` true, where its value scales lie so far apart
+// that a weight in 16 bits may have been lost.  The largest score first: a weight is
+// at most 1, and an infinite value is not scaled by zero on its way.
 template <int D, bool PAGED>
 __device__ __forceinline__ int64_t value_place(const AttendArgs &a, int64_t first, int64_t i, int g, int64_t j, int64_t *bh) {
   if (!PAGED) return (first + j) * a.v_stride + (int64_t)g * D;
@@ -145,7 +153,7 @@ __device__ __forceinline__ int64_t value_place(const AttendArgs &a, int64_t firs
 }
 
 template <int D, bool F16, bool PAGED>
-__device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_t i, int64_t t, int h, int64_t n, int64_t bound) {
+__device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_t i, int64_t t, int h, int64_t n, int64_t bound, bool all = false) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, g = h / (a.hq / a.hkv);
   const CacheView &cv = a.cache;
@@ -165,8 +173,8 @@ __device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_
       }
     }
   };
-  bool odd = false;
-  for (int64_t j = n; j < min(n + 144, bound); ++j) {
+  bool odd = all;
+  for (int64_t j = n; !all && j < min(n + 144, bound); ++j) {
     int64_t bh = 0;
     const int64_t at = value_place<D, PAGED>(a, first, i, g, j, &bh);
     if (at < 0) continue;
@@ -221,7 +229,7 @@ __device__ __noinline__ void redo_row(const AttendArgs &a, int64_t first, int64_
           has[k] = has[k] && !isnan(v[k]);
           open |= has[k];
         }
-        if (!__any_sync(~0u, open)) return;  // every NaN that it has is one that it sees
+        if (!all && !__any_sync(~0u, open)) return;  // every NaN that it has is one that it sees
         continue;
       }
       const float w = m == -INFINITY ? 0.f : exp2f(x - m);

@@ -36,6 +36,7 @@ constexpr int kChThreads = 640;
 constexpr int kChScales = 8;       // blocks whose scales are kept: more than the copies run ahead
 constexpr float kChExp = 4.f;      // weights are 2^4 at the maximum they refer to
 constexpr float kChRef = 8.f;      // largest vs / ref
+constexpr float kChThin = 0x1p-14f;  // least vs / ref under which fp16 holds 2^kChExp to 2^-15 of it (its least step is 2^-24)
 
 struct ChunkArgs {
   AttendArgs a;
@@ -61,6 +62,7 @@ struct ChunkSmem {
   PromptItem item[2];
   alignas(16) float ks[kChScales][8], vs[kChScales][8];  // of a block's strips
   float top_vs[kChScales];          // the largest |vs| of a block
+  int thin[kChScales];              // the value scales of the item so far lie further apart than kChThin
   uint32_t hidden[kChScales];       // its strips whose block is hidden, a bit each
   uint32_t state[kCodes][8];  // of a block's strips: keys that are there, bit 8: their sign is changed
   int64_t req[2], from[2];  // of each item: its request, its first block
@@ -218,6 +220,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
         bool ignore = false;
         const Span sp = request_span(a, i, &ignore);
         const int64_t keys = row_limit(a, sp, sp.p - 1);
+        float most_vs = 0.f, least_vs = INFINITY;  // of the item's blocks
         int32_t id[2];
         float ks[2], vs[2];
         auto look_up = [&](int set, int group) {
@@ -247,15 +250,20 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           const int strip = lane & 7;
           const int64_t pos = (from + j) * kPrBlock + strip * 16;
           const int there = id[0] < 0 ? 0 : (int)max((int64_t)0, min((int64_t)16, keys - pos));
-          float top = fabsf(vs[0]);
+          float top = fabsf(vs[0]), low = top > kLeastScale ? top : INFINITY;
 #pragma unroll
-          for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+          for (int x = 1; x < 8; x <<= 1) {
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+            low = fminf(low, __shfl_xor_sync(~0u, low, x));
+          }
+          most_vs = fmaxf(most_vs, __shfl_sync(~0u, top, (j & 3) * 8));
+          least_vs = fminf(least_vs, __shfl_sync(~0u, low, (j & 3) * 8));
           const uint32_t gone = __ballot_sync(~0u, id[0] < 0) >> (lane & 24) & 255;
           if (mine) {
             const uint32_t at = (block + j) % kChScales;
             sm.ks[at][strip] = fabsf(ks[0]);
             sm.vs[at][strip] = vs[0];
-            if (strip == 0) sm.top_vs[at] = top, sm.hidden[at] = gone;
+            if (strip == 0) sm.top_vs[at] = top, sm.thin[at] = least_vs < kChThin * most_vs, sm.hidden[at] = gone;
             bar_arrive(&sm.scale_full[at]);
           }
           const int64_t off = ((((int64_t)max(id[0], 0) * cv.heads + head) << cv.log_b) + (pos & ((1 << cv.log_b) - 1))) * D;
@@ -350,6 +358,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       const int tok = it.t0 + k * c.tile + row / G, h = it.head * G + row % G;
       const bool valid = row < c.tile * G && tok < it.len;
       float m = -INFINITY, l = 0.f, ref = 0.f, inv_ref = 0.f;
+      int thin = 0;                // value scales so far apart that a weight may have lost too many bits
       int64_t lim = 0, bound = 0;  // keys that the row sees, that the request has
       if (blocks > 0) {
         bool ignore = false;
@@ -524,6 +533,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           float l0, l1;
           unpair(add2(sum[0], sum[1]), &l0, &l1);
           l += l0 + l1;
+          thin = sm.thin[(block0 + j) % kChScales];
           tmem_wait_store();
           tc_before_sync();
           __syncwarp();
@@ -569,15 +579,15 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       }
       if (valid && whole && a.lse)
         a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m - kChExp + log2f(l)) * 0.6931471805599453f;
-      if (!whole) *reinterpret_cast<float2 *>(c.part_ml + 2 * at) = make_float2(m, l);
-      unsigned again = __ballot_sync(~0u, nan);
+      if (!whole) *reinterpret_cast<float2 *>(c.part_ml + 2 * at) = make_float2(m, thin ? -l : l);  // the join does it again
+      unsigned again = __ballot_sync(~0u, nan || (thin && whole && valid));
       __syncwarp();
       while (again) {
         const int r = __ffs(again) - 1;
         again &= again - 1;
         const int rt = __shfl_sync(~0u, tok, r), rh = __shfl_sync(~0u, h, r);
         const int64_t rl = __shfl_sync(~0u, lim, r);
-        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl, bound);
+        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl, bound, thin != 0);
       }
     }
   }
@@ -593,7 +603,8 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
 }
 
 // The items that several CTAs shared: a warp a row adds its parts in the line's
-// order.  A part whose keys the row does not see has l = 0 and no sums.
+// order.  A part whose keys the row does not see has l = 0 and no sums; one whose
+// weights lost bits has its l negative, and its row is done again.
 template <int D, bool F16>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
   constexpr int E = D / 32, kBatch = 4;
@@ -616,6 +627,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
       const int tok = (int)seg / a.hkv * 2 * c.tile + k * c.tile + row / G, h = (int)seg % a.hkv * G + row % G;
       if (row >= c.tile * G || tok >= sp.p) continue;
       float top = -INFINITY, l = 0.f, o[E];
+      bool thin = false;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = 0.f;
       for (int64_t x0 = w0; x0 <= w1; x0 += kBatch) {
@@ -644,7 +656,8 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
         for (int b = 0; b < kBatch; ++b) {
           if (pl[b] == 0.f) continue;
           const float f = pm[b] == -INFINITY ? 1.f : exp2_fast(pm[b] - base);
-          l += pl[b] * f;
+          l += fabsf(pl[b]) * f;
+          thin |= pl[b] < 0.f;
 #pragma unroll
           for (int e = 0; e < E; ++e) o[e] += po[b][e] * f;
         }
@@ -659,7 +672,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkArgs c, int ctas) {
         nan |= isnan(o[e]) || isnan(o[e + 1]);
       }
       if (a.lse && lane == 0) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (top - kChExp + log2f(l)) * 0.6931471805599453f;
-      if (__any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok), row_limit(a, sp, sp.p - 1));
+      if (__any_sync(~0u, nan || thin)) redo_row<D, F16, true>(a, sp.first, i, t, h, row_limit(a, sp, tok), row_limit(a, sp, sp.p - 1), thin);
     }
   }
 }

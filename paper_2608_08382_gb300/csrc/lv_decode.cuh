@@ -50,6 +50,7 @@ constexpr int kDecMinStrips = 8;   // strips a warp takes at least (5: no change
 constexpr int kDecRows = 16;       // rows of a request that go here: two row tiles of 8
 constexpr int kJoinWarps = 8;      // rows of a CTA that joins, a warp each
 constexpr float kWeightExp = 12.f;
+constexpr float kDecThin = 0x1p-22f;  // least vs / ref under which fp16 holds 2^kWeightExp to 2^-15 of it (its least step is 2^-24)
 
 struct DecodeArgs {
   AttendArgs a;
@@ -215,10 +216,25 @@ struct Strip {
   }
 };
 
+// All rows of a tile again, each alone.  A function of its own: inlined, its state takes
+// registers from the loop over strips.
+template <int D, bool F16>
+__device__ __noinline__ void redo_tile(const AttendArgs &a, int64_t i, int h, int row0, int rows) {
+  bool ignore = false;
+  const Span sp = request_span(a, i, &ignore);
+  const int G = a.hq / a.hkv;
+  __syncwarp();
+  for (int rr = row0; rr < row0 + rows && rr / G < sp.p; ++rr) {
+    const int64_t n = row_limit(a, sp, rr / G);
+    redo_row<D, F16, true>(a, sp.first, i, sp.first + rr / G, h * G + rr % G, n, n, true);
+  }
+}
+
 template <int D, bool F16, int NT>
 __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas2) k_attend_decode(DecodeArgs d) {
   constexpr int kRows = 8 * NT, kM = D / 16;  // row tile; tiles of 16 elements of the output
   __shared__ int64_t shared_sums[kScan + 1];
+  __shared__ unsigned shared_least[kDecWarps];  // a segment's least value scale, lane 0's: there is no register left for it
   const AttendArgs &a = d.a;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   wait_previous();
@@ -351,11 +367,21 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
     }
     id1 = checked(id1);
     scales_of(id1, &next_ks, &next_vs);
+    unsigned *const least_vs = shared_least + (threadIdx.x >> 5);
+    auto least_of = [&](float v) {
+      return __reduce_min_sync(~0u, __float_as_uint(fabsf(v) > kLeastScale ? fabsf(v) : INFINITY));
+    };
+    {
+      const unsigned v = least_of(vs);
+      if (lane == 0) *least_vs = v;
+    }
     for (int s = 0; s < count; ++s) {
       const float kss = __shfl_sync(~0u, ks, s & 31), vss = __shfl_sync(~0u, vs, s & 31);
       const bool here = at >= 0;
       if (((s + 1) & 31) == 0) {
         id0 = id1, ks = next_ks, vs = next_vs;
+        const unsigned v = least_of(vs);
+        if (lane == 0) *least_vs = min(*least_vs, v);
         id1 = checked(id2);
         scales_of(id1, &next_ks, &next_vs);
         id2 = look_up(s + 65);
@@ -493,6 +519,15 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
             redo_row<D, F16, true>(a, sp.first, i, sp.first + j, h * G + rr % G, row_limit(a, sp, j), row_limit(a, sp, sp.p - 1));
         }
     }
+    // value scales so far apart that a weight, or the sums where ref grew, may have lost too much
+    if (__shfl_sync(~0u, lane == 0 && __uint_as_float(*least_vs) < kDecThin * ref, 0)) {
+      if (whole) {
+        redo_tile<D, F16>(a, i, h, row0, kRows);
+      } else {  // the join does it
+        __syncwarp();
+        if (lane < kRows) d.part_ml[2 * (slot + lane) + 1] *= -1.f;
+      }
+    }
     u += s1 == strips ? all_units - s0 : s1 - s0;
   }
   if (bad) flag(a.status, kStatusData);
@@ -526,6 +561,7 @@ __global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_
     const int h = (int)seg / tiles, r = ((int)y % groups) * (per_row == 1 ? kJoinWarps : 1) + (per_row == 1 ? w : 0);
     const int row = ((int)seg % tiles) * rows + r, j = row / G, hh = h * G + row % G;
     float top = -INFINITY, l = 0.f, o[E];
+    bool thin = false;  // of a part whose weights lost bits l is negative
 #pragma unroll
     for (int k = 0; k < E; ++k) o[k] = 0.f;
     if (j < sp.p)
@@ -558,7 +594,8 @@ __global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_
         for (int b = 0; b < kBatch; ++b) {
           // a part that saw nothing has zeros, one of a NaN score NaN
           const float f = pm[b] == -INFINITY ? 1.f : exp2_fast(pm[b] - base);
-          l += pl[b] * f;
+          l += fabsf(pl[b]) * f;
+          thin |= pl[b] < 0.f;
 #pragma unroll
           for (int k = 0; k < E; ++k) o[k] += po[b][k] * f;
         }
@@ -567,14 +604,15 @@ __global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_
     if (per_row > 1) {
 #pragma unroll
       for (int k = 0; k < E; ++k) so[w][lane * E + k] = o[k];
-      if (lane == 0) sm[w % PER_ROW][0] = top, sm[w % PER_ROW][1] = l;
+      if (lane == 0) sm[w % PER_ROW][0] = top, sm[w % PER_ROW][1] = thin ? -l : l;
       __syncthreads();
       if (w == 0) {
         for (int x = 1; x < PER_ROW; ++x) {
           const float nm = fmaxf(top, sm[x][0]), base = nm == -INFINITY ? 0.f : nm;
           const float f0 = top == -INFINITY ? 1.f : exp2_fast(top - base);
           const float f1 = sm[x][0] == -INFINITY ? 1.f : exp2_fast(sm[x][0] - base);
-          l = l * f0 + sm[x][1] * f1;
+          l = l * f0 + fabsf(sm[x][1]) * f1;
+          thin |= sm[x][1] < 0.f;
 #pragma unroll
           for (int k = 0; k < E; ++k) o[k] = o[k] * f0 + so[x][lane * E + k] * f1;
           top = nm;
@@ -592,7 +630,8 @@ __global__ void __launch_bounds__((PER_ROW == 1 ? kJoinWarps : PER_ROW) * 32) k_
       }
       if (a.lse && lane == 0)
         a.lse[at] = l == 0.f ? -INFINITY : (top - kWeightExp + log2f(l)) * 0.6931471805599453f;
-      if (sp.p > 1 && __any_sync(~0u, nan)) redo_row<D, F16, true>(a, sp.first, i, sp.first + j, hh, row_limit(a, sp, j), row_limit(a, sp, sp.p - 1));
+      if (__any_sync(~0u, thin || (nan && sp.p > 1)))
+        redo_row<D, F16, true>(a, sp.first, i, sp.first + j, hh, row_limit(a, sp, j), row_limit(a, sp, sp.p - 1), thin);
     }
     if (per_row > 1) __syncthreads();
   }

@@ -65,7 +65,8 @@ def _chunk_case(lv, ctx, rng, lens, new, B, hq, hkv, d, change, dtype="bfloat16"
     q = torch.as_tensor(rng.normal(size=(X[-1], hq, d))).to(getattr(torch, dtype)).cuda()
     o, lse = torch.full_like(q, 9.0), torch.full((int(X[-1]), hq), 9.0, device="cuda")
     cache = lv.KVCache(*(_t(a, "uint8") for a in codes), *(_t(a, "float32") for a in scales))
-    lv.lv_kv_attend(ctx, cache, q, _t(lens - new, "int32"), _t(table, "int32"), o, lse=lse, token_offsets=_t(X, "int64"))
+    lv.lv_kv_attend(ctx, cache, q, _t(lens - new, "int32"), _t(table, "int32"), o, lse=lse,
+                    token_offsets=None if (new == 1).all() else _t(X, "int64"))
     assert ctx.status() == lv.LV_OK
     return X, _np(q), _np(o), _np(lse), codes, scales, table
 
@@ -111,3 +112,61 @@ def test_nan_scales_of_later_tokens(lv, ctx, which, n, new, hq, hkv, d):
     _check_own_keys(case, 0, n, new, B, hq, hkv, d, range(before))
     o, lse = case[2], case[3]
     assert np.isnan(o[before:]).all() and np.isnan(lse[before:]).all() == (which == 0)
+
+
+def _quiet(codes, table, i, B, k0, k1):
+    """Values of request i's keys k0 .. k1 - 1 to zero: their block's scale is another token's."""
+    for j in range(k0, k1):
+        codes[1, table[i, j // B], :, j % B] = 0
+
+
+@pytest.mark.parametrize("up", [2.0**10, 2.0**40, 2.0**100])
+@pytest.mark.parametrize("n, new, hq, hkv, d", [
+    (64, 64, 4, 1, 128), (400, 60, 4, 1, 64), (3000, 40, 4, 1, 128),   # chunks, the last shared by many SMs
+    (52, 3, 4, 2, 128), (900, 2, 5, 1, 64), (6000, 4, 4, 1, 128),      # few rows
+])
+def test_a_large_value_in_the_rows_own_block(lv, ctx, up, n, new, hq, hkv, d):
+    """The largest value of a block stands for none of a row's keys, but its scale is theirs too: what they bring is
+    zero, and the row's other keys keep their weights."""
+    B = 16
+    rng = np.random.default_rng(n)
+    last = (n - 1) // B * B
+
+    def change(codes, scales, table):
+        scales[1, table[0, last // B]] *= up
+        _quiet(codes, table, 0, B, last, n - 1)  # all but the last token's
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, hkv, d, change)
+    _check_own_keys(case, 0, n, new, B, hq, hkv, d, range(new - 1))
+
+
+@pytest.mark.parametrize("n, new, hq", [(700, 1, 4), (700, 1, 10), (20_000, 1, 4), (500, 1, 40), (9000, 1, 40)])
+@pytest.mark.parametrize("at", [0.0, 0.5])
+def test_a_block_of_zeros_under_a_large_scale(lv, ctx, n, new, hq, at):
+    """A block's values are zeros under a scale 2^60 above the others': it brings nothing, to blocks before and after."""
+    B, d = 16, 128
+    rng = np.random.default_rng(n + hq)
+    b = int(at * n) // B
+
+    def change(codes, scales, table):
+        scales[1, table[0, b]] = 2.0**60
+        _quiet(codes, table, 0, B, b * B, (b + 1) * B)
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, 1, d, change)
+    _check_own_keys(case, 0, n, new, B, hq, 1, d, range(new))
+
+
+@pytest.mark.parametrize("n, new, hq", [(50, 3, 4), (50, 30, 4), (5000, 3, 4), (700, 1, 40)])
+def test_values_a_hundred_binades_apart(lv, ctx, n, new, hq):
+    """Values near 2^-80, and zeros under 2^100 in the last block: in units of 2^-80 the rows are as any other's."""
+    B, d = 16, 128
+    rng = np.random.default_rng(n + hq)
+    last = (n - 1) // B * B
+
+    def change(codes, scales, table):
+        scales[1] *= 2.0**-80
+        scales[1, table[0, last // B]] = 2.0**100
+        _quiet(codes, table, 0, B, last, n)
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, 1, d, change)
+    _check_own_keys(case, 0, n, new, B, hq, 1, d, range(new), unit=2.0**80)
