@@ -443,8 +443,10 @@ lv_status lv_kv_attend(lv_ctx *ctx, const lv_kv_cache *cache, int32_t dtype, int
  * the tokens offsets[s] .. offsets[s+1]-1 of q, k and v (int64[n_seq+1], which
  * may start past 0 and may hold empty sequences; lv_kv_plan's token_offsets).
  * Token t sees the tokens of its own sequence up to itself; o and lse as for
- * lv_kv_attend.  Tokens of no sequence are not written.  Offsets that decrease
- * or leave [0, n_tok] record LV_EDATA (taken as an empty sequence). */
+ * lv_kv_attend, but a weight is rounded to the inputs' type; in f16 one below
+ * 2^-32 of the row's largest counts as zero, and gives NaN under an infinite value.
+ * Tokens of no sequence are not written.  Offsets that decrease or leave [0, n_tok]
+ * record LV_EDATA (taken as an empty sequence). */
 lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                            const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                            int64_t v_stride, int64_t n_tok, const int64_t *offsets, int64_t n_seq, float scale,

@@ -25,8 +25,10 @@
 // The running maximum that a row's weights refer to moves only when the true
 // one is more than 2^8 above it (weights are at most 2^8, sums are fp32): after
 // the first blocks of keys hardly any output is read back to be rescaled.
-// Weights are rounded to the inputs' 16-bit type, as V is; half of a block's
-// weights go to the products while the other half is formed.
+// Weights are rounded to the inputs' 16-bit type, as V is; those of f16 are 2^7 times
+// as large, so that 2^-32 of the largest is the first that is lost (bf16 has fp32's
+// range).  Half of a block's weights go to the products while the other half is
+// formed.
 //
 // Items are handed out by a counter, longest first within a sequence and the
 // longest sequence first (twelve prompts of up to 4,096 tokens: 84 us in the order
@@ -52,6 +54,7 @@ constexpr int kPrThreads = 384;
 constexpr int kPrBlock = 128;   // keys of a block
 constexpr int kSort = 512;      // sequences that are taken longest first
 constexpr float kPrLazy = 8.f;  // growth of the maximum, in powers of two, that weights absorb
+constexpr float kPrExp = 7.f;   // f16 weights are 2^7 at the maximum they refer to, and so up to 2^15
 
 struct PromptArgs {
   AttendArgs a;
@@ -306,6 +309,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   volatile int *stop = &sm.stop;
   // columns: scores of tile 0, of tile 1, outputs of tile 0, of tile 1
   constexpr uint32_t kCols = 128;
+  constexpr float kExp = F16 ? kPrExp : 0.f;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -430,7 +434,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             tmem_store16(to + c, o);
           }
         }
-        const float base = m == -INFINITY ? 0.f : m * sl;
+        const float base = m == -INFINITY ? 0.f : m * sl - kExp;
         const uint64_t sl2 = pair(sl, sl), base2 = pair(-base, -base);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -485,7 +489,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
           store64(op + c, w, p.wide);
         }
       }
-      if (valid && a.lse) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m * sl + log2f(l)) * 0.6931471805599453f;
+      if (valid && a.lse) a.lse[t * a.hq + h] = l == 0.f ? -INFINITY : (m * sl - kExp + log2f(l)) * 0.6931471805599453f;
       // the outputs are read: the next item's first product may write them (p_full says so, after this)
       unsigned again = __ballot_sync(~0u, nan);
       __syncwarp();

@@ -170,3 +170,34 @@ def test_values_a_hundred_binades_apart(lv, ctx, n, new, hq):
 
     case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, 1, d, change)
     _check_own_keys(case, 0, n, new, B, hq, 1, d, range(new), unit=2.0**80)
+
+
+def test_f16_prompt_small_weights(lv, ctx):
+    """Weights of 2^-26 under large values: 2^15 is the largest weight, so that they are held, and an infinity under one
+    is an infinity.
+
+    What is lost of a weight where it is rounded to f16 is half of the least step, 2^-25, where 2^7 stands for the
+    largest: 2^-32 of it, which takes the place of 2^-24 in the bound."""
+    import torch
+    rng = np.random.default_rng(12)
+    T, d, away = 2000, 64, -26 * np.log(2.0)
+    q, k = np.zeros((T, 1, d)), np.zeros((T, 1, d))
+    q[:, 0, 0] = 1.0
+    k[1:, 0, 0] = away + 0.3 * rng.normal(size=T - 1)
+    v = 20_000.0 + 5_000.0 * rng.normal(size=(T, 1, d))
+    v[0] = 0.0
+    v[700, 0, 7] = np.inf
+    q, k, v = (torch.as_tensor(a).half().cuda() for a in (q, k, v))
+    o, lse = torch.empty_like(q), torch.empty(T, 1, device="cuda")
+    lv.lv_prompt_attend(ctx, q, k, v, _t([0, T], "int64"), o, lse=lse, scale=1.0)
+    assert ctx.status() == lv.LV_OK
+    assert torch.isposinf(o[700:, 0, 7]).all() and torch.isfinite(o[:700]).all()
+    k64, v64, o64, l64 = _np(k)[:, 0], _np(v)[:, 0], _np(o)[:, 0], _np(lse)[:, 0]
+    v64[700, 7] = 0.0
+    for t in (0, 1, 50, 699, 700, 1500, T - 1):
+        w = np.exp(k64[:t + 1, 0])
+        want, a = w @ v64[:t + 1] / w.sum(), w @ np.abs(v64[:t + 1]) / w.sum()
+        tol = 2.0**-11 * np.abs(want) + (1.01 * 2.0**-11 + 2.0**-16) * a + 2.0**-32 * np.abs(v64[:t + 1]).sum(0) / w.sum() + 2.0**-24
+        fine = np.arange(d) != 7 if t >= 700 else np.ones(d, bool)
+        ref.close(o64[t, fine], want[fine], tol[fine], f"row {t}")
+        ref.close(l64[t], np.log(w.sum()), 2.0**-18, f"lse {t}")
