@@ -68,7 +68,7 @@ struct ChunkSmem {
   int64_t req[2], from[2];  // of each item: its request, its first block
   int whole[2], slot[2];    // no other CTA has a share of it; where its part goes
   uint32_t tmem;
-  int stop;
+  int stop[3];  // see bar_wait
 };
 
 // Pairs of tiles of a request, and blocks of keys of each, counted alike.
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   wait_previous();
   if (warp == 16) tmem_alloc(&sm.tmem, 512);
   if (threadIdx.x == 0) {
-    sm.stop = 0;
+    sm.stop[0] = sm.stop[1] = sm.stop[2] = 0;
     sm.item[0].head = sm.item[1].head = -1;
     for (int k = 0; k < 2; ++k) {
       bar_init(&sm.q_full[k], 4);
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
   __syncthreads();
   tc_after_sync();
   const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
-  volatile int *stop = &sm.stop;
+  volatile int *stop = sm.stop;
   constexpr uint32_t kCols = 128;
 
   if (warp >= 16) {
@@ -582,20 +582,14 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
       if (!whole) *reinterpret_cast<float2 *>(c.part_ml + 2 * at) = make_float2(m, thin ? -l : l);  // the join does it again
       unsigned again = __ballot_sync(~0u, nan || (thin && whole && valid));
       __syncwarp();
-      while (again) {
-        const int r = __ffs(again) - 1;
-        again &= again - 1;
-        const int rt = __shfl_sync(~0u, tok, r), rh = __shfl_sync(~0u, h, r);
-        const int64_t rl = __shfl_sync(~0u, lim, r);
-        redo_row<D, F16, true>(a, it.first, i, (int64_t)it.first + rt, rh, rl, bound, thin != 0);
-      }
+      if (again) redo_rows<D, F16, true>(a, it.first, i, tok, h, lim, bound, again, thin != 0, stop);
     }
   }
   __syncwarp();
   tc_before_sync();
   __syncthreads();
-  if (sm.stop && threadIdx.x == 0) flag(a.status, kStatusTimeout);
-  if (sm.stop)
+  if (sm.stop[0] && threadIdx.x == 0) flag(a.status, kStatusTimeout);
+  if (sm.stop[0])
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // products that were issued may still read shared memory
   if (bad) flag(a.status, kStatusData);
   __syncthreads();

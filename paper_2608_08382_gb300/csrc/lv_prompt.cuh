@@ -86,7 +86,7 @@ struct PromptSmem {
   int64_t sums[kScan + 1];
   int order[kSort], length[kSort];  // sequences, longest first; a sequence's items
   uint32_t tmem;
-  int stop;
+  int stop[3];  // see bar_wait
 };
 
 // Items of sequence i.
@@ -107,6 +107,23 @@ __global__ void __launch_bounds__(kScan) k_prompt_prefix(PromptArgs p) {
     base = scan_units<kScan>(n, p.prefix + i0, base, [&](int k) { return prompt_items(p, i0 + k, &bad); });
   }
   if (bad) flag(p.a.status, kStatusData);
+}
+
+// The lanes' rows of `again` once more, one after another by the whole warp: token tok
+// of request i, which begins at `first`, head h, on n keys.  A function of its own:
+// inlined, its state takes registers from the loop over blocks.
+template <int D, bool F16, bool PAGED>
+__device__ __noinline__ void redo_rows(const AttendArgs &a, int64_t first, int64_t i, int tok, int h, int64_t n, int64_t bound,
+                                       unsigned again, bool all, volatile int *stop) {
+  slow_begin(stop);
+  while (again) {
+    const int r = __ffs(again) - 1;
+    again &= again - 1;
+    const int rt = __shfl_sync(~0u, tok, r), rh = __shfl_sync(~0u, h, r);
+    const int64_t rn = __shfl_sync(~0u, n, r);
+    redo_row<D, F16, PAGED>(a, first, i, first + rt, rh, rn, bound, all);
+  }
+  slow_end(stop);
 }
 
 // A place in a ring of stages.
@@ -258,7 +275,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     map_ahead(&map_v);
   }
   if (threadIdx.x == 0) {
-    sm.stop = 0;
+    sm.stop[0] = sm.stop[1] = sm.stop[2] = 0;
     sm.item[0].head = sm.item[1].head = -1;
     for (int k = 0; k < 2; ++k) {
       bar_init(&sm.q_full[k], 1);
@@ -306,7 +323,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   __syncthreads();
   tc_after_sync();
   const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
-  volatile int *stop = &sm.stop;
+  volatile int *stop = sm.stop;
   // columns: scores of tile 0, of tile 1, outputs of tile 0, of tile 1
   constexpr uint32_t kCols = 128;
   constexpr float kExp = F16 ? kPrExp : 0.f;
@@ -493,19 +510,13 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       // the outputs are read: the next item's first product may write them (p_full says so, after this)
       unsigned again = __ballot_sync(~0u, nan);
       __syncwarp();
-      while (again) {
-        const int r = __ffs(again) - 1;
-        again &= again - 1;
-        const int rt = __shfl_sync(~0u, tok, r);
-        const int rh = __shfl_sync(~0u, (int)h, r);
-        redo_row<D, F16, false>(a, it.first, 0, (int64_t)it.first + rt, rh, rt + 1, a.n_tok - it.first);
-      }
+      if (again) redo_rows<D, F16, false>(a, it.first, 0, tok, (int)h, tok + 1, a.n_tok - it.first, again, false, stop);
     }
   }
   __syncwarp();
   tc_before_sync();
   __syncthreads();
-  if (sm.stop && threadIdx.x == 0) {
+  if (sm.stop[0] && threadIdx.x == 0) {
     flag(a.status, kStatusTimeout);
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // what was issued may still be at work on shared memory
   }

@@ -31,18 +31,43 @@ __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Waits for the phase of that parity, at most a few seconds.  A wait that runs out
-// sets *stop, and every later one of the block ends at once: the block runs on
-// over whatever is there, takes no further work and says at its end that it is
-// void.  So the way through the code never depends on a wait, whose answer would
-// cost the issuing warp more than the look itself.
+// Waits for the phase of that parity, at most about 3 seconds (1.4 us a try).  A
+// wait that runs out sets stop[0], and every later one of the block ends at once: the
+// block runs on over whatever is there, takes no further work and says at its end
+// that it is void.  So the way through the code never depends on a wait, whose answer
+// would cost the issuing warp more than the look itself.
+//
+// A warp that does rows again alone (redo_row) keeps the others waiting for as long as
+// its rows have keys.  stop[1] counts the warps that are at it, stop[2] those that
+// have been: a wait begins its tries anew while one is, and once after each.
 constexpr int kWaitTries = (1 << 21) - 1;
 __device__ __forceinline__ void bar_wait(uint64_t *bar, uint32_t parity, volatile int *stop) {
   if (bar_try(bar, parity)) return;
+  int been = 0;
 #pragma unroll 1
   for (int k = 0; !bar_try(bar, parity); ++k) {
-    if (k == kWaitTries) *stop = 1;
+    if (k == kWaitTries) {
+      const int at_it = stop[1], now = stop[2];  // in this order: slow_end writes them in the other
+      if (at_it > 0 || now != been) {
+        been = now;
+        k = 0;
+      } else {
+        *stop = 1;
+      }
+    }
     if ((k & 63) == 63 && *stop) return;
+  }
+}
+// Around the rows that a warp does again.
+__device__ __forceinline__ void slow_begin(volatile int *stop) {
+  if ((threadIdx.x & 31) == 0) atomicAdd((int *)stop + 1, 1);
+}
+__device__ __forceinline__ void slow_end(volatile int *stop) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    atomicAdd((int *)stop + 2, 1);
+    __threadfence_block();
+    atomicSub((int *)stop + 1, 1);
   }
 }
 

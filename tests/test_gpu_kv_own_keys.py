@@ -201,3 +201,41 @@ def test_f16_prompt_small_weights(lv, ctx):
         fine = np.arange(d) != 7 if t >= 700 else np.ones(d, bool)
         ref.close(o64[t, fine], want[fine], tol[fine], f"row {t}")
         ref.close(l64[t], np.log(w.sum()), 2.0**-18, f"lse {t}")
+
+
+def test_long_rows_done_again_in_a_prompt(lv, ctx):
+    """127 rows of 150,000 keys each are done again alone, for the last token's value is NaN: the rest of the block
+    waits for longer than its waits would last by themselves, and the call is good."""
+    import torch
+    T, d = 150_016, 64
+    assert (T - 1) % 256 == 255 or T % 256 == 0  # the last tile is whole
+    q = torch.zeros(T, 1, d, device="cuda").bfloat16()
+    k = torch.randn(T, 1, d, device="cuda").bfloat16()
+    v = torch.ones(T, 1, d, device="cuda").bfloat16()
+    v[-1, 0, 3] = float("nan")
+    o, lse = torch.empty_like(q), torch.empty(T, 1, device="cuda")
+    lv.lv_prompt_attend(ctx, q, k, v, _t([0, T], "int64"), o, lse=lse)
+    assert ctx.status() == lv.LV_OK
+    assert torch.all(o[:-1] == 1.0) and torch.isnan(o[-1, 0, 3]) and torch.all(o[-1, 0, 4:] == 1.0)
+    want = torch.log(torch.arange(1, T + 1, device="cuda", dtype=torch.float64))
+    assert float((lse[:, 0] - want).abs().max()) < 1e-4
+
+
+def test_long_rows_done_again_in_a_chunk(lv, ctx):
+    """The same over the cache, where a block has an item of 140,000 keys to itself."""
+    import torch
+    B, h, d, n, new = 128, 160, 64, 140_000, 32
+    nb = -(-n // B)
+    one = torch.full((nb, h, B, d), 0x38, dtype=torch.uint8, device="cuda")  # 1.0
+    value = one.clone()
+    value[nb - 1, :, (n - 1) % B, 3] = 0x7f  # NaN
+    scale = torch.ones(nb, h, device="cuda")
+    cache = lv.KVCache(one, value, scale, scale.clone())
+    q = torch.zeros(new, h, d, device="cuda").bfloat16()
+    o, lse = torch.empty_like(q), torch.empty(new, h, device="cuda")
+    lv.lv_kv_attend(ctx, cache, q, _t([n - new], "int32"), _t(np.arange(nb)[None], "int32"), o, lse=lse,
+                    token_offsets=_t([0, new], "int64"))
+    assert ctx.status() == lv.LV_OK
+    assert torch.all(o[:-1] == 1.0) and torch.isnan(o[-1, :, 3]).all() and torch.all(o[-1, :, 4:] == 1.0)
+    want = torch.log(torch.arange(n - new + 1, n + 1, device="cuda", dtype=torch.float64))
+    assert float((lse - want[:, None]).abs().max()) < 1e-4
