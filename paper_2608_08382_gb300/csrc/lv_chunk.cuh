@@ -176,7 +176,11 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           break;
         }
         bool ignore = false;
-        for (int64_t more; u >= before + (more = chunk_units(c, i, &ignore)); ++i) before += more;
+        if (c.given) {  // among many requests looked for, not walked to: the others' waits are bounded
+          if (u >= sums[i + 1]) i = find_unit(sums, a.n_req, u), before = sums[i];
+        } else {
+          for (int64_t more; u >= before + (more = chunk_units(c, i, &ignore)); ++i) before += more;
+        }
         const Span sp = request_span(a, i, &ignore);
         const int64_t blocks = chunk_blocks(c, sp), local = u - before, seg = local / blocks;
         const int64_t b0 = local % blocks, b1 = min(blocks, b0 + end - u);

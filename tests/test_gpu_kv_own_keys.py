@@ -239,3 +239,34 @@ def test_long_rows_done_again_in_a_chunk(lv, ctx):
     assert torch.all(o[:-1] == 1.0) and torch.isnan(o[-1, :, 3]).all() and torch.all(o[-1, :, 4:] == 1.0)
     want = torch.log(torch.arange(n - new + 1, n + 1, device="cuda", dtype=torch.float64))
     assert float((lse - want[:, None]).abs().max()) < 1e-4
+
+
+def test_chunks_far_apart_in_a_call(lv, ctx):
+    """400,000 requests without a new token between two chunks: the block whose share has the end of one and the
+    beginning of the other finds it without a walk over those between, which would outlast its waits at a few millions."""
+    import torch
+    n, B, hq, d, new, ctx_len = 400_000, 16, 4, 64, 40, 40_000
+    rng = np.random.default_rng(13)
+    total = ctx_len + new
+    codes, scales, few = _cached(rng, np.array([total, total]), B, 1, d)
+    table = torch.full((n, few.shape[1]), -1, dtype=torch.int32, device="cuda")
+    table[0], table[-1] = _t(few[0], "int32"), _t(few[1], "int32")
+    c = torch.zeros(n, dtype=torch.int32, device="cuda")
+    c[0] = c[-1] = ctx_len
+    X = torch.full((n + 1,), new, dtype=torch.int64, device="cuda")
+    X[0], X[-1] = 0, 2 * new
+    q = torch.as_tensor(rng.normal(size=(2 * new, hq, d))).bfloat16().cuda()
+    o, lse = torch.empty_like(q), torch.empty(2 * new, hq, device="cuda")
+    cache = lv.KVCache(*(_t(a, "uint8") for a in codes), *(_t(a, "float32") for a in scales))
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    for _ in range(2):
+        begin.record()
+        lv.lv_kv_attend(ctx, cache, q, c, table, o, lse=lse, token_offsets=X)
+        end.record()
+    assert ctx.status() == lv.LV_OK
+    for i in range(2):
+        rows = slice(i * new, (i + 1) * new)
+        seen = np.arange(total)[None, :] <= (ctx_len + np.arange(new))[:, None]
+        _check_rows(_np(o[rows]), _np(lse[rows]), _np(q[rows]), _gather(codes, scales, few, i, total, B), seen, d ** -0.5,
+                    "bf16", hq, 1, f"request {i}")
+    assert begin.elapsed_time(end) < 50.0, begin.elapsed_time(end)
