@@ -5,7 +5,8 @@
 A small engine's loop: prompts arrive and are attended to whole, their keys and values appended to a paged 8-bit cache;
 between arrivals every running sequence takes a token, and now and then one of them a chunk of 200 more.  Each step is a
 plan (lv_kv_plan), the append (lv_kv_store) and the attention (lv_prompt_attend for prompts on an empty cache, else
-lv_kv_attend), timed with CUDA events.  The steps' requests and times are then what the library takes as profiled
+lv_kv_attend), timed with CUDA events.  As in an engine the GPU is at other work while a step's calls are issued, so the
+times are the GPU's and not those of the Python calls, and that work leaves nothing of the cache in L2.  The steps' requests and times are then what the library takes as profiled
 batches: lv_fit gives the coefficients of Eq. 1, lv_accuracy says how well they explain the times, lv_attribute shares
 the predicted times out to the requests.  One layer, random inputs.
 """
@@ -27,19 +28,20 @@ BLOCK = 16
 class Engine:
     """The cache, the block tables and the running sequences of one layer's attention."""
 
-    def __init__(self, layout, n_blocks, max_seqs, max_len, seed):
+    def __init__(self, layout, n_blocks, max_seqs, max_len, seed, ctx=None):
         import torch
 
         import paper_2608_08382_gb300 as lv
         self.lv, self.torch = lv, torch
         self.hq, self.hkv, self.d = LAYOUTS[layout]
-        self.ctx = lv.Context()
+        self.ctx = ctx or lv.Context()
         self.cache = lv.KVCache.empty(n_blocks, self.hkv, BLOCK, self.d)
         self.free = torch.randperm(n_blocks, device="cuda").int()
         self.used = 0
         self.table = torch.full((max_seqs, -(-max_len // BLOCK)), -1, dtype=torch.int32, device="cuda")
         self.lens = np.zeros(0, np.int64)  # tokens in the cache, of each running sequence
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.other = torch.empty(2 << 30, dtype=torch.uint8, device="cuda")  # what other work writes, a third of a millisecond
 
     def step(self, first, p):
         """Runs sequences first, first + 1, .. with p new tokens each; returns c, the step's outputs and its milliseconds."""
@@ -57,6 +59,7 @@ class Engine:
         counts = torch.empty(2, dtype=torch.int64, device="cuda")
         table = self.table[first:first + n]
         begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        self.other.zero_()
         begin.record()
         lv.lv_kv_plan(self.ctx, d_p, d_c, BLOCK, self.free[self.used:], table, offsets, slots, counts)
         lv.lv_kv_store(self.ctx, self.cache, k, v, slots)
@@ -78,10 +81,14 @@ class Engine:
 def profile(layout="8b-tp1", steps=240, seed=1, max_seqs=192, most=3000):
     """Runs the loop; returns the profiled batches (p, c, phase, tenant, offsets), their latencies in seconds, and the engine."""
     rng = np.random.default_rng(seed)
-    warm = Engine(layout, 2048, 8, 4000, seed)
-    for first, p in ((0, [700, 40]), (0, [1, 1]), (0, [1, 50])):
-        warm.step(first, np.array(p))
-    e = Engine(layout, max_seqs * (most + steps * 8) // BLOCK, max_seqs, most + steps * 210, seed)
+    # a step of each kind with as many sequences as there will be: the context has its scratch and its kernels then
+    warm = Engine(layout, 3 * max_seqs + 200, max_seqs, 1000, seed)
+    for longest in (700, 1, 200):
+        p = np.ones(max_seqs, np.int64)
+        p[0] = longest
+        warm.step(0, p)
+    e = Engine(layout, max_seqs * (most + steps * 8) // BLOCK, max_seqs, most + steps * 210, seed, warm.ctx)
+    del warm
     rows, sizes, y = [], [], []
     for s in range(steps):
         n = len(e.lens)
