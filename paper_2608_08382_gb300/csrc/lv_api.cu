@@ -855,7 +855,6 @@ lv_status lv_ctx_create(lv_ctx **out) {
     lv_ctx_destroy(ctx);
     return LV_ECUDA;
   }
-  ctx->kv.device = ctx->device;
   ctx->kv.sms = ctx->sms;
   ctx->kv.d_status = ctx->d_status;
   *out = ctx;

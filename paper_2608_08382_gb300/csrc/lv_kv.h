@@ -9,7 +9,6 @@
 namespace lv {
 
 struct KvHost {
-  int device = 0;
   int sms = 0;
   int *d_status = nullptr;           // the context's status word
   unsigned char *scratch = nullptr;  // owned

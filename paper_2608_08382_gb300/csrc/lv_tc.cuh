@@ -155,13 +155,6 @@ __host__ __device__ constexpr uint32_t tc_idesc(int m, int n, bool f16, bool neg
       "=r"(r[o + 19]), "=r"(r[o + 20]), "=r"(r[o + 21]), "=r"(r[o + 22]), "=r"(r[o + 23]), "=r"(r[o + 24]),           \
       "=r"(r[o + 25]), "=r"(r[o + 26]), "=r"(r[o + 27]), "=r"(r[o + 28]), "=r"(r[o + 29]), "=r"(r[o + 30]),           \
       "=r"(r[o + 31])
-#define LV_I32(r, o)                                                                                                  \
-  "r"(r[o + 0]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]),            \
-      "r"(r[o + 7]), "r"(r[o + 8]), "r"(r[o + 9]), "r"(r[o + 10]), "r"(r[o + 11]), "r"(r[o + 12]), "r"(r[o + 13]),    \
-      "r"(r[o + 14]), "r"(r[o + 15]), "r"(r[o + 16]), "r"(r[o + 17]), "r"(r[o + 18]), "r"(r[o + 19]),                 \
-      "r"(r[o + 20]), "r"(r[o + 21]), "r"(r[o + 22]), "r"(r[o + 23]), "r"(r[o + 24]), "r"(r[o + 25]),                 \
-      "r"(r[o + 26]), "r"(r[o + 27]), "r"(r[o + 28]), "r"(r[o + 29]), "r"(r[o + 30]), "r"(r[o + 31])
-
 // 32 columns of the warp's 32 rows of tensor memory, a row a lane.
 __device__ __forceinline__ void tmem_load32(uint32_t *r, uint32_t at) {
   asm volatile(
@@ -170,14 +163,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t *r, uint32_t at) {
       "[%32];"
       : LV_R32(r, 0)
       : "r"(at));
-}
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::
-          LV_I32(r, 0),
-      "r"(at)
-      : "memory");
 }
 __device__ __forceinline__ void tmem_load16(uint32_t *r, uint32_t at) {
   asm volatile(
