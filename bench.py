@@ -48,7 +48,8 @@ ROOT = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, ROOT)
 
 METRIC = "attributed requests/sec on 1 GB300; achieved HBM GB/s vs ~8 TB/s peak"
-KERNEL_SOURCES = ["paper_2608_08382_gb300/csrc/lv_kernels.cuh", "paper_2608_08382_gb300/csrc/lv_fixed.cuh",
+KERNEL_SOURCES = ["paper_2608_08382_gb300/csrc/lv_base.cuh", "paper_2608_08382_gb300/csrc/lv_kernels.cuh",
+                  "paper_2608_08382_gb300/csrc/lv_fixed.cuh",
                   "paper_2608_08382_gb300/csrc/lv_api.cu", "paper_2608_08382_gb300/csrc/lv_fit.cuh",
                   "paper_2608_08382_gb300/csrc/lv_whatif.cuh", "paper_2608_08382_gb300/csrc/lv_step.cuh",
                   "paper_2608_08382_gb300/csrc/lv_tile.cuh", "paper_2608_08382_gb300/csrc/lv_tenant.cuh",

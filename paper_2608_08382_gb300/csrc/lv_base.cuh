@@ -1,15 +1,15 @@
-// What the attention kernels share with the others: the bits of the status word and
-// programmatic dependent launch.  The same lines stand in lv_kernels.cuh, whose
-// text the committed counter summaries are tied to; lv_kv.cu does not include it.
+// What all kernels share: the bits of the status word and programmatic dependent
+// launch.
 #pragma once
 
 #include <cstdint>
 
 namespace lv {
 
-// Bits of the sticky status word.
-constexpr int kStatusData = 1;     // invalid input data
-constexpr int kStatusTimeout = 8;  // a bounded wait inside a kernel ran out
+// Bits of the sticky status word (bit 2 is reserved).
+constexpr int kStatusData = 1;      // invalid input data
+constexpr int kStatusOverflow = 4;  // a fit feature beyond the exact range
+constexpr int kStatusTimeout = 8;   // a bounded wait inside a kernel ran out
 
 // Programmatic dependent launch.  A kernel launched so (launch_after in the host
 // code) may start while the one before it in the stream still runs: it waits

@@ -7,6 +7,7 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "lv_base.cuh"
 #include "lv_fixed.cuh"
 
 namespace lv {
@@ -14,12 +15,6 @@ namespace lv {
 constexpr int kHotMax = 512;                       // tenants kept in shared memory per CTA
 constexpr int64_t kPMaxFix = 1ll << 24;            // p beyond this uses the fp64 share path
 constexpr int kTenLsb = -72;                       // tenant totals: shares rounded to 2^-72 s, summed exactly
-
-// Bits of the sticky status word: invalid input data; a fit feature beyond
-// the exact range (bit 2 is reserved).
-constexpr int kStatusData = 1;
-constexpr int kStatusOverflow = 4;
-constexpr int kStatusTimeout = 8;  // a bounded wait inside a kernel ran out
 
 struct SegFix {
   i128 A1, A2, A3;   // exact a_k * 2^-E
@@ -114,17 +109,6 @@ struct TileArgs {
   int *status;
   ModelP mp;
 };
-
-// Programmatic dependent launch.  A kernel launched so (launch_after in the host
-// code) may start while the one before it in the stream still runs: it waits
-// here before it reads or writes anything that one does.  The other, early in
-// its run, lets it be launched.
-__device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
-__device__ __forceinline__ void flag(int *status, int bit) {
-  if (status) atomicOr(status, bit);
-}
 
 __device__ __forceinline__ int64_t clampi(int64_t v, int64_t lo, int64_t hi) {
   return v < lo ? lo : (v > hi ? hi : v);
