@@ -10,7 +10,8 @@
 // scores, its value scale vs, as vs / ref, to its weights.  ref follows the
 // largest vs of the strips that the row sees, once that is past 2^3 ref, as the
 // weights' maximum follows the true one past 2^8: a weight is at most 2^(8 + 4 + 3)
-// then.
+// then.  Rows of an item whose value scales differ by more than 2^14 are done again
+// in fp32, each by a warp (kChThin).
 //
 // The blocks of keys of all items stand in one line and every CTA takes an even
 // share of it, so a few long contexts keep every SM busy; an item that several
@@ -21,7 +22,7 @@
 // two blocks ahead, and brings the scales.
 //
 // Measured: six chunks of 512 tokens on contexts of up to 32,256, 20/4 heads of 128,
-// 497 GFLOP: 502 us with the join, 990 TFLOP/s, 0.52 of the measured rate.  A block
+// 497 GFLOP: 520 us with the join, 955 TFLOP/s, 0.50 of the measured rate.  A block
 // of both tiles takes 4,000 clocks, the products 2,048 of them; shared memory moves
 // 320 KB in that time (2,500 clocks at its rate), and a tile's softmax has the
 // converting warps beside it on the SM.

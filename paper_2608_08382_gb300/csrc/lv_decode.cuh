@@ -22,8 +22,10 @@
 // so m settles after a few strips.  The value scale vs of the strip's block goes
 // to the weight, as vs / ref with ref the largest so far; the factor 2^12 keeps
 // weights of 2^-26 of the largest normal in fp16, to which they are rounded (11
-// bits).  bf16 queries are scaled by a power of two to a largest element of 2^14,
-// where fp16 holds every one above 2^-28 of that exactly.  All sums are fp32.
+// bits); a segment whose value scales differ by more than 2^22 is done again row by
+// row in fp32 (kDecThin).  bf16 queries are scaled by a power of two to a largest
+// element of 2^14, where fp16 holds every one above 2^-28 of that exactly.  All sums
+// are fp32.
 //
 // Work is cut evenly whatever the lengths: the strips of all (request, head, row
 // tile) segments stand in one line, and each of W warps takes its W-th of it.  A
@@ -31,7 +33,7 @@
 // at most, and k_attend_join adds them in the line's order.
 //
 // Measured: 256 requests of up to 32,768 tokens, 20/4 heads of 128, 950 MB of
-// cache: 183 us with the join, 5.2 TB/s, 0.77 of the copy rate; 16 requests of up
+// cache: 181 us with the join, 5.3 TB/s, 0.78 of the copy rate; 16 requests of up
 // to 8,192 tokens, 32/8 heads: 41 us.  What is lost: the SMs are served by memory
 // at different speeds (equal shares end between 113 and 189 us), and small calls
 // wait for the scan, the first loads and the join.
@@ -42,7 +44,7 @@
 namespace lv {
 
 // CTAs of an SM, with one and two row tiles of 8: with four the registers of one
-// row tile just spill (256 requests: 183 us, three CTAs 196, five 263).
+// row tile just spill (256 requests, as this was chosen: 183 us, three CTAs 196, five 263).
 constexpr int kDecCtas1 = 4, kDecCtas2 = 2;
 constexpr int kDecWarps = 4;       // warps of a CTA; they share only the scan
 constexpr int kDecSegment = 4;     // strips' time that a segment's beginning and end cost (0: 6 % slower)

@@ -34,9 +34,9 @@
 // longest sequence first (twelve prompts of up to 4,096 tokens: 84 us in the order
 // that they came), and the loads run ahead of the products across items.
 //
-// Measured: one prompt of 8,192 tokens, 20/4 heads of 128, bf16: 231 us, 1,490
-// TFLOP/s (0.78 of the measured rate); two of 25,001 tokens in all, 10/2 heads, fp16:
-// 549 us; twelve of 8,005 tokens in all, 32/8 heads: 71 us, of which an item's
+// Measured: one prompt of 8,192 tokens, 20/4 heads of 128, bf16: 224 us, 1,530
+// TFLOP/s (0.80 of the measured rate); two of 25,001 tokens in all, 10/2 heads, fp16:
+// 540 us; twelve of 8,005 tokens in all, 32/8 heads: 73 us, of which an item's
 // beginning and its stores are a third.  A block of both tiles takes 3,000 clocks,
 // the products 2,048: a tile's softmax (1,500) and its two products (1,024) follow
 // each other, and with both tiles' scores and outputs tensor memory is full, so the
