@@ -37,6 +37,8 @@ struct AttendArgs {
 // of the largest weight a row is done again alone (redo_row).  A scale of at most
 // kLeastScale, the least that an append sets and so a block of zeros, brings nothing.
 constexpr float kLeastScale = 0x1p-100f;
+// ref is never below the normal range, where its reciprocal could be infinite.
+constexpr float kLeastRef = 0x1p-126f;
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;

@@ -489,15 +489,15 @@ __global__ void __launch_bounds__(kChThreads, 1) k_chunk(const __grid_constant__
           const bool grow_ref = !(top_vs <= kChRef * ref);
           if (j == 0) {
             m = top;
-            ref = top_vs;
-            inv_ref = ref > 0.f ? 1.f / ref : 0.f;
+            ref = fmaxf(top_vs, kLeastRef);
+            inv_ref = 1.f / ref;
           } else if (__any_sync(~0u, top - m > kPrLazy || grow_ref)) {
             const float up = m == -INFINITY ? 1.f : exp2_fast(m - top);
             m = top;
             l *= up;
-            const float nref = fmaxf(ref, top_vs), shrink = ref > 0.f ? up * (ref / nref) : up;
+            const float nref = fmaxf(ref, top_vs), shrink = up * (ref / nref);
             ref = nref;
-            inv_ref = ref > 0.f ? 1.f / ref : 0.f;
+            inv_ref = 1.f / ref;
 #pragma unroll 1
             for (int x = 0; x < D; x += 16) {
               uint32_t o[16];

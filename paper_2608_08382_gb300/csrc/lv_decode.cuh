@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
     least = min(least, __shfl_xor_sync(~0u, least, 1));
     least = min(least, __shfl_xor_sync(~0u, least, 2));
 
-    float o[NT][kM][4], m[NT][2], l[NT][2], ref = 0.f, inv_ref = 0.f;
+    float o[NT][kM][4], m[NT][2], l[NT][2], ref = kLeastRef, inv_ref = 1.f / kLeastRef;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -418,9 +418,9 @@ __global__ void __launch_bounds__(kDecWarps * 32, NT == 1 ? kDecCtas1 : kDecCtas
           grow |= fmaxf(c[nt][r], c[nt][2 + r]) > m[nt][r];
         }
       if (__any_sync(~0u, grow)) {
-        const float nref = fmaxf(ref, fabsf(vss)), shrink = ref > 0.f ? ref / nref : 1.f;
+        const float nref = fmaxf(ref, fabsf(vss)), shrink = ref / nref;
         ref = nref;
-        inv_ref = nref > 0.f ? 1.f / nref : 0.f;
+        inv_ref = 1.f / nref;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -270,3 +270,22 @@ def test_chunks_far_apart_in_a_call(lv, ctx):
         _check_rows(_np(o[rows]), _np(lse[rows]), _np(q[rows]), _gather(codes, scales, few, i, total, B), seen, d ** -0.5,
                     "bf16", hq, 1, f"request {i}")
     assert begin.elapsed_time(end) < 50.0, begin.elapsed_time(end)
+
+
+@pytest.mark.parametrize("n, new, hq", [(300, 1, 4), (300, 1, 10), (20_000, 1, 4), (300, 40, 4), (300, 3, 4)])
+def test_value_scales_below_the_normal_range(lv, ctx, n, new, hq):
+    """Value scales that have no reciprocal in fp32: their values are as good as zero, not infinite."""
+    B, d = 16, 128
+    rng = np.random.default_rng(n + new)
+
+    def tiny(codes, scales, table):
+        scales[1] = 1e-39
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, 1, d, tiny)
+    assert np.isfinite(case[2]).all() and np.abs(case[2]).max() <= 449 * 1e-39
+
+    def some(codes, scales, table):
+        scales[1, table[0, ::3][table[0, ::3] < len(codes[0])]] = 1e-42
+
+    case = _chunk_case(lv, ctx, rng, [n], [new], B, hq, 1, d, some)
+    _check_own_keys(case, 0, n, new, B, hq, 1, d, range(new))
