@@ -434,13 +434,19 @@ def _rows(x, where):
     return st[0] if x.shape[0] > 1 else x.shape[1] * x.shape[2]
 
 
+def _sizes(x, dims, where):
+    """The sizes of a tensor of that many dimensions."""
+    _want(len(x.shape) == dims, where)
+    return x.shape
+
+
 class KVCache:
     """A paged key/value cache in e4m3: uint8 codes k, v [n_blocks][n_kv_heads][block_tokens][head_dim] and float32
     scales [n_blocks][n_kv_heads], all contiguous CUDA tensors, which it keeps."""
 
     def __init__(self, k, v, k_scale, v_scale):
         t = _dtypes or _types()
-        n, h, b, d = k.shape
+        n, h, b, d = _sizes(k, 4, "KVCache")
         _want(k.dtype == v.dtype == t["u8"] and v.shape == k.shape and k.is_contiguous() and v.is_contiguous()
               and k_scale.dtype == v_scale.dtype == t["f32"] and k_scale.shape == v_scale.shape == (n, h)
               and k_scale.is_contiguous() and v_scale.is_contiguous(), "KVCache")
@@ -474,7 +480,7 @@ def lv_kv_plan(ctx: Context, p, c, block_tokens: int, free_blocks, table, token_
 def lv_kv_store(ctx: Context, cache: KVCache, k, v, slots, stream=None):
     """Appends k, v [n_tok][n_kv_heads][head_dim] (slices of a wider tensor may be given) to the cache."""
     t = _dtypes or _types()
-    s, n = cache.s, k.shape[0]
+    s, n = cache.s, _sizes(k, 3, "lv_kv_store")[0]
     _want(k.dtype == v.dtype and k.dtype in t and k.shape == v.shape == (n, s.n_kv_heads, s.head_dim)
           and slots.dtype == t["i64"] and slots.numel() == n and slots.is_contiguous(), "lv_kv_store")
     _check(_lib.lv_kv_store(ctx.h, ctypes.byref(s), t[k.dtype], k.data_ptr(), _rows(k, "lv_kv_store"), v.data_ptr(),
@@ -484,7 +490,7 @@ def lv_kv_store(ctx: Context, cache: KVCache, k, v, slots, stream=None):
 def lv_kv_attend(ctx: Context, cache: KVCache, q, c, table, o, lse=None, token_offsets=None, scale=None, stream=None):
     """Attention of queries q [n_tok][n_q_heads][head_dim] over the cache into o (and lse); scale None: 1/sqrt(head_dim)."""
     t = _dtypes or _types()
-    s, n, (n_tok, hq, d) = cache.s, c.numel(), q.shape
+    s, n, (n_tok, hq, d) = cache.s, c.numel(), _sizes(q, 3, "lv_kv_attend")
     _want(q.dtype in t and d == s.head_dim and o.dtype == q.dtype and o.shape == q.shape and o.is_contiguous()
           and c.dtype == table.dtype == t["i32"] and c.is_contiguous() and table.dim() == 2 and table.shape[0] == n
           and table.is_contiguous()
@@ -501,7 +507,7 @@ def lv_prompt_attend(ctx: Context, q, k, v, offsets, o, lse=None, scale=None, st
     """Causal attention over packed prompts: q [n_tok][n_q_heads][head_dim], k and v [n_tok][n_kv_heads][head_dim] (slices
     of a wider tensor may be given), int64 offsets [n_seq + 1]; scale None: 1/sqrt(head_dim)."""
     t = _dtypes or _types()
-    (n_tok, hq, d), hkv = q.shape, k.shape[1]
+    (n_tok, hq, d), (_, hkv, _) = _sizes(q, 3, "lv_prompt_attend"), _sizes(k, 3, "lv_prompt_attend")
     _want(q.dtype in t and k.dtype == v.dtype == o.dtype == q.dtype and k.shape == v.shape == (n_tok, hkv, d)
           and o.shape == q.shape and o.is_contiguous() and offsets.dtype == t["i64"] and offsets.numel() >= 1
           and offsets.is_contiguous()
