@@ -357,8 +357,9 @@ lv_status lv_whatif_admit(lv_ctx *ctx, const lv_model *model, const lv_batches *
  * token side by side; *_stride is the distance between tokens in elements (a
  * multiple of 8, at least n_heads * head_dim), so that they may be slices of one
  * projection's output; base pointers are 16-byte aligned; a call has at most 2^30
- * tokens and 2^24 requests.  Others: LV_EINVAL.  Waits inside their kernels are
- * bounded; one that runs out records LV_ETIMEOUT, and the call's outputs are void. */
+ * tokens and 2^24 requests.  Others: LV_EINVAL.  Outputs must not overlap inputs.
+ * Waits inside their kernels are bounded; one that runs out records LV_ETIMEOUT, and
+ * the call's outputs are void. */
 #define LV_BF16 0
 #define LV_F16 1
 #define LV_MAX_GROUP 64
