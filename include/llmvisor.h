@@ -47,7 +47,8 @@
  *  - CUDA graphs: lv_features, lv_batch_latency, lv_attribute,
  *    lv_attribute_step, lv_tenant_acc_reset, lv_tenant_accumulate,
  *    lv_tenant_totals, lv_whatif, lv_whatif_admit, lv_kv_plan, lv_kv_store,
- *    lv_kv_attend and lv_prompt_attend may be captured into a CUDA graph once an uncaptured call with
+ *    lv_kv_attend, lv_prompt_attend, lv_linear, lv_gated_linear, lv_qk_rotate and
+ *    lv_token_logprobs may be captured into a CUDA graph once an uncaptured call with
  *    the same context, model and sizes has run (it creates the context's
  *    buffers and caches the kernel configuration; a capture never allocates).
  *    The context's ordering events are then recorded and waited for by the
@@ -73,7 +74,7 @@ typedef int32_t lv_status;
 #define LV_ECUDA (-5)      /* a CUDA runtime call failed */
 #define LV_EDATA (-6)      /* invalid input data seen on the device (sticky) */
 #define LV_ENOMEM (-7)     /* device allocation failed */
-#define LV_ETIMEOUT (-8)   /* a bounded wait inside a kernel ran out (lv_accuracy, or lv_ctx_status after a serving-step or attention launch) */
+#define LV_ETIMEOUT (-8)   /* a bounded wait inside a kernel ran out (lv_accuracy, or lv_ctx_status after a serving-step, attention or product launch) */
 
 /* Model architecture; integers only.  tp is the modelled tensor-parallel degree
  * (an arithmetic input: constants are per rank).  kv_bytes is the KV-cache
@@ -152,7 +153,7 @@ lv_status lv_ctx_set_arith(lv_ctx *ctx, int32_t mode);
  * (LV_OK; LV_EDATA when a kernel met invalid input data since the last query;
  * LV_ETIMEOUT when a bounded wait inside the serving-step kernel of
  * lv_attribute / lv_attribute_step or a kernel of lv_kv_attend /
- * lv_prompt_attend ran out, which takes precedence). */
+ * lv_prompt_attend / lv_linear / lv_gated_linear ran out, which takes precedence). */
 lv_status lv_ctx_status(lv_ctx *ctx, void *stream);
 /* Static description of a status code. */
 const char *lv_status_string(lv_status s);
@@ -452,6 +453,102 @@ lv_status lv_prompt_attend(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_
                            const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                            int64_t v_stride, int64_t n_tok, const int64_t *offsets, int64_t n_seq, float scale,
                            void *o, float *lse, void *stream);
+
+/* --------------------------------------------- a step's work for each new token
+ *
+ * The third term that the model explains, sum p, is the work that a step does for
+ * each of its new tokens whatever their context: the products with the layers'
+ * weights (phi[0] of lv_arch_constants) and what stands around them.  With the calls
+ * below a step's batches can be run and timed whole: lv_linear for the projections,
+ * lv_gated_linear for the first half of a gated feed-forward block, lv_qk_rotate
+ * between a projection and lv_kv_store / lv_kv_attend / lv_prompt_attend,
+ * lv_token_logprobs after the last product.  They serve; nothing here trains, and
+ * there is no backward pass.  As above, elements are of one 16-bit type per call
+ * (logits may be LV_F32), a stride is the distance between rows in elements, and a
+ * call has at most 2^30 tokens; rows of x, w, y, residual, q and k begin at 16-byte
+ * boundaries (their strides are multiples of 8), bias and norm weights are aligned to
+ * their type.  What is past a row's width is neither read nor written.  Outputs must
+ * not overlap inputs, but residual may be y, q_out q and k_out k, with one stride.
+ * Sums, norms, angles and softmax statistics are held in 32 bits or more, and an
+ * output is rounded once.  Waits inside their kernels are bounded (LV_ETIMEOUT). */
+#define LV_F32 2  /* a type of lv_token_logprobs's logits */
+#define LV_ACT_NONE 0
+#define LV_ACT_SILU 1       /* x / (1 + exp(-x)) */
+#define LV_ACT_GELU 2       /* x/2 (1 + erf(x / sqrt 2)) */
+#define LV_ACT_GELU_TANH 3  /* x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
+#define LV_ACT_RELU 4       /* max(x, 0); a NaN stays one */
+
+/* A product with a layer's weights and what follows it:
+ *   y[t][o] = act(sum_i x[t][i] w[o][i] + bias[o]) + residual[t][o]
+ * for x[n_tok][d_in], w[d_out][d_in] (a row for each output), bias[d_out] or NULL,
+ * residual[n_tok][d_out] or NULL, y[n_tok][d_out].  Sizes are any from 1 to 2^24
+ * (n_tok from 0). */
+lv_status lv_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride, int64_t n_tok, const void *w,
+                    int64_t w_stride, int32_t d_in, int32_t d_out, const void *bias, int32_t act,
+                    const void *residual, int64_t residual_stride, void *y, int64_t y_stride, void *stream);
+
+/* The first half of a gated feed-forward block, both products, the activation and
+ * the gate in one pass:
+ *   y[t][o] = act(sum_i x[t][i] w_gate[o][i] + bias_gate[o]) * (sum_i x[t][i] w_up[o][i] + bias_up[o]).
+ * The two weight arrays have one stride and may be halves of one; either bias may be
+ * NULL.  The block's second half is lv_linear, with the residual stream as its
+ * residual.  Sizes as for lv_linear. */
+lv_status lv_gated_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride, int64_t n_tok,
+                          const void *w_gate, const void *w_up, int64_t w_stride, int32_t d_in, int32_t d_out,
+                          const void *bias_gate, const void *bias_up, int32_t act, void *y, int64_t y_stride,
+                          void *stream);
+
+/* How positions turn queries and keys (HOST memory, copied at the call): the first
+ * `dim` elements of a head are dim/2 pairs, and pair j of a token at position n is
+ * turned by the angle n * freq[j] (radians; finite, at most 8 in magnitude).  dim is a
+ * multiple of 16 up to head_dim, 0 for none.  LV_ROPE_HALVES pairs element j with
+ * element j + dim/2, LV_ROPE_NEIGHBOURS element 2j with 2j + 1. */
+#define LV_ROPE_HALVES 0
+#define LV_ROPE_NEIGHBOURS 1
+typedef struct {
+    int32_t dim, order;
+    double freq[64];
+} lv_rope;
+
+/* The norm of every query and key head, and their rotation, in one pass: with
+ * x' = x / sqrt(mean of x^2 over the head + eps) * weight  (x' = x where weight is NULL),
+ *   (a, b) -> (a cos - b sin, a sin + b cos)
+ * for the pairs of x', the other elements as they are.  Heads, head_dim and strides
+ * are as for the attention calls (q_out and k_out have strides of their own), weights
+ * [head_dim] are of the call's type.  Positions are those that lv_kv_attend gives its
+ * queries: new token j of request i, at token_offsets[i] + j, stands at c[i] + j, or at
+ * j where c is NULL (lv_prompt_attend's); where token_offsets is NULL request i has
+ * the one token i (n_tok = n_req).  Angles are reduced exactly: they are good to
+ * 2^-52 of n * freq[j] and a few 2^-24.  Tokens of no request are not written.  A
+ * negative c (taken as 0) and offsets that decrease or leave [0, n_tok] (the outputs
+ * are then void) record LV_EDATA.  Squares whose sum leaves fp32's range are summed
+ * again at a scale that fits. */
+lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                       const void *q, int64_t q_stride, const void *k, int64_t k_stride, int64_t n_tok,
+                       const int64_t *token_offsets, const int32_t *c, int64_t n_req, const void *q_weight,
+                       const void *k_weight, float eps, const lv_rope *rope, void *q_out, int64_t q_out_stride,
+                       void *k_out, int64_t k_out_stride, void *stream);
+
+/* Log probabilities of given tokens and what their distributions look like.  For
+ * each row x[vocab] of logits (of LV_BF16, LV_F16 or LV_F32, aligned to their type, any
+ * stride of at least vocab; vocab 1 to 2^24):
+ *   lse[t] = log sum_v exp x_v,  logp[t] = x_{ids[t]} - lse[t],
+ *   entropy[t] = -sum_v p_v log p_v  (p = exp(x - lse), 0 log 0 = 0),
+ *   top_ids[t][k], top_logp[t][k]: the n_top largest logits, largest first, of equal
+ *                  ones the lowest index first (0 <= n_top <= LV_MAX_TOP); past the
+ *                  vocabulary's end -1 and -inf.
+ * lse, logp, entropy and top_logp are float, ids and top_ids int32; lse, logp and
+ * entropy may be NULL, ids only where logp is, top_ids and top_logp where n_top is 0.
+ * An id outside [0, vocab) gives NaN and, unless it is -1 (no token given), records
+ * LV_EDATA.  A row of -inf alone has no distribution: its lse, logp and top_logp are
+ * -inf, its entropy 0.  A row with a NaN gives NaN throughout, with one or more +inf
+ * an lse of +inf, an entropy of NaN, and a log probability of NaN where the logit is
+ * +inf and -inf elsewhere; among the largest a NaN stands above +inf, and the two
+ * zeros are equal. */
+#define LV_MAX_TOP 32
+lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int64_t stride, int64_t n_tok,
+                            int32_t vocab, const int32_t *ids, float *logp, float *entropy, float *lse,
+                            int32_t n_top, int32_t *top_ids, float *top_logp, void *stream);
 
 /* Attribution without any allocation (the paper has no counterpart; this is a
  * service to callers that cannot allocate device memory at call time).  A

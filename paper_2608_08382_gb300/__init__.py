@@ -24,8 +24,11 @@ LV_OK, LV_EINVAL, LV_EOVERFLOW, LV_ENODATA, LV_ESINGULAR, LV_ECUDA, LV_EDATA, LV
 LV_ARITH_AUTO, LV_ARITH_FP64 = 0, 1
 LV_TIME_TILES, LV_TIME_PAIRS = 1, 2
 LV_STEP_RESET = 1
-LV_BF16, LV_F16 = 0, 1
+LV_BF16, LV_F16, LV_F32 = 0, 1, 2
 LV_MAX_GROUP = 64
+LV_ACT_NONE, LV_ACT_SILU, LV_ACT_GELU, LV_ACT_GELU_TANH, LV_ACT_RELU = range(5)
+LV_ROPE_HALVES, LV_ROPE_NEIGHBOURS = 0, 1
+LV_MAX_TOP = 32
 
 EXPORTED = [
     "lv_status_string", "lv_arch_constants", "lv_ctx_create", "lv_ctx_destroy", "lv_ctx_set_arith", "lv_ctx_status",
@@ -35,6 +38,7 @@ EXPORTED = [
     "lv_tenant_acc_reset", "lv_tenant_accumulate", "lv_tenant_totals", "lv_tenant_acc_state_bytes",
     "lv_tenant_acc_export", "lv_tenant_acc_import", "lv_fit", "lv_fit_vtc", "lv_accuracy", "lv_whatif",
     "lv_whatif_admit", "lv_attribute_noalloc", "lv_kv_plan", "lv_kv_store", "lv_kv_attend", "lv_prompt_attend",
+    "lv_linear", "lv_gated_linear", "lv_qk_rotate", "lv_token_logprobs",
 ]
 
 
@@ -80,6 +84,10 @@ class lv_kv_cache(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class lv_rope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("order", ctypes.c_int32), ("freq", ctypes.c_double * 64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"LLMVisor CUDA library not built: {LIB_PATH} is missing "
@@ -119,6 +127,11 @@ def _load():
         "lv_kv_store": ([P, P, I32, P, I64, P, I64, P, I64, P], I32),
         "lv_kv_attend": ([P, P, I32, I32, P, I64, I64, P, P, I64, P, I64, ctypes.c_float, P, P, P], I32),
         "lv_prompt_attend": ([P, I32, I32, I32, I32, P, I64, P, I64, P, I64, I64, P, I64, ctypes.c_float, P, P, P], I32),
+        "lv_linear": ([P, I32, P, I64, I64, P, I64, I32, I32, P, I32, P, I64, P, I64, P], I32),
+        "lv_gated_linear": ([P, I32, P, I64, I64, P, P, I64, I32, I32, P, P, I32, P, I64, P], I32),
+        "lv_qk_rotate": ([P, I32, I32, I32, I32, P, I64, P, I64, I64, P, P, I64, P, P, ctypes.c_float, P, P, I64, P, I64, P],
+                         I32),
+        "lv_token_logprobs": ([P, I32, P, I64, I64, I32, P, P, P, P, I32, P, P, P], I32),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -517,3 +530,106 @@ def lv_prompt_attend(ctx: Context, q, k, v, offsets, o, lse=None, scale=None, st
     _check(_lib.lv_prompt_attend(ctx.h, t[q.dtype], hq, hkv, d, q.data_ptr(), _rows(q, w), k.data_ptr(), _rows(k, w),
                                  v.data_ptr(), _rows(v, w), n_tok, offsets.data_ptr(), offsets.numel() - 1,
                                  d ** -0.5 if scale is None else scale, o.data_ptr(), _ptr(lse), _stream(stream)), w)
+
+
+# ------------------------------------------------------------------ a step's work for each new token
+
+_acts = {"none": LV_ACT_NONE, "silu": LV_ACT_SILU, "gelu": LV_ACT_GELU, "gelu_tanh": LV_ACT_GELU_TANH,
+         "relu": LV_ACT_RELU}
+
+
+def _flat(x, width, where):
+    """Row stride in elements of an [n][width] tensor on a GPU whose rows are without gaps inside."""
+    _want(x.dim() == 2 and x.shape[1] == width and x.is_cuda and (width == 1 or x.stride(1) == 1), where)
+    return x.stride(0) if x.shape[0] > 1 else -(-width // 8) * 8
+
+
+def _vector(v, n, dtype, where):
+    """Address of a vector of n elements on a GPU, or None."""
+    if v is None:
+        return None
+    _want(v.dtype == dtype and v.dim() == 1 and v.shape[0] == n and v.is_cuda and (n == 1 or v.stride(0) == 1), where)
+    return v.data_ptr()
+
+
+def lv_linear(ctx: Context, x, w, y, bias=None, act="none", residual=None, stream=None):
+    """y = act(x w^T + bias) + residual: x [n_tok][d_in], w [d_out][d_in], y and residual [n_tok][d_out] (which may be the
+    same tensor), bias [d_out]; rows may be slices of wider ones that begin at 16-byte boundaries.  act: "none", "silu",
+    "gelu", "gelu_tanh" or "relu"."""
+    t, at = _dtypes or _types(), "lv_linear"
+    (n, d_in), (d_out, _), dt = _sizes(x, 2, at), _sizes(w, 2, at), x.dtype
+    _want(dt in t and w.dtype == y.dtype == dt and y.shape[0] == n and act in _acts
+          and (residual is None or (residual.dtype == dt and residual.shape[0] == n)), at)
+    _check(_lib.lv_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, d_in, at), n, w.data_ptr(), _flat(w, d_in, at), d_in, d_out,
+                          _vector(bias, d_out, dt, at), _acts[act], _ptr(residual),
+                          0 if residual is None else _flat(residual, d_out, at), y.data_ptr(), _flat(y, d_out, at),
+                          _stream(stream)), at)
+
+
+def lv_gated_linear(ctx: Context, x, w_gate, w_up, y, bias_gate=None, bias_up=None, act="silu", stream=None):
+    """y = act(x w_gate^T + bias_gate) * (x w_up^T + bias_up): x [n_tok][d_in], w_gate and w_up [d_out][d_in] of one
+    stride, y [n_tok][d_out], biases [d_out]; as lv_linear otherwise."""
+    t, at = _dtypes or _types(), "lv_gated_linear"
+    (n, d_in), (d_out, _), dt = _sizes(x, 2, at), _sizes(w_gate, 2, at), x.dtype
+    stride = _flat(w_gate, d_in, at)
+    _want(dt in t and w_gate.dtype == w_up.dtype == y.dtype == dt and w_up.shape == w_gate.shape and y.shape[0] == n
+          and _flat(w_up, d_in, at) == stride and act in _acts, at)
+    _check(_lib.lv_gated_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, d_in, at), n, w_gate.data_ptr(), w_up.data_ptr(),
+                                stride, d_in, d_out, _vector(bias_gate, d_out, dt, at), _vector(bias_up, d_out, dt, at),
+                                _acts[act], y.data_ptr(), _flat(y, d_out, at), _stream(stream)), at)
+
+
+class Rope:
+    """How positions turn heads: pair j of a token at position n by n * freq[j] radians.  freq: up to 64 numbers, a
+    multiple of 8; pairs are elements j and j + len(freq), or with neighbours=True 2j and 2j + 1."""
+
+    def __init__(self, freq, neighbours=False):
+        freq = [float(f) for f in freq]
+        _want(len(freq) <= 64 and len(freq) % 8 == 0, "Rope")
+        self.s = lv_rope(2 * len(freq), LV_ROPE_NEIGHBOURS if neighbours else LV_ROPE_HALVES, (ctypes.c_double * 64)(*freq))
+        self.at = ctypes.addressof(self.s)
+
+    @classmethod
+    def geometric(cls, dim, base=10000.0, neighbours=False):
+        """Frequencies base^(-2j/dim) for the dim/2 pairs of a head's first dim elements."""
+        return cls([base ** (-2.0 * j / dim) for j in range(dim // 2)], neighbours)
+
+
+def lv_qk_rotate(ctx: Context, q, k, q_out, k_out, rope: Rope, c=None, token_offsets=None, q_weight=None, k_weight=None,
+                 eps=1e-6, stream=None):
+    """Norms (where weights [head_dim] are given) and rotation of q [n_tok][n_q_heads][head_dim] and
+    k [n_tok][n_kv_heads][head_dim] into q_out and k_out (slices of wider tensors may be given; q_out may be q, k_out k).
+    Positions as lv_kv_attend's: int32 c [n_req], int64 token_offsets [n_req + 1] or None for one token a request; c None
+    with token_offsets: requests that start on an empty cache."""
+    t, at = _dtypes or _types(), "lv_qk_rotate"
+    (n, hq, d), (_, hkv, _), dt = _sizes(q, 3, at), _sizes(k, 3, at), q.dtype
+    n_req = token_offsets.numel() - 1 if token_offsets is not None else n
+    _want(dt in t and k.dtype == q_out.dtype == k_out.dtype == dt and k.shape == (n, hkv, d) and q_out.shape == q.shape
+          and k_out.shape == k.shape and q.is_cuda and k.is_cuda and q_out.is_cuda and k_out.is_cuda and n_req >= 0
+          and (token_offsets is None or (token_offsets.dtype == t["i64"] and token_offsets.is_cuda
+                                         and token_offsets.is_contiguous()))
+          and (c is None or (c.dtype == t["i32"] and c.numel() == n_req and c.is_cuda and c.is_contiguous())), at)
+    _check(_lib.lv_qk_rotate(ctx.h, t[dt], hq, hkv, d, q.data_ptr(), _rows(q, at), k.data_ptr(), _rows(k, at), n,
+                             _ptr(token_offsets), _ptr(c), n_req, _vector(q_weight, d, dt, at),
+                             _vector(k_weight, d, dt, at), eps, rope.at, q_out.data_ptr(), _rows(q_out, at),
+                             k_out.data_ptr(), _rows(k_out, at), _stream(stream)), at)
+
+
+def lv_token_logprobs(ctx: Context, logits, ids=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None,
+                      stream=None):
+    """Of each row of logits [n_tok][vocab] (bfloat16, float16 or float32, any row stride): log probabilities logp of the
+    given int32 ids, entropy and lse [n_tok] float32, and the largest logits' ids and log probabilities, int32 top_ids and
+    float32 top_logp [n_tok][n_top]; what is None is left out."""
+    t, at = _dtypes or _types(), "lv_token_logprobs"
+    n, vocab = _sizes(logits, 2, at)
+    dt, n_top = logits.dtype, 0 if top_ids is None else _sizes(top_ids, 2, at)[1]
+    f32 = t["f32"]
+    _want((dt == f32 or dt in t) and logits.is_cuda and (vocab == 1 or logits.stride(1) == 1)
+          and (top_ids is None) == (top_logp is None)
+          and (top_ids is None or (top_ids.dtype == t["i32"] and top_logp.dtype == f32 and top_ids.is_cuda
+                                   and top_logp.is_cuda and top_ids.shape == top_logp.shape == (n, n_top)
+                                   and top_ids.is_contiguous() and top_logp.is_contiguous())), at)
+    _check(_lib.lv_token_logprobs(ctx.h, LV_F32 if dt == f32 else t[dt], logits.data_ptr(),
+                                  logits.stride(0) if n > 1 else vocab, n, vocab, _vector(ids, n, t["i32"], at),
+                                  _vector(logp, n, f32, at), _vector(entropy, n, f32, at), _vector(lse, n, f32, at), n_top,
+                                  _ptr(top_ids), _ptr(top_logp), _stream(stream)), at)

@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 OUT_DIR = os.path.join(HERE, "_build")
 OUT = os.path.join(OUT_DIR, "libllmvisor.so")
-SRCS = [os.path.join(HERE, "csrc", n) for n in ("lv_api.cu", "lv_kv.cu")]
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("lv_api.cu", "lv_kv.cu", "lv_layer.cu")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

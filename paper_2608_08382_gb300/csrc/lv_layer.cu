@@ -1,0 +1,163 @@
+// Host side of a step's work for each token: argument checks and launches.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "llmvisor.h"
+#include "lv_kv.h"
+#include "lv_linear.cuh"
+#include "lv_logprobs.cuh"
+#include "lv_rotate.cuh"
+
+using namespace lv;
+
+namespace {
+
+#define LV_CUDA(call)                          \
+  do {                                         \
+    if ((call) != cudaSuccess) return LV_ECUDA; \
+  } while (0)
+
+bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+constexpr int64_t kMostTokens = 1ll << 30, kMostStride = 1ll << 38;
+constexpr int kMostWidth = 1 << 24;
+
+// n rows of `width` 16-bit elements that begin at 16-byte boundaries.
+bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
+  return n == 0 || (p && aligned(p, 16) && stride % 8 == 0 && stride >= width && stride <= kMostStride);
+}
+
+bool is16(int32_t dtype) { return dtype == LV_BF16 || dtype == LV_F16; }
+
+template <bool GATED>
+lv_status run_linear(const LinearArgs &a, int32_t dtype, cudaStream_t stream) {
+  const int64_t grid = (a.d_out + kLinTile - 1) / kLinTile * ((a.n_tok + kLinTile - 1) / kLinTile);
+  if (grid > INT32_MAX) return LV_EINVAL;
+  if (dtype == LV_F16)
+    k_linear<GATED, true><<<(unsigned)grid, 256, 0, stream>>>(a);
+  else
+    k_linear<GATED, false><<<(unsigned)grid, 256, 0, stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, bool gated, cudaStream_t stream) {
+  if (!ctx || !is16(dtype) || a.n_tok < 0 || a.n_tok > kMostTokens || a.d_in < 1 || a.d_in > kMostWidth || a.d_out < 1 ||
+      a.d_out > kMostWidth || a.act < LV_ACT_NONE || a.act > LV_ACT_RELU)
+    return LV_EINVAL;
+  if (!rows_ok(a.x, a.x_stride, a.n_tok, a.d_in) || !rows_ok(a.y, a.y_stride, a.n_tok, a.d_out)) return LV_EINVAL;
+  for (int k = 0; k < (gated ? 2 : 1); ++k)
+    if (!rows_ok(a.w[k], a.w_stride, a.d_out, a.d_in) || !aligned(a.bias[k], 2)) return LV_EINVAL;
+  if (a.residual && !rows_ok(a.residual, a.r_stride, a.n_tok, a.d_out)) return LV_EINVAL;
+  if (a.residual == a.y && a.residual && a.r_stride != a.y_stride) return LV_EINVAL;
+  if (a.n_tok == 0) return LV_OK;
+  a.status = kv_host(ctx)->d_status;
+  return gated ? run_linear<true>(a, dtype, stream) : run_linear<false>(a, dtype, stream);
+}
+
+template <int D>
+lv_status run_rotate(const KvHost *kv, const RotateArgs &a, int32_t dtype, cudaStream_t stream) {
+  const int64_t items = a.n_tok * (a.heads[0] + a.heads[1]);
+  const unsigned grid = (unsigned)std::min<int64_t>((items + 3) / 4, (int64_t)kv->sms * 16);
+  if (dtype == LV_F16)
+    k_rotate<D, true><<<grid, 128, 0, stream>>>(a);
+  else
+    k_rotate<D, false><<<grid, 128, 0, stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lv_status lv_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride, int64_t n_tok, const void *w,
+                    int64_t w_stride, int32_t d_in, int32_t d_out, const void *bias, int32_t act,
+                    const void *residual, int64_t residual_stride, void *y, int64_t y_stride, void *stream) {
+  LinearArgs a{};
+  a.x = x, a.w[0] = w, a.bias[0] = bias, a.residual = residual, a.y = y;
+  a.x_stride = x_stride, a.w_stride = w_stride, a.r_stride = residual_stride, a.y_stride = y_stride;
+  a.n_tok = n_tok, a.d_in = d_in, a.d_out = d_out, a.act = act;
+  return linear(ctx, dtype, a, false, (cudaStream_t)stream);
+}
+
+lv_status lv_gated_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride, int64_t n_tok,
+                          const void *w_gate, const void *w_up, int64_t w_stride, int32_t d_in, int32_t d_out,
+                          const void *bias_gate, const void *bias_up, int32_t act, void *y, int64_t y_stride,
+                          void *stream) {
+  LinearArgs a{};
+  a.x = x, a.w[0] = w_gate, a.w[1] = w_up, a.bias[0] = bias_gate, a.bias[1] = bias_up, a.y = y;
+  a.x_stride = x_stride, a.w_stride = w_stride, a.y_stride = y_stride;
+  a.n_tok = n_tok, a.d_in = d_in, a.d_out = d_out, a.act = act;
+  return linear(ctx, dtype, a, true, (cudaStream_t)stream);
+}
+
+lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                       const void *q, int64_t q_stride, const void *k, int64_t k_stride, int64_t n_tok,
+                       const int64_t *token_offsets, const int32_t *c, int64_t n_req, const void *q_weight,
+                       const void *k_weight, float eps, const lv_rope *rope, void *q_out, int64_t q_out_stride,
+                       void *k_out, int64_t k_out_stride, void *stream_) {
+  if (!ctx || !is16(dtype) || (head_dim != 64 && head_dim != 128) || n_kv_heads < 1 || n_kv_heads > 1024 ||
+      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > LV_MAX_GROUP)
+    return LV_EINVAL;
+  if (n_tok < 0 || n_tok > kMostTokens || n_req < 0 || n_req > (1ll << 24) || (!token_offsets && n_tok != n_req) ||
+      !(eps >= 0.f) || !std::isfinite(eps))
+    return LV_EINVAL;
+  if (!rope || rope->dim < 0 || rope->dim > head_dim || rope->dim % 16 ||
+      (rope->order != LV_ROPE_HALVES && rope->order != LV_ROPE_NEIGHBOURS))
+    return LV_EINVAL;
+  RotateArgs a{};
+  for (int j = 0; j < rope->dim / 2; ++j) {
+    const double f = rope->freq[j];
+    if (!(std::fabs(f) <= 8.0)) return LV_EINVAL;
+    const double turns = std::fabs(f) / 6.283185307179586476925;  // whole ones do nothing
+    const uint64_t turn = (uint64_t)std::ldexp(turns - std::floor(turns), 64);
+    a.turn[j] = f < 0.0 ? 0 - turn : turn;
+  }
+  const int64_t dq = (int64_t)n_q_heads * head_dim, dk = (int64_t)n_kv_heads * head_dim;
+  if (!rows_ok(q, q_stride, n_tok, dq) || !rows_ok(k, k_stride, n_tok, dk) || !rows_ok(q_out, q_out_stride, n_tok, dq) ||
+      !rows_ok(k_out, k_out_stride, n_tok, dk) || !aligned(q_weight, 2) || !aligned(k_weight, 2))
+    return LV_EINVAL;
+  if ((q == q_out && q && q_stride != q_out_stride) || (k == k_out && k && k_stride != k_out_stride)) return LV_EINVAL;
+  if (n_tok == 0 || n_req == 0) return LV_OK;
+  if (!aligned(token_offsets, 8) || !aligned(c, 4)) return LV_EINVAL;
+  a.x[0] = q, a.x[1] = k, a.y[0] = q_out, a.y[1] = k_out, a.weight[0] = q_weight, a.weight[1] = k_weight;
+  a.x_stride[0] = q_stride, a.x_stride[1] = k_stride, a.y_stride[0] = q_out_stride, a.y_stride[1] = k_out_stride;
+  a.n_tok = n_tok, a.offsets = token_offsets, a.c = c, a.n_req = n_req;
+  a.heads[0] = n_q_heads, a.heads[1] = n_kv_heads;
+  a.dim = rope->dim, a.neighbours = rope->order == LV_ROPE_NEIGHBOURS, a.eps = eps;
+  const KvHost *kv = kv_host(ctx);
+  a.status = kv->d_status;
+  return head_dim == 128 ? run_rotate<128>(kv, a, dtype, (cudaStream_t)stream_)
+                         : run_rotate<64>(kv, a, dtype, (cudaStream_t)stream_);
+}
+
+lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int64_t stride, int64_t n_tok,
+                            int32_t vocab, const int32_t *ids, float *logp, float *entropy, float *lse,
+                            int32_t n_top, int32_t *top_ids, float *top_logp, void *stream_) {
+  if (!ctx || (!is16(dtype) && dtype != LV_F32) || n_tok < 0 || n_tok > kMostTokens || vocab < 1 || vocab > kMostWidth ||
+      n_top < 0 || n_top > LV_MAX_TOP)
+    return LV_EINVAL;
+  if (n_tok == 0) return LV_OK;
+  if (!logits || !aligned(logits, dtype == LV_F32 ? 4 : 2) || stride < vocab || stride > kMostStride || (logp && !ids) ||
+      (n_top > 0 && (!top_ids || !top_logp)))
+    return LV_EINVAL;
+  if (!aligned(ids, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(top_ids, 4) ||
+      !aligned(top_logp, 4))
+    return LV_EINVAL;
+  const KvHost *kv = kv_host(ctx);
+  LogprobArgs a{logits, stride, n_tok, vocab, n_top, ids, logp, entropy, lse, top_ids, top_logp, kv->d_status};
+  cudaStream_t stream = (cudaStream_t)stream_;
+  const unsigned grid = (unsigned)std::min<int64_t>(n_tok, (int64_t)kv->sms * 8);
+  if (dtype == LV_BF16) k_logprobs<LV_BF16><<<grid, 256, 0, stream>>>(a);
+  if (dtype == LV_F16) k_logprobs<LV_F16><<<grid, 256, 0, stream>>>(a);
+  if (dtype == LV_F32) k_logprobs<LV_F32><<<grid, 256, 0, stream>>>(a);
+  LV_CUDA(cudaGetLastError());
+  return LV_OK;
+}
+
+}  // extern "C"
