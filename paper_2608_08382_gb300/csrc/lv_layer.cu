@@ -33,30 +33,102 @@ bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
 
 bool is16(int32_t dtype) { return dtype == LV_BF16 || dtype == LV_F16; }
 
-template <bool GATED>
-lv_status run_linear(const LinearArgs &a, int32_t dtype, cudaStream_t stream) {
-  const int64_t grid = (a.d_out + kLinTile - 1) / kLinTile * ((a.n_tok + kLinTile - 1) / kLinTile);
-  if (grid > INT32_MAX) return LV_EINVAL;
-  if (dtype == LV_F16)
-    k_linear<GATED, true><<<(unsigned)grid, 256, 0, stream>>>(a);
-  else
-    k_linear<GATED, false><<<(unsigned)grid, 256, 0, stream>>>(a);
-  LV_CUDA(cudaGetLastError());
+// The caller's arrays of a product.
+struct Operands {
+  const void *x, *w[2];
+  int64_t x_stride, w_stride;
+  int d_in;
+};
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder of tensor maps, through the runtime (no link against the
+// driver's library); null where it is missing.
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    const cudaError_t rc = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found);
+    return rc == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(p) : nullptr;
+  }();
+  return f;
+}
+
+// The map of an array of n rows of `width` elements whose boxes are `rows` rows of 64 elements.
+lv_status map_matrix(CUtensorMap *map, const void *at, int32_t dtype, int64_t n, int64_t width, int64_t stride, int rows) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return LV_ECUDA;
+  const cuuint64_t size[2] = {(cuuint64_t)width, (cuuint64_t)n}, step[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {kPiece, (cuuint32_t)rows}, one[2] = {1, 1};
+  const CUresult rc =
+      encode(map, dtype == LV_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+             const_cast<void *>(at), size, step, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? LV_OK : LV_ECUDA;
+}
+
+// Kernels' shared-memory limits, once for a context, at the most that a block can
+// have; `kind` numbers the kernels (the attention calls' are below 8).
+constexpr int kMostSmem = 227 << 10;
+template <class K>
+lv_status limit_smem(KvHost *kv, K kernel, int kind) {
+  if (kv->configured >> kind & 1) return LV_OK;
+  LV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+  kv->configured |= 1u << kind;
   return LV_OK;
 }
 
-lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, bool gated, cudaStream_t stream) {
-  if (!ctx || !is16(dtype) || a.n_tok < 0 || a.n_tok > kMostTokens || a.d_in < 1 || a.d_in > kMostWidth || a.d_out < 1 ||
+template <bool GATED, bool F16>
+lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t stream) {
+  const int32_t dtype = F16 ? LV_F16 : LV_BF16;
+  const int64_t outputs = tile_outputs<GATED>(), row_tiles = (a.d_out + outputs - 1) / outputs;
+  a.chunks = (m.d_in + kPiece - 1) / kPiece;
+  a.tokens = (int)std::min<int64_t>((a.n_tok + 15) / 16 * 16, 128);
+  a.token_tiles = (a.n_tok + a.tokens - 1) / a.tokens;
+  a.tiles = row_tiles * a.token_tiles;
+  a.split = 1;
+  while (a.split < kSpSplit && a.tiles * a.split < kv->sms && a.split * 2 <= a.chunks) a.split *= 2;
+  a.stages = (int)std::min<size_t>((112 << 10) / split_stage(a.tokens), kSpStages);
+  if (a.tiles * a.split > INT32_MAX) return LV_EINVAL;
+  CUtensorMap mw, mu, mx;
+  lv_status st = map_matrix(&mw, m.w[0], dtype, a.d_out, m.d_in, m.w_stride, (int)outputs);
+  if (st == LV_OK) st = map_matrix(&mx, m.x, dtype, a.n_tok, m.d_in, m.x_stride, a.tokens);
+  if (st == LV_OK && GATED) st = map_matrix(&mu, m.w[1], dtype, a.d_out, m.d_in, m.w_stride, (int)outputs);
+  if (st != LV_OK) return st;
+  if (!GATED) mu = mw;
+  st = limit_smem(kv, k_product<GATED, F16>, 8 + (GATED ? 2 : 0) + (F16 ? 1 : 0));
+  if (st != LV_OK) return st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = a.split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(a.tiles * a.split));
+  cfg.blockDim = dim3(kSpThreads);
+  cfg.dynamicSmemBytes = split_smem(a.tokens, a.stages);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LV_CUDA(cudaLaunchKernelEx(&cfg, k_product<GATED, F16>, a, mw, mu, mx));
+  return LV_OK;
+}
+
+lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, const Operands &m, bool gated, cudaStream_t stream) {
+  if (!ctx || !is16(dtype) || a.n_tok < 0 || a.n_tok > kMostTokens || m.d_in < 1 || m.d_in > kMostWidth || a.d_out < 1 ||
       a.d_out > kMostWidth || a.act < LV_ACT_NONE || a.act > LV_ACT_RELU)
     return LV_EINVAL;
-  if (!rows_ok(a.x, a.x_stride, a.n_tok, a.d_in) || !rows_ok(a.y, a.y_stride, a.n_tok, a.d_out)) return LV_EINVAL;
+  if (!rows_ok(m.x, m.x_stride, a.n_tok, m.d_in) || !rows_ok(a.y, a.y_stride, a.n_tok, a.d_out)) return LV_EINVAL;
   for (int k = 0; k < (gated ? 2 : 1); ++k)
-    if (!rows_ok(a.w[k], a.w_stride, a.d_out, a.d_in) || !aligned(a.bias[k], 2)) return LV_EINVAL;
+    if (!rows_ok(m.w[k], m.w_stride, a.d_out, m.d_in) || !aligned(a.bias[k], 2)) return LV_EINVAL;
   if (a.residual && !rows_ok(a.residual, a.r_stride, a.n_tok, a.d_out)) return LV_EINVAL;
   if (a.residual == a.y && a.residual && a.r_stride != a.y_stride) return LV_EINVAL;
   if (a.n_tok == 0) return LV_OK;
-  a.status = kv_host(ctx)->d_status;
-  return gated ? run_linear<true>(a, dtype, stream) : run_linear<false>(a, dtype, stream);
+  KvHost *kv = kv_host(ctx);
+  a.status = kv->d_status;
+  if (gated) return dtype == LV_F16 ? run_linear<true, true>(kv, a, m, stream) : run_linear<true, false>(kv, a, m, stream);
+  return dtype == LV_F16 ? run_linear<false, true>(kv, a, m, stream) : run_linear<false, false>(kv, a, m, stream);
 }
 
 template <int D>
@@ -79,10 +151,10 @@ lv_status lv_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride,
                     int64_t w_stride, int32_t d_in, int32_t d_out, const void *bias, int32_t act,
                     const void *residual, int64_t residual_stride, void *y, int64_t y_stride, void *stream) {
   LinearArgs a{};
-  a.x = x, a.w[0] = w, a.bias[0] = bias, a.residual = residual, a.y = y;
-  a.x_stride = x_stride, a.w_stride = w_stride, a.r_stride = residual_stride, a.y_stride = y_stride;
-  a.n_tok = n_tok, a.d_in = d_in, a.d_out = d_out, a.act = act;
-  return linear(ctx, dtype, a, false, (cudaStream_t)stream);
+  a.bias[0] = bias, a.residual = residual, a.y = y;
+  a.r_stride = residual_stride, a.y_stride = y_stride;
+  a.n_tok = n_tok, a.d_out = d_out, a.act = act;
+  return linear(ctx, dtype, a, Operands{x, {w, nullptr}, x_stride, w_stride, d_in}, false, (cudaStream_t)stream);
 }
 
 lv_status lv_gated_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_stride, int64_t n_tok,
@@ -90,10 +162,9 @@ lv_status lv_gated_linear(lv_ctx *ctx, int32_t dtype, const void *x, int64_t x_s
                           const void *bias_gate, const void *bias_up, int32_t act, void *y, int64_t y_stride,
                           void *stream) {
   LinearArgs a{};
-  a.x = x, a.w[0] = w_gate, a.w[1] = w_up, a.bias[0] = bias_gate, a.bias[1] = bias_up, a.y = y;
-  a.x_stride = x_stride, a.w_stride = w_stride, a.y_stride = y_stride;
-  a.n_tok = n_tok, a.d_in = d_in, a.d_out = d_out, a.act = act;
-  return linear(ctx, dtype, a, true, (cudaStream_t)stream);
+  a.bias[0] = bias_gate, a.bias[1] = bias_up, a.y = y, a.y_stride = y_stride;
+  a.n_tok = n_tok, a.d_out = d_out, a.act = act;
+  return linear(ctx, dtype, a, Operands{x, {w_gate, w_up}, x_stride, w_stride, d_in}, true, (cudaStream_t)stream);
 }
 
 lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -1,18 +1,35 @@
-// Products of a step's tokens with a layer's weights (lv_linear, lv_gated_linear).
+// Products of a step's tokens with a layer's weights (lv_linear, lv_gated_linear) on
+// the tensor cores.
+//
+// D = W X^T: the weights' rows stand along the accumulator's 128 lanes and the tokens
+// along its columns, so that a call of any number of tokens, from one up, fills the
+// lanes and pays columns for the tokens it has (in steps of 16).  Both operands come
+// by TMA in pieces of 64 along the sum, 128 bytes a row, swizzled; what a piece has
+// past a row's end or past the last row is zero in both.  The gated form puts 64 rows
+// of each weight array into the lanes of one accumulator, so that it is the same
+// product: its two halves meet in shared memory on the way out.  There an
+// accumulator's column, fp32, is a token's outputs in a row; a thread takes eight of
+// them at a time, adds the bias, applies the activation, adds the residual, rounds
+// once and stores 16 bytes.
 #pragma once
 
 #include "lv_attend.cuh"
+#include "lv_tc.cuh"
 
 namespace lv {
 
 struct LinearArgs {
-  const void *x, *w[2];      // w[1]: the gated form's second weights
-  const void *bias[2];
+  const void *bias[2];       // [1]: of the gated form's second weights
   const void *residual;
   void *y;
-  int64_t x_stride, w_stride, r_stride, y_stride;
+  int64_t r_stride, y_stride;
   int64_t n_tok;
-  int d_in, d_out, act;
+  int d_out, act;
+  int chunks;                // pieces of 64 along the sum
+  int tokens;                // columns of a tile, a multiple of 16
+  int stages;
+  int split;                 // CTAs that share a tile's sum (k_product)
+  int64_t token_tiles, tiles;
   int *status;
 };
 
@@ -28,59 +45,244 @@ __device__ __forceinline__ float value_of(uint16_t b) {
 // 2 / (1 + exp(-2u)).
 __device__ __forceinline__ float activated(float x, int act) {
   switch (act) {
-    case LV_ACT_SILU: return x / (1.f + __expf(-x));
+    case LV_ACT_SILU: return __fdividef(x, 1.f + __expf(-x));
     case LV_ACT_GELU: return 0.5f * x * erfcf(x * -0.70710678118654752f);
-    case LV_ACT_GELU_TANH: return x / (1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
+    case LV_ACT_GELU_TANH: return __fdividef(x, 1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
     case LV_ACT_RELU: return x < 0.f ? 0.f : x;
     default: return x;
   }
 }
 
-// Each CTA forms 64 tokens by 64 outputs, a thread 4 by 4 of them, 16 terms a step
-// through shared memory in fp32.
-constexpr int kLinTile = 64, kLinStep = 16;
+constexpr int kPiece = 64;                    // of the sum, in a stage
+constexpr int kRows = 128;                    // weight rows of a CTA's tile
+constexpr int kWBytes = kRows * kPiece * 2;   // of a stage
+constexpr int kColFloats = kRows + 4;         // a token's sums in shared memory: 16-byte steps, spread over the banks
 
+// Outputs of a CTA's tile.
+template <bool GATED>
+__host__ __device__ constexpr int tile_outputs() { return GATED ? kRows / 2 : kRows; }
+
+template <bool F16>
+__device__ __forceinline__ void unpack8(const uint4 &b, float *v) {
+  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = value_of<F16>((uint16_t)(w[k >> 1] >> (k & 1) * 16));
+}
+
+// The biases of outputs o .. o + 7.
 template <bool GATED, bool F16>
-__global__ void __launch_bounds__(256) k_linear(const LinearArgs a) {
-  constexpr int kW = GATED ? 2 : 1;
-  __shared__ float xs[kLinStep][kLinTile + 1], ws[kW][kLinStep][kLinTile + 1];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int across = (a.d_out + kLinTile - 1) / kLinTile;
-  const int64_t t0 = (int64_t)(blockIdx.x / across) * kLinTile;
-  const int o0 = (int)(blockIdx.x % across) * kLinTile;
-  float sum[kW][4][4] = {};
-  for (int i0 = 0; i0 < a.d_in; i0 += kLinStep) {
-    for (int e = threadIdx.x; e < kLinTile * kLinStep; e += 256) {
-      const int r = e / kLinStep, i = e % kLinStep;
-      const bool in = i0 + i < a.d_in;
-      xs[i][r] = in && t0 + r < a.n_tok ? value_of<F16>(((const uint16_t *)a.x)[(t0 + r) * a.x_stride + i0 + i]) : 0.f;
-      for (int k = 0; k < kW; ++k)
-        ws[k][i][r] = in && o0 + r < a.d_out ? value_of<F16>(((const uint16_t *)a.w[k])[(o0 + r) * a.w_stride + i0 + i]) : 0.f;
-    }
-    __syncthreads();
-    for (int i = 0; i < kLinStep; ++i)
+__device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)[8]) {
 #pragma unroll
-      for (int k = 0; k < kW; ++k)
+  for (int k = 0; k < (GATED ? 2 : 1); ++k)
 #pragma unroll
-        for (int p = 0; p < 4; ++p)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) sum[k][p][q] += xs[i][ty + 16 * p] * ws[k][i][tx + 16 * q];
-    __syncthreads();
+    for (int e = 0; e < 8; ++e)
+      b[k][e] = a.bias[k] && o + e < a.d_out ? value_of<F16>(((const uint16_t *)a.bias[k])[o + e]) : 0.f;
+}
+
+// Outputs o .. o + 7 of token t from their sums (and the second ones, u).
+template <bool GATED, bool F16>
+__device__ __forceinline__ void finish8(const LinearArgs &a, int64_t t, int o, float *v, const float *u, const float (*b)[8]) {
+  if (t >= a.n_tok || o >= a.d_out) return;
+  const bool whole = o + 8 <= a.d_out;
+  float r[8] = {};
+  const uint16_t *rp = nullptr;
+  if (!GATED && a.residual) {
+    rp = (const uint16_t *)a.residual + t * a.r_stride + o;
+    if (whole) unpack8<F16>(*(const uint4 *)rp, r);
   }
 #pragma unroll
-  for (int p = 0; p < 4; ++p)
+  for (int e = 0; e < 8; ++e) {
+    v[e] = activated(v[e] + b[0][e], a.act);
+    if (GATED) v[e] *= u[e] + b[1][e];
+  }
+  uint16_t *const y = (uint16_t *)a.y + t * a.y_stride + o;
+  if (whole) {
+    if (!GATED && a.residual)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t t = t0 + ty + 16 * p;
-      const int o = o0 + tx + 16 * q;
-      if (t >= a.n_tok || o >= a.d_out) continue;
-      float v[kW];
-      for (int k = 0; k < kW; ++k) v[k] = sum[k][p][q] + (a.bias[k] ? value_of<F16>(((const uint16_t *)a.bias[k])[o]) : 0.f);
-      float y = activated(v[0], a.act);
-      if (GATED) y *= v[kW - 1];
-      if (a.residual) y += value_of<F16>(((const uint16_t *)a.residual)[t * a.r_stride + o]);
-      ((uint16_t *)a.y)[t * a.y_stride + o] = (uint16_t)pack_out<F16>(y, 0.f);
+      for (int e = 0; e < 8; ++e) v[e] += r[e];
+    *(uint4 *)y = make_uint4(pack_out<F16>(v[0], v[1]), pack_out<F16>(v[2], v[3]), pack_out<F16>(v[4], v[5]),
+                             pack_out<F16>(v[6], v[7]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (o + e < a.d_out) {
+        if (!GATED && a.residual) v[e] += value_of<F16>(rp[e]);
+        y[e] = (uint16_t)pack_out<F16>(v[e], 0.f);
+      }
+  }
+}
+
+__device__ __forceinline__ void tma_load2(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_addr(to)),
+      "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
+      : "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// All threads of the cluster; what they wrote to shared memory is seen after it.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address of a place in this block's shared memory in another block of the cluster.
+__device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void store_peer(uint32_t at, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+
+__host__ __device__ constexpr uint32_t columns_for(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+
+// Few tokens: the weights' bytes bound the call.  A CTA forms a tile of 128 rows by
+// `tokens` columns, and `split` CTAs of a cluster share its sum, each a stretch of it,
+// so that there are CTAs for every SM and, two to an SM, one's beginning and end lie
+// in the other's loads.  The parts are joined through the cluster's shared memory, in
+// the stretches' order: each CTA takes the columns that are its to finish.
+constexpr int kSpThreads = 256;
+constexpr int kSpTokens = 160;   // columns at most: with three stages, two CTAs an SM
+constexpr int kSpSplit = 8;      // a portable cluster
+constexpr int kSpStages = 16;    // at most
+
+struct SplitSmem {
+  uint64_t full[kSpStages], empty[kSpStages], done;
+  uint32_t tmem;
+  int stop[3];  // see bar_wait
+};
+// The stages stand first, from a 1,024-byte boundary on, then this.
+constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPiece * 2; }
+constexpr size_t split_smem(int tokens, int stages) { return 1024 + stages * split_stage(tokens) + sizeof(SplitSmem); }
+static_assert(3 * split_stage(kSpTokens) >= kSpTokens * kColFloats * sizeof(float), "the sums stand in the stages");
+
+template <bool GATED, bool F16>
+__global__ void __launch_bounds__(kSpThreads)
+    k_product(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_w,
+              const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x) {
+  extern __shared__ unsigned char raw_product[];
+  unsigned char *const stage0 = (unsigned char *)((reinterpret_cast<uintptr_t>(raw_product) + 1023) & ~(uintptr_t)1023);
+  const uint32_t stage_bytes = kWBytes + a.tokens * kPiece * 2;
+  SplitSmem &sm = *reinterpret_cast<SplitSmem *>(stage0 + (size_t)a.stages * stage_bytes);
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t columns = columns_for(a.tokens);
+  if (warp == 0) tmem_alloc(&sm.tmem, columns);
+  if (threadIdx.x == 32) {
+    map_ahead(&map_w);
+    if (GATED) map_ahead(&map_u);
+    map_ahead(&map_x);
+    sm.stop[0] = sm.stop[1] = sm.stop[2] = 0;
+    for (int k = 0; k < a.stages; ++k) {
+      bar_init(&sm.full[k], 1);
+      bar_init(&sm.empty[k], 1);
     }
+    bar_init(&sm.done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
+  volatile int *stop = sm.stop;
+  const uint32_t rank = blockIdx.x % a.split;
+  const int64_t tile = blockIdx.x / a.split;
+  const int64_t t0 = tile % a.token_tiles * a.tokens;
+  const int o0 = (int)(tile / a.token_tiles) * tile_outputs<GATED>();
+  const int from = (int)((int64_t)a.chunks * rank / a.split), to = (int)((int64_t)a.chunks * (rank + 1) / a.split);
+  const int n = to - from;
+
+  if (warp == 1 && lane == 0) {
+    for (int i = 0; i < n; ++i) {
+      const int st = i % a.stages;
+      if (i >= a.stages) bar_wait(&sm.empty[st], (i / a.stages - 1) & 1, stop);
+      if (*stop) break;
+      unsigned char *const at = stage0 + (size_t)st * stage_bytes;
+      bar_expect(&sm.full[st], stage_bytes);
+      const int x = (from + i) * kPiece;
+      tma_load2(at, &map_w, x, o0, &sm.full[st]);
+      if (GATED) tma_load2(at + kWBytes / 2, &map_u, x, o0, &sm.full[st]);
+      tma_load2(at + kWBytes, &map_x, x, (int)t0, &sm.full[st]);
+    }
+  } else if (warp == 0) {
+    const uint32_t idesc = tc_idesc(kRows, a.tokens, F16, false, false);
+    const uint32_t base = tc_desc(smem_addr(stage0), 16);
+    for (int i = 0; i < n; ++i) {
+      const int st = i % a.stages;
+      bar_wait(&sm.full[st], (i / a.stages) & 1, stop);
+      tc_after_sync();
+      if (elect_one()) {
+        const uint32_t w = base + (uint32_t)(st * stage_bytes >> 4), x = w + (kWBytes >> 4);
+#pragma unroll
+        for (int k = 0; k < kPiece / 16; ++k) tc_mma(tmem, w + k * 2, x + k * 2, idesc, i > 0 || k > 0);
+        tc_commit(i + 1 == n ? &sm.done : &sm.empty[st]);
+      }
+    }
+  }
+  __syncwarp();
+  bar_wait(&sm.done, 0, stop);
+  __syncwarp();
+  tc_after_sync();
+  // every CTA's products are done: the stages may hold sums
+  float *const sums = reinterpret_cast<float *>(stage0);
+  const int per = a.tokens / a.split;  // columns that a CTA finishes
+  if (a.split > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  // Warps 0-3 and 4-7 take turns of eight columns; a warp reads its quarter of the lanes.
+  const int row = (warp & 3) * 32 + lane;
+  const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
+  for (int c0 = (warp >> 2) * 16; c0 < a.tokens; c0 += 32) {
+    uint32_t r[16];
+    tmem_load16(r, lane0 + c0);
+    tmem_wait_load();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int c = c0 + k, owner = c / per;
+      float *const at = sums + (size_t)(rank * per + c - owner * per) * kColFloats + row;
+      if (a.split > 1)
+        store_peer(peer_addr(at, owner), __uint_as_float(r[k]));
+      else
+        *at = __uint_as_float(r[k]);
+    }
+  }
+  tc_before_sync();
+  if (a.split > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  constexpr int kGroups = tile_outputs<GATED>() / 8;
+  const int o = o0 + (threadIdx.x % kGroups) * 8;
+  float b[2][8];
+  load_bias<GATED, F16>(a, o, b);
+  for (int c = threadIdx.x / kGroups; c < per; c += kSpThreads / kGroups) {
+    float v[8] = {}, u[8] = {};
+    for (int s = 0; s < a.split; ++s) {
+      const float *const at = sums + (size_t)(s * per + c) * kColFloats + (threadIdx.x % kGroups) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const float4 p = *(const float4 *)(at + e);
+        v[e] += p.x, v[e + 1] += p.y, v[e + 2] += p.z, v[e + 3] += p.w;
+        if (GATED) {
+          const float4 q = *(const float4 *)(at + kRows / 2 + e);
+          u[e] += q.x, u[e + 1] += q.y, u[e + 2] += q.z, u[e + 3] += q.w;
+        }
+      }
+    }
+    finish8<GATED, F16>(a, t0 + (int64_t)rank * per + c, o, v, u, b);
+  }
+  if (threadIdx.x == 0 && *stop) {
+    flag(a.status, kStatusTimeout);
+    for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // what was issued may still be at work on shared memory
+  }
+  __syncthreads();
+  if (warp == 0) tmem_free(tmem, columns);
 }
 
 }  // namespace lv
