@@ -80,26 +80,50 @@ lv_status limit_smem(KvHost *kv, K kernel, int kind) {
   return LV_OK;
 }
 
+// How a product is cut: by pairs of CTAs, or by CTAs of which `split` share a tile's
+// sum; `tokens` columns a tile.
+struct Shape {
+  bool pair;
+  int tokens, split;
+};
+
+Shape choose(const KvHost *kv, int64_t n_tok, int64_t row_tiles, int chunks) {
+  Shape s{n_tok > 256, (int)std::min<int64_t>((n_tok + 15) / 16 * 16, n_tok > 256 ? 256 : 128), 1};
+  const int64_t tiles = row_tiles * ((n_tok + s.tokens - 1) / s.tokens);
+  while (!s.pair && s.split < kSpSplit && tiles * s.split < kv->sms && s.split * 2 <= chunks) s.split *= 2;
+  return s;
+}
+
 template <bool GATED, bool F16>
 lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t stream) {
   const int32_t dtype = F16 ? LV_F16 : LV_BF16;
   const int64_t outputs = tile_outputs<GATED>(), row_tiles = (a.d_out + outputs - 1) / outputs;
   a.chunks = (m.d_in + kPiece - 1) / kPiece;
-  a.tokens = (int)std::min<int64_t>((a.n_tok + 15) / 16 * 16, 128);
+  const Shape shape = choose(kv, a.n_tok, row_tiles, a.chunks);
+  a.tokens = shape.tokens;
+  a.split = shape.split;
   a.token_tiles = (a.n_tok + a.tokens - 1) / a.tokens;
-  a.tiles = row_tiles * a.token_tiles;
-  a.split = 1;
-  while (a.split < kSpSplit && a.tiles * a.split < kv->sms && a.split * 2 <= a.chunks) a.split *= 2;
-  a.stages = (int)std::min<size_t>((112 << 10) / split_stage(a.tokens), kSpStages);
-  if (a.tiles * a.split > INT32_MAX) return LV_EINVAL;
+  a.tiles = (shape.pair ? (row_tiles + 1) / 2 : row_tiles) * a.token_tiles;
   CUtensorMap mw, mu, mx;
   lv_status st = map_matrix(&mw, m.w[0], dtype, a.d_out, m.d_in, m.w_stride, (int)outputs);
-  if (st == LV_OK) st = map_matrix(&mx, m.x, dtype, a.n_tok, m.d_in, m.x_stride, a.tokens);
+  if (st == LV_OK) st = map_matrix(&mx, m.x, dtype, a.n_tok, m.d_in, m.x_stride, shape.pair ? a.tokens / 2 : a.tokens);
   if (st == LV_OK && GATED) st = map_matrix(&mu, m.w[1], dtype, a.d_out, m.d_in, m.w_stride, (int)outputs);
   if (st != LV_OK) return st;
   if (!GATED) mu = mw;
-  st = limit_smem(kv, k_product<GATED, F16>, 8 + (GATED ? 2 : 0) + (F16 ? 1 : 0));
+  const int kind = 8 + (GATED ? 2 : 0) + (F16 ? 1 : 0);
+  if (shape.pair) {
+    constexpr size_t smem = sizeof(PairSmem) + 1024;
+    static_assert(smem <= kMostSmem, "an SM's shared memory");
+    st = limit_smem(kv, k_product_pair<GATED, F16>, kind + 4);
+    if (st != LV_OK) return st;
+    const unsigned grid = 2 * (unsigned)std::min<int64_t>(a.tiles, kv->sms / 2);
+    k_product_pair<GATED, F16><<<grid, kPaThreads, smem, stream>>>(a, mw, mu, mx);
+    LV_CUDA(cudaGetLastError());
+    return LV_OK;
+  }
+  st = limit_smem(kv, k_product<GATED, F16>, kind);
   if (st != LV_OK) return st;
+  a.stages = (int)std::min<size_t>((112 << 10) / split_stage(a.tokens), kSpStages);
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = a.split;

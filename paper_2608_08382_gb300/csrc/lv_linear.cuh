@@ -285,4 +285,213 @@ __global__ void __launch_bounds__(kSpThreads)
   if (warp == 0) tmem_free(tmem, columns);
 }
 
+// Many tokens: the products bound the call.  A pair of CTAs on neighbouring SMs forms
+// a tile of 256 rows by `tokens` columns with instructions that take both SMs'
+// operands: each CTA loads its 128 weight rows and half of the tokens, so that a term
+// of the sum costs half the shared-memory reads of two CTAs on their own.  The pairs
+// stay and take tiles in turn; two accumulators let a tile's products run while the
+// one before is on its way out.
+//   warps 0-3  a quarter of the lanes each: sums to shared memory, 32 columns at a
+//              time, and from there the outputs;
+//   warp 4     loads (one lane); warp 5 of the first CTA issues the products of both.
+constexpr int kPaThreads = 192;
+constexpr int kPaTokens = 256;   // columns at most
+constexpr int kPaStages = 6;
+constexpr int kPaStage = kWBytes + kPaTokens / 2 * kPiece * 2;
+constexpr int kPaOut = 32;       // columns on their way out at a time
+
+struct PairSmem {
+  unsigned char stage[kPaStages][kPaStage];
+  float out[2][kPaOut * kColFloats];
+  uint64_t full[kPaStages], empty[kPaStages], sums_full[2], sums_empty[2];
+  uint32_t tmem;
+  int stop[3];  // see bar_wait
+};
+
+// Loads into this CTA's shared memory whose bytes are counted by a barrier of the
+// pair's first CTA.
+__device__ __forceinline__ void tma_load2_pair(void *to, const CUtensorMap *map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_addr(to)),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t *to, int columns) {  // one whole warp of each CTA
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t at, int columns) {  // one whole warp of each CTA
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+// One arrival at the barrier at this place in both CTAs when all that this thread has
+// issued is done.
+__device__ __forceinline__ void tc_commit_pair(uint64_t *bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 da, db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 da, {%1, %5};\nmov.b64 db, {%2, %5};\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
+      : "memory");
+}
+__device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// First outputs and tokens of a tile: bands of eight row tiles, row tile after row tile
+// and then token tile after token tile, so that the tiles at work at a time share their
+// operands in L2.
+__device__ __forceinline__ void pair_tile(const LinearArgs &a, int64_t tile, int64_t *row_tile, int64_t *token_tile) {
+  constexpr int64_t kBand = 8;
+  const int64_t rows = quotient(a.tiles, a.token_tiles), of_band = kBand * a.token_tiles;
+  const int64_t band = quotient(tile, of_band), in = tile - band * of_band;
+  const int64_t wide = min(kBand, rows - band * kBand), t = quotient(in, wide);
+  *token_tile = t;
+  *row_tile = band * kBand + in - t * wide;
+}
+
+template <bool GATED, bool F16>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
+    k_product_pair(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap map_w,
+                   const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x) {
+  extern __shared__ unsigned char raw_pair[];
+  PairSmem &sm = *reinterpret_cast<PairSmem *>((reinterpret_cast<uintptr_t>(raw_pair) + 1023) & ~(uintptr_t)1023);
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  if (warp == 5) tmem_alloc_pair(&sm.tmem, 512);
+  if (threadIdx.x == 128) {
+    map_ahead(&map_w);
+    if (GATED) map_ahead(&map_u);
+    map_ahead(&map_x);
+    sm.stop[0] = sm.stop[1] = sm.stop[2] = 0;
+    for (int k = 0; k < kPaStages; ++k) {
+      bar_init(&sm.full[k], 1);
+      bar_init(&sm.empty[k], 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      bar_init(&sm.sums_full[k], 1);
+      bar_init(&sm.sums_empty[k], 8);  // the four warps of both CTAs
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_before_sync();
+  __syncthreads();
+  cluster_sync();
+  tc_after_sync();
+  const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
+  volatile int *stop = sm.stop;
+  const int64_t pairs = gridDim.x / 2, first = blockIdx.x / 2;
+  const int half = a.tokens / 2;
+  constexpr int kOut = tile_outputs<GATED>();
+  constexpr uint32_t kCols = 256;  // of an accumulator
+
+  if (warp == 4 && lane == 0) {
+    const uint32_t bytes = 2 * (kWBytes + half * kPiece * 2);
+    int st = 0;
+    uint32_t round = 0;  // of the ring: the phase of its stages
+    for (int64_t tile = first; tile < a.tiles; tile += pairs) {
+      int64_t row_tile, token_tile;
+      pair_tile(a, tile, &row_tile, &token_tile);
+      const int o = (int)(row_tile * 2 + rank) * kOut, t = (int)(token_tile * a.tokens) + (int)rank * half;
+      for (int i = 0; i < a.chunks; ++i) {
+        if (round > 0) bar_wait(&sm.empty[st], (round - 1) & 1, stop);
+        if (*stop) break;
+        unsigned char *const at = sm.stage[st];
+        const uint32_t bar = peer_addr(&sm.full[st], 0);
+        if (rank == 0) bar_expect(&sm.full[st], bytes);
+        tma_load2_pair(at, &map_w, i * kPiece, o, bar);
+        if (GATED) tma_load2_pair(at + kWBytes / 2, &map_u, i * kPiece, o, bar);
+        tma_load2_pair(at + kWBytes, &map_x, i * kPiece, t, bar);
+        if (++st == kPaStages) st = 0, ++round;
+      }
+      if (*stop) break;
+    }
+    // the products have read, and their arrivals reached, every stage before the CTA ends
+    for (int k = 0; k < kPaStages; ++k)
+      if (round > 0 || k < st) bar_wait(&sm.empty[k], (k < st ? round : round - 1) & 1, stop);
+  } else if (warp == 5 && rank == 0) {
+    const uint32_t idesc = tc_idesc(256, a.tokens, F16, false, false), base = tc_desc(smem_addr(sm.stage), 16);
+    int st = 0;
+    uint32_t phase = 0;
+    int n = 0;
+    for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
+      if (n >= 2) bar_wait(&sm.sums_empty[n & 1], ((n >> 1) - 1) & 1, stop);
+      tc_after_sync();
+      const uint32_t d = tmem + (n & 1) * kCols;
+      for (int i = 0; i < a.chunks; ++i) {
+        bar_wait(&sm.full[st], phase, stop);
+        tc_after_sync();
+        if (elect_one()) {
+          const uint32_t w = base + (uint32_t)(st * kPaStage >> 4), x = w + (kWBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < kPiece / 16; ++k) tc_mma_pair(d, w + k * 2, x + k * 2, idesc, i > 0 || k > 0);
+          tc_commit_pair(&sm.empty[st]);
+          if (i + 1 == a.chunks) tc_commit_pair(&sm.sums_full[n & 1]);
+        }
+        if (++st == kPaStages) st = 0, phase ^= 1;
+      }
+      if (*stop) break;
+    }
+  } else if (warp < 4) {
+    constexpr int kGroups = kOut / 8;
+    const int row = warp * 32 + lane, group = threadIdx.x % kGroups;
+    const uint32_t lane0 = tmem + ((uint32_t)warp * 32 << 16);
+    int n = 0, turn = 0;
+    for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
+      int64_t row_tile, token_tile;
+      pair_tile(a, tile, &row_tile, &token_tile);
+      const int64_t t0 = token_tile * a.tokens;
+      const int o = (int)(row_tile * 2 + rank) * kOut + group * 8;
+      float b[2][8];
+      load_bias<GATED, F16>(a, o, b);
+      bar_wait(&sm.sums_full[n & 1], (n >> 1) & 1, stop);
+      __syncwarp();
+      tc_after_sync();
+      for (int c0 = 0; c0 < a.tokens; c0 += kPaOut, turn ^= 1) {
+        float *const out = sm.out[turn];
+        uint32_t r[32];
+        tmem_load32(r, lane0 + (n & 1) * kCols + c0);
+        tmem_wait_load();
+        if (c0 + kPaOut >= a.tokens) {
+          tc_before_sync();
+          __syncwarp();
+          if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) out[k * kColFloats + row] = __uint_as_float(r[k]);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+        for (int c = threadIdx.x / kGroups; c < kPaOut; c += 128 / kGroups) {
+          if (c0 + c >= a.tokens) break;
+          float v[8], u[8];
+          const float *const at = out + c * kColFloats + group * 8;
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            *(float4 *)(v + e) = *(const float4 *)(at + e);
+            if (GATED) *(float4 *)(u + e) = *(const float4 *)(at + kRows / 2 + e);
+          }
+          finish8<GATED, F16>(a, t0 + c0 + c, o, v, u, b);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  if (threadIdx.x == 0 && *stop) {
+    flag(a.status, kStatusTimeout);
+    for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // what was issued may still be at work on shared memory
+  }
+  __syncthreads();
+  cluster_sync();  // the pair ends together
+  if (warp == 5) tmem_free_pair(tmem, 512);
+}
+
 }  // namespace lv
