@@ -123,7 +123,7 @@ lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t 
   }
   st = limit_smem(kv, k_product<GATED, F16>, kind);
   if (st != LV_OK) return st;
-  a.stages = (int)std::min<size_t>((112 << 10) / split_stage(a.tokens), kSpStages);
+  a.stages = (int)std::min<size_t>((111 << 10) / split_stage(a.tokens), kSpStages);
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = a.split;

@@ -43,14 +43,19 @@ __device__ __forceinline__ float value_of(uint16_t b) {
 // 16-bit types.  The two forms of GELU are written without the difference of nearly
 // equal numbers that 1 + erf and 1 + tanh have at the left: erfc, and 1 + tanh u =
 // 2 / (1 + exp(-2u)).
-__device__ __forceinline__ float activated(float x, int act) {
-  switch (act) {
-    case LV_ACT_SILU: return __fdividef(x, 1.f + __expf(-x));
-    case LV_ACT_GELU: return 0.5f * x * erfcf(x * -0.70710678118654752f);
-    case LV_ACT_GELU_TANH: return __fdividef(x, 1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
-    case LV_ACT_RELU: return x < 0.f ? 0.f : x;
-    default: return x;
-  }
+template <int ACT>
+__device__ __forceinline__ float activated(float x) {
+  if (ACT == LV_ACT_SILU) return __fdividef(x, 1.f + __expf(-x));
+  if (ACT == LV_ACT_GELU) return 0.5f * x * erfcf(x * -0.70710678118654752f);
+  if (ACT == LV_ACT_GELU_TANH) return __fdividef(x, 1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
+  return ACT == LV_ACT_RELU && x < 0.f ? 0.f : x;
+}
+template <int ACT, int N>
+__device__ __forceinline__ void activate(float (&v)[N][8]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[k][e] = activated<ACT>(v[k][e]);
 }
 
 constexpr int kPiece = 64;                    // of the sum, in a stage
@@ -79,36 +84,55 @@ __device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)
       b[k][e] = a.bias[k] && o + e < a.d_out ? value_of<F16>(((const uint16_t *)a.bias[k])[o + e]) : 0.f;
 }
 
-// Outputs o .. o + 7 of token t from their sums (and the second ones, u).
-template <bool GATED, bool F16>
-__device__ __forceinline__ void finish8(const LinearArgs &a, int64_t t, int o, float *v, const float *u, const float (*b)[8]) {
-  if (t >= a.n_tok || o >= a.d_out) return;
+// Outputs o .. o + 7 of N tokens t, t + step, .. from their sums (and the second ones, u);
+// tokens past the call's are left out.
+template <bool GATED, bool F16, int N>
+__device__ __forceinline__ void finish(const LinearArgs &a, int64_t t, int step, int o, float (&v)[N][8],
+                                       const float (&u)[N][8], const float (&b)[2][8]) {
+  if (o >= a.d_out) return;
   const bool whole = o + 8 <= a.d_out;
-  float r[8] = {};
-  const uint16_t *rp = nullptr;
-  if (!GATED && a.residual) {
-    rp = (const uint16_t *)a.residual + t * a.r_stride + o;
-    if (whole) unpack8<F16>(*(const uint4 *)rp, r);
+  const int64_t end = a.n_tok;
+  uint4 r[N];
+  if (!GATED && a.residual && whole)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (t + k * step < end) r[k] = *(const uint4 *)((const uint16_t *)a.residual + (t + k * step) * a.r_stride + o);
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[k][e] += b[0][e];
+  switch (a.act) {
+    case LV_ACT_SILU: activate<LV_ACT_SILU>(v); break;
+    case LV_ACT_GELU: activate<LV_ACT_GELU>(v); break;
+    case LV_ACT_GELU_TANH: activate<LV_ACT_GELU_TANH>(v); break;
+    case LV_ACT_RELU: activate<LV_ACT_RELU>(v); break;
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    v[e] = activated(v[e] + b[0][e], a.act);
-    if (GATED) v[e] *= u[e] + b[1][e];
-  }
-  uint16_t *const y = (uint16_t *)a.y + t * a.y_stride + o;
-  if (whole) {
-    if (!GATED && a.residual)
+  for (int k = 0; k < N; ++k) {
+    if (t + k * step >= end) continue;
+    float(&w)[8] = v[k];
+    if (GATED)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += r[e];
-    *(uint4 *)y = make_uint4(pack_out<F16>(v[0], v[1]), pack_out<F16>(v[2], v[3]), pack_out<F16>(v[4], v[5]),
-                             pack_out<F16>(v[6], v[7]));
-  } else {
+      for (int e = 0; e < 8; ++e) w[e] *= u[k][e] + b[1][e];
+    uint16_t *const y = (uint16_t *)a.y + (t + k * step) * a.y_stride + o;
+    if (whole) {
+      if (!GATED && a.residual) {
+        float x[8];
+        unpack8<F16>(r[k], x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (o + e < a.d_out) {
-        if (!GATED && a.residual) v[e] += value_of<F16>(rp[e]);
-        y[e] = (uint16_t)pack_out<F16>(v[e], 0.f);
+        for (int e = 0; e < 8; ++e) w[e] += x[e];
       }
+      *(uint4 *)y = make_uint4(pack_out<F16>(w[0], w[1]), pack_out<F16>(w[2], w[3]), pack_out<F16>(w[4], w[5]),
+                               pack_out<F16>(w[6], w[7]));
+    } else {
+      const uint16_t *const rp = (const uint16_t *)a.residual + (t + k * step) * a.r_stride + o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (o + e < a.d_out) {
+          if (!GATED && a.residual) w[e] += value_of<F16>(rp[e]);
+          y[e] = (uint16_t)pack_out<F16>(w[e], 0.f);
+        }
+    }
   }
 }
 
@@ -197,31 +221,38 @@ __global__ void __launch_bounds__(kSpThreads)
   const int from = (int)((int64_t)a.chunks * rank / a.split), to = (int)((int64_t)a.chunks * (rank + 1) / a.split);
   const int n = to - from;
 
-  if (warp == 1 && lane == 0) {
-    for (int i = 0; i < n; ++i) {
-      const int st = i % a.stages;
-      if (i >= a.stages) bar_wait(&sm.empty[st], (i / a.stages - 1) & 1, stop);
-      if (*stop) break;
-      unsigned char *const at = stage0 + (size_t)st * stage_bytes;
-      bar_expect(&sm.full[st], stage_bytes);
-      const int x = (from + i) * kPiece;
-      tma_load2(at, &map_w, x, o0, &sm.full[st]);
-      if (GATED) tma_load2(at + kWBytes / 2, &map_u, x, o0, &sm.full[st]);
-      tma_load2(at + kWBytes, &map_x, x, (int)t0, &sm.full[st]);
+  // Both loops are the whole warp's, with one lane that issues: what they count is then
+  // the same in all lanes and stays in uniform registers.  (A loop of one lane, with its
+  // stage by a division: 540 clocks a turn, whatever it loaded.)
+  if (warp == 1) {
+    int st = 0, x = from * kPiece;
+    uint32_t round = 0;  // of the ring
+    for (int i = 0; i < n; ++i, x += kPiece) {
+      if (round > 0) bar_wait(&sm.empty[st], (round - 1) & 1, stop);
+      if (elect_one()) {
+        unsigned char *const at = stage0 + st * stage_bytes;
+        bar_expect(&sm.full[st], stage_bytes);
+        tma_load2(at, &map_w, x, o0, &sm.full[st]);
+        if (GATED) tma_load2(at + kWBytes / 2, &map_u, x, o0, &sm.full[st]);
+        tma_load2(at + kWBytes, &map_x, x, (int)t0, &sm.full[st]);
+      }
+      if (++st == a.stages) st = 0, ++round;
     }
   } else if (warp == 0) {
     const uint32_t idesc = tc_idesc(kRows, a.tokens, F16, false, false);
     const uint32_t base = tc_desc(smem_addr(stage0), 16);
+    int st = 0;
+    uint32_t phase = 0;
     for (int i = 0; i < n; ++i) {
-      const int st = i % a.stages;
-      bar_wait(&sm.full[st], (i / a.stages) & 1, stop);
+      bar_wait(&sm.full[st], phase, stop);
       tc_after_sync();
       if (elect_one()) {
-        const uint32_t w = base + (uint32_t)(st * stage_bytes >> 4), x = w + (kWBytes >> 4);
+        const uint32_t w = base + (st * stage_bytes >> 4), x = w + (kWBytes >> 4);
 #pragma unroll
         for (int k = 0; k < kPiece / 16; ++k) tc_mma(tmem, w + k * 2, x + k * 2, idesc, i > 0 || k > 0);
         tc_commit(i + 1 == n ? &sm.done : &sm.empty[st]);
       }
+      if (++st == a.stages) st = 0, phase ^= 1;
     }
   }
   __syncwarp();
@@ -258,24 +289,24 @@ __global__ void __launch_bounds__(kSpThreads)
   else
     __syncthreads();
   constexpr int kGroups = tile_outputs<GATED>() / 8;
-  const int o = o0 + (threadIdx.x % kGroups) * 8;
+  const int group = threadIdx.x % kGroups, o = o0 + group * 8;
   float b[2][8];
   load_bias<GATED, F16>(a, o, b);
   for (int c = threadIdx.x / kGroups; c < per; c += kSpThreads / kGroups) {
-    float v[8] = {}, u[8] = {};
+    float v[1][8] = {}, u[1][8] = {};
     for (int s = 0; s < a.split; ++s) {
-      const float *const at = sums + (size_t)(s * per + c) * kColFloats + (threadIdx.x % kGroups) * 8;
+      const float *const at = sums + (size_t)(s * per + c) * kColFloats + group * 8;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         const float4 p = *(const float4 *)(at + e);
-        v[e] += p.x, v[e + 1] += p.y, v[e + 2] += p.z, v[e + 3] += p.w;
+        v[0][e] += p.x, v[0][e + 1] += p.y, v[0][e + 2] += p.z, v[0][e + 3] += p.w;
         if (GATED) {
           const float4 q = *(const float4 *)(at + kRows / 2 + e);
-          u[e] += q.x, u[e + 1] += q.y, u[e + 2] += q.z, u[e + 3] += q.w;
+          u[0][e] += q.x, u[0][e + 1] += q.y, u[0][e + 2] += q.z, u[0][e + 3] += q.w;
         }
       }
     }
-    finish8<GATED, F16>(a, t0 + (int64_t)rank * per + c, o, v, u, b);
+    finish<GATED, F16>(a, t0 + (int64_t)rank * per + c, 0, o, v, u, b);
   }
   if (threadIdx.x == 0 && *stop) {
     flag(a.status, kStatusTimeout);
@@ -291,18 +322,18 @@ __global__ void __launch_bounds__(kSpThreads)
 // of the sum costs half the shared-memory reads of two CTAs on their own.  The pairs
 // stay and take tiles in turn; two accumulators let a tile's products run while the
 // one before is on its way out.
-//   warps 0-3  a quarter of the lanes each: sums to shared memory, 32 columns at a
-//              time, and from there the outputs;
-//   warp 4     loads (one lane); warp 5 of the first CTA issues the products of both.
-constexpr int kPaThreads = 192;
+//   warps 0-3, 4-7  a quarter of the lanes each: sums to shared memory, 16 columns at
+//                   a time and the two fours in turn, and from there the outputs;
+//   warp 8          loads; warp 9 of the first CTA issues the products of both.
+constexpr int kPaThreads = 320;
 constexpr int kPaTokens = 256;   // columns at most
 constexpr int kPaStages = 6;
 constexpr int kPaStage = kWBytes + kPaTokens / 2 * kPiece * 2;
-constexpr int kPaOut = 32;       // columns on their way out at a time
+constexpr int kPaOut = 16;       // columns on their way out at a time
 
 struct PairSmem {
   unsigned char stage[kPaStages][kPaStage];
-  float out[2][kPaOut * kColFloats];
+  float out[2][2][kPaOut * kColFloats];  // of each four warps, in turn
   uint64_t full[kPaStages], empty[kPaStages], sums_full[2], sums_empty[2];
   uint32_t tmem;
   int stop[3];  // see bar_wait
@@ -364,8 +395,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
   PairSmem &sm = *reinterpret_cast<PairSmem *>((reinterpret_cast<uintptr_t>(raw_pair) + 1023) & ~(uintptr_t)1023);
   const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  if (warp == 5) tmem_alloc_pair(&sm.tmem, 512);
-  if (threadIdx.x == 128) {
+  if (warp == 9) tmem_alloc_pair(&sm.tmem, 512);
+  if (threadIdx.x == 8 * 32) {
     map_ahead(&map_w);
     if (GATED) map_ahead(&map_u);
     map_ahead(&map_x);
@@ -376,7 +407,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
     }
     for (int k = 0; k < 2; ++k) {
       bar_init(&sm.sums_full[k], 1);
-      bar_init(&sm.sums_empty[k], 8);  // the four warps of both CTAs
+      bar_init(&sm.sums_empty[k], 16);  // the eight warps of both CTAs
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -392,31 +423,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
   constexpr int kOut = tile_outputs<GATED>();
   constexpr uint32_t kCols = 256;  // of an accumulator
 
-  if (warp == 4 && lane == 0) {
+  if (warp == 8) {
     const uint32_t bytes = 2 * (kWBytes + half * kPiece * 2);
     int st = 0;
-    uint32_t round = 0;  // of the ring: the phase of its stages
+    uint32_t round = 0;  // of the ring
     for (int64_t tile = first; tile < a.tiles; tile += pairs) {
       int64_t row_tile, token_tile;
       pair_tile(a, tile, &row_tile, &token_tile);
       const int o = (int)(row_tile * 2 + rank) * kOut, t = (int)(token_tile * a.tokens) + (int)rank * half;
       for (int i = 0; i < a.chunks; ++i) {
         if (round > 0) bar_wait(&sm.empty[st], (round - 1) & 1, stop);
-        if (*stop) break;
-        unsigned char *const at = sm.stage[st];
-        const uint32_t bar = peer_addr(&sm.full[st], 0);
-        if (rank == 0) bar_expect(&sm.full[st], bytes);
-        tma_load2_pair(at, &map_w, i * kPiece, o, bar);
-        if (GATED) tma_load2_pair(at + kWBytes / 2, &map_u, i * kPiece, o, bar);
-        tma_load2_pair(at + kWBytes, &map_x, i * kPiece, t, bar);
+        if (elect_one()) {
+          unsigned char *const at = sm.stage[st];
+          const uint32_t bar = peer_addr(&sm.full[st], 0);
+          if (rank == 0) bar_expect(&sm.full[st], bytes);
+          tma_load2_pair(at, &map_w, i * kPiece, o, bar);
+          if (GATED) tma_load2_pair(at + kWBytes / 2, &map_u, i * kPiece, o, bar);
+          tma_load2_pair(at + kWBytes, &map_x, i * kPiece, t, bar);
+        }
         if (++st == kPaStages) st = 0, ++round;
       }
-      if (*stop) break;
+      if (__any_sync(~0u, *stop)) break;
     }
     // the products have read, and their arrivals reached, every stage before the CTA ends
     for (int k = 0; k < kPaStages; ++k)
       if (round > 0 || k < st) bar_wait(&sm.empty[k], (k < st ? round : round - 1) & 1, stop);
-  } else if (warp == 5 && rank == 0) {
+  } else if (warp == 9 && rank == 0) {
     const uint32_t idesc = tc_idesc(256, a.tokens, F16, false, false), base = tc_desc(smem_addr(sm.stage), 16);
     int st = 0;
     uint32_t phase = 0;
@@ -437,12 +469,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
         }
         if (++st == kPaStages) st = 0, phase ^= 1;
       }
-      if (*stop) break;
+      if (__any_sync(~0u, *stop)) break;
     }
-  } else if (warp < 4) {
-    constexpr int kGroups = kOut / 8;
-    const int row = warp * 32 + lane, group = threadIdx.x % kGroups;
-    const uint32_t lane0 = tmem + ((uint32_t)warp * 32 << 16);
+  } else if (warp < 8) {
+    constexpr int kGroups = kOut / 8, kStep = 128 / kGroups, kN = kPaOut / kStep;  // tokens of a thread at a time
+    const int four = warp >> 2, row = (warp & 3) * 32 + lane, group = threadIdx.x % kGroups;
+    const int c = (threadIdx.x & 127) / kGroups;  // its first token of 16
+    const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
     int n = 0, turn = 0;
     for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
       int64_t row_tile, token_tile;
@@ -454,32 +487,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
       bar_wait(&sm.sums_full[n & 1], (n >> 1) & 1, stop);
       __syncwarp();
       tc_after_sync();
-      for (int c0 = 0; c0 < a.tokens; c0 += kPaOut, turn ^= 1) {
-        float *const out = sm.out[turn];
-        uint32_t r[32];
-        tmem_load32(r, lane0 + (n & 1) * kCols + c0);
+      for (int c0 = four * kPaOut; c0 < a.tokens; c0 += 2 * kPaOut, turn ^= 1) {
+        float *const out = sm.out[four][turn];
+        uint32_t r[16];
+        tmem_load16(r, lane0 + (n & 1) * kCols + c0);
         tmem_wait_load();
-        if (c0 + kPaOut >= a.tokens) {
-          tc_before_sync();
-          __syncwarp();
-          if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
-        }
 #pragma unroll
-        for (int k = 0; k < 32; ++k) out[k * kColFloats + row] = __uint_as_float(r[k]);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int k = 0; k < 16; ++k) out[k * kColFloats + row] = __uint_as_float(r[k]);
+        asm volatile("bar.sync %0, 128;" ::"r"(four + 1) : "memory");
+        float v[kN][8], u[kN][8];
 #pragma unroll
-        for (int c = threadIdx.x / kGroups; c < kPaOut; c += 128 / kGroups) {
-          if (c0 + c >= a.tokens) break;
-          float v[8], u[8];
-          const float *const at = out + c * kColFloats + group * 8;
+        for (int k = 0; k < kN; ++k) {
+          const float *const at = out + (c + k * kStep) * kColFloats + group * 8;
 #pragma unroll
           for (int e = 0; e < 8; e += 4) {
-            *(float4 *)(v + e) = *(const float4 *)(at + e);
-            if (GATED) *(float4 *)(u + e) = *(const float4 *)(at + kRows / 2 + e);
+            *(float4 *)(v[k] + e) = *(const float4 *)(at + e);
+            if (GATED) *(float4 *)(u[k] + e) = *(const float4 *)(at + kRows / 2 + e);
           }
-          finish8<GATED, F16>(a, t0 + c0 + c, o, v, u, b);
         }
+        finish<GATED, F16>(a, t0 + c0 + c, kStep, o, v, u, b);
       }
+      tc_before_sync();
+      __syncwarp();
+      if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
     }
   }
   __syncwarp();
@@ -491,7 +521,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
   }
   __syncthreads();
   cluster_sync();  // the pair ends together
-  if (warp == 5) tmem_free_pair(tmem, 512);
+  if (warp == 9) tmem_free_pair(tmem, 512);
 }
 
 }  // namespace lv
