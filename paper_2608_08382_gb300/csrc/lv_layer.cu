@@ -80,6 +80,29 @@ lv_status limit_smem(KvHost *kv, K kernel, int kind) {
   return LV_OK;
 }
 
+// Launches a kernel that may start while the one before it in the stream still runs
+// (it calls wait_previous itself, when its setup is done); `cluster` CTAs in a cluster,
+// 0 where the kernel says it.
+template <class... P, class... A>
+lv_status launch_after(void (*kernel)(P...), int64_t grid, unsigned block, size_t smem, int cluster, cudaStream_t stream,
+                       const A &...args) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster ? 2 : 1;
+  LV_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+  return LV_OK;
+}
+
 // How a product is cut: by pairs of CTAs, or by CTAs of which `split` share a tile's
 // sum; `tokens` columns a tile.
 struct Shape {
@@ -116,27 +139,14 @@ lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t 
     static_assert(smem <= kMostSmem, "an SM's shared memory");
     st = limit_smem(kv, k_product_pair<GATED, F16>, kind + 4);
     if (st != LV_OK) return st;
-    const unsigned grid = 2 * (unsigned)std::min<int64_t>(a.tiles, kv->sms / 2);
-    k_product_pair<GATED, F16><<<grid, kPaThreads, smem, stream>>>(a, mw, mu, mx);
-    LV_CUDA(cudaGetLastError());
-    return LV_OK;
+    const int64_t grid = 2 * std::min<int64_t>(a.tiles, kv->sms / 2);
+    return launch_after(k_product_pair<GATED, F16>, grid, kPaThreads, smem, 0, stream, a, mw, mu, mx);
   }
   st = limit_smem(kv, k_product<GATED, F16>, kind);
   if (st != LV_OK) return st;
   a.stages = (int)std::min<size_t>((111 << 10) / split_stage(a.tokens), kSpStages);
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = a.split;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(a.tiles * a.split));
-  cfg.blockDim = dim3(kSpThreads);
-  cfg.dynamicSmemBytes = split_smem(a.tokens, a.stages);
-  cfg.stream = stream;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  LV_CUDA(cudaLaunchKernelEx(&cfg, k_product<GATED, F16>, a, mw, mu, mx));
-  return LV_OK;
+  return launch_after(k_product<GATED, F16>, a.tiles * a.split, kSpThreads, split_smem(a.tokens, a.stages), a.split, stream,
+                      a, mw, mu, mx);
 }
 
 lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, const Operands &m, bool gated, cudaStream_t stream) {

@@ -144,6 +144,11 @@ __device__ __forceinline__ void tma_load2(void *to, const CUtensorMap *map, int 
       : "memory");
 }
 
+// The box to L2.
+__device__ __forceinline__ void tma_ahead2(const CUtensorMap *map, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -183,7 +188,7 @@ struct SplitSmem {
 // The stages stand first, from a 1,024-byte boundary on, then this.
 constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPiece * 2; }
 constexpr size_t split_smem(int tokens, int stages) { return 1024 + stages * split_stage(tokens) + sizeof(SplitSmem); }
-static_assert(3 * split_stage(kSpTokens) >= kSpTokens * kColFloats * sizeof(float), "the sums stand in the stages");
+static_assert(3 * split_stage(kSpTokens) >= (kSpTokens + kSpSplit) * kColFloats * sizeof(float), "the sums stand in the stages");
 
 template <bool GATED, bool F16>
 __global__ void __launch_bounds__(kSpThreads)
@@ -212,6 +217,7 @@ __global__ void __launch_bounds__(kSpThreads)
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
+  let_next();
   const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
   volatile int *stop = sm.stop;
   const uint32_t rank = blockIdx.x % a.split;
@@ -220,6 +226,15 @@ __global__ void __launch_bounds__(kSpThreads)
   const int o0 = (int)(tile / a.token_tiles) * tile_outputs<GATED>();
   const int from = (int)((int64_t)a.chunks * rank / a.split), to = (int)((int64_t)a.chunks * (rank + 1) / a.split);
   const int n = to - from;
+  // While the kernel before this one ends, the first weights come as far as L2, where
+  // whatever that kernel may still write to them is seen.
+  if (warp == 1 && elect_one()) {
+    for (int i = 0; i < min(n, a.stages); ++i) {
+      tma_ahead2(&map_w, (from + i) * kPiece, o0);
+      if (GATED) tma_ahead2(&map_u, (from + i) * kPiece, o0);
+    }
+  }
+  wait_previous();
 
   // Both loops are the whole warp's, with one lane that issues: what they count is then
   // the same in all lanes and stays in uniform registers.  (A loop of one lane, with its
@@ -261,26 +276,37 @@ __global__ void __launch_bounds__(kSpThreads)
   tc_after_sync();
   // every CTA's products are done: the stages may hold sums
   float *const sums = reinterpret_cast<float *>(stage0);
-  const int per = a.tokens / a.split;  // columns that a CTA finishes
+  // The columns that CTA r finishes begin at first(r); a part's place is by the CTA that
+  // formed it, then by the column.
+  auto first = [&](int r) { return a.tokens * r / a.split; };
+  const int most = (a.tokens + a.split - 1) / a.split;
   if (a.split > 1)
     cluster_sync();
   else
     __syncthreads();
-  // Warps 0-3 and 4-7 take turns of eight columns; a warp reads its quarter of the lanes.
+  // Warps 0-3 and 4-7 take turns of 16 columns; a warp reads its quarter of the lanes.
   const int row = (warp & 3) * 32 + lane;
   const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
   for (int c0 = (warp >> 2) * 16; c0 < a.tokens; c0 += 32) {
     uint32_t r[16];
     tmem_load16(r, lane0 + c0);
     tmem_wait_load();
+    if (a.split == 1) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const int c = c0 + k, owner = c / per;
-      float *const at = sums + (size_t)(rank * per + c - owner * per) * kColFloats + row;
-      if (a.split > 1)
-        store_peer(peer_addr(at, owner), __uint_as_float(r[k]));
-      else
-        *at = __uint_as_float(r[k]);
+      for (int k = 0; k < 16; ++k) sums[(c0 + k) * kColFloats + row] = __uint_as_float(r[k]);
+    } else {
+      int owner = ((c0 + 1) * a.split - 1) / a.tokens, begin = first(owner), end = first(owner + 1);
+      uint32_t at = peer_addr(sums + (rank * most + c0 - begin) * kColFloats + row, owner);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        if (c0 + k == end) {
+          begin = end;
+          end = first(++owner + 1);
+          at = peer_addr(sums + rank * most * kColFloats + row, owner);
+        }
+        store_peer(at, __uint_as_float(r[k]));
+        at += kColFloats * sizeof(float);
+      }
     }
   }
   tc_before_sync();
@@ -292,10 +318,11 @@ __global__ void __launch_bounds__(kSpThreads)
   const int group = threadIdx.x % kGroups, o = o0 + group * 8;
   float b[2][8];
   load_bias<GATED, F16>(a, o, b);
-  for (int c = threadIdx.x / kGroups; c < per; c += kSpThreads / kGroups) {
+  const int begin = first(rank), mine = first(rank + 1) - begin;
+  for (int c = threadIdx.x / kGroups; c < mine; c += kSpThreads / kGroups) {
     float v[1][8] = {}, u[1][8] = {};
     for (int s = 0; s < a.split; ++s) {
-      const float *const at = sums + (size_t)(s * per + c) * kColFloats + group * 8;
+      const float *const at = sums + (s * most + c) * kColFloats + group * 8;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         const float4 p = *(const float4 *)(at + e);
@@ -306,7 +333,7 @@ __global__ void __launch_bounds__(kSpThreads)
         }
       }
     }
-    finish<GATED, F16>(a, t0 + (int64_t)rank * per + c, 0, o, v, u, b);
+    finish<GATED, F16>(a, t0 + begin + c, 0, o, v, u, b);
   }
   if (threadIdx.x == 0 && *stop) {
     flag(a.status, kStatusTimeout);
@@ -416,6 +443,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
   __syncthreads();
   cluster_sync();
   tc_after_sync();
+  let_next();
+  wait_previous();
   const uint32_t tmem = __shfl_sync(~0u, sm.tmem, 0);
   volatile int *stop = sm.stop;
   const int64_t pairs = gridDim.x / 2, first = blockIdx.x / 2;
