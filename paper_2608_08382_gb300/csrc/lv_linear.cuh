@@ -84,39 +84,61 @@ __device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)
       b[k][e] = a.bias[k] && o + e < a.d_out ? value_of<F16>(((const uint16_t *)a.bias[k])[o + e]) : 0.f;
 }
 
-// Outputs o .. o + 7 of N tokens t, t + step, .. from their sums (and the second ones, u);
-// tokens past the call's are left out.
-template <bool GATED, bool F16, int N>
-__device__ __forceinline__ void finish(const LinearArgs &a, int64_t t, int step, int o, float (&v)[N][8],
-                                       const float (&u)[N][8], const float (&b)[2][8]) {
-  if (o >= a.d_out) return;
-  const bool whole = o + 8 <= a.d_out;
-  const int64_t end = a.n_tok;
-  uint4 r[N];
-  if (!GATED && a.residual && whole)
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (t + k * step < end) r[k] = *(const uint4 *)((const uint16_t *)a.residual + (t + k * step) * a.r_stride + o);
+// A thread's outputs: eight neighbours of a token, `step` tokens on at a time.
+struct Outputs {
+  uint16_t *y;
+  const uint16_t *r;   // what is added, or null
+  int64_t y_step, r_step;
+  int n;               // outputs that there are from the first on: 0 for none
+  int left;            // tokens from the first one on
+};
+template <bool GATED>
+__device__ __forceinline__ Outputs outputs_at(const LinearArgs &a, int64_t t, int step, int o) {
+  Outputs p;
+  p.y = (uint16_t *)a.y + t * a.y_stride + o;
+  p.r = !GATED && a.residual ? (const uint16_t *)a.residual + t * a.r_stride + o : nullptr;
+  p.y_step = step * a.y_stride;
+  p.r_step = step * a.r_stride;
+  p.n = a.d_out - o;
+  p.left = p.n > 0 ? (int)min((int64_t)INT_MAX, a.n_tok - t) : 0;
+  return p;
+}
+
+// What is added to the outputs of N tokens in a row of steps, `ahead` tokens on, asked
+// for before their sums where all eight are there.
+template <int N>
+__device__ __forceinline__ void load_residual(const Outputs &p, int step, int ahead, uint4 (&r)[N]) {
+  if (!p.r || p.n < 8) return;
 #pragma unroll
   for (int k = 0; k < N; ++k)
+    if (ahead + k * step < p.left) r[k] = *(const uint4 *)(p.r + ahead / step * p.r_step + k * p.r_step);
+}
+
+// The outputs of N tokens from their sums (and the second ones, u).
+template <bool GATED, bool F16, int N>
+__device__ __forceinline__ void finish(const LinearArgs &a, const Outputs &p, int step, float (&v)[N][8],
+                                       const float (&u)[N][8], const float (&b)[2][8], const uint4 (&r)[N]) {
+  if (a.bias[0])
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[k][e] += b[0][e];
-  switch (a.act) {
-    case LV_ACT_SILU: activate<LV_ACT_SILU>(v); break;
-    case LV_ACT_GELU: activate<LV_ACT_GELU>(v); break;
-    case LV_ACT_GELU_TANH: activate<LV_ACT_GELU_TANH>(v); break;
-    case LV_ACT_RELU: activate<LV_ACT_RELU>(v); break;
-  }
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[k][e] += b[0][e];
+  if (a.act != LV_ACT_NONE) switch (a.act) {
+      case LV_ACT_SILU: activate<LV_ACT_SILU>(v); break;
+      case LV_ACT_GELU: activate<LV_ACT_GELU>(v); break;
+      case LV_ACT_GELU_TANH: activate<LV_ACT_GELU_TANH>(v); break;
+      case LV_ACT_RELU: activate<LV_ACT_RELU>(v); break;
+    }
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    if (t + k * step >= end) continue;
+    if (k * step >= p.left) continue;
     float(&w)[8] = v[k];
     if (GATED)
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] *= u[k][e] + b[1][e];
-    uint16_t *const y = (uint16_t *)a.y + (t + k * step) * a.y_stride + o;
-    if (whole) {
-      if (!GATED && a.residual) {
+    uint16_t *const y = p.y + k * p.y_step;
+    if (p.n >= 8) {
+      if (!GATED && p.r) {
         float x[8];
         unpack8<F16>(r[k], x);
 #pragma unroll
@@ -125,14 +147,83 @@ __device__ __forceinline__ void finish(const LinearArgs &a, int64_t t, int step,
       *(uint4 *)y = make_uint4(pack_out<F16>(w[0], w[1]), pack_out<F16>(w[2], w[3]), pack_out<F16>(w[4], w[5]),
                                pack_out<F16>(w[6], w[7]));
     } else {
-      const uint16_t *const rp = (const uint16_t *)a.residual + (t + k * step) * a.r_stride + o;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (o + e < a.d_out) {
-          if (!GATED && a.residual) w[e] += value_of<F16>(rp[e]);
+        if (e < p.n) {
+          if (!GATED && p.r) w[e] += value_of<F16>(p.r[k * p.r_step + e]);
           y[e] = (uint16_t)pack_out<F16>(w[e], 0.f);
         }
     }
+  }
+}
+// Tokens on: `steps` steps of `step`.
+__device__ __forceinline__ void advance(Outputs &p, int steps, int step) {
+  p.y += steps * p.y_step;
+  if (p.r) p.r += steps * p.r_step;
+  p.left -= steps * step;
+}
+
+// An accumulator on its way out, by eight warps: warp w has a quarter of the lanes,
+// 32 (w & 3) on, and the 16 columns of every second turn.  16 columns of 32 rows go
+// through shared memory, without padding (a column's pieces of four floats are
+// exchanged by its number, so that neither side meets a bank twice), and come back as
+// eight outputs of a token a thread.  Plain: a warp's rows are its own outputs, and no
+// other warp is waited for.  Gated: the rows 64 on are the second sums of a warp two
+// on; the two meet at a barrier of theirs and finish eight columns each.  The next
+// columns and what is added to them are on their way meanwhile.  (With 32 columns of
+// all 128 rows between barriers of four warps, and nothing ahead: 950 clocks for 16
+// columns.)
+constexpr int kOutCols = 16, kOutFloats = kOutCols * 32;  // of a warp, twice
+template <bool GATED, bool F16, class F>
+__device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, float *out, int warp, int lane, int64_t t0, int o0,
+                                      F all_read) {
+  constexpr int kN = GATED ? 1 : 2;
+  const int four = warp >> 2, quarter = warp & 3, group = lane & 3;
+  const int o = o0 + (GATED ? quarter & 1 : quarter) * 32 + group * 8;
+  const int c = (lane >> 2) + (GATED ? (quarter >> 1) * 8 : 0);  // its first column of 16
+  const uint32_t at = tmem + ((uint32_t)quarter * 32 << 16);
+  // buffers of a warp's (or of the two warps') turns
+  float *const mine = out + warp * 2 * kOutFloats, *const first = out + (GATED ? warp & ~2 : warp) * 2 * kOutFloats,
+               *const second = out + (warp | 2) * 2 * kOutFloats;
+  float b[2][8];
+  load_bias<GATED, F16>(a, o, b);
+  constexpr int kTurn = 2 * kOutCols;  // from a warp's columns to its next
+  uint32_t r[16];
+  uint4 next[kN];
+  int c0 = four * kOutCols, turn = 0;
+  Outputs p = outputs_at<GATED>(a, t0 + c0 + c, 8, o);
+  if (c0 < a.tokens) {
+    tmem_load16(r, at + c0);
+    load_residual(p, 8, 0, next);
+  } else {
+    all_read();
+  }
+  for (; c0 < a.tokens; c0 += kTurn, turn ^= kOutFloats) {
+    tmem_wait_load();
+    const bool last = c0 + kTurn >= a.tokens;
+    if (last) all_read();
+#pragma unroll
+    for (int k = 0; k < kOutCols; ++k) mine[turn + k * 32 + (lane ^ (k & 7) * 4)] = __uint_as_float(r[k]);
+    if (GATED)
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + four * 2 + (quarter & 1)) : "memory");
+    else
+      __syncwarp();
+    if (!last) tmem_load16(r, at + c0 + kTurn);
+    float v[kN][8], u[kN][8];
+    uint4 now[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      now[k] = next[k];
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const int from = turn + (c + k * 8) * 32 + ((group * 8 + e) ^ (c & 7) * 4);
+        *(float4 *)(v[k] + e) = *(const float4 *)(first + from);
+        if (GATED) *(float4 *)(u[k] + e) = *(const float4 *)(second + from);
+      }
+    }
+    if (!last) load_residual(p, 8, kTurn, next);
+    finish<GATED, F16>(a, p, 8, v, u, b, now);
+    advance(p, kTurn / 8, 8);
   }
 }
 
@@ -189,6 +280,68 @@ struct SplitSmem {
 constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPiece * 2; }
 constexpr size_t split_smem(int tokens, int stages) { return 1024 + stages * split_stage(tokens) + sizeof(SplitSmem); }
 static_assert(3 * split_stage(kSpTokens) >= (kSpTokens + kSpSplit) * kColFloats * sizeof(float), "the sums stand in the stages");
+
+// The parts of a tile's sums to the CTAs that finish them, and out from there.  The
+// columns that CTA r finishes begin at first(r); a part's place is by the CTA that
+// formed it, then by the column.
+template <bool GATED, bool F16>
+__device__ __forceinline__ void join(const LinearArgs &a, uint32_t tmem, float *sums, int warp, int lane, uint32_t rank,
+                                     int64_t t0, int o0) {
+  auto first = [&](int r) { return a.tokens * r / a.split; };
+  const int most = (a.tokens + a.split - 1) / a.split;
+  cluster_sync();
+  // Warps 0-3 and 4-7 take turns of 16 columns; a warp reads its quarter of the lanes.
+  const int row = (warp & 3) * 32 + lane;
+  const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
+  for (int c0 = (warp >> 2) * 16; c0 < a.tokens; c0 += 32) {
+    uint32_t r[16];
+    tmem_load16(r, lane0 + c0);
+    tmem_wait_load();
+    int owner = ((c0 + 1) * a.split - 1) / a.tokens, begin = first(owner), end = first(owner + 1);
+    uint32_t at = peer_addr(sums + (rank * most + c0 - begin) * kColFloats + row, owner);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      if (c0 + k == end) {
+        begin = end;
+        end = first(++owner + 1);
+        at = peer_addr(sums + rank * most * kColFloats + row, owner);
+      }
+      store_peer(at, __uint_as_float(r[k]));
+      at += kColFloats * sizeof(float);
+    }
+  }
+  constexpr int kGroups = tile_outputs<GATED>() / 8;
+  const int group = threadIdx.x % kGroups, o = o0 + group * 8;
+  float b[2][8];
+  load_bias<GATED, F16>(a, o, b);
+  const int begin = first(rank), mine = first(rank + 1) - begin;
+  constexpr int kStep = kSpThreads / kGroups;
+  int c = threadIdx.x / kGroups;
+  Outputs p = outputs_at<GATED>(a, t0 + begin + c, kStep, o);
+  p.left = min(p.left, mine - c);
+  uint4 next[1];
+  load_residual(p, kStep, 0, next);
+  cluster_sync();
+  for (; c < mine; c += kStep) {
+    float v[1][8] = {}, u[1][8] = {};
+    for (int s = 0; s < a.split; ++s) {
+      const float *const at = sums + (s * most + c) * kColFloats + group * 8;
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const float4 q = *(const float4 *)(at + e);
+        v[0][e] += q.x, v[0][e + 1] += q.y, v[0][e + 2] += q.z, v[0][e + 3] += q.w;
+        if (GATED) {
+          const float4 w = *(const float4 *)(at + kRows / 2 + e);
+          u[0][e] += w.x, u[0][e + 1] += w.y, u[0][e + 2] += w.z, u[0][e + 3] += w.w;
+        }
+      }
+    }
+    const uint4 now[1] = {next[0]};
+    load_residual(p, kStep, kStep, next);
+    finish<GATED, F16>(a, p, kStep, v, u, b, now);
+    advance(p, 1, kStep);
+  }
+}
 
 template <bool GATED, bool F16>
 __global__ void __launch_bounds__(kSpThreads)
@@ -276,65 +429,13 @@ __global__ void __launch_bounds__(kSpThreads)
   tc_after_sync();
   // every CTA's products are done: the stages may hold sums
   float *const sums = reinterpret_cast<float *>(stage0);
-  // The columns that CTA r finishes begin at first(r); a part's place is by the CTA that
-  // formed it, then by the column.
-  auto first = [&](int r) { return a.tokens * r / a.split; };
-  const int most = (a.tokens + a.split - 1) / a.split;
-  if (a.split > 1)
-    cluster_sync();
-  else
+  if (a.split == 1) {
     __syncthreads();
-  // Warps 0-3 and 4-7 take turns of 16 columns; a warp reads its quarter of the lanes.
-  const int row = (warp & 3) * 32 + lane;
-  const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
-  for (int c0 = (warp >> 2) * 16; c0 < a.tokens; c0 += 32) {
-    uint32_t r[16];
-    tmem_load16(r, lane0 + c0);
-    tmem_wait_load();
-    if (a.split == 1) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) sums[(c0 + k) * kColFloats + row] = __uint_as_float(r[k]);
-    } else {
-      int owner = ((c0 + 1) * a.split - 1) / a.tokens, begin = first(owner), end = first(owner + 1);
-      uint32_t at = peer_addr(sums + (rank * most + c0 - begin) * kColFloats + row, owner);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        if (c0 + k == end) {
-          begin = end;
-          end = first(++owner + 1);
-          at = peer_addr(sums + rank * most * kColFloats + row, owner);
-        }
-        store_peer(at, __uint_as_float(r[k]));
-        at += kColFloats * sizeof(float);
-      }
-    }
+    drain<GATED, F16>(a, tmem, sums, warp, lane, t0, o0, [] {});
+  } else {
+    join<GATED, F16>(a, tmem, sums, warp, lane, rank, t0, o0);
   }
   tc_before_sync();
-  if (a.split > 1)
-    cluster_sync();
-  else
-    __syncthreads();
-  constexpr int kGroups = tile_outputs<GATED>() / 8;
-  const int group = threadIdx.x % kGroups, o = o0 + group * 8;
-  float b[2][8];
-  load_bias<GATED, F16>(a, o, b);
-  const int begin = first(rank), mine = first(rank + 1) - begin;
-  for (int c = threadIdx.x / kGroups; c < mine; c += kSpThreads / kGroups) {
-    float v[1][8] = {}, u[1][8] = {};
-    for (int s = 0; s < a.split; ++s) {
-      const float *const at = sums + (s * most + c) * kColFloats + group * 8;
-#pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const float4 p = *(const float4 *)(at + e);
-        v[0][e] += p.x, v[0][e + 1] += p.y, v[0][e + 2] += p.z, v[0][e + 3] += p.w;
-        if (GATED) {
-          const float4 q = *(const float4 *)(at + kRows / 2 + e);
-          u[0][e] += q.x, u[0][e + 1] += q.y, u[0][e + 2] += q.z, u[0][e + 3] += q.w;
-        }
-      }
-    }
-    finish<GATED, F16>(a, t0 + begin + c, 0, o, v, u, b);
-  }
   if (threadIdx.x == 0 && *stop) {
     flag(a.status, kStatusTimeout);
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);  // what was issued may still be at work on shared memory
@@ -349,18 +450,16 @@ __global__ void __launch_bounds__(kSpThreads)
 // of the sum costs half the shared-memory reads of two CTAs on their own.  The pairs
 // stay and take tiles in turn; two accumulators let a tile's products run while the
 // one before is on its way out.
-//   warps 0-3, 4-7  a quarter of the lanes each: sums to shared memory, 16 columns at
-//                   a time and the two fours in turn, and from there the outputs;
-//   warp 8          loads; warp 9 of the first CTA issues the products of both.
+//   warps 0-7  a tile's way out (drain);
+//   warp 8     loads; warp 9 of the first CTA issues the products of both.
 constexpr int kPaThreads = 320;
 constexpr int kPaTokens = 256;   // columns at most
 constexpr int kPaStages = 6;
 constexpr int kPaStage = kWBytes + kPaTokens / 2 * kPiece * 2;
-constexpr int kPaOut = 16;       // columns on their way out at a time
 
 struct PairSmem {
   unsigned char stage[kPaStages][kPaStage];
-  float out[2][2][kPaOut * kColFloats];  // of each four warps, in turn
+  float out[8 * 2 * kOutFloats];
   uint64_t full[kPaStages], empty[kPaStages], sums_full[2], sums_empty[2];
   uint32_t tmem;
   int stop[3];  // see bar_wait
@@ -398,8 +497,10 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t d, uint32_t a, uint32_t b, 
       "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
       : "memory");
 }
+// An arrival that says no more than that tensor memory has been read (the loads were
+// waited for); one that released the thread's stores would wait for them.
 __device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // First outputs and tokens of a tile: bands of eight row tiles, row tile after row tile
@@ -501,44 +602,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
       if (__any_sync(~0u, *stop)) break;
     }
   } else if (warp < 8) {
-    constexpr int kGroups = kOut / 8, kStep = 128 / kGroups, kN = kPaOut / kStep;  // tokens of a thread at a time
-    const int four = warp >> 2, row = (warp & 3) * 32 + lane, group = threadIdx.x % kGroups;
-    const int c = (threadIdx.x & 127) / kGroups;  // its first token of 16
-    const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
-    int n = 0, turn = 0;
+    int n = 0;
     for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
       int64_t row_tile, token_tile;
       pair_tile(a, tile, &row_tile, &token_tile);
-      const int64_t t0 = token_tile * a.tokens;
-      const int o = (int)(row_tile * 2 + rank) * kOut + group * 8;
-      float b[2][8];
-      load_bias<GATED, F16>(a, o, b);
       bar_wait(&sm.sums_full[n & 1], (n >> 1) & 1, stop);
       __syncwarp();
       tc_after_sync();
-      for (int c0 = four * kPaOut; c0 < a.tokens; c0 += 2 * kPaOut, turn ^= 1) {
-        float *const out = sm.out[four][turn];
-        uint32_t r[16];
-        tmem_load16(r, lane0 + (n & 1) * kCols + c0);
-        tmem_wait_load();
-#pragma unroll
-        for (int k = 0; k < 16; ++k) out[k * kColFloats + row] = __uint_as_float(r[k]);
-        asm volatile("bar.sync %0, 128;" ::"r"(four + 1) : "memory");
-        float v[kN][8], u[kN][8];
-#pragma unroll
-        for (int k = 0; k < kN; ++k) {
-          const float *const at = out + (c + k * kStep) * kColFloats + group * 8;
-#pragma unroll
-          for (int e = 0; e < 8; e += 4) {
-            *(float4 *)(v[k] + e) = *(const float4 *)(at + e);
-            if (GATED) *(float4 *)(u[k] + e) = *(const float4 *)(at + kRows / 2 + e);
-          }
-        }
-        finish<GATED, F16>(a, t0 + c0 + c, kStep, o, v, u, b);
-      }
-      tc_before_sync();
-      __syncwarp();
-      if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
+      drain<GATED, F16>(a, tmem + (n & 1) * kCols, sm.out, warp, lane, token_tile * a.tokens,
+                        (int)(row_tile * 2 + rank) * kOut, [&] {
+                          tc_before_sync();
+                          __syncwarp();
+                          if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
+                        });
     }
   }
   __syncwarp();
