@@ -51,11 +51,22 @@ __device__ __forceinline__ float activated(float x) {
   return ACT == LV_ACT_RELU && x < 0.f ? 0.f : x;
 }
 template <int ACT, int N>
-__device__ __forceinline__ void activate(float (&v)[N][8]) {
+__device__ __forceinline__ void activate_all(float *v) {
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[k][e] = activated<ACT>(v[k][e]);
+  for (int k = 0; k < N; ++k) v[k] = activated<ACT>(v[k]);
+}
+// Of a whole array: one decision.
+template <class A>
+__device__ __forceinline__ void activate(A &array, int act) {
+  constexpr int kN = sizeof(A) / sizeof(float);
+  float *const v = reinterpret_cast<float *>(&array);
+  if (act == LV_ACT_NONE) return;
+  switch (act) {
+    case LV_ACT_SILU: activate_all<LV_ACT_SILU, kN>(v); break;
+    case LV_ACT_GELU: activate_all<LV_ACT_GELU, kN>(v); break;
+    case LV_ACT_GELU_TANH: activate_all<LV_ACT_GELU_TANH, kN>(v); break;
+    default: activate_all<LV_ACT_RELU, kN>(v);
+  }
 }
 
 constexpr int kPiece = 64;                    // of the sum, in a stage
@@ -123,12 +134,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, const Outputs &p, in
     for (int k = 0; k < N; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[k][e] += b[0][e];
-  if (a.act != LV_ACT_NONE) switch (a.act) {
-      case LV_ACT_SILU: activate<LV_ACT_SILU>(v); break;
-      case LV_ACT_GELU: activate<LV_ACT_GELU>(v); break;
-      case LV_ACT_GELU_TANH: activate<LV_ACT_GELU_TANH>(v); break;
-      case LV_ACT_RELU: activate<LV_ACT_RELU>(v); break;
-    }
+  activate(v, a.act);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     if (k * step >= p.left) continue;
@@ -163,67 +169,189 @@ __device__ __forceinline__ void advance(Outputs &p, int steps, int step) {
   p.left -= steps * step;
 }
 
+// 16 rows by 16 columns of tensor memory, as four 8 x 8 blocks: r[4 h + 2 g + k] is column
+// 8 h + 2 (lane & 3) + k of row 8 g + lane / 4.
+__device__ __forceinline__ void tmem_load_blocks(uint32_t *r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(at));
+}
+// Four 8 x 8 blocks of 16-bit values, a pair of columns of row lane / 4 a register, to
+// or from shared memory with their columns as its rows: lane l gives the place of
+// column l & 7 of block l / 8.
+__device__ __forceinline__ void store_turned(uint32_t at, const uint32_t *w) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]),
+               "r"(w[2]), "r"(w[3])
+               : "memory");
+}
+__device__ __forceinline__ void load_turned(uint32_t *w, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(at)
+               : "memory");
+}
+
+// Eight outputs in a row from or to memory; n of them are there.
+__device__ __forceinline__ uint4 load_some(const uint16_t *p, int n) {
+  if (n >= 8) return *(const uint4 *)p;
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) w[e >> 1] |= (uint32_t)p[e] << (e & 1) * 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
+  if (n >= 8) {
+    *(uint4 *)p = v;
+    return;
+  }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) p[e] = (uint16_t)(w[e >> 1] >> (e & 1) * 16);
+}
+
 // An accumulator on its way out, by eight warps: warp w has a quarter of the lanes,
-// 32 (w & 3) on, and the 16 columns of every second turn.  16 columns of 32 rows go
-// through shared memory, without padding (a column's pieces of four floats are
-// exchanged by its number, so that neither side meets a bank twice), and come back as
-// eight outputs of a token a thread.  Plain: a warp's rows are its own outputs, and no
-// other warp is waited for.  Gated: the rows 64 on are the second sums of a warp two
-// on; the two meet at a barrier of theirs and finish eight columns each.  The next
-// columns and what is added to them are on their way meanwhile.  (With 32 columns of
-// all 128 rows between barriers of four warps, and nothing ahead: 950 clocks for 16
-// columns.)
-constexpr int kOutCols = 16, kOutFloats = kOutCols * 32;  // of a warp, twice
+// 32 (w & 3) on, and the 16 columns of every second turn.  It reads them in 8 x 8
+// blocks, which hold a row's neighbouring columns; turned on their way through shared
+// memory as 16-bit values they become a token's neighbouring outputs, 16 bytes a
+// thread, 64 a token.  The residual comes in the other way round.  A token's 64 bytes
+// stand at 64 times its number there, their four pieces exchanged by half the number,
+// so that no access meets a bank twice.  Plain: a warp's rows are its own outputs, and
+// no other warp is waited for.  Gated: the rows 64 on are the second sums of a warp
+// two on; the two exchange eight columns each, in fp32.  The next columns and what is
+// added to them are on their way meanwhile.  (In fp32 through shared memory, a row a
+// thread: 160 instructions and 1,200 clocks for 16 columns.)
+constexpr int kOutCols = 16;
+struct OutRoom {             // of a warp, for two turns
+  uint4 out[2][kOutCols * 4];
+  uint4 add[2][kOutCols * 4];  // the residual, or the other warp's sums
+};
 template <bool GATED, bool F16, class F>
-__device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, float *out, int warp, int lane, int64_t t0, int o0,
+__device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoom *rooms, int warp, int lane, int64_t t0, int o0,
                                       F all_read) {
-  constexpr int kN = GATED ? 1 : 2;
-  const int four = warp >> 2, quarter = warp & 3, group = lane & 3;
-  const int o = o0 + (GATED ? quarter & 1 : quarter) * 32 + group * 8;
-  const int c = (lane >> 2) + (GATED ? (quarter >> 1) * 8 : 0);  // its first column of 16
+  constexpr int kHalves = GATED ? 1 : 2;  // eights of columns that a warp finishes
+  constexpr int kTurn = 2 * kOutCols;     // from a warp's columns to its next
+  const int four = warp >> 2, quarter = warp & 3;
+  const int row0 = o0 + (GATED ? quarter & 1 : quarter) * 32;  // the output of the warp's first row
+  const int own = GATED ? quarter >> 1 : 0;                    // its first eight
   const uint32_t at = tmem + ((uint32_t)quarter * 32 << 16);
-  // buffers of a warp's (or of the two warps') turns
-  float *const mine = out + warp * 2 * kOutFloats, *const first = out + (GATED ? warp & ~2 : warp) * 2 * kOutFloats,
-               *const second = out + (warp | 2) * 2 * kOutFloats;
-  float b[2][8];
-  load_bias<GATED, F16>(a, o, b);
-  constexpr int kTurn = 2 * kOutCols;  // from a warp's columns to its next
+  OutRoom &room = rooms[warp], &other = rooms[warp ^ 2];
+  // in shared memory: this lane's place among the blocks, and its token and piece
+  const int bt = lane & 7, bp = (lane >> 3) ^ (bt >> 1 & 3), block = bt * 4 + bp;
+  const int mt = lane >> 2, piece = mt * 4 + ((lane & 3) ^ (mt >> 1 & 3));
+  // in memory
+  int c0 = four * kOutCols;
+  const int o = row0 + (lane & 3) * 8, n = a.d_out - o;
+  const int64_t first = t0 + c0 + own * 8 + mt;
+  int left = n > 0 ? (int)min((int64_t)INT_MAX, a.n_tok - first) : 0;
+  uint16_t *y = (uint16_t *)a.y + first * a.y_stride + o;
+  const uint16_t *rp = (const uint16_t *)a.residual + first * a.r_stride + o;
+  const bool adds = !GATED && a.residual;
+  float b[2][4] = {};
+#pragma unroll
+  for (int k = 0; k < (GATED ? 2 : 1); ++k)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int f = row0 + g * 8 + (lane >> 2);
+      if (a.bias[k] && f < a.d_out) b[k][g] = value_of<F16>(((const uint16_t *)a.bias[k])[f]);
+    }
   uint32_t r[16];
-  uint4 next[kN];
-  int c0 = four * kOutCols, turn = 0;
-  Outputs p = outputs_at<GATED>(a, t0 + c0 + c, 8, o);
+  uint4 next[2];
+  auto ask = [&] {
+    if (adds)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (h * 8 < left) next[h] = load_some(rp + h * 8 * a.r_stride, n);
+  };
+  auto read = [&](int c) {
+    tmem_load_blocks(r, at + c);
+    tmem_load_blocks(r + 8, at + (16u << 16) + c);
+  };
   if (c0 < a.tokens) {
-    tmem_load16(r, at + c0);
-    load_residual(p, 8, 0, next);
+    read(c0);
+    ask();
   } else {
     all_read();
   }
-  for (; c0 < a.tokens; c0 += kTurn, turn ^= kOutFloats) {
+  for (int turn = 0; c0 < a.tokens; c0 += kTurn, turn ^= 1) {
+    if (adds) {
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) room.add[turn][h * 32 + piece] = next[h];
+      __syncwarp();
+    }
     tmem_wait_load();
     const bool last = c0 + kTurn >= a.tokens;
     if (last) all_read();
+    float v[kHalves][4][2], u[4][2];
+    if (GATED) {
+      float *const to = (float *)room.add[turn], *const from = (float *)other.add[turn];
 #pragma unroll
-    for (int k = 0; k < kOutCols; ++k) mine[turn + k * 32 + (lane ^ (k & 7) * 4)] = __uint_as_float(r[k]);
-    if (GATED)
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t mine = (g >> 1) * 8 + (g & 1) * 2 + k;  // in r, of the first eight columns
+          const float p = __uint_as_float(r[mine]), q = __uint_as_float(r[mine + 4]);
+          v[0][g][k] = own ? q : p;
+          to[(g * 2 + k) * 32 + lane] = own ? p : q;
+        }
       asm volatile("bar.sync %0, 64;" ::"r"(1 + four * 2 + (quarter & 1)) : "memory");
-    else
-      __syncwarp();
-    if (!last) tmem_load16(r, at + c0 + kTurn);
-    float v[kN][8], u[kN][8];
-    uint4 now[kN];
 #pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      now[k] = next[k];
+      for (int g = 0; g < 4; ++g)
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const int from = turn + (c + k * 8) * 32 + ((group * 8 + e) ^ (c & 7) * 4);
-        *(float4 *)(v[k] + e) = *(const float4 *)(first + from);
-        if (GATED) *(float4 *)(u[k] + e) = *(const float4 *)(second + from);
-      }
+        for (int k = 0; k < 2; ++k) {
+          u[g][k] = from[(g * 2 + k) * 32 + lane];
+          if (own) {  // these rows are the second sums
+            const float x = v[0][g][k];
+            v[0][g][k] = u[g][k];
+            u[g][k] = x;
+          }
+        }
+    } else {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) v[h][g][k] = __uint_as_float(r[(g >> 1) * 8 + h * 4 + (g & 1) * 2 + k]);
     }
-    if (!last) load_residual(p, 8, kTurn, next);
-    finish<GATED, F16>(a, p, 8, v, u, b, now);
-    advance(p, kTurn / 8, 8);
+    if (!last) read(c0 + kTurn);
+    left -= kTurn;
+    rp += kTurn * a.r_stride;
+    if (!last) ask();
+    if (a.bias[0])
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) v[h][g][k] += b[0][g];
+    activate(v, a.act);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      uint32_t w[4];
+      if (GATED)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) v[h][g][k] *= u[g][k] + b[1][g];
+      if (adds) {
+        load_turned(w, smem_addr(&room.add[turn][h * 32 + block]));
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) v[h][g][k] += value_of<F16>((uint16_t)(w[g] >> k * 16));
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) w[g] = pack_out<F16>(v[h][g][0], v[h][g][1]);
+      store_turned(smem_addr(&room.out[turn][h * 32 + block]), w);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+      if (h * 8 < left + kTurn) store_some(y + h * 8 * a.y_stride, room.out[turn][h * 32 + piece], n);
+    y += kTurn * a.y_stride;
   }
 }
 
@@ -431,7 +559,7 @@ __global__ void __launch_bounds__(kSpThreads)
   float *const sums = reinterpret_cast<float *>(stage0);
   if (a.split == 1) {
     __syncthreads();
-    drain<GATED, F16>(a, tmem, sums, warp, lane, t0, o0, [] {});
+    drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, [] {});
   } else {
     join<GATED, F16>(a, tmem, sums, warp, lane, rank, t0, o0);
   }
@@ -459,7 +587,7 @@ constexpr int kPaStage = kWBytes + kPaTokens / 2 * kPiece * 2;
 
 struct PairSmem {
   unsigned char stage[kPaStages][kPaStage];
-  float out[8 * 2 * kOutFloats];
+  OutRoom out[8];
   uint64_t full[kPaStages], empty[kPaStages], sums_full[2], sums_empty[2];
   uint32_t tmem;
   int stop[3];  // see bar_wait
