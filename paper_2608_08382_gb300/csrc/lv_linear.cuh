@@ -191,14 +191,11 @@ __device__ __forceinline__ void load_turned(uint32_t *w, uint32_t at) {
                : "memory");
 }
 
-// Eight outputs in a row from or to memory; n of them are there.
-__device__ __forceinline__ uint4 load_some(const uint16_t *p, int n) {
-  if (n >= 8) return *(const uint4 *)p;
-  uint32_t w[4] = {};
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) w[e >> 1] |= (uint32_t)p[e] << (e & 1) * 16;
-  return make_uint4(w[0], w[1], w[2], w[3]);
+// Eight 16-bit values in a row to memory, or from there to shared memory with zeros for
+// those that are not there; n of them are.
+__device__ __forceinline__ void copy_some(uint4 *to, const uint16_t *p, int n) {
+  const int bytes = min(max(n, 0), 8) * 2;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(p), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
   if (n >= 8) {
@@ -219,17 +216,19 @@ __device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
 // stand at 64 times its number there, their four pieces exchanged by half the number,
 // so that no access meets a bank twice.  Plain: a warp's rows are its own outputs, and
 // no other warp is waited for.  Gated: the rows 64 on are the second sums of a warp
-// two on; the two exchange eight columns each, in fp32.  The next columns and what is
-// added to them are on their way meanwhile.  (In fp32 through shared memory, a row a
+// two on; the two exchange eight columns each, in fp32.  The next columns are on their
+// way meanwhile, and what is added to them two turns ahead, from before the sums are
+// ready on.  (In fp32 through shared memory, a row a
 // thread: 160 instructions and 1,200 clocks for 16 columns.)
 constexpr int kOutCols = 16;
-struct OutRoom {             // of a warp, for two turns
-  uint4 out[2][kOutCols * 4];
-  uint4 add[2][kOutCols * 4];  // the residual, or the other warp's sums
+constexpr int kAhead = 3;    // turns whose residual has a place
+struct OutRoom {             // of a warp
+  uint4 out[kOutCols * 4];
+  uint4 add[kAhead][kOutCols * 4];  // the residual, or the other warp's sums
 };
-template <bool GATED, bool F16, class F>
+template <bool GATED, bool F16, class R, class F>
 __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoom *rooms, int warp, int lane, int64_t t0, int o0,
-                                      F all_read) {
+                                      R ready, F all_read) {
   constexpr int kHalves = GATED ? 1 : 2;  // eights of columns that a warp finishes
   constexpr int kTurn = 2 * kOutCols;     // from a warp's columns to its next
   const int four = warp >> 2, quarter = warp & 3;
@@ -257,28 +256,33 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
       if (a.bias[k] && f < a.d_out) b[k][g] = value_of<F16>(((const uint16_t *)a.bias[k])[f]);
     }
   uint32_t r[16];
-  uint4 next[2];
-  auto ask = [&] {
-    if (adds)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (h * 8 < left) next[h] = load_some(rp + h * 8 * a.r_stride, n);
-  };
   auto read = [&](int c) {
     tmem_load_blocks(r, at + c);
     tmem_load_blocks(r + 8, at + (16u << 16) + c);
   };
-  if (c0 < a.tokens) {
-    read(c0);
-    ask();
-  } else {
-    all_read();
-  }
-  for (int turn = 0; c0 < a.tokens; c0 += kTurn, turn ^= 1) {
-    if (adds) {
-      __syncwarp();
+  int ask_left = left, ask_at = 0;  // of the turn whose residual is asked for next
+  auto ask = [&] {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) room.add[turn][h * 32 + piece] = next[h];
+    for (int h = 0; h < 2; ++h) copy_some(&room.add[ask_at][h * 32 + piece], rp + h * 8 * a.r_stride, h * 8 < ask_left ? n : 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    rp += kTurn * a.r_stride;
+    ask_left -= kTurn;
+    ask_at = ask_at + 1 == kAhead ? 0 : ask_at + 1;
+  };
+  if (adds) {
+    __syncwarp();  // the tile before has been read
+    for (int k = 0; k + 1 < kAhead; ++k) ask();
+  }
+  ready();
+  if (c0 < a.tokens)
+    read(c0);
+  else
+    all_read();
+  for (int turn = 0; c0 < a.tokens; c0 += kTurn, turn = turn + 1 == kAhead ? 0 : turn + 1) {
+    __syncwarp();
+    if (adds) {
+      ask();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
       __syncwarp();
     }
     tmem_wait_load();
@@ -317,9 +321,6 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
           for (int k = 0; k < 2; ++k) v[h][g][k] = __uint_as_float(r[(g >> 1) * 8 + h * 4 + (g & 1) * 2 + k]);
     }
     if (!last) read(c0 + kTurn);
-    left -= kTurn;
-    rp += kTurn * a.r_stride;
-    if (!last) ask();
     if (a.bias[0])
 #pragma unroll
       for (int h = 0; h < kHalves; ++h)
@@ -345,14 +346,17 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) w[g] = pack_out<F16>(v[h][g][0], v[h][g][1]);
-      store_turned(smem_addr(&room.out[turn][h * 32 + block]), w);
+      store_turned(smem_addr(&room.out[h * 32 + block]), w);
     }
     __syncwarp();
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
-      if (h * 8 < left + kTurn) store_some(y + h * 8 * a.y_stride, room.out[turn][h * 32 + piece], n);
+      if (h * 8 < left) store_some(y + h * 8 * a.y_stride, room.out[h * 32 + piece], n);
     y += kTurn * a.y_stride;
+    left -= kTurn;
   }
+  // what was asked for past the tile's end (zeros) does not come after the next tile's
+  if (adds) asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 __device__ __forceinline__ void tma_load2(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar) {
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(kSpThreads)
   float *const sums = reinterpret_cast<float *>(stage0);
   if (a.split == 1) {
     __syncthreads();
-    drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, [] {});
+    drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, [] {}, [] {});
   } else {
     join<GATED, F16>(a, tmem, sums, warp, lane, rank, t0, o0);
   }
@@ -734,15 +738,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
     for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
       int64_t row_tile, token_tile;
       pair_tile(a, tile, &row_tile, &token_tile);
-      bar_wait(&sm.sums_full[n & 1], (n >> 1) & 1, stop);
-      __syncwarp();
-      tc_after_sync();
+      auto ready = [&] {
+        bar_wait(&sm.sums_full[n & 1], (n >> 1) & 1, stop);
+        __syncwarp();
+        tc_after_sync();
+      };
+      auto all_read = [&] {
+        tc_before_sync();
+        __syncwarp();
+        if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
+      };
       drain<GATED, F16>(a, tmem + (n & 1) * kCols, sm.out, warp, lane, token_tile * a.tokens,
-                        (int)(row_tile * 2 + rank) * kOut, [&] {
-                          tc_before_sync();
-                          __syncwarp();
-                          if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
-                        });
+                        (int)(row_tile * 2 + rank) * kOut, ready, all_read);
     }
   }
   __syncwarp();
