@@ -233,15 +233,17 @@ lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, const Operands &m, b
 }
 
 template <int D>
-lv_status run_rotate(const KvHost *kv, const RotateArgs &a, int32_t dtype, cudaStream_t stream) {
-  const int64_t items = a.n_tok * (a.heads[0] + a.heads[1]);
-  const unsigned grid = (unsigned)std::min<int64_t>((items + 3) / 4, (int64_t)kv->sms * 16);
-  if (dtype == LV_F16)
-    k_rotate<D, true><<<grid, 128, 0, stream>>>(a);
-  else
-    k_rotate<D, false><<<grid, 128, 0, stream>>>(a);
-  LV_CUDA(cudaGetLastError());
-  return LV_OK;
+lv_status run_rotate(const KvHost *kv, RotateArgs &a, int32_t dtype, cudaStream_t stream) {
+  // a token's heads to as many warps as there have to be for 96 an SM, two or four heads
+  // each at least
+  constexpr int kAtOnce = 32 / (D / 8);
+  const int heads = a.heads[0] + a.heads[1];
+  const int64_t parts = std::min<int64_t>((kv->sms * 96 + a.n_tok - 1) / a.n_tok, (heads + kAtOnce - 1) / kAtOnce);
+  a.part = (int)(((heads + parts - 1) / parts + kAtOnce - 1) / kAtOnce * kAtOnce);
+  a.parts = (heads + a.part - 1) / a.part;
+  const int64_t grid = std::min<int64_t>((a.n_tok * a.parts + kRoWarps - 1) / kRoWarps, INT32_MAX);
+  return dtype == LV_F16 ? launch_after(k_rotate<D, true>, grid, kRoWarps * 32, 0, 0, stream, a)
+                         : launch_after(k_rotate<D, false>, grid, kRoWarps * 32, 0, 0, stream, a);
 }
 
 }  // namespace
