@@ -232,18 +232,22 @@ lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, const Operands &m, b
   return dtype == LV_F16 ? run_linear<false, true>(kv, a, m, stream) : run_linear<false, false>(kv, a, m, stream);
 }
 
-template <int D>
-lv_status run_rotate(const KvHost *kv, RotateArgs &a, int32_t dtype, cudaStream_t stream) {
-  // a token's heads to as many warps as there have to be for 96 an SM, two or four heads
+template <int D, bool F16>
+lv_status run_rotate(const KvHost *kv, RotateArgs &a, bool neighbours, cudaStream_t stream) {
+  // a token's heads to as many warps as there have to be to fill the SMs, two or four heads
   // each at least
   constexpr int kAtOnce = 32 / (D / 8);
   const int heads = a.heads[0] + a.heads[1];
-  const int64_t parts = std::min<int64_t>((kv->sms * 96 + a.n_tok - 1) / a.n_tok, (heads + kAtOnce - 1) / kAtOnce);
+  const int64_t parts = std::min<int64_t>((kv->sms * kRoCtas * kRoWarps + a.n_tok - 1) / a.n_tok, (heads + kAtOnce - 1) / kAtOnce);
   a.part = (int)(((heads + parts - 1) / parts + kAtOnce - 1) / kAtOnce * kAtOnce);
   a.parts = (heads + a.part - 1) / a.part;
-  const int64_t grid = std::min<int64_t>((a.n_tok * a.parts + kRoWarps - 1) / kRoWarps, INT32_MAX);
-  return dtype == LV_F16 ? launch_after(k_rotate<D, true>, grid, kRoWarps * 32, 0, 0, stream, a)
-                         : launch_after(k_rotate<D, false>, grid, kRoWarps * 32, 0, 0, stream, a);
+  const int64_t grid = std::min<int64_t>((a.n_tok * a.parts + kRoWarps - 1) / kRoWarps, kv->sms * kRoCtas);
+  constexpr unsigned kThreads = kRoWarps * 32;
+  if (a.weight[0] || a.weight[1])
+    return neighbours ? launch_after(k_rotate<D, F16, true, true>, grid, kThreads, 0, 0, stream, a)
+                      : launch_after(k_rotate<D, F16, true, false>, grid, kThreads, 0, 0, stream, a);
+  return neighbours ? launch_after(k_rotate<D, F16, false, true>, grid, kThreads, 0, 0, stream, a)
+                    : launch_after(k_rotate<D, F16, false, false>, grid, kThreads, 0, 0, stream, a);
 }
 
 }  // namespace
@@ -303,11 +307,14 @@ lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_
   a.x_stride[0] = q_stride, a.x_stride[1] = k_stride, a.y_stride[0] = q_out_stride, a.y_stride[1] = k_out_stride;
   a.n_tok = n_tok, a.offsets = token_offsets, a.c = c, a.n_req = n_req;
   a.heads[0] = n_q_heads, a.heads[1] = n_kv_heads;
-  a.dim = rope->dim, a.neighbours = rope->order == LV_ROPE_NEIGHBOURS, a.eps = eps;
+  a.dim = rope->dim, a.eps = eps;
+  const bool next = rope->order == LV_ROPE_NEIGHBOURS;
   const KvHost *kv = kv_host(ctx);
   a.status = kv->d_status;
-  return head_dim == 128 ? run_rotate<128>(kv, a, dtype, (cudaStream_t)stream_)
-                         : run_rotate<64>(kv, a, dtype, (cudaStream_t)stream_);
+  cudaStream_t stream = (cudaStream_t)stream_;
+  if (head_dim == 128)
+    return dtype == LV_F16 ? run_rotate<128, true>(kv, a, next, stream) : run_rotate<128, false>(kv, a, next, stream);
+  return dtype == LV_F16 ? run_rotate<64, true>(kv, a, next, stream) : run_rotate<64, false>(kv, a, next, stream);
 }
 
 lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int64_t stride, int64_t n_tok,

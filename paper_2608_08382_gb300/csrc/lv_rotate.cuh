@@ -1,10 +1,12 @@
 // Norms of query and key heads with their rotation (lv_qk_rotate).
 //
 // Each element is read and written once, 16 bytes a lane: D / 8 lanes hold a head.
-// The squares of a head are added up among them; a pair of elements that stand apart
-// (halves) is brought together by a shuffle.  Cosines and sines are the same for all
-// heads of a token: a warp forms them once, two a lane, for the heads that it takes,
-// and keeps those that a lane's elements need in registers.
+// With x' = x s w (s of the head, w the weight) an element and its partner p give
+// x' cos -+ p' sin = s (x A + p B), A = w cos, B = -+ w_p sin, which are the same for all
+// heads of a token.  A warp takes a token's heads, or some of them: it forms the angles
+// once, two a lane, and a lane its eight A and B; a head then costs the sum of its
+// squares among its lanes, the partners by a shuffle of the 16-bit values, and three
+// multiplications a pair of elements.  The next heads are asked for meanwhile.
 #pragma once
 
 #include "lv_linear.cuh"
@@ -21,7 +23,7 @@ struct RotateArgs {
   const int32_t *c;          // or null
   int64_t n_req;
   int heads[2];
-  int dim, neighbours;
+  int dim;
   int parts, part;           // warps of a token, heads of a warp (queries first, then keys)
   float eps;
   int *status;
@@ -54,41 +56,92 @@ __device__ __forceinline__ float2 angle_of(uint64_t turns) {
   return r;
 }
 
-constexpr int kRoWarps = 4;  // of a CTA; nothing among them
+constexpr int kRoWarps = 4;  // of a CTA
 constexpr int kAsked = 4;    // loads of a lane at a time
+constexpr int kRoCtas = 5;   // of an SM
 
-template <int D, bool F16>
-__global__ void __launch_bounds__(kRoWarps * 32) k_rotate(const __grid_constant__ RotateArgs a) {
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+template <bool F16>
+__device__ __forceinline__ void unpack_pairs(const uint4 &b, uint64_t *v) {
+  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (F16) {
+      const float2 f = __half22float2(*(const __half2 *)&w[k]);
+      v[k] = pair(f.x, f.y);
+    } else {
+      v[k] = pair(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+    }
+  }
+}
+__device__ __forceinline__ float rsqrt_fast(float x) {  // of a normal number
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void swap_pair(uint64_t x, uint64_t *y) {
+  float a, b;
+  unpair(x, &a, &b);
+  *y = pair(b, a);
+}
+// The eight elements of lane `from`, or zeros: 0 times an infinity would be NaN.
+__device__ __forceinline__ uint4 partners(const uint4 &mine, int from, bool turns) {
+  uint4 r;
+  r.x = __shfl_sync(~0u, mine.x, from);
+  r.y = __shfl_sync(~0u, mine.y, from);
+  r.z = __shfl_sync(~0u, mine.z, from);
+  r.w = __shfl_sync(~0u, mine.w, from);
+  return turns ? r : make_uint4(0, 0, 0, 0);
+}
+
+template <int D, bool F16, bool NORM, bool NEXT>
+__global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_constant__ RotateArgs a) {
   constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;  // lanes of a head, heads of a warp at a time
-  __shared__ float2 turned[kRoWarps][64];
+  __shared__ float2 turned[kRoWarps][64];               // a token's cosines and sines
+  __shared__ float weight[2][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int l = lane % kLanes, sub = lane / kLanes;
+  const int l = lane % kLanes, sub = lane / kLanes, heads = a.heads[0] + a.heads[1];
   let_next();
   wait_previous();
+  for (int k = threadIdx.x; k < 2 * D; k += kRoWarps * 32) {
+    const void *const w = k < D ? a.weight[0] : a.weight[1];
+    weight[k / D][k % D] = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
+  }
+  __syncthreads();
   bool bad = false;
   if (a.offsets)
     for (int64_t i = (int64_t)blockIdx.x * (kRoWarps * 32) + threadIdx.x; i < a.n_req; i += (int64_t)gridDim.x * (kRoWarps * 32))
       bad |= a.offsets[i] < 0 || a.offsets[i + 1] < a.offsets[i] || a.offsets[i + 1] > a.n_tok;
-  const bool normed = a.weight[0] || a.weight[1];
-  uint4 weight[2];  // the lane's eight, of queries and keys
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    uint32_t packed[4] = {};
-    if (a.weight[w])
-#pragma unroll
-      for (int k = 0; k < 8; ++k) packed[k >> 1] |= (uint32_t)((const uint16_t *)a.weight[w])[l * 8 + k] << (k & 1) * 16;
-    weight[w] = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-  }
-  // the lane's elements in a rotation by halves: its own and its partner's are pairs
-  // first .. first + 7
-  const int turn_lanes = a.dim / 8, half_lanes = turn_lanes / 2;
-  const bool turns = l < turn_lanes, upper = l >= half_lanes;
-  const int partner = !turns || a.neighbours ? lane : upper ? lane - half_lanes : lane + half_lanes;
-  const int first = a.neighbours ? l * 4 : (upper ? l - half_lanes : l) * 8;
+  // by halves the lane's eight elements are of pairs first .. first + 7, and their
+  // partners another lane's; by neighbours they are pairs first .. first + 3
+  const int half_lanes = a.dim / 16;
+  const bool turns = l < 2 * half_lanes, upper = !NEXT && l >= half_lanes;
+  const int away = !turns || NEXT ? 0 : upper ? -half_lanes : half_lanes;
+  const int first = NEXT ? l * 4 : (upper ? l - half_lanes : l) * 8;
+  constexpr int kBatch = kAtOnce * kAsked;  // heads that a warp has asked for
   const int64_t units = a.n_tok * a.parts;
   for (int64_t u = (int64_t)blockIdx.x * kRoWarps + warp; u < units; u += (int64_t)gridDim.x * kRoWarps) {
     const int64_t t = a.parts == 1 ? u : quotient(u, a.parts);
-    const int h0 = (int)(u - t * a.parts) * a.part, h1 = min(h0 + a.part, a.heads[0] + a.heads[1]);
+    const int h0 = (int)(u - t * a.parts) * a.part, h1 = min(h0 + a.part, heads);
+    // the warp's queries, then its keys: heads at[w] .. end[w] - 1 of array w
+    const int at[2] = {min(h0, a.heads[0]), max(h0 - a.heads[0], 0)}, end[2] = {min(h1, a.heads[0]), max(h1 - a.heads[0], 0)};
+    uint4 next[kAsked];
+    auto ask = [&](int w, int from) {
+      const uint16_t *const x = (const uint16_t *)a.x[w] + t * a.x_stride[w] + (from + sub) * D + l * 8;
+#pragma unroll
+      for (int b = 0; b < kAsked; ++b) {
+        next[b] = make_uint4(0, 0, 0, 0);
+        if (from + b * kAtOnce + sub < end[w]) next[b] = *(const uint4 *)(x + b * kAtOnce * D);
+      }
+    };
+    if (at[0] < end[0])
+      ask(0, at[0]);
+    else
+      ask(1, at[1]);
     const int64_t i = a.offsets ? request_of(a.offsets, a.n_req, t, lane) : t;
     if (i < 0) continue;
     int64_t pos = a.offsets ? t - a.offsets[i] : 0;
@@ -100,90 +153,101 @@ __global__ void __launch_bounds__(kRoWarps * 32) k_rotate(const __grid_constant_
     __syncwarp();
     for (int j = lane; j < a.dim / 2; j += 32) turned[warp][j] = angle_of((uint64_t)pos * a.turn[j]);
     __syncwarp();
-    float2 cs[8];  // by neighbours four of them
-    if (turns) {
+#pragma unroll 1
+    for (int w = 0; w < 2; ++w) {
+      if (at[w] >= end[w]) continue;
+      uint64_t A[4], B[4];
+      const float *const own = weight[w] + l * 8, *const theirs = own + away * 8;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        cs[k] = turned[warp][(first + k) & 63];
-        if (!a.neighbours && !upper) cs[k].y = -cs[k].y;  // a cos - b sin below, b cos + a sin above
+      for (int k = 0; k < 8; k += 2) {
+        float2 e = make_float2(1.f, 0.f), f = e;
+        if (NEXT) {
+          if (turns) e = f = turned[warp][(first + k / 2) & 63];
+          A[k / 2] = pair(own[k] * e.x, own[k + 1] * e.x);
+          B[k / 2] = pair(own[k + 1] * -e.y, own[k] * e.y);
+        } else {
+          if (turns) e = turned[warp][(first + k) & 63], f = turned[warp][(first + k + 1) & 63];
+          A[k / 2] = pair(own[k] * e.x, own[k + 1] * f.x);
+          B[k / 2] = upper ? pair(theirs[k] * e.y, theirs[k + 1] * f.y) : pair(theirs[k] * -e.y, theirs[k + 1] * -f.y);
+        }
       }
-    }
-    for (int g0 = h0; g0 < h1; g0 += kAtOnce * kAsked) {
-      uint4 raw[kAsked];
+      const bool normed = NORM && a.weight[w];
+      uint16_t *y = (uint16_t *)a.y[w] + t * a.y_stride[w] + (at[w] + sub) * D + l * 8;
+#pragma unroll 1
+      for (int from = at[w]; from < end[w]; from += kBatch, y += kBatch * D) {
+        uint4 raw[kAsked];
 #pragma unroll
-      for (int b = 0; b < kAsked; ++b) {
-        const int h = g0 + b * kAtOnce + sub, which = h >= a.heads[0];
-        raw[b] = make_uint4(0, 0, 0, 0);
-        if (h < h1)
-          raw[b] = *(const uint4 *)((const uint16_t *)a.x[which] + t * a.x_stride[which] +
-                                    (int64_t)(which ? h - a.heads[0] : h) * D + l * 8);
-      }
+        for (int b = 0; b < kAsked; ++b) raw[b] = next[b];
+        if (from + kBatch < end[w])
+          ask(w, from + kBatch);
+        else if (w == 0)
+          ask(1, at[1]);
+        // a head's outputs, its elements multiplied by `by` first
+        auto turn = [&](int b, float by, float scale) {
+          uint64_t v[4], o[4];
+          unpack_pairs<F16>(raw[b], v);
+          if (NEXT) {
 #pragma unroll
-      for (int b = 0; b < kAsked; ++b) {
-        if (g0 + b * kAtOnce >= h1) break;
-        const int h = g0 + b * kAtOnce + sub, which = h >= a.heads[0];
-        float v[8];
-        unpack8<F16>(raw[b], v);
+            for (int k = 0; k < 4; ++k) swap_pair(turns ? v[k] : 0, &o[k]);
+          } else {
+            unpack_pairs<F16>(partners(raw[b], lane + away, turns), o);
+          }
+          uint32_t r[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (by != 1.f) v[k] = mul2(v[k], pair(by, by)), o[k] = mul2(o[k], pair(by, by));
+            float p, q;
+            const uint64_t z = fma2(v[k], A[k], mul2(o[k], B[k]));
+            unpair(normed ? mul2(z, pair(scale, scale)) : z, &p, &q);
+            r[k] = pack_out<F16>(p, q);
+          }
+          if (from + b * kAtOnce + sub < end[w]) *(uint4 *)(y + b * kAtOnce * D) = make_uint4(r[0], r[1], r[2], r[3]);
+        };
+        float sum[kAsked];
+        bool far = false;
         if (normed) {
-          const bool own_norm = a.weight[which] != nullptr;
-          float sum = 0.f, eps = a.eps;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) sum += v[k] * v[k];
+          for (int b = 0; b < kAsked; ++b) {
+            uint64_t v[4], s2;
+            unpack_pairs<F16>(raw[b], v);
+            s2 = mul2(v[0], v[0]);
 #pragma unroll
-          for (int s = kLanes / 2; s; s >>= 1) sum += __shfl_xor_sync(~0u, sum, s);
-          const bool far = !(sum < 0x1p120f) || (sum < 0x1p-90f && eps < 0x1p-60f);
-          if (__any_sync(~0u, far)) {
-            float top = 0.f;
+            for (int k = 1; k < 4; ++k) s2 = fma2(v[k], v[k], s2);
+            float s1;
+            unpair(s2, &sum[b], &s1);
+            sum[b] += s1;
+          }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(v[k]));
+          for (int s = kLanes / 2; s; s >>= 1)
 #pragma unroll
-            for (int s = kLanes / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
+            for (int b = 0; b < kAsked; ++b) sum[b] += __shfl_xor_sync(~0u, sum[b], s);
+#pragma unroll
+          for (int b = 0; b < kAsked; ++b)
+            far |= from + b * kAtOnce + sub < end[w] && (!(sum[b] < 0x1p120f) || (sum[b] < 0x1p-90f && a.eps < 0x1p-60f));
+        }
+        if (__any_sync(~0u, far)) {
+#pragma unroll
+          for (int b = 0; b < kAsked; ++b) {
             // The squares again, relative to a power of two near the largest element, or to
             // eps where that is larger still: what is far below either does not count
-            const bool again = far && own_norm && top > 0.f && top < INFINITY;
-            const int e = max(max(ilogbf(again ? top : 1.f), eps > 0.f ? ilogbf(eps) / 2 : -126), -126);
-            const float by = again ? scalbnf(1.f, -e) : 1.f;
-            float other = 0.f;
+            float e8[8], top = 0.f, again = 0.f, by = 1.f, eps = a.eps;
+            unpack8<F16>(raw[b], e8);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              v[k] *= by;
-              other += v[k] * v[k];
-            }
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(e8[k]));
 #pragma unroll
-            for (int s = kLanes / 2; s; s >>= 1) other += __shfl_xor_sync(~0u, other, s);
-            if (again) {
-              sum = other;
-              eps = eps * by * by;
-            }
+            for (int s = kLanes / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
+            if (top > 0.f && top < INFINITY)
+              by = scalbnf(1.f, -max(max(ilogbf(top), eps > 0.f ? ilogbf(eps) / 2 : -126), -126));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) again += e8[k] * by * (e8[k] * by);
+#pragma unroll
+            for (int s = kLanes / 2; s; s >>= 1) again += __shfl_xor_sync(~0u, again, s);
+            turn(b, by, rsqrtf(again * (1.f / D) + eps * by * by));
           }
-          if (own_norm) {
-            const float scale = rsqrtf(sum * (1.f / D) + eps);
-            float w[8];
-            unpack8<F16>(which ? weight[1] : weight[0], w);
+        } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = v[k] * scale * w[k];
-          }
+          for (int b = 0; b < kAsked; ++b) turn(b, 1.f, normed ? rsqrt_fast(sum[b] * (1.f / D) + a.eps) : 1.f);
         }
-        if (a.neighbours) {
-          if (turns)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float p = v[2 * k], q = v[2 * k + 1];
-              v[2 * k] = p * cs[k].x - q * cs[k].y;
-              v[2 * k + 1] = p * cs[k].y + q * cs[k].x;
-            }
-        } else if (a.dim > 0) {
-          float other[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) other[k] = __shfl_sync(~0u, v[k], partner);
-          if (turns)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = v[k] * cs[k].x + other[k] * cs[k].y;
-        }
-        if (h < h1)
-          *(uint4 *)((uint16_t *)a.y[which] + t * a.y_stride[which] + (int64_t)(which ? h - a.heads[0] : h) * D + l * 8) =
-              make_uint4(pack_out<F16>(v[0], v[1]), pack_out<F16>(v[2], v[3]), pack_out<F16>(v[4], v[5]),
-                         pack_out<F16>(v[6], v[7]));
       }
     }
   }
