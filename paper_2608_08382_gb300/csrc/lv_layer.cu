@@ -331,14 +331,16 @@ lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int6
       !aligned(top_logp, 4))
     return LV_EINVAL;
   const KvHost *kv = kv_host(ctx);
-  LogprobArgs a{logits, stride, n_tok, vocab, n_top, ids, logp, entropy, lse, top_ids, top_logp, kv->d_status};
+  LogprobArgs a{logits, stride, n_tok, vocab, n_top, 1, ids, logp, entropy, lse, top_ids, top_logp, kv->d_status};
+  // CTAs for every SM, four of them, where a row has loads for more
+  const int64_t vectors = vocab / (dtype == LV_F32 ? 4 : 8);
+  while (a.cluster < kLpCluster && n_tok * a.cluster < 4 * kv->sms && vectors >= 2 * a.cluster * 2 * kLpThreads) a.cluster *= 2;
+  if (n_tok * a.cluster > INT32_MAX) return LV_EINVAL;
   cudaStream_t stream = (cudaStream_t)stream_;
-  const unsigned grid = (unsigned)std::min<int64_t>(n_tok, (int64_t)kv->sms * 8);
-  if (dtype == LV_BF16) k_logprobs<LV_BF16><<<grid, 256, 0, stream>>>(a);
-  if (dtype == LV_F16) k_logprobs<LV_F16><<<grid, 256, 0, stream>>>(a);
-  if (dtype == LV_F32) k_logprobs<LV_F32><<<grid, 256, 0, stream>>>(a);
-  LV_CUDA(cudaGetLastError());
-  return LV_OK;
+  const int64_t grid = n_tok * a.cluster;
+  if (dtype == LV_BF16) return launch_after(k_logprobs<LV_BF16>, grid, kLpThreads, 0, a.cluster, stream, a);
+  if (dtype == LV_F16) return launch_after(k_logprobs<LV_F16>, grid, kLpThreads, 0, a.cluster, stream, a);
+  return launch_after(k_logprobs<LV_F32>, grid, kLpThreads, 0, a.cluster, stream, a);
 }
 
 }  // extern "C"

@@ -85,6 +85,25 @@ __device__ __forceinline__ void unpack8(const uint4 &b, float *v) {
   for (int k = 0; k < 8; ++k) v[k] = value_of<F16>((uint16_t)(w[k >> 1] >> (k & 1) * 16));
 }
 
+// Two fp32 products in one instruction, and eight 16-bit values as pairs of floats.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+template <bool F16>
+__device__ __forceinline__ void unpack_pairs(const uint4 &b, uint64_t *v) {
+  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (F16) {
+      const float2 f = __half22float2(*(const __half2 *)&w[k]);
+      v[k] = pair(f.x, f.y);
+    } else {
+      v[k] = pair(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+    }
+  }
+}
 // The biases of outputs o .. o + 7.
 template <bool GATED, bool F16>
 __device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)[8]) {

@@ -60,24 +60,6 @@ constexpr int kRoWarps = 4;  // of a CTA
 constexpr int kAsked = 4;    // loads of a lane at a time
 constexpr int kRoCtas = 5;   // of an SM
 
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-template <bool F16>
-__device__ __forceinline__ void unpack_pairs(const uint4 &b, uint64_t *v) {
-  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (F16) {
-      const float2 f = __half22float2(*(const __half2 *)&w[k]);
-      v[k] = pair(f.x, f.y);
-    } else {
-      v[k] = pair(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
-    }
-  }
-}
 __device__ __forceinline__ float rsqrt_fast(float x) {  // of a normal number
   float r;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -107,11 +89,6 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
   const int l = lane % kLanes, sub = lane / kLanes, heads = a.heads[0] + a.heads[1];
   let_next();
   wait_previous();
-  for (int k = threadIdx.x; k < 2 * D; k += kRoWarps * 32) {
-    const void *const w = k < D ? a.weight[0] : a.weight[1];
-    weight[k / D][k % D] = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
-  }
-  __syncthreads();
   bool bad = false;
   if (a.offsets)
     for (int64_t i = (int64_t)blockIdx.x * (kRoWarps * 32) + threadIdx.x; i < a.n_req; i += (int64_t)gridDim.x * (kRoWarps * 32))
@@ -124,24 +101,33 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
   const int first = NEXT ? l * 4 : (upper ? l - half_lanes : l) * 8;
   constexpr int kBatch = kAtOnce * kAsked;  // heads that a warp has asked for
   const int64_t units = a.n_tok * a.parts;
-  for (int64_t u = (int64_t)blockIdx.x * kRoWarps + warp; u < units; u += (int64_t)gridDim.x * kRoWarps) {
-    const int64_t t = a.parts == 1 ? u : quotient(u, a.parts);
-    const int h0 = (int)(u - t * a.parts) * a.part, h1 = min(h0 + a.part, heads);
-    // the warp's queries, then its keys: heads at[w] .. end[w] - 1 of array w
-    const int at[2] = {min(h0, a.heads[0]), max(h0 - a.heads[0], 0)}, end[2] = {min(h1, a.heads[0]), max(h1 - a.heads[0], 0)};
-    uint4 next[kAsked];
-    auto ask = [&](int w, int from) {
-      const uint16_t *const x = (const uint16_t *)a.x[w] + t * a.x_stride[w] + (from + sub) * D + l * 8;
+  int64_t u = (int64_t)blockIdx.x * kRoWarps + warp, t = 0;
+  int at0 = 0, end0 = 0, at1 = 0, end1 = 0;  // the warp's queries, then its keys
+  uint4 next[kAsked];
+  auto ask = [&](int w, int from) {
+    const uint16_t *const x = (const uint16_t *)a.x[w] + t * a.x_stride[w] + (from + sub) * D + l * 8;
+    const int end = w ? end1 : end0;
 #pragma unroll
-      for (int b = 0; b < kAsked; ++b) {
-        next[b] = make_uint4(0, 0, 0, 0);
-        if (from + b * kAtOnce + sub < end[w]) next[b] = *(const uint4 *)(x + b * kAtOnce * D);
-      }
-    };
-    if (at[0] < end[0])
-      ask(0, at[0]);
-    else
-      ask(1, at[1]);
+    for (int b = 0; b < kAsked; ++b) {
+      next[b] = make_uint4(0, 0, 0, 0);
+      if (from + b * kAtOnce + sub < end) next[b] = *(const uint4 *)(x + b * kAtOnce * D);
+    }
+  };
+  auto begin = [&] {  // unit u: its heads, and the first of them asked for
+    t = a.parts == 1 ? u : quotient(u, a.parts);
+    const int h0 = (int)(u - t * a.parts) * a.part, h1 = min(h0 + a.part, heads);
+    at0 = min(h0, a.heads[0]), end0 = min(h1, a.heads[0]);
+    at1 = max(h0 - a.heads[0], 0), end1 = max(h1 - a.heads[0], 0);
+    ask(at0 < end0 ? 0 : 1, at0 < end0 ? at0 : at1);
+  };
+  if (u < units) begin();
+  for (int k = threadIdx.x; k < 2 * D; k += kRoWarps * 32) {
+    const void *const w = k < D ? a.weight[0] : a.weight[1];
+    weight[k / D][k % D] = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
+  }
+  __syncthreads();
+  for (bool begun = true; u < units; u += (int64_t)gridDim.x * kRoWarps, begun = false) {
+    if (!begun) begin();
     const int64_t i = a.offsets ? request_of(a.offsets, a.n_req, t, lane) : t;
     if (i < 0) continue;
     int64_t pos = a.offsets ? t - a.offsets[i] : 0;
@@ -155,7 +141,8 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
     __syncwarp();
 #pragma unroll 1
     for (int w = 0; w < 2; ++w) {
-      if (at[w] >= end[w]) continue;
+      const int at = w ? at1 : at0, end = w ? end1 : end0;
+      if (at >= end) continue;
       uint64_t A[4], B[4];
       const float *const own = weight[w] + l * 8, *const theirs = own + away * 8;
 #pragma unroll
@@ -172,16 +159,16 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
         }
       }
       const bool normed = NORM && a.weight[w];
-      uint16_t *y = (uint16_t *)a.y[w] + t * a.y_stride[w] + (at[w] + sub) * D + l * 8;
+      uint16_t *y = (uint16_t *)a.y[w] + t * a.y_stride[w] + (at + sub) * D + l * 8;
 #pragma unroll 1
-      for (int from = at[w]; from < end[w]; from += kBatch, y += kBatch * D) {
+      for (int from = at; from < end; from += kBatch, y += kBatch * D) {
         uint4 raw[kAsked];
 #pragma unroll
         for (int b = 0; b < kAsked; ++b) raw[b] = next[b];
-        if (from + kBatch < end[w])
+        if (from + kBatch < end)
           ask(w, from + kBatch);
         else if (w == 0)
-          ask(1, at[1]);
+          ask(1, at1);
         // a head's outputs, its elements multiplied by `by` first
         auto turn = [&](int b, float by, float scale) {
           uint64_t v[4], o[4];
@@ -201,7 +188,7 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
             unpair(normed ? mul2(z, pair(scale, scale)) : z, &p, &q);
             r[k] = pack_out<F16>(p, q);
           }
-          if (from + b * kAtOnce + sub < end[w]) *(uint4 *)(y + b * kAtOnce * D) = make_uint4(r[0], r[1], r[2], r[3]);
+          if (from + b * kAtOnce + sub < end) *(uint4 *)(y + b * kAtOnce * D) = make_uint4(r[0], r[1], r[2], r[3]);
         };
         float sum[kAsked];
         bool far = false;
@@ -223,7 +210,7 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
             for (int b = 0; b < kAsked; ++b) sum[b] += __shfl_xor_sync(~0u, sum[b], s);
 #pragma unroll
           for (int b = 0; b < kAsked; ++b)
-            far |= from + b * kAtOnce + sub < end[w] && (!(sum[b] < 0x1p120f) || (sum[b] < 0x1p-90f && a.eps < 0x1p-60f));
+            far |= from + b * kAtOnce + sub < end && (!(sum[b] < 0x1p120f) || (sum[b] < 0x1p-90f && a.eps < 0x1p-60f));
         }
         if (__any_sync(~0u, far)) {
 #pragma unroll
