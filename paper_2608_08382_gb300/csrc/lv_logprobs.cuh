@@ -3,13 +3,16 @@
 // W = sum exp(x - m) (x - m),
 //   lse = m + log S,  log p_v = (x_v - m) - log S,  entropy = log S - W / S.
 //
-// One pass over a row, by the 256 threads of a CTA, 16 bytes a load, four in a row; a
-// thread keeps its own m, S and W, which are scaled again where its m grows, and where
-// its largest logit stands.  Few rows are shared by clusters of up to eight CTAs, whose
+// One pass over a row, by the 256 threads of a CTA, 16 bytes a load, four asked for while
+// four are added up; a thread keeps S and W relative to a logit of its own, which it
+// takes anew only where one comes that is more than 8 above it (a scale that follows
+// the maximum costs every warp a scaling every few loads), and which of its vectors
+// holds its largest logit.  Few rows are shared by clusters of up to eight CTAs, whose
 // sums and largest meet in the first one's shared memory.
 //
 // The n_top largest: of the 32 groups of eight threads each has a largest logit, and the
-// n_top-th of those bounds the row's n_top-th from below.  Only threads whose own
+// n_top-th of those bounds the row's n_top-th from below (of equal ones by index; that of
+// its vector will do).  Only threads whose own
 // largest reaches the bound hold candidates; their warps read their logits once more
 // (a few of 256, still in L2) and the candidates are put in order by counting for each
 // those above it.  Where there are more candidates than room (a row in descending
@@ -66,15 +69,17 @@ static_assert(kLpGroups >= LV_MAX_TOP && kLpGroups * 8 * 8 <= kLpRoom, "a bound 
 constexpr float kLpFar = -1e30f;
 
 struct LpPart {       // of a CTA's share of a row
-  float m, S, W;      // W in units of the natural logarithm
-  uint32_t top;       // the largest's order key
+  float base, S, W;   // sums of exp(x - base) and of that times (x - base)
+  uint32_t top;       // the largest's order key, 0 where there is no logit
 };
 struct LpSmem {
   uint64_t room[kLpRoom];
   uint64_t of_cluster[kLpCluster * LV_MAX_TOP];  // the first CTA's: everyone's largest
   uint64_t group[kLpGroups];
   uint64_t warp_key[kLpWarps];
-  LpPart warp[kLpWarps], part[kLpCluster];
+  float warp_base[kLpWarps], warp_S[kLpWarps], warp_W[kLpWarps];
+  uint32_t warp_top[kLpWarps];
+  LpPart part[kLpCluster];
   uint64_t bound;
   int n;
 };
@@ -95,16 +100,44 @@ __device__ __forceinline__ void logit_pairs(const uint4 &b, uint64_t *v) {
   }
 }
 
-// A thread's running m, S, W.
+// The largest logit of a vector; NaNs are passed over.
+template <int TYPE>
+__device__ __forceinline__ float largest_of(const uint4 &b) {
+  if (TYPE == LV_F32)
+    return fmaxf(fmaxf(__uint_as_float(b.x), __uint_as_float(b.y)), fmaxf(__uint_as_float(b.z), __uint_as_float(b.w)));
+  if (TYPE == LV_F16) {
+    const __half2 m = __hmax2(__hmax2(*(const __half2 *)&b.x, *(const __half2 *)&b.y),
+                              __hmax2(*(const __half2 *)&b.z, *(const __half2 *)&b.w));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  const __nv_bfloat162 m = __hmax2(__hmax2(*(const __nv_bfloat162 *)&b.x, *(const __nv_bfloat162 *)&b.y),
+                                   __hmax2(*(const __nv_bfloat162 *)&b.z, *(const __nv_bfloat162 *)&b.w));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+
+// A thread's running sums.
+constexpr float kLpLazy = 8.f;
 struct LpRun {
-  float m = -INFINITY, base = 0.f;  // base: m, or 0 while there is none
-  uint64_t S = 0, W = 0;            // two sums each
-  int where = -1;                   // vector of the first logit that equals m
-  __device__ __forceinline__ void grow(float to) {
-    const float f = m == -INFINITY ? 0.f : exp2_fast((m - to) * 1.4426950408889634f), d = m == -INFINITY ? 0.f : fmaxf(m - to, kLpFar);
-    W = mul2(fma2(S, pair(d, d), W), pair(f, f));
-    S = mul2(S, pair(f, f));
-    m = base = to;
+  float m = -INFINITY;     // its largest logit
+  float base = 0.f;        // what the sums are relative to, once `set`
+  bool set = false;
+  uint64_t S = 0, W = 0;   // two sums each
+  int where = -1;          // the first vector with a logit that equals m
+  // Vectors of which the largest logit is `top`, the first of them at j.
+  __device__ __forceinline__ void seen(float top, int j) {
+    if (where < 0 || top > m) where = j;
+    m = fmaxf(m, top);
+  }
+  __device__ __forceinline__ void rebase() {  // before what makes m as it is is added
+    if (set ? m > base + kLpLazy : m > -INFINITY) {
+      if (set) {  // else there is nothing yet
+        const float d = fmaxf(base - m, kLpFar), f = exp2_fast(d * 1.4426950408889634f);
+        W = mul2(fma2(S, pair(d, d), W), pair(f, f));
+        S = mul2(S, pair(f, f));
+      }
+      base = m;
+      set = true;
+    }
   }
   template <int N>
   __device__ __forceinline__ void add(const uint64_t (&v)[N]) {
@@ -121,29 +154,12 @@ struct LpRun {
     }
   }
 };
-template <int N>
-__device__ __forceinline__ float largest_of(const uint64_t (&v)[N]) {
-  float top = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float a, b;
-    unpair(v[k], &a, &b);
-    top = fmaxf(top, fmaxf(a, b));
-  }
-  return top;
-}
 
-// Two parts together.
-__device__ __forceinline__ LpPart join(const LpPart &a, const LpPart &b) {
-  LpPart r;
-  r.m = fmaxf(a.m, b.m);
-  r.top = max(a.top, b.top);
-  const float da = a.m == r.m ? 0.f : fmaxf(a.m - r.m, kLpFar), db = b.m == r.m ? 0.f : fmaxf(b.m - r.m, kLpFar);
-  const float fa = exp2_fast(da * 1.4426950408889634f), fb = exp2_fast(db * 1.4426950408889634f);
-  // a part of m = -inf has no sums
-  r.S = a.S * fa + b.S * fb;
-  r.W = (a.m == -INFINITY ? 0.f : fa * (a.W + a.S * da)) + (b.m == -INFINITY ? 0.f : fb * (b.W + b.S * db));
-  return r;
+// Sums relative to another base, at least their own.
+__device__ __forceinline__ void rescale(float base, float to, float *S, float *W) {
+  const float d = fmaxf(base - to, kLpFar), f = exp2_fast(d * 1.4426950408889634f);
+  *W = f * (*W + *S * d);
+  *S *= f;
 }
 
 template <int TYPE>
@@ -180,101 +196,110 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
   LpRun run;
   auto edge = [&](int j) {  // a vector that is the row's in part
     uint64_t v[kE / 2];
+    float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < kE; e += 2)
-      v[e / 2] = pair(in_row(index(j, e)) ? logit(j, e) : -INFINITY, in_row(index(j, e + 1)) ? logit(j, e + 1) : -INFINITY);
-    const float top = largest_of(v);
-    if (run.where < 0) run.where = j;
-    if (top > run.m) {
-      run.grow(top);
-      run.where = j;
+    for (int e = 0; e < kE; e += 2) {
+      const float p = in_row(index(j, e)) ? logit(j, e) : -INFINITY, q = in_row(index(j, e + 1)) ? logit(j, e + 1) : -INFINITY;
+      v[e / 2] = pair(p, q);
+      top = fmaxf(top, fmaxf(p, q));
     }
+    run.seen(top, j);
+    run.rebase();
     run.add(v);
   };
   if (head && tid == 0) edge(from);
-  for (int j = whole0 + tid; j < whole1; j += kLpThreads * kAsk) {
-    uint4 raw[kAsk];
-    const int n = min(kAsk, (whole1 - j + kLpThreads - 1) / kLpThreads);
+  uint4 next[kAsk];
+  auto ask = [&](int j) {
 #pragma unroll
     for (int k = 0; k < kAsk; ++k)
-      if (k < n) raw[k] = load_once(line + (int64_t)(j + k * kLpThreads) * 16);
-    if (run.where < 0) run.where = j;
-    float top[kAsk], most = -INFINITY;
+      if (j + k * kLpThreads < whole1) next[k] = load_once(line + (int64_t)(j + k * kLpThreads) * 16);
+  };
+  ask(whole0 + tid);
+  for (int j = whole0 + tid; j < whole1; j += kLpThreads * kAsk) {
+    uint4 raw[kAsk];
 #pragma unroll
-    for (int k = 0; k < kAsk; ++k) {
-      uint64_t v[kE / 2];
-      logit_pairs<TYPE>(raw[k], v);
-      top[k] = k < n ? largest_of(v) : -INFINITY;
-      most = fmaxf(most, top[k]);
-    }
-    if (most > run.m) {
-      bool found = false;
+    for (int k = 0; k < kAsk; ++k) raw[k] = next[k];
+    ask(j + kLpThreads * kAsk);
 #pragma unroll
-      for (int k = 0; k < kAsk; ++k)
-        if (!found && top[k] == most) run.where = j + k * kLpThreads, found = true;
-      run.grow(most);
-    }
+    for (int k = 0; k < kAsk; ++k)
+      if (j + k * kLpThreads < whole1) run.seen(largest_of<TYPE>(raw[k]), j + k * kLpThreads);
+    run.rebase();
 #pragma unroll
-    for (int k = 0; k < kAsk; ++k) {
-      uint64_t v[kE / 2];
-      logit_pairs<TYPE>(raw[k], v);
-      if (k < n) run.add(v);
-    }
+    for (int k = 0; k < kAsk; ++k)
+      if (j + k * kLpThreads < whole1) {
+        uint64_t v[kE / 2];
+        logit_pairs<TYPE>(raw[k], v);
+        run.add(v);
+      }
   }
   if (tail && tid == kLpThreads - 1) edge(to - 1);
-  // ---- the CTA's sums
-  float s0, s1, w0, w1;
-  unpair(run.S, &s0, &s1);
-  unpair(run.W, &w0, &w1);
-  LpPart part{run.m, s0 + s1, w0 + w1, run.where < 0 ? 0 : order_key(run.m)};
+  // ---- the CTA's sums, relative to the largest base
+  LpPart part{run.set ? run.base : -INFINITY, 0.f, 0.f, run.where < 0 ? 0 : order_key(run.m)};
 #pragma unroll
   for (int s = 16; s; s >>= 1) {
-    const LpPart other{__shfl_xor_sync(~0u, part.m, s), __shfl_xor_sync(~0u, part.S, s), __shfl_xor_sync(~0u, part.W, s),
-                       __shfl_xor_sync(~0u, part.top, s)};
-    // the same way in both lanes
-    part = lane & s ? join(other, part) : join(part, other);
+    part.base = fmaxf(part.base, __shfl_xor_sync(~0u, part.base, s));
+    part.top = max(part.top, __shfl_xor_sync(~0u, part.top, s));
   }
-  if (lane == 0) sm.warp[warp] = part;
-  // each thread's largest, and its group's
-  uint64_t best = 0;
+  if (lane == 0) sm.warp_base[warp] = part.base, sm.warp_top[warp] = part.top;
+  // the vector's last index for a bound from below, its first one for one from above
+  uint64_t reach = 0;
   if (a.n_top > 0) {
+    uint64_t least = 0;
     if (run.where >= 0) {
-      int e = 0;
-      for (; e < kE - 1; ++e)
-        if (in_row(index(run.where, e)) && logit(run.where, e) == run.m) break;
-      best = full_key(order_key(run.m), index(run.where, e));
+      const uint32_t key = order_key(run.m);
+      least = full_key(key, min(index(run.where, kE - 1), a.vocab - 1));
+      reach = full_key(key, max(index(run.where, 0), 0));
     }
-    uint64_t top = best;
 #pragma unroll
-    for (int s = 4; s; s >>= 1) top = larger(top, __shfl_xor_sync(~0u, top, s));
-    if ((lane & 7) == 0) sm.group[tid >> 3] = top;
+    for (int s = 4; s; s >>= 1) least = larger(least, __shfl_xor_sync(~0u, least, s));
+    if ((lane & 7) == 0) sm.group[tid >> 3] = least;
   }
   if (tid == 0) sm.n = 0;
   __syncthreads();
-  part = sm.warp[0];
 #pragma unroll
-  for (int k = 1; k < kLpWarps; ++k) part = join(part, sm.warp[k]);
+  for (int k = 0; k < kLpWarps; ++k) {
+    part.base = fmaxf(part.base, sm.warp_base[k]);
+    part.top = max(part.top, sm.warp_top[k]);
+  }
+  {
+    float s0, s1, w0, w1;
+    unpair(run.S, &s0, &s1);
+    unpair(run.W, &w0, &w1);
+    part.S = s0 + s1;
+    part.W = w0 + w1;
+    if (run.set) rescale(run.base, part.base, &part.S, &part.W);  // else they are 0, or NaN
+  }
+#pragma unroll
+  for (int s = 16; s; s >>= 1) {
+    part.S += __shfl_xor_sync(~0u, part.S, s);
+    part.W += __shfl_xor_sync(~0u, part.W, s);
+  }
+  if (lane == 0) sm.warp_S[warp] = part.S, sm.warp_W[warp] = part.W;
+  // the n_top-th of the groups' largest, or everything where there is none
+  if (a.n_top > 0 && warp == 1) {
+    const uint64_t mine = sm.group[lane];
+    int above = 0;
+#pragma unroll
+    for (int k = 0; k < kLpGroups; ++k) above += sm.group[k] > mine;
+    const bool counts = mine != 0 && above < a.n_top;
+    uint64_t least = counts ? mine : ~0ull;
+#pragma unroll
+    for (int s = 16; s; s >>= 1) {
+      const uint64_t other = __shfl_xor_sync(~0u, least, s);
+      least = other < least ? other : least;
+    }
+    const unsigned at = __ballot_sync(~0u, counts);
+    if (lane == 0) sm.bound = __popc(at) < a.n_top ? 1 : least;
+  }
+  __syncthreads();
+  part.S = sm.warp_S[0], part.W = sm.warp_W[0];
+#pragma unroll
+  for (int k = 1; k < kLpWarps; ++k) part.S += sm.warp_S[k], part.W += sm.warp_W[k];
   bool slow = part.S != part.S;  // a NaN, or an infinity less itself
   if (a.n_top > 0 && !slow) {
     // ---- candidates
-    if (warp == 0) {
-      const uint64_t mine = sm.group[lane];
-      int above = 0;
-#pragma unroll
-      for (int k = 0; k < kLpGroups; ++k) above += sm.group[k] > mine;
-      // the n_top-th, or everything where there is none; empty groups are all 0 and equal
-      const unsigned at = __ballot_sync(~0u, above < a.n_top && mine != 0);
-      uint64_t least = mine != 0 && above < a.n_top ? mine : ~0ull;
-#pragma unroll
-      for (int s = 16; s; s >>= 1) {
-        const uint64_t other = __shfl_xor_sync(~0u, least, s);
-        least = other < least ? other : least;
-      }
-      if (lane == 0) sm.bound = __popc(at) < a.n_top ? 1 : least;
-    }
-    __syncthreads();
     const uint64_t bound = sm.bound;
-    unsigned hits = __ballot_sync(~0u, best >= bound);
+    unsigned hits = __ballot_sync(~0u, reach >= bound);
     while (hits) {
       const int h = __ffs(hits) - 1, ht = warp * 32 + h;
       hits &= hits - 1;
@@ -327,7 +352,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
     // to the first CTA: the sums, and the largest in order
     cluster_sync();  // it is there
     if (tid < 4) store_peer(peer_addr((float *)&sm.part[rank] + tid, 0),
-                            tid == 0 ? part.m : tid == 1 ? part.S : tid == 2 ? part.W : __uint_as_float(part.top));
+                            tid == 0 ? part.base : tid == 1 ? part.S : tid == 2 ? part.W : __uint_as_float(part.top));
     auto send = [&](int at, uint64_t key) {
       asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_addr(&sm.of_cluster[rank * LV_MAX_TOP + at], 0)), "l"(key) : "memory");
     };
@@ -343,16 +368,26 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
         if (!sm.room[i]) send(i, 0);
     cluster_sync();
     if (rank != 0) return;
-    part = sm.part[0];
-    for (int k = 1; k < a.cluster; ++k) part = join(part, sm.part[k]);
-    n = 0;
+    float most = sm.part[0].base;
+    for (int k = 1; k < a.cluster; ++k) most = fmaxf(most, sm.part[k].base);
+    part = LpPart{most, 0.f, 0.f, 0};
+    for (int k = 0; k < a.cluster; ++k) {
+      LpPart p = sm.part[k];
+      rescale(p.base, most, &p.S, &p.W);
+      part.S += p.S;
+      part.W += p.W;
+      part.top = max(part.top, p.top);
+    }
     for (int i = tid; i < a.cluster * k_top; i += kLpThreads) sm.room[i] = sm.of_cluster[i / k_top * LV_MAX_TOP + i % k_top];
     n = a.cluster * k_top;
     __syncthreads();
   }
   // ---- the row's values
-  const float m = key_value(part.top), log_s = logf(part.S);
+  const float m = key_value(part.top);
   const bool none = m == -INFINITY;
+  // to the largest, whose exponential is 1
+  if (m == m && m != INFINITY && !none) rescale(part.base, m, &part.S, &part.W);
+  const float log_s = m == m ? logf(part.S) : NAN;
   auto log_p = [&](float x) { return none ? m : m == INFINITY ? x - m : (x - m) - log_s; };
   if (tid == 0) {
     if (a.lse) a.lse[t] = none || m == INFINITY ? m : m + log_s;
