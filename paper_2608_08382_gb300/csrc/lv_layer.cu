@@ -250,6 +250,17 @@ lv_status run_rotate(const KvHost *kv, RotateArgs &a, bool neighbours, cudaStrea
                     : launch_after(k_rotate<D, F16, false, false>, grid, kThreads, 0, 0, stream, a);
 }
 
+template <int TYPE>
+lv_status run_logprobs(const KvHost *kv, LogprobArgs &a, cudaStream_t stream) {
+  const int64_t vectors = a.vocab / (TYPE == LV_F32 ? 4 : 8);
+  int threads = a.n_tok >= 16 * kv->sms ? 128 : 256;
+  while (a.cluster < kLpCluster && a.n_tok * a.cluster * 2 <= 4 * kv->sms && vectors >= 2 * a.cluster * 8 * threads) a.cluster *= 2;
+  const int64_t grid = a.n_tok * a.cluster;
+  if (grid > INT32_MAX) return LV_EINVAL;
+  return threads == 256 ? launch_after(k_logprobs<TYPE, 256>, grid, 256, 0, a.cluster, stream, a)
+                        : launch_after(k_logprobs<TYPE, 128>, grid, 128, 0, a.cluster, stream, a);
+}
+
 }  // namespace
 
 extern "C" {
@@ -332,15 +343,9 @@ lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int6
     return LV_EINVAL;
   const KvHost *kv = kv_host(ctx);
   LogprobArgs a{logits, stride, n_tok, vocab, n_top, 1, ids, logp, entropy, lse, top_ids, top_logp, kv->d_status};
-  // CTAs for every SM, four of them, where a row has loads for more
-  const int64_t vectors = vocab / (dtype == LV_F32 ? 4 : 8);
-  while (a.cluster < kLpCluster && n_tok * a.cluster < 4 * kv->sms && vectors >= 2 * a.cluster * 2 * kLpThreads) a.cluster *= 2;
-  if (n_tok * a.cluster > INT32_MAX) return LV_EINVAL;
   cudaStream_t stream = (cudaStream_t)stream_;
-  const int64_t grid = n_tok * a.cluster;
-  if (dtype == LV_BF16) return launch_after(k_logprobs<LV_BF16>, grid, kLpThreads, 0, a.cluster, stream, a);
-  if (dtype == LV_F16) return launch_after(k_logprobs<LV_F16>, grid, kLpThreads, 0, a.cluster, stream, a);
-  return launch_after(k_logprobs<LV_F32>, grid, kLpThreads, 0, a.cluster, stream, a);
+  if (dtype == LV_BF16) return run_logprobs<LV_BF16>(kv, a, stream);
+  return dtype == LV_F16 ? run_logprobs<LV_F16>(kv, a, stream) : run_logprobs<LV_F32>(kv, a, stream);
 }
 
 }  // extern "C"

@@ -3,18 +3,19 @@
 // W = sum exp(x - m) (x - m),
 //   lse = m + log S,  log p_v = (x_v - m) - log S,  entropy = log S - W / S.
 //
-// One pass over a row, by the 256 threads of a CTA, 16 bytes a load, four asked for while
+// One pass over a row, by the threads of a CTA, 16 bytes a load, four asked for while
 // four are added up; a thread keeps S and W relative to a logit of its own, which it
 // takes anew only where one comes that is more than 8 above it (a scale that follows
 // the maximum costs every warp a scaling every few loads), and which of its vectors
 // holds its largest logit.  Few rows are shared by clusters of up to eight CTAs, whose
 // sums and largest meet in the first one's shared memory.
 //
-// The n_top largest: of the 32 groups of eight threads each has a largest logit, and the
+// The n_top largest: of 32 groups of its threads each has a largest logit, and the
 // n_top-th of those bounds the row's n_top-th from below (of equal ones by index; that of
 // its vector will do).  Only threads whose own
-// largest reaches the bound hold candidates; their warps read their logits once more
-// (a few of 256, still in L2) and the candidates are put in order by counting for each
+// largest reaches the bound hold candidates; their logits are read once more, by all
+// threads (a few threads' logits, still in L2; by the warps that had them, one hit after
+// another: 9 us for 20 of 128,000), and the candidates are put in order by counting for each
 // those above it.  Where there are more candidates than room (a row in descending
 // order), or the row has a NaN or +inf, the largest are looked for one after another.
 // Every comparison is of a value and its index, so that nothing depends on an order of
@@ -59,11 +60,10 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 __device__ __forceinline__ uint64_t full_key(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (uint32_t)~index; }
 __device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32;
-constexpr int kLpGroups = kLpThreads / 8;
+constexpr int kLpGroups = 32;
 constexpr int kLpRoom = 2048;   // candidates; also the logits of a row that leaves a group empty
 constexpr int kLpCluster = 8;
-static_assert(kLpGroups >= LV_MAX_TOP && kLpGroups * 8 * 8 <= kLpRoom, "a bound from the groups, or all logits");
+static_assert(kLpGroups >= LV_MAX_TOP, "a bound from the groups");
 
 // A difference of logits beyond which the exponential is 0, and that times it too.
 constexpr float kLpFar = -1e30f;
@@ -72,16 +72,18 @@ struct LpPart {       // of a CTA's share of a row
   float base, S, W;   // sums of exp(x - base) and of that times (x - base)
   uint32_t top;       // the largest's order key, 0 where there is no logit
 };
+template <int WARPS>
 struct LpSmem {
   uint64_t room[kLpRoom];
   uint64_t of_cluster[kLpCluster * LV_MAX_TOP];  // the first CTA's: everyone's largest
   uint64_t group[kLpGroups];
-  uint64_t warp_key[kLpWarps];
-  float warp_base[kLpWarps], warp_S[kLpWarps], warp_W[kLpWarps];
-  uint32_t warp_top[kLpWarps];
+  uint64_t warp_key[WARPS];
+  float warp_base[WARPS], warp_S[WARPS], warp_W[WARPS];
+  uint32_t warp_top[WARPS];
   LpPart part[kLpCluster];
   uint64_t bound;
-  int n;
+  uint16_t hit[WARPS * 32];  // threads with a largest that reaches the bound
+  int hits, n;
 };
 
 __device__ __forceinline__ uint4 load_once(const void *p) {
@@ -162,10 +164,13 @@ __device__ __forceinline__ void rescale(float base, float to, float *S, float *W
   *S *= f;
 }
 
-template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a) {
+template <int TYPE, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const LogprobArgs a) {
   constexpr int kSize = TYPE == LV_F32 ? 4 : 2, kE = 16 / kSize, kAsk = 4;
-  __shared__ LpSmem sm;
+  constexpr int kWarps = THREADS / 32, kLanes = THREADS / kLpGroups;  // lanes of a group
+  // where a group has no logit there is none past it either, but for two vectors in part
+  static_assert((THREADS - kLanes + 2) * kE <= kLpRoom, "all logits");
+  __shared__ LpSmem<kWarps> sm;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t t = blockIdx.x / a.cluster;
   const uint32_t rank = blockIdx.x % a.cluster;
@@ -212,27 +217,27 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
   auto ask = [&](int j) {
 #pragma unroll
     for (int k = 0; k < kAsk; ++k)
-      if (j + k * kLpThreads < whole1) next[k] = load_once(line + (int64_t)(j + k * kLpThreads) * 16);
+      if (j + k * THREADS < whole1) next[k] = load_once(line + (int64_t)(j + k * THREADS) * 16);
   };
   ask(whole0 + tid);
-  for (int j = whole0 + tid; j < whole1; j += kLpThreads * kAsk) {
+  for (int j = whole0 + tid; j < whole1; j += THREADS * kAsk) {
     uint4 raw[kAsk];
 #pragma unroll
     for (int k = 0; k < kAsk; ++k) raw[k] = next[k];
-    ask(j + kLpThreads * kAsk);
+    ask(j + THREADS * kAsk);
 #pragma unroll
     for (int k = 0; k < kAsk; ++k)
-      if (j + k * kLpThreads < whole1) run.seen(largest_of<TYPE>(raw[k]), j + k * kLpThreads);
+      if (j + k * THREADS < whole1) run.seen(largest_of<TYPE>(raw[k]), j + k * THREADS);
     run.rebase();
 #pragma unroll
     for (int k = 0; k < kAsk; ++k)
-      if (j + k * kLpThreads < whole1) {
+      if (j + k * THREADS < whole1) {
         uint64_t v[kE / 2];
         logit_pairs<TYPE>(raw[k], v);
         run.add(v);
       }
   }
-  if (tail && tid == kLpThreads - 1) edge(to - 1);
+  if (tail && tid == THREADS - 1) edge(to - 1);
   // ---- the CTA's sums, relative to the largest base
   LpPart part{run.set ? run.base : -INFINITY, 0.f, 0.f, run.where < 0 ? 0 : order_key(run.m)};
 #pragma unroll
@@ -251,13 +256,13 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
       reach = full_key(key, max(index(run.where, 0), 0));
     }
 #pragma unroll
-    for (int s = 4; s; s >>= 1) least = larger(least, __shfl_xor_sync(~0u, least, s));
-    if ((lane & 7) == 0) sm.group[tid >> 3] = least;
+    for (int s = kLanes / 2; s; s >>= 1) least = larger(least, __shfl_xor_sync(~0u, least, s));
+    if (lane % kLanes == 0) sm.group[tid / kLanes] = least;
   }
-  if (tid == 0) sm.n = 0;
+  if (tid == 0) sm.n = sm.hits = 0;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kLpWarps; ++k) {
+  for (int k = 0; k < kWarps; ++k) {
     part.base = fmaxf(part.base, sm.warp_base[k]);
     part.top = max(part.top, sm.warp_top[k]);
   }
@@ -294,30 +299,41 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
   __syncthreads();
   part.S = sm.warp_S[0], part.W = sm.warp_W[0];
 #pragma unroll
-  for (int k = 1; k < kLpWarps; ++k) part.S += sm.warp_S[k], part.W += sm.warp_W[k];
+  for (int k = 1; k < kWarps; ++k) part.S += sm.warp_S[k], part.W += sm.warp_W[k];
   bool slow = part.S != part.S;  // a NaN, or an infinity less itself
   if (a.n_top > 0 && !slow) {
     // ---- candidates
     const uint64_t bound = sm.bound;
-    unsigned hits = __ballot_sync(~0u, reach >= bound);
-    while (hits) {
-      const int h = __ffs(hits) - 1, ht = warp * 32 + h;
-      hits &= hits - 1;
-      auto look = [&](int j) {
-#pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          const int i = index(j, e);
-          if (!in_row(i)) continue;
-          const uint64_t key = full_key(order_key(logit(j, e)), i);
-          if (key >= bound) {
-            const int n = atomicAdd(&sm.n, 1);
-            if (n < kLpRoom) sm.room[n] = key;
-          }
-        }
-      };
-      for (int j = whole0 + ht + lane * kLpThreads; j < whole1; j += 32 * kLpThreads) look(j);
-      if (head && ht == 0 && lane == 0) look(from);
-      if (tail && ht == kLpThreads - 1 && lane == 0) look(to - 1);
+    const uint32_t bound_key = (uint32_t)(bound >> 32);
+    const bool hit = reach >= bound;
+    const unsigned hits = __ballot_sync(~0u, hit);
+    if (hits) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&sm.hits, __popc(hits));
+      at = __shfl_sync(~0u, at, 0) + __popc(hits & ((1u << lane) - 1));
+      if (hit) sm.hit[at] = (uint16_t)tid;
+    }
+    auto keep = [&](int j, int e) {
+      const int i = index(j, e);
+      if (!in_row(i)) return;
+      const uint64_t key = full_key(order_key(logit(j, e)), i);
+      if (key < bound) return;
+      const int n = atomicAdd(&sm.n, 1);
+      if (n < kLpRoom) sm.room[n] = key;
+    };
+    if (head && tid == 0 && hit)
+      for (int e = 0; e < kE; ++e) keep(from, e);
+    if (tail && tid == THREADS - 1 && hit)
+      for (int e = 0; e < kE; ++e) keep(to - 1, e);
+    __syncthreads();
+    // all their vectors, dealt out to all threads
+    const unsigned per = (unsigned)(whole1 - whole0 + THREADS - 1) / THREADS, looks = sm.hits * per;
+#pragma unroll 2
+    for (unsigned i = tid; i < looks; i += THREADS) {
+      const unsigned h = i / per;
+      const int j = whole0 + sm.hit[h] + (int)(i - h * per) * THREADS;
+      if (j < whole1 && order_key(largest_of<TYPE>(load_once(line + (int64_t)j * 16))) >= bound_key)
+        for (int e = 0; e < kE; ++e) keep(j, e);
     }
     __syncthreads();
     slow = sm.n > kLpRoom;
@@ -328,7 +344,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
     uint64_t below = ~0ull;
     for (int k = 0; k < max(k_top, 1); ++k) {
       uint64_t next = 0;
-      for (int j = from + tid; j < to; j += kLpThreads)
+      for (int j = from + tid; j < to; j += THREADS)
         for (int e = 0; e < kE; ++e) {
           const int i = index(j, e);
           if (!in_row(i)) continue;
@@ -340,7 +356,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
       __syncthreads();
       if (lane == 0) sm.warp_key[warp] = next;
       __syncthreads();
-      for (int w = 0; w < kLpWarps; ++w) next = larger(next, sm.warp_key[w]);
+      for (int w = 0; w < kWarps; ++w) next = larger(next, sm.warp_key[w]);
       if (k == 0) part.top = max(part.top, (uint32_t)(next >> 32));
       if (tid == 0) sm.room[k] = next;
       below = next;
@@ -356,15 +372,15 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
     auto send = [&](int at, uint64_t key) {
       asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_addr(&sm.of_cluster[rank * LV_MAX_TOP + at], 0)), "l"(key) : "memory");
     };
-    for (int i = tid; i < n; i += kLpThreads) {
+    for (int i = tid; i < n; i += THREADS) {
       const uint64_t mine = sm.room[i];
       int above = 0;
       for (int k = 0; k < n; ++k) above += sm.room[k] > mine;
       if (above < k_top && mine) send(above, mine);
     }
-    for (int i = n + tid; i < k_top; i += kLpThreads) send(i, 0);
+    for (int i = n + tid; i < k_top; i += THREADS) send(i, 0);
     if (slow)
-      for (int i = tid; i < k_top; i += kLpThreads)
+      for (int i = tid; i < k_top; i += THREADS)
         if (!sm.room[i]) send(i, 0);
     cluster_sync();
     if (rank != 0) return;
@@ -378,7 +394,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
       part.W += p.W;
       part.top = max(part.top, p.top);
     }
-    for (int i = tid; i < a.cluster * k_top; i += kLpThreads) sm.room[i] = sm.of_cluster[i / k_top * LV_MAX_TOP + i % k_top];
+    for (int i = tid; i < a.cluster * k_top; i += THREADS) sm.room[i] = sm.of_cluster[i / k_top * LV_MAX_TOP + i % k_top];
     n = a.cluster * k_top;
     __syncthreads();
   }
@@ -397,7 +413,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
   if (k_top > 0) {
     int32_t *const ids = a.top_ids + t * k_top;
     float *const lp = a.top_logp + t * k_top;
-    for (int i = tid; i < n; i += kLpThreads) {
+    for (int i = tid; i < n; i += THREADS) {
       const uint64_t mine = sm.room[i];
       if (!mine) continue;
       int above = 0;
@@ -407,7 +423,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) k_logprobs(const LogprobArgs a)
         lp[above] = log_p(key_value((uint32_t)(mine >> 32)));
       }
     }
-    for (int i = a.vocab + tid; i < k_top; i += kLpThreads) {  // past the vocabulary's end
+    for (int i = a.vocab + tid; i < k_top; i += THREADS) {  // past the vocabulary's end
       ids[i] = -1;
       lp[i] = -INFINITY;
     }
