@@ -313,18 +313,18 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
       at = __shfl_sync(~0u, at, 0) + __popc(hits & ((1u << lane) - 1));
       if (hit) sm.hit[at] = (uint16_t)tid;
     }
-    auto keep = [&](int j, int e) {
-      const int i = index(j, e);
-      if (!in_row(i)) return;
-      const uint64_t key = full_key(order_key(logit(j, e)), i);
+    auto keep = [&](int j, int e, float v) {
+      const uint64_t key = full_key(order_key(v), index(j, e));
       if (key < bound) return;
       const int n = atomicAdd(&sm.n, 1);
       if (n < kLpRoom) sm.room[n] = key;
     };
     if (head && tid == 0 && hit)
-      for (int e = 0; e < kE; ++e) keep(from, e);
+      for (int e = 0; e < kE; ++e)
+        if (in_row(index(from, e))) keep(from, e, logit(from, e));
     if (tail && tid == THREADS - 1 && hit)
-      for (int e = 0; e < kE; ++e) keep(to - 1, e);
+      for (int e = 0; e < kE; ++e)
+        if (in_row(index(to - 1, e))) keep(to - 1, e, logit(to - 1, e));
     __syncthreads();
     // all their vectors, dealt out to all threads
     const unsigned per = (unsigned)(whole1 - whole0 + THREADS - 1) / THREADS, looks = sm.hits * per;
@@ -332,8 +332,18 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
     for (unsigned i = tid; i < looks; i += THREADS) {
       const unsigned h = i / per;
       const int j = whole0 + sm.hit[h] + (int)(i - h * per) * THREADS;
-      if (j < whole1 && order_key(largest_of<TYPE>(load_once(line + (int64_t)j * 16))) >= bound_key)
-        for (int e = 0; e < kE; ++e) keep(j, e);
+      if (j >= whole1) continue;
+      const uint4 raw = load_once(line + (int64_t)j * 16);
+      if (order_key(largest_of<TYPE>(raw)) < bound_key) continue;
+      uint64_t v[kE / 2];
+      logit_pairs<TYPE>(raw, v);
+#pragma unroll
+      for (int e = 0; e < kE; e += 2) {
+        float p, q;
+        unpair(v[e / 2], &p, &q);
+        keep(j, e, p);
+        keep(j, e + 1, q);
+      }
     }
     __syncthreads();
     slow = sm.n > kLpRoom;
