@@ -171,7 +171,7 @@ Shape choose(const Clusters &hold, int64_t n_tok, int64_t row_tiles, int64_t chu
     if (t > kSpTokens || row_tiles * token_tiles > 4096) continue;
     for (int split = 1; split <= kSpSplit && split <= chunks; ++split) {
       const int64_t tiles = row_tiles * token_tiles, at_once = hold.most[split].load(std::memory_order_relaxed);
-      if (split > 1 && tiles > 2 * at_once) break;
+      if (split > 1 && (tiles > 2 * at_once || split_sums((int)t, split) > kSpRoom)) break;
       const int64_t share = tiles > at_once ? 2 : 1, rounds = (tiles + 2 * at_once - 1) / (2 * at_once);
       const int64_t piece = std::max<int64_t>(std::max<int64_t>(255, share * 170), share * std::max(2 * t, 128 + t) * 10 / 19);
       const int64_t cost = rounds * ((chunks + split - 1) / split * piece + 1500 + 56 * t) + (split > 1 ? 510 * split : 0);
@@ -211,8 +211,9 @@ lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t 
   }
   st = limit_smem(kv, k_product<GATED, F16>, kind);
   if (st != LV_OK) return st;
-  a.stages = (int)std::min<size_t>((111 << 10) / split_stage(a.tokens), kSpStages);
-  return launch_after(k_product<GATED, F16>, a.tiles * a.split, kSpThreads, split_smem(a.tokens, a.stages), a.split, stream,
+  a.stages = (int)std::min<size_t>(kSpRoom / split_stage(a.tokens), kSpStages);
+  a.room = (int)((std::max(a.stages * split_stage(a.tokens), split_sums(a.tokens, a.split)) + 15) / 16 * 16);
+  return launch_after(k_product<GATED, F16>, a.tiles * a.split, kSpThreads, 1024 + a.room + sizeof(SplitSmem), a.split, stream,
                       a, mw, mu, mx);
 }
 

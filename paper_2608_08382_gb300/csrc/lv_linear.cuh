@@ -27,7 +27,7 @@ struct LinearArgs {
   int d_out, act;
   int chunks;                // pieces of 64 along the sum
   int tokens;                // columns of a tile, a multiple of 16
-  int stages;
+  int stages, room;          // of the stages, and the bytes that they or the sums take (k_product)
   int split;                 // CTAs that share a tile's sum (k_product)
   int64_t token_tiles, tiles;
   int *status;
@@ -406,6 +406,13 @@ __device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
   return r;
 }
+// n bytes in a row from this block's shared memory to that of another one, counted by a
+// barrier there: addresses and n multiples of 16.
+__device__ __forceinline__ void send_bytes(uint32_t to, const void *from, uint32_t n, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+               "r"(smem_addr(from)), "r"(n), "r"(bar)
+               : "memory");
+}
 __device__ __forceinline__ void store_peer(uint32_t at, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
 }
@@ -423,24 +430,31 @@ constexpr int kSpSplit = 8;      // a portable cluster
 constexpr int kSpStages = 16;    // at most
 
 struct SplitSmem {
-  uint64_t full[kSpStages], empty[kSpStages], done;
+  uint64_t full[kSpStages], empty[kSpStages], done, joined;
   uint32_t tmem;
   int stop[3];  // see bar_wait
 };
-// The stages stand first, from a 1,024-byte boundary on, then this.
+// The stages stand first, from a 1,024-byte boundary on, and later a tile's sums in
+// their place: a CTA's own and those that it gets, or the way out's rooms.  Then this.
 constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPiece * 2; }
-constexpr size_t split_smem(int tokens, int stages) { return 1024 + stages * split_stage(tokens) + sizeof(SplitSmem); }
-static_assert(3 * split_stage(kSpTokens) >= (kSpTokens + kSpSplit) * kColFloats * sizeof(float), "the sums stand in the stages");
+constexpr size_t split_sums(int tokens, int split) {
+  return split == 1 ? 8 * sizeof(OutRoom) : (tokens + (split - 1) * (size_t)((tokens + split - 1) / split)) * kColFloats * sizeof(float);
+}
+constexpr size_t kSpRoom = 111 << 10;  // of both: two CTAs an SM
 
 // The parts of a tile's sums to the CTAs that finish them, and out from there.  The
-// columns that CTA r finishes begin at first(r); a part's place is by the CTA that
-// formed it, then by the column.
+// columns that CTA r finishes begin at r tokens / split.  A CTA puts its accumulator into
+// its own shared memory, a column of 132 floats after the other, and sends each other
+// CTA its columns by one bulk copy; what it gets stands behind, by the sender.  (By
+// stores of four bytes a lane into the others' shared memory: 2 to 5 us longer for 96
+// tokens.)
 template <bool GATED, bool F16>
-__device__ __forceinline__ void join(const LinearArgs &a, uint32_t tmem, float *sums, int warp, int lane, uint32_t rank,
-                                     int64_t t0, int o0) {
+__device__ __forceinline__ void join(const LinearArgs &a, SplitSmem &sm, uint32_t tmem, float *sums, int warp, int lane,
+                                     uint32_t rank, int64_t t0, int o0, volatile int *stop) {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this CTA's stages are free
   auto first = [&](int r) { return a.tokens * r / a.split; };
   const int most = (a.tokens + a.split - 1) / a.split;
-  cluster_sync();
+  float *const got = sums + a.tokens * kColFloats;
   // Warps 0-3 and 4-7 take turns of 16 columns; a warp reads its quarter of the lanes.
   const int row = (warp & 3) * 32 + lane;
   const uint32_t lane0 = tmem + ((uint32_t)(warp & 3) * 32 << 16);
@@ -448,18 +462,16 @@ __device__ __forceinline__ void join(const LinearArgs &a, uint32_t tmem, float *
     uint32_t r[16];
     tmem_load16(r, lane0 + c0);
     tmem_wait_load();
-    int owner = ((c0 + 1) * a.split - 1) / a.tokens, begin = first(owner), end = first(owner + 1);
-    uint32_t at = peer_addr(sums + (rank * most + c0 - begin) * kColFloats + row, owner);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      if (c0 + k == end) {
-        begin = end;
-        end = first(++owner + 1);
-        at = peer_addr(sums + rank * most * kColFloats + row, owner);
-      }
-      store_peer(at, __uint_as_float(r[k]));
-      at += kColFloats * sizeof(float);
-    }
+    for (int k = 0; k < 16; ++k) sums[(c0 + k) * kColFloats + row] = __uint_as_float(r[k]);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncthreads();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (threadIdx.x < a.split && threadIdx.x != rank) {
+    const int to = threadIdx.x, begin = first(to);
+    send_bytes(peer_addr(got + (rank < to ? rank : rank - 1) * most * kColFloats, to), sums + begin * kColFloats,
+               (uint32_t)((first(to + 1) - begin) * kColFloats * sizeof(float)), peer_addr(&sm.joined, to));
   }
   constexpr int kGroups = tile_outputs<GATED>() / 8;
   const int group = threadIdx.x % kGroups, o = o0 + group * 8;
@@ -472,11 +484,12 @@ __device__ __forceinline__ void join(const LinearArgs &a, uint32_t tmem, float *
   p.left = min(p.left, mine - c);
   uint4 next[1];
   load_residual(p, kStep, 0, next);
-  cluster_sync();
+  bar_wait(&sm.joined, 0, stop);
   for (; c < mine; c += kStep) {
     float v[1][8] = {}, u[1][8] = {};
     for (int s = 0; s < a.split; ++s) {
-      const float *const at = sums + (s * most + c) * kColFloats + group * 8;
+      const float *const at =
+          (s == rank ? sums + (begin + c) * kColFloats : got + ((s < rank ? s : s - 1) * most + c) * kColFloats) + group * 8;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         const float4 q = *(const float4 *)(at + e);
@@ -492,6 +505,8 @@ __device__ __forceinline__ void join(const LinearArgs &a, uint32_t tmem, float *
     finish<GATED, F16>(a, p, kStep, v, u, b, now);
     advance(p, 1, kStep);
   }
+  __syncwarp();
+  cluster_sync();  // what this CTA sent has arrived
 }
 
 template <bool GATED, bool F16>
@@ -501,7 +516,7 @@ __global__ void __launch_bounds__(kSpThreads)
   extern __shared__ unsigned char raw_product[];
   unsigned char *const stage0 = (unsigned char *)((reinterpret_cast<uintptr_t>(raw_product) + 1023) & ~(uintptr_t)1023);
   const uint32_t stage_bytes = kWBytes + a.tokens * kPiece * 2;
-  SplitSmem &sm = *reinterpret_cast<SplitSmem *>(stage0 + (size_t)a.stages * stage_bytes);
+  SplitSmem &sm = *reinterpret_cast<SplitSmem *>(stage0 + a.room);
   const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t columns = columns_for(a.tokens);
   if (warp == 0) tmem_alloc(&sm.tmem, columns);
@@ -515,6 +530,7 @@ __global__ void __launch_bounds__(kSpThreads)
       bar_init(&sm.empty[k], 1);
     }
     bar_init(&sm.done, 1);
+    bar_init(&sm.joined, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -530,6 +546,8 @@ __global__ void __launch_bounds__(kSpThreads)
   const int o0 = (int)(tile / a.token_tiles) * tile_outputs<GATED>();
   const int from = (int)((int64_t)a.chunks * rank / a.split), to = (int)((int64_t)a.chunks * (rank + 1) / a.split);
   const int n = to - from;
+  if (threadIdx.x == 0 && a.split > 1)
+    bar_expect(&sm.joined, (uint32_t)((a.split - 1) * (a.tokens * (rank + 1) / a.split - a.tokens * rank / a.split) * kColFloats * 4));
   // While the kernel before this one ends, the first weights come as far as L2, where
   // whatever that kernel may still write to them is seen.
   if (warp == 1 && elect_one()) {
@@ -584,7 +602,7 @@ __global__ void __launch_bounds__(kSpThreads)
     __syncthreads();
     drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, [] {}, [] {});
   } else {
-    join<GATED, F16>(a, tmem, sums, warp, lane, rank, t0, o0);
+    join<GATED, F16>(a, sm, tmem, sums, warp, lane, rank, t0, o0, stop);
   }
   tc_before_sync();
   if (threadIdx.x == 0 && *stop) {
