@@ -220,23 +220,36 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
       if (j + k * THREADS < whole1) next[k] = load_once(line + (int64_t)(j + k * THREADS) * 16);
   };
   ask(whole0 + tid);
-  for (int j = whole0 + tid; j < whole1; j += THREADS * kAsk) {
+  auto batch = [&](int j, auto there) {  // the vectors in `next`, or those that there are
     uint4 raw[kAsk];
 #pragma unroll
     for (int k = 0; k < kAsk; ++k) raw[k] = next[k];
     ask(j + THREADS * kAsk);
+    float top[kAsk], most = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kAsk; ++k) {
+      top[k] = there(k) ? largest_of<TYPE>(raw[k]) : -INFINITY;
+      most = fmaxf(most, top[k]);
+    }
+    if (run.where < 0) run.where = j;
+    if (most > run.m) {
+      run.m = most;
+#pragma unroll
+      for (int k = kAsk - 1; k >= 0; --k)
+        if (top[k] == most) run.where = j + k * THREADS;
+      run.rebase();
+    }
 #pragma unroll
     for (int k = 0; k < kAsk; ++k)
-      if (j + k * THREADS < whole1) run.seen(largest_of<TYPE>(raw[k]), j + k * THREADS);
-    run.rebase();
-#pragma unroll
-    for (int k = 0; k < kAsk; ++k)
-      if (j + k * THREADS < whole1) {
+      if (there(k)) {
         uint64_t v[kE / 2];
         logit_pairs<TYPE>(raw[k], v);
         run.add(v);
       }
-  }
+  };
+  int j = whole0 + tid;
+  for (; j + (kAsk - 1) * THREADS < whole1; j += THREADS * kAsk) batch(j, [](int) { return true; });
+  if (j < whole1) batch(j, [&](int k) { return j + k * THREADS < whole1; });
   if (tail && tid == THREADS - 1) edge(to - 1);
   // ---- the CTA's sums, relative to the largest base
   LpPart part{run.set ? run.base : -INFINITY, 0.f, 0.f, run.where < 0 ? 0 : order_key(run.m)};
