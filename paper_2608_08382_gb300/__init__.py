@@ -538,17 +538,36 @@ _acts = {"none": LV_ACT_NONE, "silu": LV_ACT_SILU, "gelu": LV_ACT_GELU, "gelu_ta
          "relu": LV_ACT_RELU}
 
 
-def _flat(x, width, where):
-    """Row stride in elements of an [n][width] tensor on a GPU whose rows are without gaps inside."""
-    _want(x.dim() == 2 and x.shape[1] == width and x.is_cuda and (width == 1 or x.stride(1) == 1), where)
-    return x.stride(0) if x.shape[0] > 1 else -(-width // 8) * 8
+# What a call of these costs on the host is what a small step waits for: the checks below ask a tensor for each thing
+# once, and raise in one place.
+
+def _flat(x, shape, dtype, where):
+    """Row stride in elements of a tensor of that shape and type on a GPU whose rows are without gaps inside."""
+    if x.shape != shape or x.dtype != dtype or not x.is_cuda:
+        raise LVError(LV_EINVAL, where)
+    rows, one = x.stride()
+    if one != 1 and shape[1] != 1:
+        raise LVError(LV_EINVAL, where)
+    return rows if shape[0] > 1 else -(-shape[1] // 8) * 8
+
+
+def _heads(x, shape, dtype, where):
+    """Token stride in elements of a [token][head][element] tensor of that shape and type on a GPU, without gaps inside a
+    token."""
+    if x.shape != shape or x.dtype != dtype or not x.is_cuda:
+        raise LVError(LV_EINVAL, where)
+    tokens, heads, one = x.stride()
+    if one != 1 or (heads != shape[2] and shape[1] != 1):
+        raise LVError(LV_EINVAL, where)
+    return tokens if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _vector(v, n, dtype, where):
     """Address of a vector of n elements on a GPU, or None."""
     if v is None:
         return None
-    _want(v.dtype == dtype and v.dim() == 1 and v.shape[0] == n and v.is_cuda and (n == 1 or v.stride(0) == 1), where)
+    if v.dtype != dtype or v.shape != (n,) or not v.is_cuda or (n > 1 and v.stride(0) != 1):
+        raise LVError(LV_EINVAL, where)
     return v.data_ptr()
 
 
@@ -556,27 +575,31 @@ def lv_linear(ctx: Context, x, w, y, bias=None, act="none", residual=None, strea
     """y = act(x w^T + bias) + residual: x [n_tok][d_in], w [d_out][d_in], y and residual [n_tok][d_out] (which may be the
     same tensor), bias [d_out]; rows may be slices of wider ones that begin at 16-byte boundaries.  act: "none", "silu",
     "gelu", "gelu_tanh" or "relu"."""
-    t, at = _dtypes or _types(), "lv_linear"
-    (n, d_in), (d_out, _), dt = _sizes(x, 2, at), _sizes(w, 2, at), x.dtype
-    _want(dt in t and w.dtype == y.dtype == dt and y.shape[0] == n and act in _acts
-          and (residual is None or (residual.dtype == dt and residual.shape[0] == n)), at)
-    _check(_lib.lv_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, d_in, at), n, w.data_ptr(), _flat(w, d_in, at), d_in, d_out,
-                          _vector(bias, d_out, dt, at), _acts[act], _ptr(residual),
-                          0 if residual is None else _flat(residual, d_out, at), y.data_ptr(), _flat(y, d_out, at),
+    t, at, dt = _dtypes or _types(), "lv_linear", x.dtype
+    (n, d_in), (d_out, _) = _sizes(x, 2, at), _sizes(w, 2, at)
+    out = (n, d_out)
+    if dt not in t or act not in _acts:
+        raise LVError(LV_EINVAL, at)
+    _check(_lib.lv_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, (n, d_in), dt, at), n, w.data_ptr(),
+                          _flat(w, (d_out, d_in), dt, at), d_in, d_out,
+                          None if bias is None else _vector(bias, d_out, dt, at), _acts[act],
+                          None if residual is None else residual.data_ptr(),
+                          0 if residual is None else _flat(residual, out, dt, at), y.data_ptr(), _flat(y, out, dt, at),
                           _stream(stream)), at)
 
 
 def lv_gated_linear(ctx: Context, x, w_gate, w_up, y, bias_gate=None, bias_up=None, act="silu", stream=None):
     """y = act(x w_gate^T + bias_gate) * (x w_up^T + bias_up): x [n_tok][d_in], w_gate and w_up [d_out][d_in] of one
     stride, y [n_tok][d_out], biases [d_out]; as lv_linear otherwise."""
-    t, at = _dtypes or _types(), "lv_gated_linear"
-    (n, d_in), (d_out, _), dt = _sizes(x, 2, at), _sizes(w_gate, 2, at), x.dtype
-    stride = _flat(w_gate, d_in, at)
-    _want(dt in t and w_gate.dtype == w_up.dtype == y.dtype == dt and w_up.shape == w_gate.shape and y.shape[0] == n
-          and _flat(w_up, d_in, at) == stride and act in _acts, at)
-    _check(_lib.lv_gated_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, d_in, at), n, w_gate.data_ptr(), w_up.data_ptr(),
-                                stride, d_in, d_out, _vector(bias_gate, d_out, dt, at), _vector(bias_up, d_out, dt, at),
-                                _acts[act], y.data_ptr(), _flat(y, d_out, at), _stream(stream)), at)
+    t, at, dt = _dtypes or _types(), "lv_gated_linear", x.dtype
+    (n, d_in), (d_out, _) = _sizes(x, 2, at), _sizes(w_gate, 2, at)
+    stride = _flat(w_gate, (d_out, d_in), dt, at)
+    if dt not in t or act not in _acts or _flat(w_up, (d_out, d_in), dt, at) != stride:
+        raise LVError(LV_EINVAL, at)
+    _check(_lib.lv_gated_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, (n, d_in), dt, at), n, w_gate.data_ptr(),
+                                w_up.data_ptr(), stride, d_in, d_out, _vector(bias_gate, d_out, dt, at),
+                                _vector(bias_up, d_out, dt, at), _acts[act], y.data_ptr(), _flat(y, (n, d_out), dt, at),
+                                _stream(stream)), at)
 
 
 class Rope:
@@ -601,18 +624,17 @@ def lv_qk_rotate(ctx: Context, q, k, q_out, k_out, rope: Rope, c=None, token_off
     k [n_tok][n_kv_heads][head_dim] into q_out and k_out (slices of wider tensors may be given; q_out may be q, k_out k).
     Positions as lv_kv_attend's: int32 c [n_req], int64 token_offsets [n_req + 1] or None for one token a request; c None
     with token_offsets: requests that start on an empty cache."""
-    t, at = _dtypes or _types(), "lv_qk_rotate"
-    (n, hq, d), (_, hkv, _), dt = _sizes(q, 3, at), _sizes(k, 3, at), q.dtype
-    n_req = token_offsets.numel() - 1 if token_offsets is not None else n
-    _want(dt in t and k.dtype == q_out.dtype == k_out.dtype == dt and k.shape == (n, hkv, d) and q_out.shape == q.shape
-          and k_out.shape == k.shape and q.is_cuda and k.is_cuda and q_out.is_cuda and k_out.is_cuda and n_req >= 0
-          and (token_offsets is None or (token_offsets.dtype == t["i64"] and token_offsets.is_cuda
-                                         and token_offsets.is_contiguous()))
-          and (c is None or (c.dtype == t["i32"] and c.numel() == n_req and c.is_cuda and c.is_contiguous())), at)
-    _check(_lib.lv_qk_rotate(ctx.h, t[dt], hq, hkv, d, q.data_ptr(), _rows(q, at), k.data_ptr(), _rows(k, at), n,
-                             _ptr(token_offsets), _ptr(c), n_req, _vector(q_weight, d, dt, at),
-                             _vector(k_weight, d, dt, at), eps, rope.at, q_out.data_ptr(), _rows(q_out, at),
-                             k_out.data_ptr(), _rows(k_out, at), _stream(stream)), at)
+    t, at, dt = _dtypes or _types(), "lv_qk_rotate", q.dtype
+    qs, ks = _sizes(q, 3, at), _sizes(k, 3, at)
+    n, hq, d = qs
+    n_req = n if token_offsets is None else token_offsets.numel() - 1
+    if dt not in t or n_req < 0 or ks[0] != n or ks[2] != d:
+        raise LVError(LV_EINVAL, at)
+    _check(_lib.lv_qk_rotate(ctx.h, t[dt], hq, ks[1], d, q.data_ptr(), _heads(q, qs, dt, at), k.data_ptr(),
+                             _heads(k, ks, dt, at), n, _vector(token_offsets, n_req + 1, t["i64"], at),
+                             _vector(c, n_req, t["i32"], at), n_req, _vector(q_weight, d, dt, at),
+                             _vector(k_weight, d, dt, at), eps, rope.at, q_out.data_ptr(), _heads(q_out, qs, dt, at),
+                             k_out.data_ptr(), _heads(k_out, ks, dt, at), _stream(stream)), at)
 
 
 def lv_token_logprobs(ctx: Context, logits, ids=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None,
@@ -620,16 +642,18 @@ def lv_token_logprobs(ctx: Context, logits, ids=None, logp=None, entropy=None, l
     """Of each row of logits [n_tok][vocab] (bfloat16, float16 or float32, any row stride): log probabilities logp of the
     given int32 ids, entropy and lse [n_tok] float32, and the largest logits' ids and log probabilities, int32 top_ids and
     float32 top_logp [n_tok][n_top]; what is None is left out."""
-    t, at = _dtypes or _types(), "lv_token_logprobs"
+    t, at, dt = _dtypes or _types(), "lv_token_logprobs", logits.dtype
     n, vocab = _sizes(logits, 2, at)
-    dt, n_top = logits.dtype, 0 if top_ids is None else _sizes(top_ids, 2, at)[1]
-    f32 = t["f32"]
-    _want((dt == f32 or dt in t) and logits.is_cuda and (vocab == 1 or logits.stride(1) == 1)
-          and (top_ids is None) == (top_logp is None)
-          and (top_ids is None or (top_ids.dtype == t["i32"] and top_logp.dtype == f32 and top_ids.is_cuda
-                                   and top_logp.is_cuda and top_ids.shape == top_logp.shape == (n, n_top)
-                                   and top_ids.is_contiguous() and top_logp.is_contiguous())), at)
-    _check(_lib.lv_token_logprobs(ctx.h, LV_F32 if dt == f32 else t[dt], logits.data_ptr(),
-                                  logits.stride(0) if n > 1 else vocab, n, vocab, _vector(ids, n, t["i32"], at),
-                                  _vector(logp, n, f32, at), _vector(entropy, n, f32, at), _vector(lse, n, f32, at), n_top,
-                                  _ptr(top_ids), _ptr(top_logp), _stream(stream)), at)
+    n_top, f32 = 0 if top_ids is None else _sizes(top_ids, 2, at)[1], t["f32"]
+    kind = LV_F32 if dt == f32 else t.get(dt)
+    rows, one = logits.stride()
+    if kind is None or not logits.is_cuda or (one != 1 and vocab != 1) or (top_ids is None) != (top_logp is None):
+        raise LVError(LV_EINVAL, at)
+    if top_ids is not None and not (top_ids.dtype == t["i32"] and top_logp.dtype == f32 and top_ids.is_cuda
+                                    and top_logp.is_cuda and top_ids.shape == top_logp.shape == (n, n_top)
+                                    and top_ids.is_contiguous() and top_logp.is_contiguous()):
+        raise LVError(LV_EINVAL, at)
+    _check(_lib.lv_token_logprobs(ctx.h, kind, logits.data_ptr(), rows if n > 1 else vocab, n, vocab,
+                                  _vector(ids, n, t["i32"], at), _vector(logp, n, f32, at), _vector(entropy, n, f32, at),
+                                  _vector(lse, n, f32, at), n_top, None if top_ids is None else top_ids.data_ptr(),
+                                  None if top_logp is None else top_logp.data_ptr(), _stream(stream)), at)
