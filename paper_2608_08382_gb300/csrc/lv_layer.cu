@@ -311,7 +311,7 @@ lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_
     const double f = rope->freq[j];
     if (!(std::fabs(f) <= 8.0)) return LV_EINVAL;
     const double turns = std::fabs(f) / 6.283185307179586476925;  // whole ones do nothing
-    const uint64_t turn = (uint64_t)std::ldexp(turns - std::floor(turns), 64);
+    const uint64_t turn = (uint64_t)((turns - (double)(int64_t)turns) * 0x1p64);
     a.turn[j] = f < 0.0 ? 0 - turn : turn;
   }
   const int64_t dq = (int64_t)n_q_heads * head_dim, dk = (int64_t)n_kv_heads * head_dim;

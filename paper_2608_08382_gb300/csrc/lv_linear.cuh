@@ -38,16 +38,20 @@ __device__ __forceinline__ float value_of(uint16_t b) {
   return F16 ? __half2float(__ushort_as_half(b)) : __uint_as_float((uint32_t)b << 16);
 }
 
-// The activation in fp32.  1 + exp(-x) is infinite where x is below -88: x over it is
-// then -0 where the exact value is above -1e-36, and below every normal number of the
-// 16-bit types.  The two forms of GELU are written without the difference of nearly
-// equal numbers that 1 + erf and 1 + tanh have at the left: erfc, and 1 + tanh u =
+// 1 / (1 + exp(-x)), of whichever sign the exponential is small: nothing overflows, and
+// far to the left what is left is exp(x) and not the reciprocal of an infinity.
+__device__ __forceinline__ float logistic(float x) {
+  const float e = __expf(-fabsf(x));
+  return __fdividef(x < 0.f ? e : 1.f, 1.f + e);
+}
+// The activation in fp32.  The two forms of GELU are written without the difference of
+// nearly equal numbers that 1 + erf and 1 + tanh have at the left: erfc, and 1 + tanh u =
 // 2 / (1 + exp(-2u)).
 template <int ACT>
 __device__ __forceinline__ float activated(float x) {
-  if (ACT == LV_ACT_SILU) return __fdividef(x, 1.f + __expf(-x));
+  if (ACT == LV_ACT_SILU) return x * logistic(x);
   if (ACT == LV_ACT_GELU) return 0.5f * x * erfcf(x * -0.70710678118654752f);
-  if (ACT == LV_ACT_GELU_TANH) return __fdividef(x, 1.f + __expf(-1.5957691216057308f * (x + 0.044715f * x * x * x)));
+  if (ACT == LV_ACT_GELU_TANH) return x * logistic(1.5957691216057308f * (x + 0.044715f * x * x * x));
   return ACT == LV_ACT_RELU && x < 0.f ? 0.f : x;
 }
 template <int ACT, int N>

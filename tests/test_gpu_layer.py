@@ -182,6 +182,20 @@ def test_products_of_large_values(lv, ctx):
     assert ctx.status() == lv.LV_OK
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_activations_far_to_the_left(lv, ctx, act):
+    """Where the activation is small it keeps its size: within 2^-7 of itself down to the least normal number (an output's
+    half step 2^-8, and 2^-13 for an exponential of an argument of at most 90 that is rounded to 2^-23 of itself, six
+    times)."""
+    x = _held(-np.concatenate([np.linspace(0.01, 14, 200), np.linspace(14, 95, 200)]), "bf16")[:, None]
+    y, _ = _rows(np.zeros((len(x), 1)), "bf16")
+    lv.lv_linear(ctx, _rows(x, "bf16")[0], _rows(np.ones((1, 1)), "bf16")[0], y, act=act)
+    want, got = ref.act(x, act), _np(y)
+    normal = np.abs(want) > 2.0**-126
+    assert np.all(np.abs(got - want)[normal] <= 2.0**-7 * np.abs(want)[normal])
+    assert np.all(np.abs(got)[~normal] <= 2.0**-125)
+
+
 # ------------------------------------------------------------------ rotation
 
 LAYOUTS = [(32, 8, 128), (20, 4, 128), (10, 2, 128), (12, 12, 64), (16, 1, 64), (8, 1, 128), (1, 1, 64), (3, 3, 128),
