@@ -1,6 +1,6 @@
-"""Profiles the attention work of serving steps on this machine and fits the latency model to it.
+"""Profiles the attention work of serving steps on this machine, or the whole layer, and fits the latency model to it.
 
-    python examples/profile_steps.py [--layout 8b-tp1] [--steps 240] [--seed 1]
+    python examples/profile_steps.py [--whole] [--layout 8b-tp1] [--steps 240] [--seed 1]
 
 A small engine's loop: prompts arrive and are attended to whole, their keys and values appended to a paged 8-bit cache;
 between arrivals every running sequence takes a token, and now and then one of them a chunk of 200 more.  Each step is a
@@ -9,6 +9,12 @@ lv_kv_attend), timed with CUDA events.  As in an engine the GPU is at other work
 times are the GPU's and not those of the Python calls, and that work leaves nothing of the cache in L2.  The steps' requests and times are then what the library takes as profiled
 batches: lv_fit gives the coefficients of Eq. 1, lv_accuracy says how well they explain the times, lv_attribute shares
 the predicted times out to the requests.  One layer, random inputs.
+
+With --whole a step is all that the layer does for its tokens, the term of Eq. 1 that grows with their number among it:
+the projection to queries, keys and values (lv_linear), the norm and rotation of their heads (lv_qk_rotate), the attention
+as above, the output projection onto the residual stream (lv_linear), the feed-forward block (lv_gated_linear, lv_linear),
+and for each sequence's last token the logits and the log probability of a next one with its alternatives (lv_linear,
+lv_token_logprobs).
 """
 
 from __future__ import annotations
@@ -22,13 +28,65 @@ import numpy as np
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 LAYOUTS = {"8b-tp1": (32, 8, 128), "14b-tp2": (20, 4, 128), "32b-tp4": (10, 2, 128)}  # query, key/value heads, head size
+WIDTHS = {"8b-tp1": (4096, 14336), "14b-tp2": (5120, 6912), "32b-tp4": (5120, 6912)}  # hidden state, a rank's feed-forward
+VOCAB = 32_000
 BLOCK = 16
+
+
+class Layer:
+    """The weights of a layer on one rank and the work on its tokens outside the attention."""
+
+    def __init__(self, layout, ctx, gen):
+        import torch
+
+        import paper_2608_08382_gb300 as lv
+        self.lv, self.torch, self.ctx, self.gen = lv, torch, ctx, gen
+        self.hq, self.hkv, self.d = LAYOUTS[layout]
+        self.width, ffn = WIDTHS[layout]
+        heads = (self.hq + 2 * self.hkv) * self.d
+        self.w_qkv, self.w_o = self._w(heads, self.width), self._w(self.width, self.hq * self.d)
+        self.w_gate, self.w_up, self.w_down = self._w(ffn, self.width), self._w(ffn, self.width), self._w(self.width, ffn)
+        self.w_vocab, self.b_qkv = self._w(VOCAB, self.width), self.random(1, heads)[0]
+        self.w_q, self.w_k = self.random(1, self.d)[0] * 0.1 + 1, self.random(1, self.d)[0] * 0.1 + 1
+        self.rope = lv.Rope.geometric(self.d, 1e6)
+
+    def random(self, n, d):
+        return self.torch.randn(n, d, device="cuda", generator=self.gen).bfloat16()
+
+    def _w(self, d_out, d_in):
+        return self.random(d_out, d_in) * d_in**-0.5
+
+    def empty(self, *shape, dtype=None):
+        return self.torch.empty(shape, dtype=dtype or self.torch.bfloat16, device="cuda")
+
+    def before(self, h, qkv, c, offsets):
+        """Queries, keys and values [token][head][element] of hidden states h, at their sequences' positions."""
+        lv, n = self.lv, len(h)
+        lv.lv_linear(self.ctx, h, self.w_qkv, qkv.view(n, -1), bias=self.b_qkv)
+        q, k = qkv[:, :self.hq], qkv[:, self.hq:self.hq + self.hkv]
+        lv.lv_qk_rotate(self.ctx, q, k, q, k, self.rope, c=c, token_offsets=offsets, q_weight=self.w_q, k_weight=self.w_k)
+
+    def after(self, h, o, last, ids, out):
+        """What follows the attention's outputs o: the block's hidden states out["h"], and of the tokens `last` the log
+        probabilities of ids and the five most likely ones."""
+        lv, ctx = self.lv, self.ctx
+        lv.lv_linear(ctx, o.view(len(h), -1), self.w_o, out["h"], residual=h)
+        lv.lv_gated_linear(ctx, out["h"], self.w_gate, self.w_up, out["mid"])
+        lv.lv_linear(ctx, out["mid"], self.w_down, out["h"], residual=out["h"])
+        lv.lv_linear(ctx, out["h"].index_select(0, last), self.w_vocab, out["logits"])
+        lv.lv_token_logprobs(ctx, out["logits"], ids=ids, logp=out["logp"], top_ids=out["top_ids"], top_logp=out["top_logp"])
+
+    def outputs(self, n_tok, n_seq):
+        f32, i32 = self.torch.float32, self.torch.int32
+        return dict(h=self.empty(n_tok, self.width), mid=self.empty(n_tok, len(self.w_gate)), logits=self.empty(n_seq, VOCAB),
+                    logp=self.empty(n_seq, dtype=f32), top_ids=self.empty(n_seq, 5, dtype=i32),
+                    top_logp=self.empty(n_seq, 5, dtype=f32))
 
 
 class Engine:
     """The cache, the block tables and the running sequences of one layer's attention."""
 
-    def __init__(self, layout, n_blocks, max_seqs, max_len, seed, ctx=None):
+    def __init__(self, layout, n_blocks, max_seqs, max_len, seed, ctx=None, whole=False):
         import torch
 
         import paper_2608_08382_gb300 as lv
@@ -41,6 +99,7 @@ class Engine:
         self.table = torch.full((max_seqs, -(-max_len // BLOCK)), -1, dtype=torch.int32, device="cuda")
         self.lens = np.zeros(0, np.int64)  # tokens in the cache, of each running sequence
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.layer = Layer(layout, self.ctx, self.gen) if whole else None
         self.other = torch.empty(2 << 30, dtype=torch.uint8, device="cuda")  # what other work writes, a third of a millisecond
 
     def step(self, first, p):
@@ -58,15 +117,23 @@ class Engine:
         slots = torch.empty(tok, dtype=torch.int64, device="cuda")
         counts = torch.empty(2, dtype=torch.int64, device="cuda")
         table = self.table[first:first + n]
+        if self.layer:
+            h, self.out = self.layer.random(tok, self.layer.width), self.layer.outputs(tok, n)
+            last = torch.as_tensor(np.cumsum(p) - 1, device="cuda")
+            ids = torch.randint(0, VOCAB, (n,), device="cuda", generator=self.gen).int()
         begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
         self.other.zero_()
         begin.record()
         lv.lv_kv_plan(self.ctx, d_p, d_c, BLOCK, self.free[self.used:], table, offsets, slots, counts)
+        if self.layer:
+            self.layer.before(h, qkv, d_c, offsets)
         lv.lv_kv_store(self.ctx, self.cache, k, v, slots)
         if not c.any():
             lv.lv_prompt_attend(self.ctx, q, k, v, offsets, o)
         else:
             lv.lv_kv_attend(self.ctx, self.cache, q, d_c, table, o, token_offsets=None if tok == n else offsets)
+        if self.layer:
+            self.layer.after(h, o, last, ids, self.out)
         end.record()
         end.synchronize()
         tokens, blocks = counts.tolist()
@@ -78,16 +145,19 @@ class Engine:
         return c, o, begin.elapsed_time(end)
 
 
-def profile(layout="8b-tp1", steps=240, seed=1, max_seqs=192, most=3000):
+def profile(layout="8b-tp1", steps=240, seed=1, max_seqs=192, most=3000, whole=False):
     """Runs the loop; returns the profiled batches (p, c, phase, tenant, offsets), their latencies in seconds, and the engine."""
     rng = np.random.default_rng(seed)
     # a step of each kind with as many sequences as there will be: the context has its scratch and its kernels then
-    warm = Engine(layout, 3 * max_seqs + 200, max_seqs, 1000, seed)
+    warm = Engine(layout, 3 * max_seqs + 200, max_seqs, 1000, seed, whole=whole)
     for longest in (700, 1, 200):
         p = np.ones(max_seqs, np.int64)
         p[0] = longest
         warm.step(0, p)
-    e = Engine(layout, max_seqs * (most + steps * 8) // BLOCK, max_seqs, most + steps * 210, seed, warm.ctx)
+    if whole:
+        warm.step(0, np.ones(2, np.int64))  # torch picks rows by another kernel where they are few
+    e = Engine(layout, max_seqs * (most + steps * 8) // BLOCK, max_seqs, most + steps * 210, seed, warm.ctx,
+               whole)
     del warm
     rows, sizes, y = [], [], []
     for s in range(steps):
@@ -131,10 +201,11 @@ def fit(batches, y, engine):
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--layout", choices=sorted(LAYOUTS), default="8b-tp1")
+    ap.add_argument("--whole", action="store_true", help="the whole layer, not its attention alone")
     ap.add_argument("--steps", type=int, default=240)
     ap.add_argument("--seed", type=int, default=1)
     a = ap.parse_args()
-    batches, y, engine = profile(a.layout, a.steps, a.seed)
+    batches, y, engine = profile(a.layout, a.steps, a.seed, whole=a.whole)
     model, report, accuracy, T, _, L = fit(batches, y, engine)
     print(f"{a.steps} steps, {int(batches['p'].sum())} tokens, {1e3 * y.sum():.2f} ms in all")
     for g, (n, st, r2) in enumerate(zip(report["n"], report["status"], report["r2"])):
