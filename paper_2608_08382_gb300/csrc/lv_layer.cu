@@ -206,12 +206,14 @@ lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t 
     static_assert(smem <= kMostSmem, "an SM's shared memory");
     st = limit_smem(kv, k_product_pair<GATED, F16>, kind + 4);
     if (st != LV_OK) return st;
+    a.stages = (int)std::min<size_t>(kPaRoom / pair_stage(a.tokens), kPaStages);
     const int64_t grid = 2 * std::min<int64_t>(a.tiles, hold->most[2].load(std::memory_order_relaxed));
     return launch_after(k_product_pair<GATED, F16>, grid, kPaThreads, smem, 0, stream, a, mw, mu, mx);
   }
   st = limit_smem(kv, k_product<GATED, F16>, kind);
   if (st != LV_OK) return st;
-  a.stages = (int)std::min<size_t>(kSpRoom / split_stage(a.tokens), kSpStages);
+  const bool alone = a.tiles <= hold->most[a.split].load(std::memory_order_relaxed);
+  a.stages = (int)std::min<size_t>((alone ? kSpRoomAlone : kSpRoom) / split_stage(a.tokens), kSpStages);
   a.room = (int)((std::max(a.stages * split_stage(a.tokens), split_sums(a.tokens, a.split)) + 15) / 16 * 16);
   return launch_after(k_product<GATED, F16>, a.tiles * a.split, kSpThreads, 1024 + a.room + sizeof(SplitSmem), a.split, stream,
                       a, mw, mu, mx);

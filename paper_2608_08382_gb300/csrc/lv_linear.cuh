@@ -444,7 +444,8 @@ constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPi
 constexpr size_t split_sums(int tokens, int split) {
   return split == 1 ? 8 * sizeof(OutRoom) : (tokens + (split - 1) * (size_t)((tokens + split - 1) / split)) * kColFloats * sizeof(float);
 }
-constexpr size_t kSpRoom = 111 << 10;  // of both: two CTAs an SM
+constexpr size_t kSpRoom = 111 << 10;      // of both: two CTAs an SM
+constexpr size_t kSpRoomAlone = 222 << 10;  // where there is one for each SM at most
 
 // The parts of a tile's sums to the CTAs that finish them, and out from there.  The
 // columns that CTA r finishes begin at r tokens / split.  A CTA puts its accumulator into
@@ -627,11 +628,12 @@ __global__ void __launch_bounds__(kSpThreads)
 //   warp 8     loads; warp 9 of the first CTA issues the products of both.
 constexpr int kPaThreads = 320;
 constexpr int kPaTokens = 256;   // columns at most
-constexpr int kPaStages = 6;
-constexpr int kPaStage = kWBytes + kPaTokens / 2 * kPiece * 2;
+constexpr int kPaStages = 11;    // at most: what fits of a tile's width (a load takes about 1.1 us to come)
+constexpr size_t pair_stage(int tokens) { return kWBytes + (size_t)(tokens / 2) * kPiece * 2; }
+constexpr size_t kPaRoom = 6 * pair_stage(kPaTokens);
 
 struct PairSmem {
-  unsigned char stage[kPaStages][kPaStage];
+  unsigned char stage[kPaRoom];
   OutRoom out[8];
   uint64_t full[kPaStages], empty[kPaStages], sums_full[2], sums_empty[2];
   uint32_t tmem;
@@ -702,7 +704,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
     if (GATED) map_ahead(&map_u);
     map_ahead(&map_x);
     sm.stop[0] = sm.stop[1] = sm.stop[2] = 0;
-    for (int k = 0; k < kPaStages; ++k) {
+    for (int k = 0; k < a.stages; ++k) {
       bar_init(&sm.full[k], 1);
       bar_init(&sm.empty[k], 1);
     }
@@ -723,11 +725,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
   volatile int *stop = sm.stop;
   const int64_t pairs = gridDim.x / 2, first = blockIdx.x / 2;
   const int half = a.tokens / 2;
+  const uint32_t stage_bytes = kWBytes + half * kPiece * 2;
   constexpr int kOut = tile_outputs<GATED>();
   constexpr uint32_t kCols = 256;  // of an accumulator
 
   if (warp == 8) {
-    const uint32_t bytes = 2 * (kWBytes + half * kPiece * 2);
+    const uint32_t bytes = 2 * stage_bytes;
     int st = 0;
     uint32_t round = 0;  // of the ring
     for (int64_t tile = first; tile < a.tiles; tile += pairs) {
@@ -737,19 +740,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
       for (int i = 0; i < a.chunks; ++i) {
         if (round > 0) bar_wait(&sm.empty[st], (round - 1) & 1, stop);
         if (elect_one()) {
-          unsigned char *const at = sm.stage[st];
+          unsigned char *const at = sm.stage + st * stage_bytes;
           const uint32_t bar = peer_addr(&sm.full[st], 0);
           if (rank == 0) bar_expect(&sm.full[st], bytes);
           tma_load2_pair(at, &map_w, i * kPiece, o, bar);
           if (GATED) tma_load2_pair(at + kWBytes / 2, &map_u, i * kPiece, o, bar);
           tma_load2_pair(at + kWBytes, &map_x, i * kPiece, t, bar);
         }
-        if (++st == kPaStages) st = 0, ++round;
+        if (++st == a.stages) st = 0, ++round;
       }
       if (__any_sync(~0u, *stop)) break;
     }
     // the products have read, and their arrivals reached, every stage before the CTA ends
-    for (int k = 0; k < kPaStages; ++k)
+    for (int k = 0; k < a.stages; ++k)
       if (round > 0 || k < st) bar_wait(&sm.empty[k], (k < st ? round : round - 1) & 1, stop);
   } else if (warp == 9 && rank == 0) {
     const uint32_t idesc = tc_idesc(256, a.tokens, F16, false, false), base = tc_desc(smem_addr(sm.stage), 16);
@@ -764,13 +767,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
         bar_wait(&sm.full[st], phase, stop);
         tc_after_sync();
         if (elect_one()) {
-          const uint32_t w = base + (uint32_t)(st * kPaStage >> 4), x = w + (kWBytes >> 4);
+          const uint32_t w = base + (st * stage_bytes >> 4), x = w + (kWBytes >> 4);
 #pragma unroll
           for (int k = 0; k < kPiece / 16; ++k) tc_mma_pair(d, w + k * 2, x + k * 2, idesc, i > 0 || k > 0);
           tc_commit_pair(&sm.empty[st]);
           if (i + 1 == a.chunks) tc_commit_pair(&sm.sums_full[n & 1]);
         }
-        if (++st == kPaStages) st = 0, phase ^= 1;
+        if (++st == a.stages) st = 0, phase ^= 1;
       }
       if (__any_sync(~0u, *stop)) break;
     }
