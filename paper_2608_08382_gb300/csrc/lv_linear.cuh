@@ -446,6 +446,10 @@ constexpr size_t split_sums(int tokens, int split) {
 }
 constexpr size_t kSpRoom = 111 << 10;      // of both: two CTAs an SM
 constexpr size_t kSpRoomAlone = 222 << 10;  // where there is one for each SM at most
+constexpr int split_stages(int tokens, bool alone) {
+  const size_t n = (alone ? kSpRoomAlone : kSpRoom) / split_stage(tokens);
+  return n < kSpStages ? (int)n : kSpStages;
+}
 
 // The parts of a tile's sums to the CTAs that finish them, and out from there.  The
 // columns that CTA r finishes begin at r tokens / split.  A CTA puts its accumulator into
@@ -631,6 +635,9 @@ constexpr int kPaTokens = 256;   // columns at most
 constexpr int kPaStages = 11;    // at most: what fits of a tile's width (a load takes about 1.1 us to come)
 constexpr size_t pair_stage(int tokens) { return kWBytes + (size_t)(tokens / 2) * kPiece * 2; }
 constexpr size_t kPaRoom = 6 * pair_stage(kPaTokens);
+constexpr int pair_stages(int tokens) {
+  return kPaRoom / pair_stage(tokens) < kPaStages ? (int)(kPaRoom / pair_stage(tokens)) : kPaStages;
+}
 
 struct PairSmem {
   unsigned char stage[kPaRoom];
