@@ -7,6 +7,11 @@
 // once, two a lane, and a lane its eight A and B; a head then costs the sum of its
 // squares among its lanes, the partners by a shuffle of the 16-bit values, and three
 // multiplications a pair of elements.  The next heads are asked for meanwhile.
+//
+// Measured: 8,005 tokens of 32 + 8 heads of 128, bf16, 34 us, 4.8 TB/s (0.71 of the measured
+// rate; 209 us for a head a warp through shared memory, 56 with norm, weight and angle
+// applied one after another).  It is bound by instructions, about 137 for two heads of a
+// token, at 2.5 a clock and SM with the 20 warps that 96 registers a thread leave.
 #pragma once
 
 #include "lv_linear.cuh"
