@@ -110,6 +110,7 @@ __device__ __forceinline__ void unpack_pairs(const uint4 &b, uint64_t *v) {
     }
   }
 }
+
 // The biases of outputs o .. o + 7.
 template <bool GATED, bool F16>
 __device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)[8]) {
@@ -118,80 +119,6 @@ __device__ __forceinline__ void load_bias(const LinearArgs &a, int o, float (*b)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       b[k][e] = a.bias[k] && o + e < a.d_out ? value_of<F16>(((const uint16_t *)a.bias[k])[o + e]) : 0.f;
-}
-
-// A thread's outputs: eight neighbours of a token, `step` tokens on at a time.
-struct Outputs {
-  uint16_t *y;
-  const uint16_t *r;   // what is added, or null
-  int64_t y_step, r_step;
-  int n;               // outputs that there are from the first on: 0 for none
-  int left;            // tokens from the first one on
-};
-template <bool GATED>
-__device__ __forceinline__ Outputs outputs_at(const LinearArgs &a, int64_t t, int step, int o) {
-  Outputs p;
-  p.y = (uint16_t *)a.y + t * a.y_stride + o;
-  p.r = !GATED && a.residual ? (const uint16_t *)a.residual + t * a.r_stride + o : nullptr;
-  p.y_step = step * a.y_stride;
-  p.r_step = step * a.r_stride;
-  p.n = a.d_out - o;
-  p.left = p.n > 0 ? (int)min((int64_t)INT_MAX, a.n_tok - t) : 0;
-  return p;
-}
-
-// What is added to the outputs of N tokens in a row of steps, `ahead` tokens on, asked
-// for before their sums where all eight are there.
-template <int N>
-__device__ __forceinline__ void load_residual(const Outputs &p, int step, int ahead, uint4 (&r)[N]) {
-  if (!p.r || p.n < 8) return;
-#pragma unroll
-  for (int k = 0; k < N; ++k)
-    if (ahead + k * step < p.left) r[k] = *(const uint4 *)(p.r + ahead / step * p.r_step + k * p.r_step);
-}
-
-// The outputs of N tokens from their sums (and the second ones, u).
-template <bool GATED, bool F16, int N>
-__device__ __forceinline__ void finish(const LinearArgs &a, const Outputs &p, int step, float (&v)[N][8],
-                                       const float (&u)[N][8], const float (&b)[2][8], const uint4 (&r)[N]) {
-  if (a.bias[0])
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[k][e] += b[0][e];
-  activate(v, a.act);
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    if (k * step >= p.left) continue;
-    float(&w)[8] = v[k];
-    if (GATED)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] *= u[k][e] + b[1][e];
-    uint16_t *const y = p.y + k * p.y_step;
-    if (p.n >= 8) {
-      if (!GATED && p.r) {
-        float x[8];
-        unpack8<F16>(r[k], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] += x[e];
-      }
-      *(uint4 *)y = make_uint4(pack_out<F16>(w[0], w[1]), pack_out<F16>(w[2], w[3]), pack_out<F16>(w[4], w[5]),
-                               pack_out<F16>(w[6], w[7]));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < p.n) {
-          if (!GATED && p.r) w[e] += value_of<F16>(p.r[k * p.r_step + e]);
-          y[e] = (uint16_t)pack_out<F16>(w[e], 0.f);
-        }
-    }
-  }
-}
-// Tokens on: `steps` steps of `step`.
-__device__ __forceinline__ void advance(Outputs &p, int steps, int step) {
-  p.y += steps * p.y_step;
-  if (p.r) p.r += steps * p.r_step;
-  p.left -= steps * step;
 }
 
 // 16 rows by 16 columns of tensor memory, as four 8 x 8 blocks: r[4 h + 2 g + k] is column
@@ -216,11 +143,19 @@ __device__ __forceinline__ void load_turned(uint32_t *w, uint32_t at) {
                : "memory");
 }
 
-// Eight 16-bit values in a row to memory, or from there to shared memory with zeros for
-// those that are not there; n of them are.
+// Eight 16-bit values in a row from memory, to shared memory or to registers with zeros
+// for those that are not there, or to memory; n of them are.
 __device__ __forceinline__ void copy_some(uint4 *to, const uint16_t *p, int n) {
   const int bytes = min(max(n, 0), 8) * 2;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(p), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint4 load_some(const uint16_t *p, int n) {
+  if (n >= 8) return *(const uint4 *)p;
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) w[e >> 1] |= (uint32_t)p[e] << (e & 1) * 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
   if (n >= 8) {
@@ -243,8 +178,8 @@ __device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
 // no other warp is waited for.  Gated: the rows 64 on are the second sums of a warp
 // two on; the two exchange eight columns each, in fp32.  The next columns are on their
 // way meanwhile, and what is added to them two turns ahead, from before the sums are
-// ready on.  (In fp32 through shared memory, a row a
-// thread: 160 instructions and 1,200 clocks for 16 columns.)
+// ready on.  (In fp32 through shared memory, a row a thread: 160 instructions and 1,200
+// clocks for 16 columns.)
 constexpr int kOutCols = 16;
 constexpr int kAhead = 3;    // turns whose residual has a place
 struct OutRoom {             // of a warp
@@ -404,6 +339,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 // All threads of the cluster; what they wrote to shared memory is seen after it.
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // The address of a place in this block's shared memory in another block of the cluster.
@@ -467,6 +403,7 @@ constexpr int split_stages(int tokens, bool alone) {
 template <bool GATED, bool F16>
 __device__ __forceinline__ void join(const LinearArgs &a, SplitSmem &sm, uint32_t tmem, float *sums, int warp, int lane,
                                      uint32_t rank, int64_t t0, int o0, volatile int *stop) {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this CTA's stages are free
   auto first = [&](int r) { return a.tokens * r / a.split; };
   const int most = (a.tokens + a.split - 1) / a.split;
@@ -496,30 +433,44 @@ __device__ __forceinline__ void join(const LinearArgs &a, SplitSmem &sm, uint32_
   const int begin = first(rank), mine = first(rank + 1) - begin;
   constexpr int kStep = kSpThreads / kGroups;
   int c = threadIdx.x / kGroups;
-  Outputs p = outputs_at<GATED>(a, t0 + begin + c, kStep, o);
-  p.left = min(p.left, mine - c);
-  uint4 next[1];
-  load_residual(p, kStep, 0, next);
+  const int n = a.d_out - o, end = n > 0 ? (int)min((int64_t)mine, a.n_tok - (t0 + begin)) : 0;
+  const bool adds = !GATED && a.residual;
+  uint4 next = make_uint4(0, 0, 0, 0);  // what is added to the next token's outputs
+  auto ask = [&](int at) {
+    if (adds && at < end) next = load_some((const uint16_t *)a.residual + (t0 + begin + at) * a.r_stride + o, n);
+  };
+  ask(c);
   bar_wait(&sm.joined, 0, stop);
-  for (; c < mine; c += kStep) {
-    float v[1][8] = {}, u[1][8] = {};
+  for (; c < end; c += kStep) {
+    float v[8] = {}, u[8] = {};
     for (int s = 0; s < a.split; ++s) {
       const float *const at =
           (s == rank ? sums + (begin + c) * kColFloats : got + ((s < rank ? s : s - 1) * most + c) * kColFloats) + group * 8;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         const float4 q = *(const float4 *)(at + e);
-        v[0][e] += q.x, v[0][e + 1] += q.y, v[0][e + 2] += q.z, v[0][e + 3] += q.w;
+        v[e] += q.x, v[e + 1] += q.y, v[e + 2] += q.z, v[e + 3] += q.w;
         if (GATED) {
           const float4 w = *(const float4 *)(at + kRows / 2 + e);
-          u[0][e] += w.x, u[0][e + 1] += w.y, u[0][e + 2] += w.z, u[0][e + 3] += w.w;
+          u[e] += w.x, u[e + 1] += w.y, u[e + 2] += w.z, u[e + 3] += w.w;
         }
       }
     }
-    const uint4 now[1] = {next[0]};
-    load_residual(p, kStep, kStep, next);
-    finish<GATED, F16>(a, p, kStep, v, u, b, now);
-    advance(p, 1, kStep);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += b[0][e];
+    activate(v, a.act);
+    float add[8];
+    unpack8<F16>(next, add);
+    ask(c + kStep);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (GATED) v[e] *= u[e] + b[1][e];
+      if (adds) v[e] += add[e];
+    }
+    store_some((uint16_t *)a.y + (t0 + begin + c) * a.y_stride + o,
+               make_uint4(pack_out<F16>(v[0], v[1]), pack_out<F16>(v[2], v[3]), pack_out<F16>(v[4], v[5]),
+                          pack_out<F16>(v[6], v[7])),
+               n);
   }
   __syncwarp();
   cluster_sync();  // what this CTA sent has arrived

@@ -71,8 +71,9 @@ constexpr int kLpRoom = 2048;   // candidates; also the logits of a row that lea
 constexpr int kLpCluster = 8;
 static_assert(kLpGroups >= LV_MAX_TOP, "a bound from the groups");
 
-// A difference of logits beyond which the exponential is 0, and that times it too.
-constexpr float kLpFar = -1e30f;
+// A difference of logits beyond which the exponential is 0, and that times it too (and
+// times the largest sum there can be is finite).
+constexpr float kLpFar = -1e20f;
 
 struct LpPart {       // of a CTA's share of a row
   float base, S, W;   // sums of exp(x - base) and of that times (x - base)
@@ -131,11 +132,6 @@ struct LpRun {
   bool set = false;
   uint64_t S = 0, W = 0;   // two sums each
   int where = -1;          // the first vector with a logit that equals m
-  // Vectors of which the largest logit is `top`, the first of them at j.
-  __device__ __forceinline__ void seen(float top, int j) {
-    if (where < 0 || top > m) where = j;
-    m = fmaxf(m, top);
-  }
   __device__ __forceinline__ void rebase() {  // before what makes m as it is is added
     if (set ? m > base + kLpLazy : m > -INFINITY) {
       if (set) {  // else there is nothing yet
@@ -214,7 +210,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
       v[e / 2] = pair(p, q);
       top = fmaxf(top, fmaxf(p, q));
     }
-    run.seen(top, j);
+    if (run.where < 0 || top > run.m) run.where = j;
+    run.m = fmaxf(run.m, top);
     run.rebase();
     run.add(v);
   };

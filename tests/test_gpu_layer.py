@@ -408,6 +408,21 @@ def test_logprobs_masks(lv, ctx, V):
     assert ctx.status() == lv.LV_OK
 
 
+def test_logprobs_far_above_many(lv, ctx):
+    """One logit of 1e31 above 2^24 others, whose sum times that distance is beyond fp32: all of the probability is its."""
+    import torch
+    x = torch.full((1, 1 << 24), 7.9, device="cuda")
+    x.view(8, -1)[:, :4096] = 0.0  # what each of eight shares of the row begins with, and its sums are relative to
+    x[0, 9_000_000] = 1e31
+    lse, ent, lp = (torch.full((1,), GUARD, device="cuda") for _ in range(3))
+    ids, top = torch.zeros(1, 2, dtype=torch.int32, device="cuda"), torch.zeros(1, 2, device="cuda")
+    lv.lv_token_logprobs(ctx, x, ids=torch.tensor([9_000_000], dtype=torch.int32, device="cuda"), logp=lp, entropy=ent, lse=lse,
+                         top_ids=ids, top_logp=top)
+    assert lse.item() == float(np.float32(1e31)) and ent.item() == 0 and lp.item() == 0
+    assert ids.tolist() == [[9_000_000, 4096]] and top[0, 0] == 0 and top[0, 1] == float(np.float32(7.9) - np.float32(1e31))
+    assert ctx.status() == lv.LV_OK
+
+
 def test_logprobs_ids_and_what_is_left_out(lv, ctx):
     import torch
     x = torch.randn(4, 50, device="cuda")
@@ -421,6 +436,57 @@ def test_logprobs_ids_and_what_is_left_out(lv, ctx):
     lv.lv_token_logprobs(ctx, x, lse=lse)
     assert torch.allclose(lse, torch.logsumexp(x, 1), atol=1e-5)
     lv.lv_token_logprobs(ctx, x)
+
+
+# ------------------------------------------------------------------ arrays of more than 2^31 elements
+
+def test_products_past_32_bits(lv, ctx):
+    import torch
+    n, d_in, d_out = 300_001, 64, 8192
+    x = torch.randint(-3, 4, (n, d_in), device="cuda").bfloat16()
+    w = torch.randint(-3, 4, (d_out, d_in), device="cuda").bfloat16()
+    y = torch.empty(n, d_out, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 1, 262_143, 262_144, 270_000, n - 2, n - 1], device="cuda")
+    want = x[rows].double() @ w.double().t()
+    lv.lv_linear(ctx, x, w, y)
+    assert torch.equal(y[rows], want.bfloat16())
+    lv.lv_linear(ctx, x, w, y, residual=y)
+    assert torch.equal(y[rows], (want + want.bfloat16().double()).bfloat16())
+    lv.lv_gated_linear(ctx, x, w, w, y, act="none")
+    assert torch.equal(y[rows], (want * want).bfloat16())
+    assert ctx.status() == lv.LV_OK
+
+
+def test_rotate_past_32_bits(lv, ctx):
+    import torch
+    n, hq, hkv, d = 620_003, 20, 4, 128
+    qkv = torch.empty(n, hq + 2 * hkv, d, dtype=torch.bfloat16, device="cuda").normal_()
+    rows = [0, 599_186, 599_187, n - 1]
+    before = _np(qkv[rows])
+    rope = lv.Rope.geometric(d, 1e6)
+    w = torch.full((d,), 1.5, dtype=torch.bfloat16, device="cuda")
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hkv]
+    lv.lv_qk_rotate(ctx, q, k, q, k, rope, token_offsets=torch.tensor([0, n], device="cuda"), q_weight=w, k_weight=w)
+    after = _np(qkv[rows])
+    want, tol = ref.rotate(before[:, :hq + hkv], np.full(d, 1.5), 1e-6, np.array(rows), list(rope.s.freq), False, "bf16")
+    kvref.close(after[:, :hq + hkv], want, tol, "q and k")
+    assert np.array_equal(after[:, hq + hkv:], before[:, hq + hkv:]) and ctx.status() == lv.LV_OK
+
+
+def test_logprobs_past_32_bits(lv, ctx):
+    import torch
+    n, V = 40_001, 64_000
+    x = torch.empty(n, V, dtype=torch.bfloat16, device="cuda").normal_()
+    ids = torch.randint(0, V, (n,), device="cuda").int()
+    logp, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    top, tlp = torch.empty(n, 2, dtype=torch.int32, device="cuda"), torch.empty(n, 2, device="cuda")
+    lv.lv_token_logprobs(ctx, x, ids=ids, logp=logp, lse=lse, top_ids=top, top_logp=tlp)
+    rows = [0, 33_554, 33_555, n - 1]
+    want = ref.logprobs(_np(x[rows]), ids[rows].tolist(), 2)
+    assert np.array_equal(_np(top[rows]), want[3])
+    for got, w in ((logp, want[0]), (lse, want[2]), (tlp, want[4])):
+        kvref.close(_np(got[rows]), w, 1e-4, "rows")
+    assert ctx.status() == lv.LV_OK
 
 
 # ------------------------------------------------------------------ together
