@@ -239,11 +239,13 @@ lv_status linear(lv_ctx *ctx, int32_t dtype, LinearArgs &a, const Operands &m, b
 
 template <int D, bool F16>
 lv_status run_rotate(const KvHost *kv, RotateArgs &a, bool neighbours, cudaStream_t stream) {
-  // a token's heads to as many warps as there have to be to fill the SMs, two or four heads
-  // each at least
+  // A token's heads to as many warps as there have to be for one on each of an SM's four
+  // schedulers, two or four heads each at least: what a warp does once for its heads (the
+  // angles) is half of what eight heads cost it.  (us of 128, 512 and 2,048 tokens, for
+  // four warps an SM 4.9, 6.8 and 10.7, for twenty 5.9, 6.1 and 12.2)
   constexpr int kAtOnce = 32 / (D / 8);
   const int heads = a.heads[0] + a.heads[1];
-  const int64_t parts = std::min<int64_t>((kv->sms * kRoCtas * kRoWarps + a.n_tok - 1) / a.n_tok, (heads + kAtOnce - 1) / kAtOnce);
+  const int64_t parts = std::min<int64_t>((kv->sms * 4 + a.n_tok - 1) / a.n_tok, (heads + kAtOnce - 1) / kAtOnce);
   a.part = (int)(((heads + parts - 1) / parts + kAtOnce - 1) / kAtOnce * kAtOnce);
   a.parts = (heads + a.part - 1) / a.part;
   const int64_t grid = std::min<int64_t>((a.n_tok * a.parts + kRoWarps - 1) / kRoWarps, kv->sms * kRoCtas);

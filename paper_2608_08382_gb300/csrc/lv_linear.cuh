@@ -327,11 +327,6 @@ __device__ __forceinline__ void tma_load2(void *to, const CUtensorMap *map, int 
       : "memory");
 }
 
-// The box to L2.
-__device__ __forceinline__ void tma_ahead2(const CUtensorMap *map, int x, int y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
-}
-
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -515,14 +510,6 @@ __global__ void __launch_bounds__(kSpThreads)
   const int n = to - from;
   if (threadIdx.x == 0 && a.split > 1)
     bar_expect(&sm.joined, (uint32_t)((a.split - 1) * (a.tokens * (rank + 1) / a.split - a.tokens * rank / a.split) * kColFloats * 4));
-  // While the kernel before this one ends, the first weights come as far as L2, where
-  // whatever that kernel may still write to them is seen.
-  if (warp == 1 && elect_one()) {
-    for (int i = 0; i < min(n, a.stages); ++i) {
-      tma_ahead2(&map_w, (from + i) * kPiece, o0);
-      if (GATED) tma_ahead2(&map_u, (from + i) * kPiece, o0);
-    }
-  }
   wait_previous();
 
   // Both loops are the whole warp's, with one lane that issues: what they count is then
