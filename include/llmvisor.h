@@ -544,7 +544,8 @@ lv_status lv_qk_rotate(lv_ctx *ctx, int32_t dtype, int32_t n_q_heads, int32_t n_
  * -inf, its entropy 0.  A row with a NaN gives NaN throughout, with one or more +inf
  * an lse of +inf, an entropy of NaN, and a log probability of NaN where the logit is
  * +inf and -inf elsewhere; among the largest a NaN stands above +inf, and the two
- * zeros are equal. */
+ * zeros are equal.  A row is read once and its likeliest places twice; one with a NaN
+ * or +inf once more for each of the n_top. */
 #define LV_MAX_TOP 32
 lv_status lv_token_logprobs(lv_ctx *ctx, int32_t dtype, const void *logits, int64_t stride, int64_t n_tok,
                             int32_t vocab, const int32_t *ids, float *logp, float *entropy, float *lse,

@@ -16,8 +16,9 @@
 // largest reaches the bound hold candidates; their logits are read once more, by all
 // threads (a few threads' logits, still in L2; by the warps that had them, one hit after
 // another: 9 us for 20 of 128,000), and the candidates are put in order by counting for each
-// those above it.  Where there are more candidates than room (a row in descending
-// order), or the row has a NaN or +inf, the largest are looked for one after another.
+// those above it.  Where there are more candidates than room (a row's largest all in one
+// group's places: sorted rows have n_top times 64 at most), or the row has a NaN or
+// +inf, the largest are looked for one after another.
 // Every comparison is of a value and its index, so that nothing depends on an order of
 // arrival.
 //

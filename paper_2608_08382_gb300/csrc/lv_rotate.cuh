@@ -36,9 +36,10 @@ struct RotateArgs {
 };
 
 // Request of token t: the last one whose offset is at most t; -1 where t is before the
-// first or past the last.  By a whole warp, 32 ways at a time.
-__device__ __forceinline__ int64_t request_of(const int64_t *offsets, int64_t n_req, int64_t t, int lane) {
-  if (t < offsets[0] || t >= offsets[n_req]) return -1;
+// first, at `begin`, or past the last one's end.  By a whole warp, 32 ways at a time.
+__device__ __forceinline__ int64_t request_of(const int64_t *offsets, int64_t n_req, int64_t begin, int64_t end, int64_t t,
+                                              int lane) {
+  if (t < begin || t >= end) return -1;
   int64_t lo = 0, hi = n_req;  // offsets[lo] <= t < offsets[hi]
   while (hi - lo > 1) {
     const int64_t step = (hi - lo + 32) / 33, at = lo + (lane + 1) * step;
@@ -88,8 +89,8 @@ __device__ __forceinline__ uint4 partners(const uint4 &mine, int from, bool turn
 template <int D, bool F16, bool NORM, bool NEXT>
 __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_constant__ RotateArgs a) {
   constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;  // lanes of a head, heads of a warp at a time
-  __shared__ float2 turned[kRoWarps][64];               // a token's cosines and sines
-  __shared__ float weight[2][D];
+  __shared__ __align__(16) float2 turned[kRoWarps][64];  // a token's cosines and sines
+  __shared__ __align__(16) float weight[2][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int l = lane % kLanes, sub = lane / kLanes, heads = a.heads[0] + a.heads[1];
   let_next();
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
     ask(at0 < end0 ? 0 : 1, at0 < end0 ? at0 : at1);
   };
   if (u < units) begin();
+  const int64_t begin_tok = a.offsets ? a.offsets[0] : 0, end_tok = a.offsets ? a.offsets[a.n_req] : 0;
   for (int k = threadIdx.x; k < 2 * D; k += kRoWarps * 32) {
     const void *const w = k < D ? a.weight[0] : a.weight[1];
     weight[k / D][k % D] = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
@@ -133,7 +135,7 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
   __syncthreads();
   for (bool begun = true; u < units; u += (int64_t)gridDim.x * kRoWarps, begun = false) {
     if (!begun) begin();
-    const int64_t i = a.offsets ? request_of(a.offsets, a.n_req, t, lane) : t;
+    const int64_t i = a.offsets ? request_of(a.offsets, a.n_req, begin_tok, end_tok, t, lane) : t;
     if (i < 0) continue;
     int64_t pos = a.offsets ? t - a.offsets[i] : 0;
     if (a.c) {
@@ -149,18 +151,26 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
       const int at = w ? at1 : at0, end = w ? end1 : end0;
       if (at >= end) continue;
       uint64_t A[4], B[4];
-      const float *const own = weight[w] + l * 8, *const theirs = own + away * 8;
+      // the lane's weights and its partners', and the pairs' cosines and sines, 16 bytes a load
+      const float4 *const own = (const float4 *)(weight[w] + l * 8), *const theirs = own + away * 2;
+      const float4 *const angle = (const float4 *)(turned[warp] + (first & 63));
 #pragma unroll
-      for (int k = 0; k < 8; k += 2) {
-        float2 e = make_float2(1.f, 0.f), f = e;
+      for (int k = 0; k < 8; k += 4) {
+        const float4 x = own[k / 4];
         if (NEXT) {
-          if (turns) e = f = turned[warp][(first + k / 2) & 63];
-          A[k / 2] = pair(own[k] * e.x, own[k + 1] * e.x);
-          B[k / 2] = pair(own[k + 1] * -e.y, own[k] * e.y);
+          float4 e = make_float4(1.f, 0.f, 1.f, 0.f);
+          if (turns) e = angle[k / 4];
+          A[k / 2] = pair(x.x * e.x, x.y * e.x), A[k / 2 + 1] = pair(x.z * e.z, x.w * e.z);
+          B[k / 2] = turns ? pair(x.y * -e.y, x.x * e.y) : 0;
+          B[k / 2 + 1] = turns ? pair(x.w * -e.w, x.z * e.w) : 0;
         } else {
-          if (turns) e = turned[warp][(first + k) & 63], f = turned[warp][(first + k + 1) & 63];
-          A[k / 2] = pair(own[k] * e.x, own[k + 1] * f.x);
-          B[k / 2] = upper ? pair(theirs[k] * e.y, theirs[k + 1] * f.y) : pair(theirs[k] * -e.y, theirs[k + 1] * -f.y);
+          float4 e = make_float4(1.f, 0.f, 1.f, 0.f), f = e;
+          if (turns) e = angle[k / 2], f = angle[k / 2 + 1];
+          float4 p = make_float4(0.f, 0.f, 0.f, 0.f);  // nothing of a weight that is infinite
+          if (turns) p = theirs[k / 4];
+          if (!upper) p.x = -p.x, p.y = -p.y, p.z = -p.z, p.w = -p.w;
+          A[k / 2] = pair(x.x * e.x, x.y * e.z), A[k / 2 + 1] = pair(x.z * f.x, x.w * f.z);
+          B[k / 2] = pair(p.x * e.y, p.y * e.w), B[k / 2 + 1] = pair(p.z * f.y, p.w * f.w);
         }
       }
       const bool normed = NORM && a.weight[w];

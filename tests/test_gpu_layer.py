@@ -304,6 +304,24 @@ def test_rotate_keeps_a_nan_to_its_head(lv, ctx):
     assert torch.isnan(y[2, 0, [0, 32]]).all() and (y[2, 0, 1:32] == 0).all()  # a finite value over infinity
 
 
+@pytest.mark.parametrize("order", ["halves", "neighbours"])
+def test_rotate_leaves_the_rest_of_a_head(lv, ctx, order):
+    """Elements past the rotated ones are scaled alone: an infinite weight or value there is an infinity, not a NaN."""
+    import torch
+    d = 64
+    x = torch.ones(2, 2, d, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    w[40] = float("inf")
+    y = torch.zeros_like(x)
+    rope, c = lv.Rope.geometric(16, neighbours=order == "neighbours"), torch.tensor([3, 4], dtype=torch.int32, device="cuda")
+    lv.lv_qk_rotate(ctx, x[:, :1], x[:, 1:], y[:, :1], y[:, 1:], rope, c=c, q_weight=w, k_weight=w)
+    assert torch.isposinf(y[..., 40]).all() and torch.isfinite(y).sum() == 4 * (d - 1)
+    x[0, 0, 50] = float("-inf")
+    lv.lv_qk_rotate(ctx, x[:, :1], x[:, 1:], y[:, :1], y[:, 1:], rope, c=c)
+    assert torch.isneginf(y[0, 0, 50]) and torch.isfinite(y).sum() == 4 * d - 1
+    assert ctx.status() == lv.LV_OK
+
+
 def test_rotate_bad_data(lv, ctx):
     """A negative context counts as none; offsets that decrease or leave the call are said."""
     import torch
@@ -383,6 +401,24 @@ def test_logprobs_orders(lv, ctx, law, V):
     for dtype in ("bf16", "f32"):
         for n_top in (1, 32):
             _lp_close(lv, ctx, x, np.array([0, V - 1, V // 2]), n_top, dtype)
+    assert ctx.status() == lv.LV_OK
+
+
+@pytest.mark.parametrize("n, V, every, first", [(320, 128_000, 256, 8), (2450, 100_000, 128, 4)])
+def test_logprobs_with_the_largest_in_one_place(lv, ctx, n, V, every, first):
+    """The largest logits of a row all where a few threads read, thousands of them: more candidates than there is room for."""
+    import torch
+    x = torch.randn(n, V, device="cuda").bfloat16()
+    piece = torch.arange(V, device="cuda") // 8 % every
+    x = torch.where(piece < first, x + 20, x)
+    ids, lp = torch.empty(n, 32, dtype=torch.int32, device="cuda"), torch.empty(n, 32, device="cuda")
+    lv.lv_token_logprobs(ctx, x, top_ids=ids, top_logp=lp)
+    for a in range(0, n, 400):
+        part = x[a:a + 400].float()
+        v, i = torch.sort(part, dim=1, descending=True, stable=True)
+        assert torch.equal(ids[a:a + 400], i[:, :32].int())
+        want = v[:, :32].double() - torch.logsumexp(part.double(), 1, keepdim=True)
+        assert (lp[a:a + 400].double() - want).abs().max() < 1e-4
     assert ctx.status() == lv.LV_OK
 
 
