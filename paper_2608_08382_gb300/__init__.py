@@ -543,7 +543,7 @@ _acts = {"none": LV_ACT_NONE, "silu": LV_ACT_SILU, "gelu": LV_ACT_GELU, "gelu_ta
 
 def _flat(x, shape, dtype, where):
     """Row stride in elements of a tensor of that shape and type on a GPU whose rows are without gaps inside."""
-    if x.shape != shape or x.dtype != dtype or not x.is_cuda:
+    if x.dtype != dtype or x.shape != shape or not x.is_cuda:
         raise LVError(LV_EINVAL, where)
     rows, one = x.stride()
     if one != 1 and shape[1] != 1:
@@ -576,30 +576,34 @@ def lv_linear(ctx: Context, x, w, y, bias=None, act="none", residual=None, strea
     same tensor), bias [d_out]; rows may be slices of wider ones that begin at 16-byte boundaries.  act: "none", "silu",
     "gelu", "gelu_tanh" or "relu"."""
     t, at, dt = _dtypes or _types(), "lv_linear", x.dtype
-    (n, d_in), (d_out, _) = _sizes(x, 2, at), _sizes(w, 2, at)
-    out = (n, d_out)
-    if dt not in t or act not in _acts:
+    xs, ws, kind, act = x.shape, w.shape, t.get(dt), _acts.get(act)
+    if len(xs) != 2 or len(ws) != 2 or ws[1] != xs[1] or kind is None or act is None:
         raise LVError(LV_EINVAL, at)
-    _check(_lib.lv_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, (n, d_in), dt, at), n, w.data_ptr(),
-                          _flat(w, (d_out, d_in), dt, at), d_in, d_out,
-                          None if bias is None else _vector(bias, d_out, dt, at), _acts[act],
-                          None if residual is None else residual.data_ptr(),
-                          0 if residual is None else _flat(residual, out, dt, at), y.data_ptr(), _flat(y, out, dt, at),
-                          _stream(stream)), at)
+    out = (xs[0], ws[0])
+    st = _lib.lv_linear(ctx.h, kind, x.data_ptr(), _flat(x, xs, dt, at), xs[0], w.data_ptr(), _flat(w, ws, dt, at), xs[1],
+                        ws[0], None if bias is None else _vector(bias, ws[0], dt, at), act,
+                        None if residual is None else residual.data_ptr(),
+                        0 if residual is None else _flat(residual, out, dt, at), y.data_ptr(), _flat(y, out, dt, at),
+                        _stream(stream))
+    if st:
+        raise LVError(st, at)
 
 
 def lv_gated_linear(ctx: Context, x, w_gate, w_up, y, bias_gate=None, bias_up=None, act="silu", stream=None):
     """y = act(x w_gate^T + bias_gate) * (x w_up^T + bias_up): x [n_tok][d_in], w_gate and w_up [d_out][d_in] of one
     stride, y [n_tok][d_out], biases [d_out]; as lv_linear otherwise."""
     t, at, dt = _dtypes or _types(), "lv_gated_linear", x.dtype
-    (n, d_in), (d_out, _) = _sizes(x, 2, at), _sizes(w_gate, 2, at)
-    stride = _flat(w_gate, (d_out, d_in), dt, at)
-    if dt not in t or act not in _acts or _flat(w_up, (d_out, d_in), dt, at) != stride:
+    xs, ws, kind, act = x.shape, w_gate.shape, t.get(dt), _acts.get(act)
+    if len(xs) != 2 or len(ws) != 2 or ws[1] != xs[1] or kind is None or act is None:
         raise LVError(LV_EINVAL, at)
-    _check(_lib.lv_gated_linear(ctx.h, t[dt], x.data_ptr(), _flat(x, (n, d_in), dt, at), n, w_gate.data_ptr(),
-                                w_up.data_ptr(), stride, d_in, d_out, _vector(bias_gate, d_out, dt, at),
-                                _vector(bias_up, d_out, dt, at), _acts[act], y.data_ptr(), _flat(y, (n, d_out), dt, at),
-                                _stream(stream)), at)
+    stride = _flat(w_gate, ws, dt, at)
+    if _flat(w_up, ws, dt, at) != stride:
+        raise LVError(LV_EINVAL, at)
+    st = _lib.lv_gated_linear(ctx.h, kind, x.data_ptr(), _flat(x, xs, dt, at), xs[0], w_gate.data_ptr(), w_up.data_ptr(),
+                              stride, xs[1], ws[0], _vector(bias_gate, ws[0], dt, at), _vector(bias_up, ws[0], dt, at), act,
+                              y.data_ptr(), _flat(y, (xs[0], ws[0]), dt, at), _stream(stream))
+    if st:
+        raise LVError(st, at)
 
 
 class Rope:
@@ -625,12 +629,14 @@ def lv_qk_rotate(ctx: Context, q, k, q_out, k_out, rope: Rope, c=None, token_off
     Positions as lv_kv_attend's: int32 c [n_req], int64 token_offsets [n_req + 1] or None for one token a request; c None
     with token_offsets: requests that start on an empty cache."""
     t, at, dt = _dtypes or _types(), "lv_qk_rotate", q.dtype
-    qs, ks = _sizes(q, 3, at), _sizes(k, 3, at)
+    qs, ks, kind = q.shape, k.shape, t.get(dt)
+    if len(qs) != 3 or len(ks) != 3 or kind is None or ks[0] != qs[0] or ks[2] != qs[2]:
+        raise LVError(LV_EINVAL, at)
     n, hq, d = qs
     n_req = n if token_offsets is None else token_offsets.numel() - 1
-    if dt not in t or n_req < 0 or ks[0] != n or ks[2] != d:
+    if n_req < 0:
         raise LVError(LV_EINVAL, at)
-    _check(_lib.lv_qk_rotate(ctx.h, t[dt], hq, ks[1], d, q.data_ptr(), _heads(q, qs, dt, at), k.data_ptr(),
+    _check(_lib.lv_qk_rotate(ctx.h, kind, hq, ks[1], d, q.data_ptr(), _heads(q, qs, dt, at), k.data_ptr(),
                              _heads(k, ks, dt, at), n, _vector(token_offsets, n_req + 1, t["i64"], at),
                              _vector(c, n_req, t["i32"], at), n_req, _vector(q_weight, d, dt, at),
                              _vector(k_weight, d, dt, at), eps, rope.at, q_out.data_ptr(), _heads(q_out, qs, dt, at),
