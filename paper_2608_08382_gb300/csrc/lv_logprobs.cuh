@@ -12,7 +12,8 @@
 //
 // The n_top largest: of 32 groups of its threads each has a largest logit, and the
 // n_top-th of those bounds the row's n_top-th from below (of equal ones by index; that of
-// its vector will do).  Only threads whose own
+// its vector will do); the threads' own do so more closely, at the cost of 256
+// comparisons each.  Only threads whose own
 // largest reaches the bound hold candidates; their logits are read once more, by all
 // threads (a few threads' logits, still in L2; by the warps that had them, one hit after
 // another: 9 us for 20 of 128,000), and the candidates are put in order by counting for each
@@ -69,6 +70,7 @@ __device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > 
 
 constexpr int kLpGroups = 32;
 constexpr int kLpRoom = 2048;   // candidates; also the logits of a row that leaves a group empty
+constexpr int kLpFew = 256;     // candidates that are put in order as they are
 constexpr int kLpCluster = 8;
 static_assert(kLpGroups >= LV_MAX_TOP, "a bound from the groups");
 
@@ -84,7 +86,7 @@ template <int WARPS>
 struct LpSmem {
   uint64_t room[kLpRoom];
   uint64_t of_cluster[kLpCluster * LV_MAX_TOP];  // the first CTA's: everyone's largest
-  uint64_t group[kLpGroups];
+  uint64_t group[kLpGroups], key[WARPS * 32];  // bounds from below of a group's and a thread's largest
   uint64_t warp_key[WARPS];
   float warp_base[WARPS], warp_S[WARPS], warp_W[WARPS];
   uint32_t warp_top[WARPS];
@@ -272,6 +274,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
       least = full_key(key, min(index(run.where, kE - 1), a.vocab - 1));
       reach = full_key(key, max(index(run.where, 0), 0));
     }
+    sm.key[tid] = least;
 #pragma unroll
     for (int s = kLanes / 2; s; s >>= 1) least = larger(least, __shfl_xor_sync(~0u, least, s));
     if (lane % kLanes == 0) sm.group[tid / kLanes] = least;
@@ -319,50 +322,65 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprobs(const Logp
   for (int k = 1; k < kWarps; ++k) part.S += sm.warp_S[k], part.W += sm.warp_W[k];
   bool slow = part.S != part.S;  // a NaN, or an infinity less itself
   if (a.n_top > 0 && !slow) {
-    // ---- candidates
-    const uint64_t bound = sm.bound;
-    const uint32_t bound_key = (uint32_t)(bound >> 32);
-    const bool hit = reach >= bound;
-    const unsigned hits = __ballot_sync(~0u, hit);
-    if (hits) {
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&sm.hits, __popc(hits));
-      at = __shfl_sync(~0u, at, 0) + __popc(hits & ((1u << lane) - 1));
-      if (hit) sm.hit[at] = (uint16_t)tid;
-    }
-    auto keep = [&](int j, int e, float v) {
-      const uint64_t key = full_key(order_key(v), index(j, e));
-      if (key < bound) return;
-      const int n = atomicAdd(&sm.n, 1);
-      if (n < kLpRoom) sm.room[n] = key;
-    };
-    if (head && tid == 0 && hit)
-      for (int e = 0; e < kE; ++e)
-        if (in_row(index(from, e))) keep(from, e, logit(from, e));
-    if (tail && tid == THREADS - 1 && hit)
-      for (int e = 0; e < kE; ++e)
-        if (in_row(index(to - 1, e))) keep(to - 1, e, logit(to - 1, e));
-    __syncthreads();
-    // all their vectors, dealt out to all threads
-    const unsigned per = (unsigned)(whole1 - whole0 + THREADS - 1) / THREADS, looks = sm.hits * per;
-#pragma unroll 2
-    for (unsigned i = tid; i < looks; i += THREADS) {
-      const unsigned h = i / per;
-      const int j = whole0 + sm.hit[h] + (int)(i - h * per) * THREADS;
-      if (j >= whole1) continue;
-      const uint4 raw = load_once(line + (int64_t)j * 16);
-      if (order_key(largest_of<TYPE>(raw)) < bound_key) continue;
-      uint64_t v[kE / 2];
-      logit_pairs<TYPE>(raw, v);
-#pragma unroll
-      for (int e = 0; e < kE; e += 2) {
-        float p, q;
-        unpair(v[e / 2], &p, &q);
-        keep(j, e, p);
-        keep(j, e + 1, q);
+    // ---- candidates: above the groups' bound, and where there is none (a short row) or
+    // they are many (equal logits, masks) above the threads', which takes longer to find
+    for (bool fine = sm.bound == 1;; fine = true) {
+      if (fine) {
+        __syncthreads();
+        if (tid == 0) sm.bound = 1, sm.n = sm.hits = 0;
+        __syncthreads();
+        const uint64_t mine = sm.key[tid];
+        int above = 0;
+#pragma unroll 8
+        for (int k = 0; k < THREADS; ++k) above += sm.key[k] > mine;
+        if (mine != 0 && above == a.n_top - 1) sm.bound = mine;
+        __syncthreads();
       }
+      const uint64_t bound = sm.bound;
+      const uint32_t bound_key = (uint32_t)(bound >> 32);
+      const bool hit = reach >= bound;
+      const unsigned hits = __ballot_sync(~0u, hit);
+      if (hits) {
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sm.hits, __popc(hits));
+        at = __shfl_sync(~0u, at, 0) + __popc(hits & ((1u << lane) - 1));
+        if (hit) sm.hit[at] = (uint16_t)tid;
+      }
+      auto keep = [&](int j, int e, float v) {
+        const uint64_t key = full_key(order_key(v), index(j, e));
+        if (key < bound) return;
+        const int n = atomicAdd(&sm.n, 1);
+        if (n < kLpRoom) sm.room[n] = key;
+      };
+      if (head && tid == 0 && hit)
+        for (int e = 0; e < kE; ++e)
+          if (in_row(index(from, e))) keep(from, e, logit(from, e));
+      if (tail && tid == THREADS - 1 && hit)
+        for (int e = 0; e < kE; ++e)
+          if (in_row(index(to - 1, e))) keep(to - 1, e, logit(to - 1, e));
+      __syncthreads();
+      // all the hits' vectors, dealt out to all threads
+      const unsigned per = (unsigned)(whole1 - whole0 + THREADS - 1) / THREADS, looks = sm.hits * per;
+#pragma unroll 2
+      for (unsigned i = tid; i < looks; i += THREADS) {
+        const unsigned h = i / per;
+        const int j = whole0 + sm.hit[h] + (int)(i - h * per) * THREADS;
+        if (j >= whole1) continue;
+        const uint4 raw = load_once(line + (int64_t)j * 16);
+        if (order_key(largest_of<TYPE>(raw)) < bound_key) continue;
+        uint64_t v[kE / 2];
+        logit_pairs<TYPE>(raw, v);
+#pragma unroll
+        for (int e = 0; e < kE; e += 2) {
+          float p, q;
+          unpair(v[e / 2], &p, &q);
+          keep(j, e, p);
+          keep(j, e + 1, q);
+        }
+      }
+      __syncthreads();
+      if (fine || sm.n <= kLpFew) break;
     }
-    __syncthreads();
     slow = sm.n > kLpRoom;
   }
   const int k_top = a.n_top;
