@@ -180,15 +180,21 @@ __device__ __forceinline__ void store_some(uint16_t *p, const uint4 &v, int n) {
 // way meanwhile, and what is added to them two turns ahead, from before the sums are
 // ready on.  (In fp32 through shared memory, a row a thread: 160 instructions and 1,200
 // clocks for 16 columns.)
+//
+// An exchange is written, the two warps meet, and it is read.  Its place is free again
+// when they have met once more, since each has then read what it got: turn after turn a
+// place is not the one before's, nor is it from a tile's last turn to the next tile's
+// first, which nothing else puts in order (`slot` runs on through all of a warp's tiles).
 constexpr int kOutCols = 16;
-constexpr int kAhead = 3;    // turns whose residual has a place
+constexpr int kAhead = 3;    // turns whose residual, or exchange, has a place
+static_assert(kAhead >= 2, "a turn's place is not the one before's");
 struct OutRoom {             // of a warp
   uint4 out[kOutCols * 4];
   uint4 add[kAhead][kOutCols * 4];  // the residual, or the other warp's sums
 };
 template <bool GATED, bool F16, class R, class F>
 __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoom *rooms, int warp, int lane, int64_t t0, int o0,
-                                      R ready, F all_read) {
+                                      int &slot, R ready, F all_read) {
   constexpr int kHalves = GATED ? 1 : 2;  // eights of columns that a warp finishes
   constexpr int kTurn = 2 * kOutCols;     // from a warp's columns to its next
   const int four = warp >> 2, quarter = warp & 3;
@@ -220,7 +226,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
     tmem_load_blocks(r, at + c);
     tmem_load_blocks(r + 8, at + (16u << 16) + c);
   };
-  int ask_left = left, ask_at = 0;  // of the turn whose residual is asked for next
+  int ask_left = left, ask_at = slot;  // of the turn whose residual is asked for next
   auto ask = [&] {
 #pragma unroll
     for (int h = 0; h < 2; ++h) copy_some(&room.add[ask_at][h * 32 + piece], rp + h * 8 * a.r_stride, h * 8 < ask_left ? n : 0);
@@ -238,7 +244,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
     read(c0);
   else
     all_read();
-  for (int turn = 0; c0 < a.tokens; c0 += kTurn, turn = turn + 1 == kAhead ? 0 : turn + 1) {
+  for (; c0 < a.tokens; c0 += kTurn, slot = slot + 1 == kAhead ? 0 : slot + 1) {
     __syncwarp();
     if (adds) {
       ask();
@@ -250,7 +256,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
     if (last) all_read();
     float v[kHalves][4][2], u[4][2];
     if (GATED) {
-      float *const to = (float *)room.add[turn], *const from = (float *)other.add[turn];
+      float *const to = (float *)room.add[slot], *const from = (float *)other.add[slot];
 #pragma unroll
       for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -298,7 +304,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
 #pragma unroll
           for (int k = 0; k < 2; ++k) v[h][g][k] *= u[g][k] + b[1][g];
       if (adds) {
-        load_turned(w, smem_addr(&room.add[turn][h * 32 + block]));
+        load_turned(w, smem_addr(&room.add[slot][h * 32 + block]));
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -554,7 +560,8 @@ __global__ void __launch_bounds__(kSpThreads)
   float *const sums = reinterpret_cast<float *>(stage0);
   if (a.split == 1) {
     __syncthreads();
-    drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, [] {}, [] {});
+    int slot = 0;
+    drain<GATED, F16>(a, tmem, reinterpret_cast<OutRoom *>(stage0), warp, lane, t0, o0, slot, [] {}, [] {});
   } else {
     join<GATED, F16>(a, sm, tmem, sums, warp, lane, rank, t0, o0, stop);
   }
@@ -737,7 +744,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
       if (__any_sync(~0u, *stop)) break;
     }
   } else if (warp < 8) {
-    int n = 0;
+    int n = 0, slot = 0;
     for (int64_t tile = first; tile < a.tiles; tile += pairs, ++n) {
       int64_t row_tile, token_tile;
       pair_tile(a, tile, &row_tile, &token_tile);
@@ -752,7 +759,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPaThreads, 1)
         if (lane == 0) bar_arrive_peer(peer_addr(&sm.sums_empty[n & 1], 0));
       };
       drain<GATED, F16>(a, tmem + (n & 1) * kCols, sm.out, warp, lane, token_tile * a.tokens,
-                        (int)(row_tile * 2 + rank) * kOut, ready, all_read);
+                        (int)(row_tile * 2 + rank) * kOut, slot, ready, all_read);
     }
   }
   __syncwarp();
