@@ -209,7 +209,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
   int c0 = four * kOutCols;
   const int o = row0 + (lane & 3) * 8, n = a.d_out - o;
   const int64_t first = t0 + c0 + own * 8 + mt;
-  int left = n > 0 ? (int)min((int64_t)INT_MAX, a.n_tok - first) : 0;
+  int left = n > 0 ? (int)(min(a.n_tok, t0 + a.tokens) - first) : 0;  // of the tile's tokens, from this lane's on
   uint16_t *y = (uint16_t *)a.y + first * a.y_stride + o;
   const uint16_t *rp = (const uint16_t *)a.residual + first * a.r_stride + o;
   const bool adds = !GATED && a.residual;
@@ -321,7 +321,7 @@ __device__ __forceinline__ void drain(const LinearArgs &a, uint32_t tmem, OutRoo
     y += kTurn * a.y_stride;
     left -= kTurn;
   }
-  // what was asked for past the tile's end (zeros) does not come after the next tile's
+  // what was asked for past the tile's end (zeros, of no memory) does not come after the next tile's
   if (adds) asm volatile("cp.async.wait_all;" ::: "memory");
 }
 

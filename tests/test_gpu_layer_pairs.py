@@ -63,3 +63,23 @@ def test_gated_exchange_from_tile_to_tile(lv, ctx, case, dtype):
     import torch
     for seed in (1, 2, 3):
         _gated(lv, ctx, *case[1:4], getattr(torch, dtype), 10 * seed)
+
+
+@pytest.mark.parametrize("case", layer_cases.LINEAR, ids=str)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_residual_from_tile_to_tile(lv, ctx, case, dtype):
+    """All outputs of relu(x w^T + b) + r, r apart from the outputs and in their place: what is added is the tile's own."""
+    import torch
+    dt, (n, d_in, d_out) = getattr(torch, dtype), case[1:4]
+    x, w, r = (_rows(m, k, dt, 7 + d) for m, k, d in ((n, d_in, 0), (d_out, d_in, 1), (n, d_out, 2)))
+    b = _rows(1, d_out, dt, 10)[0]
+    want = (_product(x, w, b).clamp(min=0) + r.double()).to(dt)
+    for in_place in (False, True):
+        y, whole = _out(n, d_out, dt)
+        if in_place:
+            y.copy_(r)
+        lv.lv_linear(ctx, x, w, y, bias=b, act="relu", residual=y if in_place else r)
+        wrong = (y != want).nonzero()
+        assert len(wrong) == 0, (in_place, len(wrong), wrong[:4].tolist())
+        _only_inside(whole, n, d_out)
+    assert ctx.status() == lv.LV_OK
