@@ -142,47 +142,6 @@ lv_status clusters_of(const Clusters **out) {
   return LV_OK;
 }
 
-// How a product is cut: by pairs of CTAs, or by CTAs of which `split` share a tile's
-// sum; `tokens` columns a tile.
-struct Shape {
-  bool pair;
-  int tokens, split;
-};
-
-// The cut that takes least by a model of both kernels' times, in ns: a piece of the sum
-// costs its matrix instructions (4 of max(tokens / 2, the clocks that reading their
-// operands from shared memory takes), at 1.9 GHz), never less than a turn of the loading
-// and issuing loops, nor than its part of the 1.3 to 1.5 us that a load takes to come
-// with all stages under way; a tile its way out; CTAs beyond what the device holds wait
-// for others to end; of the split kernel an SM holds two.  Fitted to 1,556 measured
-// times of 63 calls of 1 to 8,192 tokens (3 to 300 us): the cut that it takes is 1.4 %
-// above the best one on average.
-Shape choose(const Clusters &hold, int64_t n_tok, int64_t row_tiles, int64_t chunks) {
-  Shape best{true, 256, 1};
-  int64_t least = INT64_MAX;
-  const int64_t most = (std::min<int64_t>(n_tok, kPaTokens) + 15) / 16 * 16;
-  for (int64_t t = 16; t <= most; t += 16) {
-    const int64_t token_tiles = (n_tok + t - 1) / t;
-    if ((n_tok + token_tiles - 1) / token_tiles + 15 < t && t > 16) continue;  // as many tiles of fewer tokens do
-    const int64_t pairs = hold.most[2].load(std::memory_order_relaxed);
-    const int64_t waves = ((row_tiles + 1) / 2 * token_tiles + pairs - 1) / pairs, out = 180 + 14 * t;
-    const int64_t main = chunks * std::max(std::max<int64_t>(130, 1500 / pair_stages((int)t)), std::max(2 * t, 128 + t / 2) * 10 / 19);
-    const int64_t cost = 2000 + main * waves + std::max<int64_t>(0, out - main) * (waves - 1) + out;
-    if (cost < least) least = cost, best = Shape{true, (int)t, 1};
-    if (t > kSpTokens || row_tiles * token_tiles > 4096) continue;
-    for (int split = 1; split <= kSpSplit && split <= chunks; ++split) {
-      const int64_t tiles = row_tiles * token_tiles, at_once = hold.most[split].load(std::memory_order_relaxed);
-      if (split > 1 && (tiles > 2 * at_once || split_sums((int)t, split) > kSpRoom)) break;
-      const int64_t share = tiles > at_once ? 2 : 1, rounds = (tiles + 2 * at_once - 1) / (2 * at_once);
-      const int64_t piece = std::max(std::max<int64_t>(std::max<int64_t>(230, share * 140), 1300 / split_stages((int)t, share == 1)),
-                                     share * std::max(2 * t, 128 + t) * 10 / 19);
-      const int64_t cost = rounds * ((chunks + split - 1) / split * piece + 1300 + 17 * t) + (split > 1 ? 830 + 230 * split : 0);
-      if (cost < least) least = cost, best = Shape{false, (int)t, split};
-    }
-  }
-  return best;
-}
-
 template <bool GATED, bool F16>
 lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t stream) {
   const int32_t dtype = F16 ? LV_F16 : LV_BF16;
@@ -191,7 +150,8 @@ lv_status run_linear(KvHost *kv, LinearArgs &a, const Operands &m, cudaStream_t 
   const Clusters *hold;
   lv_status st = clusters_of(&hold);
   if (st != LV_OK) return st;
-  const Shape shape = choose(*hold, a.n_tok, row_tiles, a.chunks);
+  const Shape shape = choose([&](int n) { return (int64_t)hold->most[n].load(std::memory_order_relaxed); }, a.n_tok, row_tiles,
+                             a.chunks);
   a.tokens = shape.tokens;
   a.split = shape.split;
   a.token_tiles = (a.n_tok + a.tokens - 1) / a.tokens;

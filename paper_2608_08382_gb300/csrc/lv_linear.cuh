@@ -16,6 +16,7 @@
 #pragma once
 
 #include "lv_attend.cuh"
+#include "lv_cut.h"
 #include "lv_tc.cuh"
 
 namespace lv {
@@ -74,11 +75,6 @@ __device__ __forceinline__ void activate(A &array, int act) {
     default: activate_all<LV_ACT_RELU, kN>(v);
   }
 }
-
-constexpr int kPiece = 64;                    // of the sum, in a stage
-constexpr int kRows = 128;                    // weight rows of a CTA's tile
-constexpr int kWBytes = kRows * kPiece * 2;   // of a stage
-constexpr int kColFloats = kRows + 4;         // a token's sums in shared memory: 16-byte steps, spread over the banks
 
 // Outputs of a CTA's tile.
 template <bool GATED>
@@ -373,9 +369,6 @@ __host__ __device__ constexpr uint32_t columns_for(int n) { return n <= 32 ? 32 
 // 5120 -> 3584 9.1 us (5.4): the rest is the first loads' latency, the join (1.5 us) and a
 // kernel's beginning and end, of which the setup lies beside the kernel before.
 constexpr int kSpThreads = 256;
-constexpr int kSpTokens = 160;   // columns at most: with three stages, two CTAs an SM
-constexpr int kSpSplit = 8;      // a portable cluster
-constexpr int kSpStages = 16;    // at most
 
 struct SplitSmem {
   uint64_t full[kSpStages], empty[kSpStages], done, joined;
@@ -384,16 +377,7 @@ struct SplitSmem {
 };
 // The stages stand first, from a 1,024-byte boundary on, and later a tile's sums in
 // their place: a CTA's own and those that it gets, or the way out's rooms.  Then this.
-constexpr size_t split_stage(int tokens) { return kWBytes + (size_t)tokens * kPiece * 2; }
-constexpr size_t split_sums(int tokens, int split) {
-  return split == 1 ? 8 * sizeof(OutRoom) : (tokens + (split - 1) * (size_t)((tokens + split - 1) / split)) * kColFloats * sizeof(float);
-}
-constexpr size_t kSpRoom = 111 << 10;      // of both: two CTAs an SM
-constexpr size_t kSpRoomAlone = 222 << 10;  // where there is one for each SM at most
-constexpr int split_stages(int tokens, bool alone) {
-  const size_t n = (alone ? kSpRoomAlone : kSpRoom) / split_stage(tokens);
-  return n < kSpStages ? (int)n : kSpStages;
-}
+static_assert(kOutRooms == 8 * sizeof(OutRoom), "what a cut counts with");
 
 // The parts of a tile's sums to the CTAs that finish them, and out from there.  The
 // columns that CTA r finishes begin at r tokens / split.  A CTA puts its accumulator into
@@ -589,13 +573,6 @@ __global__ void __launch_bounds__(kSpThreads)
 //   warps 0-7  a tile's way out (drain);
 //   warp 8     loads; warp 9 of the first CTA issues the products of both.
 constexpr int kPaThreads = 320;
-constexpr int kPaTokens = 256;   // columns at most
-constexpr int kPaStages = 11;    // at most: what fits of a tile's width (a load takes about 1.1 us to come)
-constexpr size_t pair_stage(int tokens) { return kWBytes + (size_t)(tokens / 2) * kPiece * 2; }
-constexpr size_t kPaRoom = 6 * pair_stage(kPaTokens);
-constexpr int pair_stages(int tokens) {
-  return kPaRoom / pair_stage(tokens) < kPaStages ? (int)(kPaRoom / pair_stage(tokens)) : kPaStages;
-}
 
 struct PairSmem {
   unsigned char stage[kPaRoom];

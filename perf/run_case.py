@@ -12,8 +12,8 @@ import sys
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCES = ["lv_base.cuh", "lv_attend.cuh", "lv_chunk.cuh", "lv_decode.cuh", "lv_kv.cu", "lv_kv.h", "lv_kv_plan.cuh",
            "lv_kv_store.cuh", "lv_prompt.cuh", "lv_tc.cuh"]
-LAYER_SOURCES = ["lv_base.cuh", "lv_attend.cuh", "lv_kv_store.cuh", "lv_layer.cu", "lv_linear.cuh", "lv_logprobs.cuh",
-                 "lv_rotate.cuh", "lv_tc.cuh"]
+LAYER_SOURCES = ["lv_base.cuh", "lv_attend.cuh", "lv_cut.h", "lv_kv_store.cuh", "lv_layer.cu", "lv_linear.cuh",
+                 "lv_logprobs.cuh", "lv_rotate.cuh", "lv_tc.cuh"]
 
 
 def sources(names):

@@ -65,6 +65,19 @@ def test_gated_exchange_from_tile_to_tile(lv, ctx, case, dtype):
         _gated(lv, ctx, *case[1:4], getattr(torch, dtype), 10 * seed)
 
 
+@pytest.mark.parametrize("case", layer_cases.GATED, ids=str)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_gated_of_other_widths(lv, ctx, case, dtype):
+    import torch
+    _gated(lv, ctx, *case[1:4], getattr(torch, dtype), 4)
+
+
+def test_the_device_cuts_as_listed():
+    """The sizes were looked out for the clusters that this device holds (the rule itself: test_layer_cut)."""
+    import torch
+    assert torch.cuda.get_device_properties(0).multi_processor_count == layer_cases.HOLD[1]
+
+
 @pytest.mark.parametrize("case", layer_cases.LINEAR, ids=str)
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 def test_residual_from_tile_to_tile(lv, ctx, case, dtype):
