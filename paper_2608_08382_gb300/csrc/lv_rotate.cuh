@@ -91,6 +91,20 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
   constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;  // lanes of a head, heads of a warp at a time
   __shared__ __align__(16) float2 turned[kRoWarps][64];  // a token's cosines and sines
   __shared__ __align__(16) float weight[2][D];
+  // An element times its weight is formed before the head's scale is known, and leaves
+  // fp32's range where either is extreme (of bf16; fp16's stay within it).  A head whose sum
+  // of squares is not within these limits is brought near 1 first.  Up to 2^120 an element
+  // is below 2^60, and below 2^128 times a weight of at most 2^64.  An underflow counts where
+  // the scale, at most 1 / sqrt(mean + eps), lifts it back: from mean + eps of 2^-24 on it
+  // ends below 2^-126 again, whatever the weight; with weights of at least 2^-4, which leave
+  // 2^-137 of the least element, it is exact enough down to 2^-97.
+  __shared__ float least, most;
+  constexpr bool kFar = NORM && !F16;
+  if (NORM && threadIdx.x == 0) {
+    least = a.eps < 0x1p-60f ? 0x1p-90f : 0.f;
+    most = 0x1p120f;
+  }
+  if (kFar) __syncthreads();  // beside the kernel before
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int l = lane % kLanes, sub = lane / kLanes, heads = a.heads[0] + a.heads[1];
   let_next();
@@ -130,7 +144,11 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
   const int64_t begin_tok = a.offsets ? a.offsets[0] : 0, end_tok = a.offsets ? a.offsets[a.n_req] : 0;
   for (int k = threadIdx.x; k < 2 * D; k += kRoWarps * 32) {
     const void *const w = k < D ? a.weight[0] : a.weight[1];
-    weight[k / D][k % D] = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
+    const float v = w ? value_of<F16>(((const uint16_t *)w)[k % D]) : 1.f;
+    weight[k / D][k % D] = v;
+    // whoever writes a limit writes the same
+    if (kFar && fabsf(v) > 0x1p64f) most = 0.f;
+    if (kFar && v != 0.f && fabsf(v) < 0x1p-4f && a.eps < 0x1p-24f) least = D * 0x1p-24f;
   }
   __syncthreads();
   for (bool begun = true; u < units; u += (int64_t)gridDim.x * kRoWarps, begun = false) {
@@ -223,15 +241,17 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
           for (int s = kLanes / 2; s; s >>= 1)
 #pragma unroll
             for (int b = 0; b < kAsked; ++b) sum[b] += __shfl_xor_sync(~0u, sum[b], s);
+          const float low = least, high = most;
 #pragma unroll
           for (int b = 0; b < kAsked; ++b)
-            far |= from + b * kAtOnce + sub < end && (!(sum[b] < 0x1p120f) || (sum[b] < 0x1p-90f && a.eps < 0x1p-60f));
+            far |= from + b * kAtOnce + sub < end && (!(sum[b] < high) || sum[b] < low);
         }
         if (__any_sync(~0u, far)) {
 #pragma unroll
           for (int b = 0; b < kAsked; ++b) {
-            // The squares again, relative to a power of two near the largest element, or to
-            // eps where that is larger still: what is far below either does not count
+            // The squares again, relative to a power of two above twice the largest element (so
+            // that two of them times a weight are within range), or to eps where that is larger
+            // still: what is far below either does not count
             float e8[8], top = 0.f, again = 0.f, by = 1.f, eps = a.eps;
             unpack8<F16>(raw[b], e8);
 #pragma unroll
@@ -239,7 +259,7 @@ __global__ void __launch_bounds__(kRoWarps * 32, kRoCtas) k_rotate(const __grid_
 #pragma unroll
             for (int s = kLanes / 2; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
             if (top > 0.f && top < INFINITY)
-              by = scalbnf(1.f, -max(max(ilogbf(top), eps > 0.f ? ilogbf(eps) / 2 : -126), -126));
+              by = scalbnf(1.f, -2 - max(max(ilogbf(top), eps > 0.f ? ilogbf(eps) / 2 : -126), -126));
 #pragma unroll
             for (int k = 0; k < 8; ++k) again += e8[k] * by * (e8[k] * by);
 #pragma unroll
