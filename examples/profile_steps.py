@@ -1,4 +1,4 @@
-"""Profiles the attention work of serving steps on this machine, or the whole layer, and fits the latency model to it.
+"""Profiles the attention work of serving steps on this machine, or the layer around it too, and fits the latency model to it.
 
     python examples/profile_steps.py [--whole] [--layout 8b-tp1] [--steps 240] [--seed 1]
 
@@ -10,11 +10,12 @@ times are the GPU's and not those of the Python calls, and that work leaves noth
 batches: lv_fit gives the coefficients of Eq. 1, lv_accuracy says how well they explain the times, lv_attribute shares
 the predicted times out to the requests.  One layer, random inputs.
 
-With --whole a step is all that the layer does for its tokens, the term of Eq. 1 that grows with their number among it:
+With --whole a step is also what the library does for its tokens around that, the term of Eq. 1 that grows with their number:
 the projection to queries, keys and values (lv_linear), the norm and rotation of their heads (lv_qk_rotate), the attention
 as above, the output projection onto the residual stream (lv_linear), the feed-forward block (lv_gated_linear, lv_linear),
 and for each sequence's last token the logits and the log probability of a next one with its alternatives (lv_linear,
-lv_token_logprobs).
+lv_token_logprobs).  A layer's two norms of the residual stream are not among it: the library has no call for them.  The rows
+of the sequences' last tokens are picked by torch, between begin and end as the rest is.
 """
 
 from __future__ import annotations
@@ -73,14 +74,15 @@ class Layer:
         lv.lv_linear(ctx, o.view(len(h), -1), self.w_o, out["h"], residual=h)
         lv.lv_gated_linear(ctx, out["h"], self.w_gate, self.w_up, out["mid"])
         lv.lv_linear(ctx, out["mid"], self.w_down, out["h"], residual=out["h"])
-        lv.lv_linear(ctx, out["h"].index_select(0, last), self.w_vocab, out["logits"])
+        self.torch.index_select(out["h"], 0, last, out=out["last"])
+        lv.lv_linear(ctx, out["last"], self.w_vocab, out["logits"])
         lv.lv_token_logprobs(ctx, out["logits"], ids=ids, logp=out["logp"], top_ids=out["top_ids"], top_logp=out["top_logp"])
 
     def outputs(self, n_tok, n_seq):
         f32, i32 = self.torch.float32, self.torch.int32
-        return dict(h=self.empty(n_tok, self.width), mid=self.empty(n_tok, len(self.w_gate)), logits=self.empty(n_seq, VOCAB),
-                    logp=self.empty(n_seq, dtype=f32), top_ids=self.empty(n_seq, 5, dtype=i32),
-                    top_logp=self.empty(n_seq, 5, dtype=f32))
+        return dict(h=self.empty(n_tok, self.width), mid=self.empty(n_tok, len(self.w_gate)),
+                    last=self.empty(n_seq, self.width), logits=self.empty(n_seq, VOCAB), logp=self.empty(n_seq, dtype=f32),
+                    top_ids=self.empty(n_seq, 5, dtype=i32), top_logp=self.empty(n_seq, 5, dtype=f32))
 
 
 class Engine:
@@ -201,7 +203,7 @@ def fit(batches, y, engine):
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--layout", choices=sorted(LAYOUTS), default="8b-tp1")
-    ap.add_argument("--whole", action="store_true", help="the whole layer, not its attention alone")
+    ap.add_argument("--whole", action="store_true", help="the layer's products, head norms and scores too, not its attention alone")
     ap.add_argument("--steps", type=int, default=240)
     ap.add_argument("--seed", type=int, default=1)
     a = ap.parse_args()
