@@ -365,9 +365,12 @@ __host__ __device__ constexpr uint32_t columns_for(int n) { return n <= 32 ? 32 
 // the stretches' order: each CTA takes the columns that are its to finish.
 //
 // Measured: 16 tokens, gated, 4096 -> 14336 in bf16 37.5 us, 6.3 TB/s (0.92 of the
-// measured rate); 96 tokens 6912 -> 5120 with a residual 17.8 us (10.9 of bytes), one token
-// 5120 -> 3584 9.1 us (5.4): the rest is the first loads' latency, the join (1.5 us) and a
-// kernel's beginning and end, of which the setup lies beside the kernel before.
+// measured rate); 96 tokens 6912 -> 5120 with a residual 17.4 us (10.9 of bytes; the 40 row
+// tiles in clusters of three are 120 CTAs, so 32 SMs load nothing), one token 5120 -> 3584
+// 9.1 us (5.4): the rest is the first loads' latency, the join (1.5 us) and a kernel's
+// beginning and end, of which the setup lies beside the kernel before.  1,100 tokens
+// 1280 -> 5120 with a residual 15.4 us (7.5 of operations): 280 CTAs come to their way out
+// together (4 us by the cut's model), and ask for the residual only then.
 constexpr int kSpThreads = 256;
 
 struct SplitSmem {
@@ -565,11 +568,11 @@ __global__ void __launch_bounds__(kSpThreads)
 // stay and take tiles in turn; two accumulators let a tile's products run while the
 // one before is on its way out.
 //
-// Measured: 8,192 tokens, 4096 -> 6144 in bf16, 214 us in a burst, 1,930 TFLOP/s (1.00 of the
-// measured rate: a library's product of these sizes takes 212), 253 us kept up under the
-// power limit (238); 4,001 tokens, gated, 5120 -> 6912 in fp16 310 us, 1,830 TFLOP/s; 333
-// tokens 45 us: 108 tiles on 76 pairs are two rounds, and a tile's way out (4 us) stands
-// behind the last.
+// Measured: 8,192 tokens, 4096 -> 6144 in bf16, 212 us in a burst, 1,945 TFLOP/s (1.01 of the
+// measured rate: a library's product of these sizes takes 212), 239 us kept up under the
+// power limit (238); 4,001 tokens, gated, 5120 -> 6912 in fp16 315 to 331 us, 1,710 to 1,800
+// TFLOP/s, kept up 357; 333 tokens 43 to 45 us: 108 tiles on 76 pairs are two rounds, and a
+// tile's way out (4 us) stands behind the last.
 //   warps 0-7  a tile's way out (drain);
 //   warp 8     loads; warp 9 of the first CTA issues the products of both.
 constexpr int kPaThreads = 320;
@@ -622,8 +625,9 @@ __device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
 
 // First outputs and tokens of a tile: bands of twelve row tiles, row tile after row tile
 // and then token tile after token tile, so that the tiles at work at a time share their
-// operands in L2 (us kept up of 8,192 tokens, 4096 -> 6144: bands of 4 248, 8 245, 12 241,
-// 24 246).
+// operands in L2 (us kept up of 8,192 tokens, 4096 -> 6144, whose 24 row tiles they divide:
+// bands of 4 248, 8 245, 12 241, 24 246; other numbers of row tiles, and the gated form,
+// were not measured).
 __device__ __forceinline__ void pair_tile(const LinearArgs &a, int64_t tile, int64_t *row_tile, int64_t *token_tile) {
   constexpr int64_t kBand = 12;
   const int64_t rows = quotient(a.tiles, a.token_tiles), of_band = kBand * a.token_tiles;

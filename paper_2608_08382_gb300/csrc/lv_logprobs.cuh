@@ -23,11 +23,11 @@
 // Every comparison is of a value and its index, so that nothing depends on an order of
 // arrival.
 //
-// Measured: 4,096 rows of 32,000 in bf16 53 us, 4.9 TB/s (0.72 of the measured rate), bound by
-// instructions (12 a logit, 0.76 of the issue slots; 78 us with 20 alternatives); 256 fp32
-// rows of 128,000 with five alternatives 26.6 us (19.3 of bytes): the rows are one wave,
-// and what follows its loads (4 us) lies behind them; one row of 128,000 with 20
-// alternatives 8.9 us.
+// Measured: 4,096 rows of 32,000 in bf16 52 us, 5.0 TB/s (0.74 of the measured rate): 10.5
+// instructions a logit keep 0.7 of the issue slots busy, through 3.4 rounds of rows of which
+// the last is in part (with 20 alternatives 78 us); 256 fp32 rows of 128,000 with five
+// alternatives 26.5 us (19.3 of bytes): the rows are one wave, and what follows its loads
+// (4 us) lies behind them; one row of 128,000 with 20 alternatives 9.1 us.
 #pragma once
 
 #include "lv_linear.cuh"

@@ -10,8 +10,10 @@
 //
 // Measured: 8,005 tokens of 32 + 8 heads of 128, bf16, 34 us, 4.8 TB/s (0.71 of the measured
 // rate; 209 us for a head a warp through shared memory, 56 with norm, weight and angle
-// applied one after another).  It is bound by instructions, about 137 for two heads of a
-// token, at 2.5 a clock and SM with the 20 warps that 96 registers a thread leave.
+// applied one after another).  Neither memory (0.42 busy) nor the issue slots (0.62) are
+// full: about 136 instructions for two heads of a token, which wait for one another's
+// shuffles and conversions, and with 95 registers a thread (and 8 bytes in local memory, a
+// load a token) there are 20 warps an SM to fill the gaps.
 #pragma once
 
 #include "lv_linear.cuh"
